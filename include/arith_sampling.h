@@ -63,6 +63,7 @@ extern "C" {
 #define AS_ERR_CUDA (-3)         /* a CUDA runtime call failed (no device, launch error) */
 #define AS_ERR_TIMEOUT (-4)      /* a bounded on-device wait ran out (reported per lane) */
 #define AS_ERR_NUMERIC (-5)      /* per-lane: non-finite logits / empty row / bad code */
+#define AS_ERR_NO_PAGES (-6)     /* per-lane: the pool has too few free pages */
 
 /* Largest vocabulary size accepted by as_step / as_decode_bigram* / as_encode_bigram. */
 #define AS_MAX_V (1 << 20)
@@ -366,6 +367,180 @@ int as_ngram_diversity(const int32_t *d_seq, const int32_t *d_len, int S, int N,
 int as_reward_mean(const int32_t *d_seq, const int32_t *d_len, int S, int N, int T,
                    const double *d_r, int V, double *d_lane_reward, double *d_mean,
                    int32_t *d_group_status, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Around the step.  The paper decodes codes against "a language model's next-token distribution";
+ * the calls below are the parts of such a model's decode loop that N lanes per prompt make their
+ * own: the edits of the logits in front of as_step, and the cache of keys and values that the
+ * lanes of one prompt share.  They have no counterpart in the paper.
+ * --------------------------------------------------------------------------------------------- */
+
+/*
+ * Logit edits: penalties for repeated tokens, a bias and a grammar mask, applied to every lane's
+ * row in this order, in binary32, rounded once to the row's type:
+ *   seen tokens (anywhere in the lane's history):  x = x > 0 ? x / repetition : x * repetition
+ *   x = x - (frequency * n + presence * [n > 0])   n = how often the token occurs in the output,
+ *                                                  that is at history positions >= d_prompt_len
+ *   x = x + d_bias[row, j]
+ *   x = -inf where the mask's bit for token j is 0, whatever x was (NaN and +inf included)
+ *   d_seq         [lanes, T] i32 device, T = seq_ld: the tokens so far, in the layout that
+ *                 as_decode_bigram writes; NULL = no history (then no penalties)
+ *   d_len         [lanes] i32 device: tokens of d_seq that count, 0..T
+ *   d_prompt_len  NULL (0 for every lane) or [lanes] i32: leading tokens that are the prompt
+ *   repetition    > 0 and finite (1 = off);  presence, frequency: finite (0 = off)
+ *   d_bias        NULL or f32 device, row of lane i at d_bias + i * bias_ld (bias_ld = 0: one row
+ *                 for all lanes); bias_ld is 0 or >= V
+ *   d_mask        NULL or u32 device [mask_rows, mask_ld], mask_ld >= ceil(V / 32) words: bit j % 32
+ *                 of word j / 32 set = token j allowed
+ *   d_mask_row    NULL or [lanes] i32 device: the lane's row of d_mask (a grammar's state, say);
+ *                 -1 = this lane is not masked.  NULL: lane i uses row i, or row 0 if mask_rows is 1
+ */
+typedef struct as_logit_edits {
+    const int32_t *d_seq;
+    long long seq_ld;
+    const int32_t *d_len;
+    const int32_t *d_prompt_len;
+    float repetition, presence, frequency;
+    const float *d_bias;
+    long long bias_ld;
+    const uint32_t *d_mask;
+    long long mask_ld;
+    int mask_rows;
+    const int32_t *d_mask_row;
+} as_logit_edits;
+
+/*
+ *   d_logits  [lanes, ld] device, dtype AS_F32 or AS_BF16;  d_out [lanes, out_ld], same dtype.
+ *             d_out may be d_logits with out_ld = ld: the call then only touches what changes.
+ *             Otherwise the two must not overlap.
+ *   d_lane_status  NULL or [lanes] i32 device: AS_OK, or AS_ERR_INVALID_ARG where a history token
+ *             lies outside [0, V), d_len outside [0, T] or d_mask_row outside [-1, mask_rows)
+ *             (such a token is skipped, such a length clamped, such a row read as -1)
+ * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (V > AS_MAX_V), AS_ERR_CUDA, as for as_step.
+ */
+int as_logits_edit(const void *d_logits, int dtype, int lanes, int V, long long ld,
+                   const as_logit_edits *edits, void *d_out, long long out_ld,
+                   int32_t *d_lane_status, void *stream);
+
+/*
+ * A cache of keys and values held in 4 bits, in pages (one layer of a model).
+ *   d_pages    [n_pages, heads, page_size / 16 tiles, 18 * head_dim bytes] device, 16-byte aligned.
+ *              A tile holds 16 tokens of one head:
+ *                key codes    [16 tokens][head_dim / 2 bytes]
+ *                value codes  [head_dim / 16 blocks][16 tokens][8 bytes]
+ *                key scales   [16 tokens][head_dim / 16 bytes]
+ *                value scales [head_dim / 16 blocks][16 tokens]
+ *              A code is 4 bits: sign, two exponent bits, one mantissa bit (0, 0.5, 1, 1.5, 2, 3, 4,
+ *              6 and their negatives), the even dimension in the low half of its byte.  A scale is
+ *              8 bits (e4m3) for 16 neighbouring dimensions of one token.
+ *   heads      key / value heads, >= 1;  head_dim 64 or 128;  page_size 16, 32, 64 or 128 tokens
+ *   d_k_scale, d_v_scale  NULL (1) or [heads] f32 device, finite and > 0: what a head's keys / values
+ *              are divided by before they are stored, so that they lie in the scales' range
+ * The value stored for x is code * scale * head scale; with y = x / head scale, scale is max|y| of
+ * the block over 6, rounded to e4m3 (at most 448), and code is y / scale rounded to nearest (half way:
+ * to the even code), at most 6.  code * scale is exact in bf16 and in binary16.
+ */
+typedef struct as_cache4 {
+    void *d_pages;
+    int n_pages, heads, head_dim, page_size;
+    const float *d_k_scale, *d_v_scale;
+} as_cache4;
+size_t as_cache4_bytes(int n_pages, int heads, int head_dim, int page_size);
+
+/*
+ * A lane's tokens lie in the pages of its row of the page table: position p in page
+ * d_table[lane, p / page_size], d_table [lanes, max_pages] i32 device.  In the next three calls the T
+ * tokens of a lane are those at positions d_len[lane] - T .. d_len[lane] - 1 (d_len [lanes] i32
+ * device); a position below 0 is no token (prompts of several lengths are padded at their front).
+ * T >= 1; dtype is that of the keys, values and queries.
+ *   d_k, d_v   token i of a lane at d_k + (lane * T + i) * k_ld elements, [heads, head_dim] there;
+ *              k_ld, v_ld >= heads * head_dim
+ *   d_lane_status  NULL or [lanes] i32 device: AS_OK; AS_ERR_NUMERIC for a NaN or infinite key or
+ *              value (stored as 0 and as the largest value); AS_ERR_INVALID_ARG for a d_len outside
+ *              [0, max_pages * page_size] or a page id outside [0, n_pages) (those tokens are skipped)
+ * as_cache4_append stores; lanes must not share the pages that it writes.  as_cache4_load writes what
+ * is stored to d_k, d_v [lanes, T, heads, head_dim] (contiguous), zeros where there is no token.
+ */
+int as_cache4_append(const as_cache4 *cache, const void *d_k, long long k_ld, const void *d_v,
+                     long long v_ld, int dtype, int lanes, int T, const int32_t *d_table, int max_pages,
+                     const int32_t *d_len, int32_t *d_lane_status, void *stream);
+int as_cache4_load(const as_cache4 *cache, void *d_k, void *d_v, int dtype, int lanes, int T,
+                   const int32_t *d_table, int max_pages, const int32_t *d_len,
+                   int32_t *d_lane_status, void *stream);
+
+/*
+ * Attention over the cache: for query token i of a lane and query head h
+ *   out = sum_t softmax_t(scale * q . k_t) v_t    over positions t < d_len[lane] - T + 1 + i,
+ * k, v those of head h / (q_heads / heads).  T = 1 is the decode step, T > 1 a chunk of a prompt whose
+ * tokens have been appended before.  A row that sees nothing gives zeros (and -inf in d_lse).
+ *   d_q        token i of a lane at d_q + (lane * T + i) * q_ld, [q_heads, head_dim] there
+ *   q_heads    a multiple of heads;  scale finite
+ *   N, d_shared  lanes g*N .. g*N+N-1 form group g (lanes is a multiple of N; the lanes of one prompt).
+ *              d_shared NULL, or [lanes / N] i32 device: the first d_shared[g] positions of the
+ *              group's lanes lie in the same pages (a multiple of page_size, <= every d_len of the
+ *              group; read as 0 otherwise).  They are then read once for the group, through the row
+ *              of its first lane.  The result is the same.
+ *   d_out      [lanes, T, q_heads, head_dim], written
+ *   d_lse      NULL or [lanes, T, q_heads] f32 device: ln sum_t exp(scale * q . k_t)
+ *   d_lane_status  NULL or [lanes]: AS_OK, or AS_ERR_INVALID_ARG for a d_len outside
+ *              [0, max_pages * page_size] (the lane is then empty) or a page id outside [0, n_pages)
+ *              (page 0 is read in its place)
+ *   d_work     as_cache4_attend_work_bytes(...) bytes of device scratch, 256-byte aligned
+ * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (head_dim, page_size), AS_ERR_CUDA.
+ */
+size_t as_cache4_attend_work_bytes(const as_cache4 *cache, int dtype, int lanes, int T, int q_heads, int N);
+int as_cache4_attend(const as_cache4 *cache, const void *d_q, long long q_ld, int dtype, int lanes, int T,
+                     int q_heads, const int32_t *d_table, int max_pages, const int32_t *d_len,
+                     double scale, int N, const int32_t *d_shared, void *d_out, float *d_lse,
+                     int32_t *d_lane_status, void *d_work, size_t work_bytes, void *stream);
+
+/*
+ * The pages of a cache: a page table [lanes, max_pages] i32 (-1 behind a lane's last page), lengths
+ * [lanes] i32, and for every page the number of lanes that hold it, d_ref [n_pages] i32 (0 = free).
+ * A lane's partly filled last page is held by that lane alone; full pages may be held by many.  Free
+ * pages are given out by number, the lowest first, to the lanes in their order, so that results do
+ * not depend on scheduling.
+ *
+ * as_pages_fork: lane i of the result continues lane d_parent[i] of the lanes in hand (-1: it holds
+ * nothing).  Every full page is shared; the first child of a lane keeps its partly filled last page,
+ * every other child gets a page of its own with the contents copied; pages that no lane holds any
+ * more become free (and may be given out by the same call).  So one call hands a prompt to N lanes,
+ * drops lanes that have ended, or moves lanes about.
+ *   d_data     NULL (no copying) or the pool: plane p, page g at d_data + p * plane_stride +
+ *              g * page_bytes (a plane is a layer, say); d_data and page_bytes multiples of 16 bytes,
+ *              plane_stride a multiple of 16 and >= n_pages * page_bytes
+ *   d_table_out [lanes_out, max_pages], d_len_out [lanes_out], d_ref_out [n_pages]: written; d_table_out
+ *              and d_len_out must not be d_table and d_len, d_ref_out may be d_ref
+ *   d_lane_status  NULL or [lanes_out]: AS_OK; AS_ERR_NO_PAGES: no page for the copy, the lane ends at
+ *              its last full page; AS_ERR_INVALID_ARG: parent outside [-1, lanes_in) (read as -1), or
+ *              a parent whose length or pages are out of range (read as empty)
+ *
+ * as_pages_grow: lane i gets the pages for d_add[i] >= 0 more tokens and its length grows by them, in
+ * place.  Lanes that the free pages do not reach keep what they have: once a lane's pages do not
+ * suffice, neither do those of the lanes behind it that need any (AS_ERR_NO_PAGES); a lane that would
+ * pass max_pages or has a bad length or a negative d_add: AS_ERR_INVALID_ARG, unchanged.
+ *
+ * as_pages_compact: with U pages in use, every page in use at U or above moves into a free page
+ * below U (the lowest into the lowest), so that the pool's end is free.
+ *   d_table_out may be d_table, d_ref_out may be d_ref;  d_used  [1] i32 device, written: U
+ *
+ *   d_work     as_pages_work_bytes(lanes_in, lanes_out, n_pages) bytes of device scratch, 256-byte aligned
+ *              (lanes_in = lanes_out = lanes for the last two calls)
+ * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (n_pages > 2^20, max_pages * page_size > 2^30), AS_ERR_CUDA.
+ */
+size_t as_pages_work_bytes(int lanes_in, int lanes_out, int n_pages);
+int as_pages_fork(const int32_t *d_parent, int lanes_in, int lanes_out, int max_pages, int page_size,
+                  int n_pages, const int32_t *d_table, const int32_t *d_len, const int32_t *d_ref,
+                  int32_t *d_table_out, int32_t *d_len_out, int32_t *d_ref_out, void *d_data, int planes,
+                  long long plane_stride, long long page_bytes, int32_t *d_lane_status, void *d_work,
+                  size_t work_bytes, void *stream);
+int as_pages_grow(const int32_t *d_add, int lanes, int max_pages, int page_size, int n_pages,
+                  int32_t *d_table, int32_t *d_len, int32_t *d_ref, int32_t *d_lane_status, void *d_work,
+                  size_t work_bytes, void *stream);
+int as_pages_compact(int lanes, int max_pages, int n_pages, const int32_t *d_table, const int32_t *d_ref,
+                     int32_t *d_table_out, int32_t *d_ref_out, int32_t *d_used, void *d_data, int planes,
+                     long long plane_stride, long long page_bytes, void *d_work, size_t work_bytes,
+                     void *stream);
 
 /*
  * Launch-shape overrides for measurement sweeps and tests (0 restores the built-in

@@ -2,16 +2,18 @@
 from __future__ import annotations
 
 import os
+import re
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libarith_sampling.so")
 # the same sources with every shared-memory index checked (-DAS_BOUNDS_CHECK): for the tests
 LIB_CHECKED = os.path.join(_HERE, "libarith_sampling_check.so")
-SOURCES = ["as_api.cu"]
+SOURCES = ["as_api.cu", "as_edit.cu", "as_cache4.cu", "as_pages.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC"]
 
 
 def _nvcc() -> str:
@@ -30,16 +32,42 @@ def _newest_source_mtime() -> float:
     return m
 
 
+def _depends(path: str, seen=None) -> set:
+    """A source file and the project headers that it includes, directly or not."""
+    seen = set() if seen is None else seen
+    path = os.path.normpath(path)
+    if path not in seen and os.path.exists(path):
+        seen.add(path)
+        with open(path) as f:
+            for name in re.findall(r'^\s*#include "([^"]+)"', f.read(), re.M):
+                _depends(os.path.join(os.path.dirname(path), name), seen)
+    return seen
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
     """Compile csrc/*.cu into libarith_sampling.so (checked: libarith_sampling_check.so, with
-    -DAS_BOUNDS_CHECK) if it is missing or stale."""
+    -DAS_BOUNDS_CHECK) if it is missing or stale: the sources whose object file is older than what
+    they include, side by side, then one link."""
     lib = LIB_CHECKED if checked else LIB
     if not force and os.path.exists(lib) and os.path.getmtime(lib) >= _newest_source_mtime():
         return lib
+    objdir = os.path.join(_HERE, "_build_check" if checked else "_build_lib")
+    os.makedirs(objdir, exist_ok=True)
+    flags = NVCC_FLAGS + (["-DAS_BOUNDS_CHECK"] if checked else []) + (["-Xptxas", "-v"] if verbose else [])
+
+    def compile_one(name):
+        src, obj = os.path.join(CSRC, name), os.path.join(objdir, name[:-3] + ".o")
+        newest = max(os.path.getmtime(f) for f in _depends(src))
+        if force or not os.path.exists(obj) or os.path.getmtime(obj) < newest:
+            part = obj + ".tmp.%d" % os.getpid()
+            subprocess.check_call([_nvcc()] + flags + ["-c", "-o", part, src])
+            os.replace(part, obj)
+        return obj
+
+    with ThreadPoolExecutor(len(SOURCES)) as pool:
+        objs = list(pool.map(compile_one, SOURCES))
     tmp = lib + ".tmp.%d" % os.getpid()
-    cmd = [_nvcc()] + NVCC_FLAGS + (["-DAS_BOUNDS_CHECK"] if checked else []) + (["-Xptxas", "-v"] if verbose else []) + \
-          ["-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
-    subprocess.check_call(cmd)
+    subprocess.check_call([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", tmp] + objs)
     os.replace(tmp, lib)
     return lib
 

@@ -24,6 +24,7 @@ ERR_UNSUPPORTED = -2
 ERR_CUDA = -3
 ERR_TIMEOUT = -4
 ERR_NUMERIC = -5
+ERR_NO_PAGES = -6
 
 PATH_COMPACT = 0
 PATH_GENERAL = 1
@@ -40,7 +41,9 @@ TUNE_RADIX_NUCLEUS = 9
 
 EXPORTS = ["as_lattice_codes", "as_lattice_codes_variant", "as_step", "as_step_typical", "as_step_lattice", "as_step_host", "as_step_host_work_bytes", "as_step_host_static",
            "as_decode_bigram",
-           "as_decode_bigram_codes", "as_xp_lattice_state", "as_decode_bigram_xp", "as_encode_bigram", "as_ngram_diversity", "as_reward_mean", "as_tune",
+           "as_decode_bigram_codes", "as_xp_lattice_state", "as_decode_bigram_xp", "as_encode_bigram", "as_ngram_diversity", "as_reward_mean", "as_logits_edit",
+           "as_cache4_bytes", "as_cache4_append", "as_cache4_load", "as_cache4_attend_work_bytes", "as_cache4_attend",
+           "as_pages_work_bytes", "as_pages_fork", "as_pages_grow", "as_pages_compact", "as_tune",
            "as_last_error", "as_version"]
 
 
@@ -54,6 +57,20 @@ class as_step_diag(ctypes.Structure):
     _fields_ = [("d_p_tok", ctypes.c_void_p), ("d_cdf_lo", ctypes.c_void_p),
                 ("d_n_kept", ctypes.c_void_p), ("d_lane_status", ctypes.c_void_p),
                 ("d_path", ctypes.c_void_p)]
+
+
+class as_logit_edits(ctypes.Structure):
+    _fields_ = [("d_seq", ctypes.c_void_p), ("seq_ld", ctypes.c_longlong), ("d_len", ctypes.c_void_p),
+                ("d_prompt_len", ctypes.c_void_p), ("repetition", ctypes.c_float), ("presence", ctypes.c_float),
+                ("frequency", ctypes.c_float), ("d_bias", ctypes.c_void_p), ("bias_ld", ctypes.c_longlong),
+                ("d_mask", ctypes.c_void_p), ("mask_ld", ctypes.c_longlong), ("mask_rows", ctypes.c_int),
+                ("d_mask_row", ctypes.c_void_p)]
+
+
+class as_cache4(ctypes.Structure):
+    _fields_ = [("d_pages", ctypes.c_void_p), ("n_pages", ctypes.c_int), ("heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int), ("d_k_scale", ctypes.c_void_p),
+                ("d_v_scale", ctypes.c_void_p)]
 
 
 _lib = None
@@ -114,11 +131,25 @@ def lib():
         L.as_xp_lattice_state.restype = I
         L.as_decode_bigram_xp.argtypes = [P, I, I, LL, P, P, I, I, I, I, D, I, D, P, P, P, P]
         L.as_decode_bigram_xp.restype = I
+        Z, PC = ctypes.c_size_t, ctypes.POINTER(as_cache4)
+        L.as_logits_edit.argtypes = [P, I, I, I, LL, ctypes.POINTER(as_logit_edits), P, LL, P, P]
+        L.as_cache4_bytes.argtypes = [I, I, I, I]
+        L.as_cache4_append.argtypes = [PC, P, LL, P, LL, I, I, I, P, I, P, P, P]
+        L.as_cache4_load.argtypes = [PC, P, P, I, I, I, P, I, P, P, P]
+        L.as_cache4_attend_work_bytes.argtypes = [PC, I, I, I, I, I]
+        L.as_cache4_attend.argtypes = [PC, P, LL, I, I, I, I, P, I, P, D, I, P, P, P, P, P, Z, P]
+        L.as_pages_work_bytes.argtypes = [I, I, I]
+        L.as_pages_fork.argtypes = [P, I, I, I, I, I, P, P, P, P, P, P, P, I, LL, LL, P, P, Z, P]
+        L.as_pages_grow.argtypes = [P, I, I, I, I, P, P, P, P, P, Z, P]
+        L.as_pages_compact.argtypes = [I, I, I, P, P, P, P, P, P, I, LL, LL, P, Z, P]
+        for n in ("as_cache4_bytes", "as_cache4_attend_work_bytes", "as_pages_work_bytes"):
+            getattr(L, n).restype = Z
         L.as_tune.argtypes = [I, I]
         L.as_last_error.restype = ctypes.c_char_p
         for n in ("as_lattice_codes", "as_step", "as_step_host", "as_decode_bigram",
-                  "as_decode_bigram_codes", "as_xp_lattice_state", "as_decode_bigram_xp", "as_encode_bigram", "as_ngram_diversity", "as_reward_mean", "as_tune",
-                  "as_version"):
+                  "as_decode_bigram_codes", "as_xp_lattice_state", "as_decode_bigram_xp", "as_encode_bigram", "as_ngram_diversity", "as_reward_mean",
+                  "as_logits_edit", "as_cache4_append", "as_cache4_load", "as_cache4_attend", "as_pages_fork", "as_pages_grow",
+                  "as_pages_compact", "as_tune", "as_version"):
             getattr(L, n).restype = I
         _lib = L
     return _lib
@@ -403,3 +434,221 @@ def as_reward_mean(seq: torch.Tensor, length: torch.Tensor, N: int, r: torch.Ten
     _check(lib().as_reward_mean(_ptr(seq), _ptr(length), S, N, T, _ptr(r), r.numel(), _ptr(lane_reward),
                                 _ptr(mean), _ptr(group_status), _stream(stream)))
     return lane_reward, mean
+
+
+def _int32(t: Optional[torch.Tensor], name: str, numel: Optional[int] = None):
+    """Device pointer of a contiguous int32 tensor (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        raise ValueError("%s must be a contiguous int32 tensor%s" % (name, "" if numel is None else " of %d entries" % numel))
+    return t.data_ptr()
+
+
+def as_logits_edit(logits: torch.Tensor, seq: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None,
+                   prompt_length: Optional[torch.Tensor] = None, repetition: float = 1.0, presence: float = 0.0,
+                   frequency: float = 0.0, bias: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                   mask_row: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   lane_status: Optional[torch.Tensor] = None, V: Optional[int] = None, stream=None) -> torch.Tensor:
+    """Penalties, bias and grammar mask on logits [lanes, V].  seq [lanes, T] int32 with length [lanes]
+    is the history (as_decode_bigram's layout), bias float32 [V] or [lanes, V], mask int32 [rows, ceil(V/32)]
+    (bit set = allowed) with mask_row [lanes] (-1 = none).  out=logits edits in place."""
+    lanes, width, ld = _logits_layout(logits)
+    V = width if V is None else V
+    if out is None:
+        out = torch.empty((lanes, V), dtype=logits.dtype, device=logits.device)
+    elif out.dtype != logits.dtype or out.dim() != 2 or out.shape[0] != lanes or out.shape[1] < V:
+        raise ValueError("out must have the logits' dtype and a row of at least V for each lane")
+    e = as_logit_edits()
+    e.repetition, e.presence, e.frequency = repetition, presence, frequency
+    if seq is not None:
+        if seq.dim() != 2 or seq.shape[0] != lanes or length is None:
+            raise ValueError("seq must be [lanes, T] and comes with a length for each lane")
+        e.d_seq, e.seq_ld = _int32(seq, "seq"), seq.shape[1]
+        e.d_len, e.d_prompt_len = _int32(length, "length", lanes), _int32(prompt_length, "prompt_length", lanes)
+    if bias is not None:
+        if bias.dtype != torch.float32 or bias.stride(-1) != 1 or bias.shape[-1] < V or (bias.dim() == 2 and bias.shape[0] not in (1, lanes)):
+            raise ValueError("bias must be float32, [V] or [lanes, V], with unit stride along the vocabulary")
+        e.d_bias, e.bias_ld = bias.data_ptr(), (bias.stride(0) if bias.dim() == 2 and bias.shape[0] > 1 else 0)
+    if mask is not None:
+        if mask.dtype != torch.int32 or mask.dim() != 2 or mask.stride(1) != 1 or mask.shape[1] < (V + 31) // 32:
+            raise ValueError("mask must be int32 [rows, ceil(V / 32)] with unit stride along a row")
+        e.d_mask, e.mask_rows = mask.data_ptr(), mask.shape[0]
+        e.mask_ld = mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
+        e.d_mask_row = _int32(mask_row, "mask_row", lanes)
+    _check(lib().as_logits_edit(logits.data_ptr(), _logits_dtype(logits), lanes, V, ld, ctypes.byref(e), out.data_ptr(),
+                                _logits_layout(out)[2], _int32(lane_status, "lane_status", lanes), _stream(stream)))
+    return out
+
+
+def as_cache4_bytes(n_pages: int, heads: int, head_dim: int, page_size: int) -> int:
+    return lib().as_cache4_bytes(n_pages, heads, head_dim, page_size)
+
+
+def cache4_pages(n_pages: int, heads: int, head_dim: int, page_size: int, planes: Optional[int] = None,
+                 device="cuda") -> torch.Tensor:
+    """Zeroed pages of a 4-bit cache, uint8 [n_pages, heads, page_size / 16, 18 * head_dim], the shape that tells the
+    calls below heads, head_dim and page_size; with `planes`, one such tensor for each layer ([planes, ...])."""
+    shape = (n_pages, heads, page_size // 16, 18 * head_dim)
+    return torch.zeros(shape if planes is None else (planes,) + shape, dtype=torch.uint8, device=device)
+
+
+def _cache4(pages: torch.Tensor, k_scale, v_scale) -> as_cache4:
+    if pages.dtype != torch.uint8 or pages.dim() != 4 or not pages.is_contiguous() or pages.shape[3] % 18:
+        raise ValueError("pages must be a contiguous uint8 tensor [n_pages, heads, page_size / 16, 18 * head_dim]")
+    n, heads, tiles, width = pages.shape
+    for s in (k_scale, v_scale):
+        if s is not None and (s.dtype != torch.float32 or s.numel() != heads or not s.is_contiguous()):
+            raise ValueError("k_scale and v_scale must be contiguous float32 with an entry for each head")
+    return as_cache4(pages.data_ptr(), n, heads, width // 18, tiles * 16, _ptr(k_scale), _ptr(v_scale))
+
+
+def _tokens(t: torch.Tensor, D: int, name: str):
+    """(lanes, T, heads, elements from token to token) of a [lanes, T, heads, D] tensor whose heads lie side by side."""
+    if t.dim() != 4 or t.shape[3] != D:
+        raise ValueError("%s must be [lanes, T, heads, %d]" % (name, D))
+    lanes, T, heads, _ = t.shape
+    sl, st, sh, sd = t.stride()
+    ld = st if T > 1 else sl if lanes > 1 else heads * D
+    if sd != 1 or (heads > 1 and sh != D) or (lanes > 1 and T > 1 and sl != T * st):
+        raise ValueError("%s: heads must lie side by side and tokens at one distance" % name)
+    return lanes, T, heads, ld
+
+
+def _table(table: torch.Tensor, length: torch.Tensor, lanes: int):
+    if table.dim() != 2 or table.shape[0] != lanes:
+        raise ValueError("table must be [lanes, max_pages]")
+    return _int32(table, "table"), table.shape[1], _int32(length, "length", lanes)
+
+
+def as_cache4_append(pages: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
+                     k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                     lane_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Store k, v [lanes, T, heads, D] as the last T of each lane's length[lane] tokens."""
+    c = _cache4(pages, k_scale, v_scale)
+    lanes, T, heads, k_ld = _tokens(k, c.head_dim, "k")
+    if v.shape != k.shape or v.dtype != k.dtype or heads != c.heads:
+        raise ValueError("k and v must have the same shape and dtype, and the cache's heads")
+    tp, max_pages, lp = _table(table, length, lanes)
+    _check(lib().as_cache4_append(ctypes.byref(c), k.data_ptr(), k_ld, v.data_ptr(), _tokens(v, c.head_dim, "v")[3],
+                                  _logits_dtype(k), lanes, T, tp, max_pages, lp,
+                                  _int32(lane_status, "lane_status", lanes), _stream(stream)))
+
+
+def as_cache4_load(pages: torch.Tensor, table: torch.Tensor, length: torch.Tensor, T: int,
+                   k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, dtype=torch.bfloat16,
+                   lane_status: Optional[torch.Tensor] = None, stream=None):
+    """(k, v) [lanes, T, heads, D]: what is stored for the last T tokens of each lane (zeros where there is none)."""
+    c = _cache4(pages, k_scale, v_scale)
+    lanes = length.numel()
+    k = torch.empty((lanes, T, c.heads, c.head_dim), dtype=dtype, device=pages.device)
+    v = torch.empty_like(k)
+    tp, max_pages, lp = _table(table, length, lanes)
+    _check(lib().as_cache4_load(ctypes.byref(c), k.data_ptr(), v.data_ptr(), _logits_dtype(k), lanes, T, tp, max_pages, lp,
+                                _int32(lane_status, "lane_status", lanes), _stream(stream)))
+    return k, v
+
+
+def as_cache4_attend_work_bytes(pages: torch.Tensor, dtype: int, lanes: int, T: int, q_heads: int, N: int = 1) -> int:
+    return lib().as_cache4_attend_work_bytes(ctypes.byref(_cache4(pages, None, None)), dtype, lanes, T, q_heads, N)
+
+
+def as_cache4_attend(pages: torch.Tensor, q: torch.Tensor, table: torch.Tensor, length: torch.Tensor, scale: float,
+                     k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, N: int = 1,
+                     shared: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, lane_status: Optional[torch.Tensor] = None,
+                     work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of q [lanes, T, q_heads, D], the last T tokens of each lane, over the lane's cached tokens (causal).
+    shared [lanes / N] int32: how many leading tokens the N lanes of a group have in the same pages."""
+    c = _cache4(pages, k_scale, v_scale)
+    lanes, T, heads, q_ld = _tokens(q, c.head_dim, "q")
+    if out is None:
+        out = torch.empty((lanes, T, heads, c.head_dim), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be contiguous, with the shape and dtype of q")
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != lanes * T * heads or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous float32 [lanes, T, q_heads]")
+    L = lib()
+    dt = _logits_dtype(q)
+    need = L.as_cache4_attend_work_bytes(ctypes.byref(c), dt, lanes, T, heads, N)
+    if work is None:
+        work = torch.empty(need, dtype=torch.uint8, device=q.device)
+    tp, max_pages, lp = _table(table, length, lanes)
+    _check(L.as_cache4_attend(ctypes.byref(c), q.data_ptr(), q_ld, dt, lanes, T, heads, tp, max_pages, lp, scale, N,
+                              _int32(shared, "shared", lanes // N if N > 0 else None), out.data_ptr(), _ptr(lse),
+                              _int32(lane_status, "lane_status", lanes), work.data_ptr(),
+                              work.numel() * work.element_size(), _stream(stream)))
+    return out
+
+
+def as_pages_work_bytes(lanes_in: int, lanes_out: int, n_pages: int) -> int:
+    return lib().as_pages_work_bytes(lanes_in, lanes_out, n_pages)
+
+
+def _pool(pool: Optional[torch.Tensor], n_pages: int):
+    """(pointer, planes, bytes from plane to plane, bytes of a page) of a pool [planes, n_pages, ...]."""
+    if pool is None:
+        return None, 0, 0, 16
+    if pool.dim() < 2 or pool.shape[1] != n_pages or not pool[0].is_contiguous():
+        raise ValueError("pool must be [planes, n_pages, ...] with contiguous planes")
+    e = pool.element_size()
+    return pool.data_ptr(), pool.shape[0], pool.stride(0) * e, pool.stride(1) * e
+
+
+def _pages_work(work: Optional[torch.Tensor], lanes_in: int, lanes_out: int, n_pages: int, device):
+    if work is None:
+        work = torch.empty(lib().as_pages_work_bytes(lanes_in, lanes_out, n_pages), dtype=torch.uint8, device=device)
+    return work, work.numel() * work.element_size()
+
+
+def as_pages_fork(parent: torch.Tensor, table: torch.Tensor, length: torch.Tensor, ref: torch.Tensor, page_size: int,
+                  pool: Optional[torch.Tensor] = None, table_out: Optional[torch.Tensor] = None,
+                  length_out: Optional[torch.Tensor] = None, ref_out: Optional[torch.Tensor] = None,
+                  lane_status: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None, stream=None):
+    """(table, length, ref) in which lane i continues lane parent[i] (-1: nothing); pool [planes, n_pages, ...] is the
+    cache whose partly filled last pages are copied.  ref_out may be ref; the other outputs are new tensors."""
+    lanes, max_pages = table.shape
+    n = parent.numel()
+    if table_out is None:
+        table_out = torch.empty((n, max_pages), dtype=torch.int32, device=table.device)
+    if length_out is None:
+        length_out = torch.empty(n, dtype=torch.int32, device=table.device)
+    if ref_out is None:
+        ref_out = torch.empty_like(ref)
+    data, planes, stride, page_bytes = _pool(pool, ref.numel())
+    work, nbytes = _pages_work(work, lanes, n, ref.numel(), table.device)
+    _check(lib().as_pages_fork(_int32(parent, "parent"), lanes, n, max_pages, page_size, ref.numel(), _int32(table, "table"),
+                               _int32(length, "length", lanes), _int32(ref, "ref"),
+                               _int32(table_out, "table_out", n * max_pages), _int32(length_out, "length_out", n),
+                               _int32(ref_out, "ref_out", ref.numel()), data, planes, stride, page_bytes,
+                               _int32(lane_status, "lane_status", n), work.data_ptr(), nbytes, _stream(stream)))
+    return table_out, length_out, ref_out
+
+
+def as_pages_grow(add: torch.Tensor, table: torch.Tensor, length: torch.Tensor, ref: torch.Tensor, page_size: int,
+                  lane_status: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Give every lane the pages for add[lane] more tokens; table, length and ref are updated in place."""
+    lanes, max_pages = table.shape
+    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), table.device)
+    _check(lib().as_pages_grow(_int32(add, "add", lanes), lanes, max_pages, page_size, ref.numel(), _int32(table, "table"),
+                               _int32(length, "length", lanes), _int32(ref, "ref"),
+                               _int32(lane_status, "lane_status", lanes), work.data_ptr(), nbytes, _stream(stream)))
+
+
+def as_pages_compact(table: torch.Tensor, ref: torch.Tensor, pool: Optional[torch.Tensor] = None,
+                     table_out: Optional[torch.Tensor] = None, ref_out: Optional[torch.Tensor] = None,
+                     used: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Move the pages in use to the front of the pool; returns their number (int32 [] on the device).  Without
+    table_out / ref_out the table and the reference counts are updated in place."""
+    lanes, max_pages = table.shape
+    table_out = table if table_out is None else table_out
+    ref_out = ref if ref_out is None else ref_out
+    if used is None:
+        used = torch.empty((), dtype=torch.int32, device=table.device)
+    data, planes, stride, page_bytes = _pool(pool, ref.numel())
+    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), table.device)
+    _check(lib().as_pages_compact(lanes, max_pages, ref.numel(), _int32(table, "table"), _int32(ref, "ref"),
+                                  _int32(table_out, "table_out", table.numel()), _int32(ref_out, "ref_out", ref.numel()),
+                                  _int32(used, "used", 1), data, planes, stride, page_bytes, work.data_ptr(), nbytes,
+                                  _stream(stream)))
+    return used

@@ -1,5 +1,6 @@
 // C-ABI entry points (see include/arith_sampling.h) and the kernels behind them.
 #include "../../include/arith_sampling.h"
+#include "as_host.h"
 #include "as_stream.cuh"
 #include "as_nocut.cuh"
 #include "as_metrics.cuh"
@@ -31,7 +32,7 @@ static long long wait_cycles_now() {
     return k > 0 ? (long long)k * 1000 : ST_WAIT_CYCLES;
 }
 
-static int set_err(int code, const char* fmt, ...) {
+int set_err(int code, const char* fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(g_err, sizeof g_err, fmt, ap);
@@ -39,17 +40,13 @@ static int set_err(int code, const char* fmt, ...) {
     return code;
 }
 
-static int cuda_fail(cudaError_t e, const char* what) {
+int cuda_fail(cudaError_t e, const char* what) {
     return set_err(AS_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-struct DeviceInfo {
-    int sms = 0;
-    bool ok = false;
-};
 static DeviceInfo g_dev[64];
 
-static int device_info(const DeviceInfo** out) {
+int device_info(const DeviceInfo** out) {
     int dev = -1;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
@@ -70,8 +67,6 @@ using DiagPtrs = DiagOut;
 // ---------------------------------------------------------------------------
 // staged step kernel: launch shape
 // ---------------------------------------------------------------------------
-constexpr size_t SMEM_OPTIN_MAX = 232448;   // 227 KB per CTA on sm_100
-
 static size_t staged_fixed_bytes() { return (sizeof(StagedSmem<ST_NT>) + 127) & ~(size_t)127; }
 
 template <int DT, int CS>
@@ -514,6 +509,8 @@ static int grid_for(int lanes, int sms, int per_sm) {
     return (int)(lanes < cap ? lanes : cap);
 }
 
+ASX_BOUNDS_READER(bounds_step)
+
 }  // namespace asx
 
 using namespace asx;
@@ -544,9 +541,15 @@ int as_debug_counts(unsigned long long* h_out) {
 // checked builds only: the record of out-of-range indices (failures, first site, its index, its
 // bound) since the last reset
 int as_debug_bounds(int* h_out4, int reset) {
-    int zero[4] = {0, 0, 0, 0};
-    if (h_out4 && cudaMemcpyFromSymbol(h_out4, g_asx_bounds, sizeof(zero)) != cudaSuccess) return AS_ERR_CUDA;
-    if (reset && cudaMemcpyToSymbol(g_asx_bounds, zero, sizeof(zero)) != cudaSuccess) return AS_ERR_CUDA;
+    int (*const unit[])(int*, int) = {bounds_step, bounds_edit, bounds_cache4, bounds_pages};
+    int got[4] = {0, 0, 0, 0};
+    for (auto f : unit) {           // the failures of all units, the first one's place
+        int one[4] = {0, 0, 0, 0};
+        if (f(one, reset) != AS_OK) return AS_ERR_CUDA;
+        if (got[0] == 0) memcpy(got, one, sizeof got);
+        else got[0] += one[0];
+    }
+    if (h_out4) memcpy(h_out4, got, sizeof got);
     return AS_OK;
 }
 #endif

@@ -1,0 +1,174 @@
+// C-ABI entry points of the 4-bit cache and of attention over it.
+#include "as_attend.cuh"
+#include "as_cache4.cuh"
+
+#include <cmath>
+
+namespace asx {
+
+ASX_BOUNDS_READER(bounds_cache4)
+
+static int check_cache(const as_cache4* c) {
+    if (!c) return set_err(AS_ERR_INVALID_ARG, "cache is NULL");
+    if (c->n_pages < 1 || c->heads < 1) return set_err(AS_ERR_INVALID_ARG, "n_pages = %d and heads = %d must be >= 1", c->n_pages, c->heads);
+    if (c->head_dim != 64 && c->head_dim != 128) return set_err(AS_ERR_UNSUPPORTED, "head_dim = %d is not 64 or 128", c->head_dim);
+    if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128)
+        return set_err(AS_ERR_UNSUPPORTED, "page_size = %d is not 16, 32, 64 or 128", c->page_size);
+    if (!c->d_pages) return set_err(AS_ERR_INVALID_ARG, "d_pages is NULL");
+    if (reinterpret_cast<uintptr_t>(c->d_pages) & 15) return set_err(AS_ERR_INVALID_ARG, "d_pages is not 16-byte aligned");
+    return AS_OK;
+}
+
+static int check_lanes(int dtype, int lanes, int T, const void* table, int max_pages, const void* len, int page_size) {
+    if (dtype != AS_F32 && dtype != AS_BF16) return set_err(AS_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    if (lanes < 0) return set_err(AS_ERR_INVALID_ARG, "lanes = %d must be >= 0", lanes);
+    if (T < 1) return set_err(AS_ERR_INVALID_ARG, "T = %d must be >= 1", T);
+    if (max_pages < 1) return set_err(AS_ERR_INVALID_ARG, "max_pages = %d must be >= 1", max_pages);
+    if ((long long)max_pages * page_size > (1LL << 30) || (long long)lanes * T > (1LL << 30))
+        return set_err(AS_ERR_UNSUPPORTED, "max_pages * page_size and lanes * T must not exceed 2^30");
+    if (lanes > 0 && (!table || !len)) return set_err(AS_ERR_INVALID_ARG, "d_table or d_len is NULL");
+    return AS_OK;
+}
+
+static CacheArgs cache_args(const as_cache4* c, int lanes, int T, const int* table, int max_pages, const int* len, int* status) {
+    CacheArgs a;
+    a.pages = static_cast<char*>(c->d_pages);
+    a.n_pages = c->n_pages; a.heads = c->heads;
+    a.page_shift = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
+    a.k_scale = c->d_k_scale; a.v_scale = c->d_v_scale;
+    a.table = table; a.max_pages = max_pages; a.len = len; a.lane_status = status;
+    a.lanes = lanes; a.T = T;
+    return a;
+}
+
+static int clear_status(int* status, int lanes, cudaStream_t st) {
+    if (!status) return AS_OK;
+    const cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int) * (size_t)lanes, st);
+    return e == cudaSuccess ? AS_OK : cuda_fail(e, "lane status");
+}
+
+static unsigned grid_of(long long threads, int nt) {
+    const long long n = (threads + nt - 1) / nt;
+    return (unsigned)(n < (1 << 30) ? n : (1 << 30));
+}
+
+template <int DT, int D>
+static void launch_append(const CacheArgs& a, const void* k, long long k_ld, const void* v, long long v_ld, bool vec, cudaStream_t st) {
+    using E = typename Io<DT>::type;
+    const long long n = (long long)a.lanes * a.T * 2 * a.heads * (D / 16);
+    append_kernel<DT, D><<<grid_of(n, C4_NT), C4_NT, 0, st>>>(a, static_cast<const E*>(k), k_ld, static_cast<const E*>(v), v_ld, vec);
+}
+template <int DT, int D>
+static void launch_load(const CacheArgs& a, void* k, void* v, cudaStream_t st) {
+    using E = typename Io<DT>::type;
+    const long long n = (long long)a.lanes * a.T * 2 * a.heads * (D / 16);
+    load_kernel<DT, D><<<grid_of(n, C4_NT), C4_NT, 0, st>>>(a, static_cast<E*>(k), static_cast<E*>(v));
+}
+
+}  // namespace asx
+
+using namespace asx;
+
+extern "C" {
+
+size_t as_cache4_bytes(int n_pages, int heads, int head_dim, int page_size) {
+    if (n_pages < 1 || heads < 1 || head_dim < 1 || page_size < 1) return 0;
+    return (size_t)n_pages * heads * (page_size / 16) * 18 * head_dim;
+}
+
+int as_cache4_append(const as_cache4* cache, const void* d_k, long long k_ld, const void* d_v, long long v_ld, int dtype, int lanes,
+                     int T, const int32_t* d_table, int max_pages, const int32_t* d_len, int32_t* d_lane_status, void* stream) {
+    int rc = check_cache(cache);
+    if (rc != AS_OK) return rc;
+    if ((rc = check_lanes(dtype, lanes, T, d_table, max_pages, d_len, cache->page_size)) != AS_OK) return rc;
+    const long long row = (long long)cache->heads * cache->head_dim;
+    if (k_ld < row || v_ld < row) return set_err(AS_ERR_INVALID_ARG, "k_ld = %lld or v_ld = %lld is smaller than heads * head_dim = %lld", k_ld, v_ld, row);
+    if (lanes == 0) return AS_OK;
+    if (!d_k || !d_v) return set_err(AS_ERR_INVALID_ARG, "d_k or d_v is NULL");
+    const int es = dtype == AS_F32 ? 4 : 2;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(d_k) | reinterpret_cast<uintptr_t>(d_v);
+    if (at % es) return set_err(AS_ERR_INVALID_ARG, "d_k or d_v is not element-aligned");
+    const DeviceInfo* di;
+    if ((rc = device_info(&di)) != AS_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = clear_status(d_lane_status, lanes, st)) != AS_OK) return rc;
+    const bool vec = ((at | (uintptr_t)(k_ld * es) | (uintptr_t)(v_ld * es)) & 15) == 0;
+    const CacheArgs a = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
+    if (dtype == AS_F32) {
+        if (cache->head_dim == 64) launch_append<AS_F32, 64>(a, d_k, k_ld, d_v, v_ld, vec, st);
+        else launch_append<AS_F32, 128>(a, d_k, k_ld, d_v, v_ld, vec, st);
+    } else {
+        if (cache->head_dim == 64) launch_append<AS_BF16, 64>(a, d_k, k_ld, d_v, v_ld, vec, st);
+        else launch_append<AS_BF16, 128>(a, d_k, k_ld, d_v, v_ld, vec, st);
+    }
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? AS_OK : cuda_fail(e, "cache append kernel launch");
+}
+
+int as_cache4_load(const as_cache4* cache, void* d_k, void* d_v, int dtype, int lanes, int T, const int32_t* d_table, int max_pages,
+                   const int32_t* d_len, int32_t* d_lane_status, void* stream) {
+    int rc = check_cache(cache);
+    if (rc != AS_OK) return rc;
+    if ((rc = check_lanes(dtype, lanes, T, d_table, max_pages, d_len, cache->page_size)) != AS_OK) return rc;
+    if (lanes == 0) return AS_OK;
+    if (!d_k || !d_v) return set_err(AS_ERR_INVALID_ARG, "d_k or d_v is NULL");
+    if ((reinterpret_cast<uintptr_t>(d_k) | reinterpret_cast<uintptr_t>(d_v)) & 15) return set_err(AS_ERR_INVALID_ARG, "d_k or d_v is not 16-byte aligned");
+    const DeviceInfo* di;
+    if ((rc = device_info(&di)) != AS_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = clear_status(d_lane_status, lanes, st)) != AS_OK) return rc;
+    const CacheArgs a = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
+    if (dtype == AS_F32) {
+        if (cache->head_dim == 64) launch_load<AS_F32, 64>(a, d_k, d_v, st);
+        else launch_load<AS_F32, 128>(a, d_k, d_v, st);
+    } else {
+        if (cache->head_dim == 64) launch_load<AS_BF16, 64>(a, d_k, d_v, st);
+        else launch_load<AS_BF16, 128>(a, d_k, d_v, st);
+    }
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? AS_OK : cuda_fail(e, "cache load kernel launch");
+}
+
+size_t as_cache4_attend_work_bytes(const as_cache4* cache, int dtype, int lanes, int T, int q_heads, int N) {
+    (void)cache; (void)dtype; (void)lanes; (void)T; (void)q_heads; (void)N;
+    return 256;
+}
+
+int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, int dtype, int lanes, int T, int q_heads,
+                     const int32_t* d_table, int max_pages, const int32_t* d_len, double scale, int N, const int32_t* d_shared,
+                     void* d_out, float* d_lse, int32_t* d_lane_status, void* d_work, size_t work_bytes, void* stream) {
+    int rc = check_cache(cache);
+    if (rc != AS_OK) return rc;
+    if ((rc = check_lanes(dtype, lanes, T, d_table, max_pages, d_len, cache->page_size)) != AS_OK) return rc;
+    if (q_heads < 1 || q_heads % cache->heads) return set_err(AS_ERR_INVALID_ARG, "q_heads = %d must be a multiple of heads = %d", q_heads, cache->heads);
+    if (q_ld < (long long)q_heads * cache->head_dim) return set_err(AS_ERR_INVALID_ARG, "q_ld = %lld is smaller than q_heads * head_dim", q_ld);
+    if (!std::isfinite(scale)) return set_err(AS_ERR_INVALID_ARG, "scale must be finite");
+    if (N < 1 || lanes % N) return set_err(AS_ERR_INVALID_ARG, "N = %d must be >= 1 and divide lanes = %d", N, lanes);
+    if (lanes == 0) return AS_OK;
+    if (!d_q || !d_out) return set_err(AS_ERR_INVALID_ARG, "d_q or d_out is NULL");
+    const int es = dtype == AS_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(d_q) % es || (reinterpret_cast<uintptr_t>(d_out) & 15))
+        return set_err(AS_ERR_INVALID_ARG, "d_q is not element-aligned or d_out not 16-byte aligned");
+    const size_t need = as_cache4_attend_work_bytes(cache, dtype, lanes, T, q_heads, N);
+    if (!d_work || work_bytes < need) return set_err(AS_ERR_INVALID_ARG, "d_work of %zu bytes is needed", need);
+    if (reinterpret_cast<uintptr_t>(d_work) & 255) return set_err(AS_ERR_INVALID_ARG, "d_work is not 256-byte aligned");
+    const DeviceInfo* di;
+    if ((rc = device_info(&di)) != AS_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = clear_status(d_lane_status, lanes, st)) != AS_OK) return rc;
+    AttendArgs a;
+    a.c = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
+    a.q = d_q; a.q_ld = q_ld; a.q_heads = q_heads; a.scale = (float)scale; a.N = N; a.shared = d_shared; a.out = d_out; a.lse = d_lse;
+    const unsigned grid = grid_of((long long)lanes * T * q_heads, 4);
+    if (dtype == AS_F32) {
+        if (cache->head_dim == 64) attend_rows_kernel<AS_F32, 64><<<grid, 128, 0, st>>>(a);
+        else attend_rows_kernel<AS_F32, 128><<<grid, 128, 0, st>>>(a);
+    } else {
+        if (cache->head_dim == 64) attend_rows_kernel<AS_BF16, 64><<<grid, 128, 0, st>>>(a);
+        else attend_rows_kernel<AS_BF16, 128><<<grid, 128, 0, st>>>(a);
+    }
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? AS_OK : cuda_fail(e, "attention kernel launch");
+}
+
+}  // extern "C"

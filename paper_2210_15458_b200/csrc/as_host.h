@@ -1,0 +1,28 @@
+// Host-side helpers that the translation units share; defined in as_api.cu.
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace asx {
+
+int set_err(int code, const char* fmt, ...);        // records the calling thread's error text, returns code
+int cuda_fail(cudaError_t e, const char* what);     // the same for a CUDA runtime error
+
+struct DeviceInfo {
+    int sms = 0;
+    bool ok = false;
+};
+int device_info(const DeviceInfo** out);            // the current device's, looked up once
+
+constexpr size_t SMEM_OPTIN_MAX = 232448;           // 227 KB per CTA on sm_100
+
+// Checked builds: each translation unit keeps its own record of out-of-range indices; these copy
+// it out (failures, first site, index, bound) and reset it.
+#ifdef AS_BOUNDS_CHECK
+int bounds_edit(int* h_out4, int reset);
+int bounds_cache4(int* h_out4, int reset);
+int bounds_pages(int* h_out4, int reset);
+#endif
+
+}  // namespace asx
