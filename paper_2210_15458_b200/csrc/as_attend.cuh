@@ -1,8 +1,19 @@
 // Attention over the 4-bit cache.
+//
+// For a query row: o = sum_t softmax_t(scale q.k_t) v_t, taken tile by tile (16 tokens) with a running
+// maximum m and sum l:  o <- o 2^(m-m') + sum_t 2^(s_t-m') v_t, l likewise, scores s in units of log 2.
+// Two such states over different tokens join into one the same way, so the tokens of a row may be
+// split over warps, CTAs and passes.
 #pragma once
 #include "as_cache4.cuh"
 
 namespace asx {
+
+constexpr int AT_W = 4;                     // warps of a CTA; a unit of work is a tile of 16 tokens for each
+constexpr int AT_NT = 32 * AT_W;
+constexpr int AT_STAGES = 3;                // tiles that a warp has in flight or in use
+constexpr int AT_MAX_CTAS = 1024;
+constexpr float AT_LAZY = 8.f;              // the running maximum may lag by 8 (weights stay below 2^8, well within f16)
 
 struct AttendArgs {
     CacheArgs c;
@@ -10,68 +21,595 @@ struct AttendArgs {
     long long q_ld;
     int q_heads;
     float scale;
-    int N;
-    const int* shared;
     void* out;
     float* lse;
 };
 
-// One warp takes one query row (token, head): it walks the lane's tokens with the running maximum
-// and sum of a softmax; lane l of the warp holds dimensions l * D/32 and up.
-template <int DT, int D>
-__global__ void __launch_bounds__(128) attend_rows_kernel(const AttendArgs a) {
+// One pass over the cache.  An item is a set of query rows that read the same tokens of one head: the
+// rows of `group` lanes (1, or all N lanes of a group for their shared beginning) x T tokens x the
+// query heads of a key head, cut into row tiles of 8 * NT.  Items are ordered by lane (or group), then
+// head, then row tile; their units are dealt out to the CTAs in equal contiguous runs.
+struct PassArgs {
+    int n;                                  // lanes, or groups
+    int group;                              // lanes of an item
+    bool prefix;                            // tokens [0, begin[b]) of group b, else [begin[b / N], len) of lane b
+    int N;
+    const int* begin;                       // [lanes / N] usable shared lengths, or null (0)
+    int rows, row_tiles;
+    int* cum;                               // [n + 1] units of one (head, row tile) in front of lane b, written by CTA 0
+    float* part_item;                       // states of items that one CTA saw whole; null: it writes the output itself
+    float* part_cta;                        // [2 * gridDim] states of the others: a CTA's first and last item
+    int ctas;                               // gridDim of the pass
+};
+
+__device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad = nullptr) {
+    const int len = c.len[lane];
+    const bool b = len < 0 || len > ((long long)c.max_pages << c.page_shift);
+    if (bad) *bad = b;
+    return b ? 0 : len;
+}
+__device__ __forceinline__ void token_range(const CacheArgs& c, const PassArgs& p, int b, int& lo, int& hi) {
+    const int s = p.begin ? p.begin[p.prefix ? b : b / p.N] : 0;
+    lo = p.prefix ? 0 : s;
+    hi = p.prefix ? s : lane_len(c, b);
+}
+__device__ __forceinline__ int units_of(int lo, int hi) { return (hi - lo + 16 * AT_W - 1) / (16 * AT_W); }
+// the CTA of `ctas` <= U whose run holds unit x of U
+__device__ __forceinline__ int cta_of(long long x, long long U, int ctas) { return (int)(((x + 1) * ctas - 1) / U); }
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+__device__ __forceinline__ uint32_t mul_f16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t e4m3_f16x2(uint32_t two) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((unsigned short)two));
+    return d;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <class V> __device__ __forceinline__ V lds(uint32_t at);
+template <> __device__ __forceinline__ uint4 lds<uint4>(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+template <> __device__ __forceinline__ uint2 lds<uint2>(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+template <> __device__ __forceinline__ uint32_t lds<uint32_t>(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at));
+    return v;
+}
+template <> __device__ __forceinline__ unsigned short lds<unsigned short>(uint32_t at) {
+    unsigned short v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+    return v;
+}
+template <> __device__ __forceinline__ unsigned char lds<unsigned char>(uint32_t at) {
+    unsigned short v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=h"(v) : "r"(at));
+    return (unsigned char)v;
+}
+
+// Where a CTA stands in its run of units.
+struct Cursor {
+    int b, sub, u, nu, lo, hi;
+    __device__ void enter(const CacheArgs& c, const PassArgs& p) {
+        for (; b < p.n; ++b) {
+            token_range(c, p, b, lo, hi);
+            nu = units_of(lo, hi);
+            if (nu > 0) return;
+        }
+    }
+    __device__ void step(const CacheArgs& c, const PassArgs& p) {
+        if (++u < nu) return;
+        u = 0;
+        if (++sub < c.heads * p.row_tiles) return;
+        sub = 0;
+        ++b;
+        enter(c, p);
+    }
+};
+
+
+// A state as it is kept in scratch: rows x D sums, then m and l of each row.
+template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(int rows) { return rows * (D + 2); }
+
+// Each warp takes every fourth tile of the CTA's run.  Scores are formed transposed, S^T = K q^T (tokens
+// x rows, so that 16 x 16 keys go through one instruction whatever the number of rows up to 8), and
+// so is the output, O^T = V^T P^T.  Keys and values become f16 in registers: code x scale is exact
+// there; queries are scaled by a power of two to lie in f16's range (bf16: exact) or split in two f16
+// (32 bits).  Which dimension of a tile goes to which index of the products is free, and chosen so that a
+// thread's keys are 16 neighbouring bytes and its values the 16 dimensions of one block, which share
+// their scale.  Token l of the products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, const PassArgs p) {
     using Ti = Tile4<D>;
+    constexpr bool F32 = DT == AS_F32;
+    constexpr int PARTS = F32 ? 2 : 1;
+    constexpr int KS = D / 16;                      // steps of 16 dimensions
+    constexpr int PITCH = D + 20;                   // floats of a row in the joining buffer
+    __shared__ __align__(16) char ring[AT_W][AT_STAGES][Ti::BYTES];
+    __shared__ float join[AT_W][8][PITCH];
+    __shared__ float join_m[AT_W][8], join_l[AT_W][8];
+    __shared__ int sh_start[3], sh_warp[AT_W];
+    const CacheArgs& c = a.c;
+    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, r = lane >> 2, cc = lane & 3;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- the run: units [x0, x1) of all; the lane, head and row tile in which it starts ----
+    const int subs = c.heads * p.row_tiles;
+    const int per = (p.n + AT_NT - 1) / AT_NT, j0 = min(tid * per, p.n), j1 = min(j0 + per, p.n);
+    int mine = 0;
+    for (int j = j0; j < j1; ++j) {
+        int lo, hi;
+        token_range(c, p, j, lo, hi);
+        mine += units_of(lo, hi);
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) sh_warp[w] = incl;
+    __syncthreads();
+    int before = incl - mine, total = 0;
+#pragma unroll
+    for (int i = 0; i < AT_W; ++i) {
+        if (i < w) before += sh_warp[i];
+        total += sh_warp[i];
+    }
+    const long long U = (long long)total * subs;
+    const int G = (int)min((long long)p.ctas, U);   // no run is empty
+    const long long x0 = blockIdx.x < G ? U * blockIdx.x / G : 0, x1 = blockIdx.x < G ? U * (blockIdx.x + 1) / G : 0;
+    if (blockIdx.x == 0) {
+        int at = before;
+        for (int j = j0; j < j1; ++j) {
+            int lo, hi;
+            token_range(c, p, j, lo, hi);
+            p.cum[j] = at;
+            at += units_of(lo, hi);
+        }
+        if (tid == 0) p.cum[p.n] = total;
+    }
+    if (x0 >= x1) return;
+    {
+        long long at = (long long)before * subs;
+        for (int j = j0; j < j1; ++j) {
+            int lo, hi;
+            token_range(c, p, j, lo, hi);
+            const int nu = units_of(lo, hi);
+            if (x0 >= at && x0 < at + (long long)nu * subs) {
+                sh_start[0] = j;
+                sh_start[1] = (int)((x0 - at) / nu);
+                sh_start[2] = (int)((x0 - at) % nu);
+            }
+            at += (long long)nu * subs;
+        }
+    }
+    __syncthreads();
+    Cursor cu, ahead;
+    cu.b = sh_start[0]; cu.sub = sh_start[1]; cu.u = sh_start[2];
+    cu.enter(c, p);
+    ahead = cu;
+    const long long units = x1 - x0;
+
+    // ---- copies: tile `w` of a unit into the warp's ring, the page id fetched one unit before ----
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(&ring[w][0][0]);
+    const int page_mask = (1 << c.page_shift) - 1, tiles_per_page = 1 << (c.page_shift - 4);
+    int page = 0;
+    auto look = [&]() {                             // page id of the tile under `ahead`
+        const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
+        if (pos < ahead.hi) page = c.table[(size_t)(p.prefix ? ahead.b * p.N : ahead.b) * c.max_pages + (pos >> c.page_shift)];
+    };
+    auto issue = [&](int stage) {
+        const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
+        if (pos < ahead.hi) {
+            if (page < 0 || page >= c.n_pages) {
+                if (lane == 0 && c.lane_status) {
+                    const int l0 = p.prefix ? ahead.b * p.N : ahead.b;
+                    for (int j = 0; j < p.group; ++j) flag_lane(c.lane_status, l0 + j, AS_ERR_INVALID_ARG);
+                }
+                page = 0;
+            }
+            const char* src = c.pages + (((size_t)page * c.heads + ahead.sub / p.row_tiles) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
+            const uint32_t dst = ring0 + stage * Ti::BYTES;
+#pragma unroll
+            for (int i = 0; i < (Ti::BYTES / 16 + 31) / 32; ++i)
+                if (i * 32 + lane < Ti::BYTES / 16) cp_async16(dst + (i * 32 + lane) * 16, src + (i * 32 + lane) * 16);
+        }
+    };
+    long long issued = 0;
+    look();
+#pragma unroll
+    for (int s = 0; s < AT_STAGES - 1; ++s) {
+        if (issued < units) {
+            issue(s);
+            ++issued;
+            ahead.step(c, p);
+            if (issued < units) look();
+        }
+        cp_commit();
+    }
+
+    const int g = a.q_heads / c.heads;
+    using E = typename Io<DT>::type;
+    uint32_t qf[PARTS][NT][KS][2];
+    float o[NT][KS][4], m[NT][2], mu[NT][2], l[NT][2], k2[NT][2];
+    int lim[NT][2], lim_min = 0;
+    int seg_u0 = 0, stage = 0;
+    bool fresh = true;
+    for (long long x = x0; x < x1; ++x) {
+        if (fresh) {                                // ---- a new item: its query rows ----
+            fresh = false;
+            seg_u0 = cu.u;
+            const int head = cu.sub / p.row_tiles, row0 = (cu.sub % p.row_tiles) * 8 * NT;
+            const float kg = c.k_scale ? c.k_scale[head] : 1.f;
+            const float to_log2 = a.scale * kg * 1.44269504088896f;
+            lim_min = 0x7FFFFFFF;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int row = row0 + n * 8 + r;
+                float top = 0.f, xq[D / 4];
+#pragma unroll
+                for (int e = 0; e < D / 4; ++e) xq[e] = 0.f;
+                if (row < p.rows) {
+                    const int ln = (p.prefix ? cu.b * p.N : cu.b) + row / (c.T * g), t = row / g % c.T;
+                    const E* src = static_cast<const E*>(a.q) + ((long long)ln * c.T + t) * a.q_ld + (head * g + row % g) * D + cc * (D / 4);
+                    const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
+#pragma unroll
+                    for (int e = 0; e < D / 4; e += 16) Io<DT>::read16(src + e, vec, *reinterpret_cast<float(*)[16]>(&xq[e]));
+                }
+#pragma unroll
+                for (int e = 0; e < D / 4; ++e) top = fmaxf(top, fabsf(xq[e]));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                // the row's largest magnitude is brought into [1, 2)
+                int ex = (int)(__float_as_uint(top) >> 23) - 127;
+                ex = ex > 126 ? 126 : ex < -126 ? -126 : ex;
+                const float down = __uint_as_float((uint32_t)(127 - ex) << 23), up = __uint_as_float((uint32_t)(127 + ex) << 23);
+#pragma unroll
+                for (int j = 0; j < KS; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float f0 = xq[4 * j + 2 * h] * down, f1 = xq[4 * j + 2 * h + 1] * down;
+                        qf[0][n][j][h] = pack_f16(f0, f1);
+                        if (F32) {
+                            const float2 hi = unpack_f16(qf[0][n][j][h]);
+                            qf[PARTS - 1][n][j][h] = pack_f16(f0 - hi.x, f1 - hi.y);
+                        }
+                    }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int rw = row0 + n * 8 + 2 * cc + h;
+                    k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
+                    const int ln = (p.prefix ? cu.b * p.N : cu.b) + rw / (c.T * g);
+                    lim[n][h] = rw < p.rows ? min(lane_len(c, ln) - c.T + 1 + rw / g % c.T, cu.hi) : 0;
+                    if (rw < p.rows) lim_min = min(lim_min, lim[n][h]);
+                    m[n][h] = -INFINITY; mu[n][h] = 0.f; l[n][h] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < KS; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
+            }
+            lim_min = __reduce_min_sync(0xFFFFFFFFu, lim_min);
+        }
+        cp_wait<AT_STAGES - 2>();
+        __syncwarp();
+        if (issued < units) {
+            int into = stage + AT_STAGES - 1;
+            if (into >= AT_STAGES) into -= AT_STAGES;
+            issue(into);
+            ++issued;
+            ahead.step(c, p);
+            if (issued < units) look();
+        }
+        cp_commit();
+        const int pos = cu.lo + (cu.u * AT_W + w) * 16;
+        if (pos < cu.hi) {
+            const uint32_t st = ring0 + stage * Ti::BYTES;
+            // ---- S^T = K q^T ----
+            const int t0 = 4 * (r >> 1) + (r & 1);      // the thread's tokens: t0 and t0 + 2
+            uint32_t kw[2][D / 32], ks[2][D / 64];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int t = t0 + 2 * i;
+                if (D == 128) {
+                    const uint4 v = lds<uint4>(st + Ti::K + t * (D / 2) + cc * 16);
+                    kw[i][0] = v.x; kw[i][1] = v.y; kw[i][D / 32 - 2] = v.z; kw[i][D / 32 - 1] = v.w;
+                    const uint32_t s2 = e4m3_f16x2(lds<unsigned short>(st + Ti::KS + t * Ti::NB + 2 * cc));
+                    ks[i][0] = __byte_perm(s2, s2, 0x1010);
+                    ks[i][D / 64 - 1] = __byte_perm(s2, s2, 0x3232);
+                } else {
+                    const uint2 v = lds<uint2>(st + Ti::K + t * (D / 2) + cc * 8);
+                    kw[i][0] = v.x; kw[i][1] = v.y;
+                    const uint32_t s2 = e4m3_f16x2(lds<unsigned char>(st + Ti::KS + t * Ti::NB + cc));
+                    ks[i][0] = __byte_perm(s2, s2, 0x1010);
+                }
+            }
+            float s[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+            for (int j = 0; j < KS; ++j) {
+                uint32_t f[4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        f[2 * h + i] = mul_f16(codes_f16x2(kw[i][j / 2] >> (16 * (j & 1) + 8 * h)), ks[i][j / 4]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    mma_f16(s[n], f[0], f[1], f[2], f[3], qf[0][n][j][0], qf[0][n][j][1]);
+                    if (F32) mma_f16(s[n], f[0], f[1], f[2], f[3], qf[PARTS - 1][n][j][0], qf[PARTS - 1][n][j][1]);
+                }
+            }
+            // ---- weights ----
+            bool rise = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    s[n][h] *= k2[n][h];
+                    s[n][2 + h] *= k2[n][h];
+                    if (pos + 16 > lim_min) {
+                        if (pos + t0 >= lim[n][h]) s[n][h] = -INFINITY;
+                        if (pos + t0 + 2 >= lim[n][h]) s[n][2 + h] = -INFINITY;
+                    }
+                    rise |= fmaxf(s[n][h], s[n][2 + h]) > m[n][h] + AT_LAZY;
+                }
+            if (__any_sync(0xFFFFFFFFu, rise)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float top = fmaxf(s[n][h], s[n][2 + h]);
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                        top = fmaxf(top, m[n][h]);
+                        const float f = top == -INFINITY ? 1.f : ex2(m[n][h] - top);
+                        m[n][h] = top;
+                        mu[n][h] = top == -INFINITY ? 0.f : top;
+                        l[n][h] *= f;
+#pragma unroll
+                        for (int i = 0; i < KS; ++i) { o[n][i][h] *= f; o[n][i][2 + h] *= f; }
+                    }
+            }
+            uint32_t pf[PARTS][NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float pr[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pr[e] = ex2(s[n][e] - mu[n][e & 1]);
+                l[n][0] += pr[0] + pr[2];
+                l[n][1] += pr[1] + pr[3];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t hi = pack_f16(pr[2 * i], pr[2 * i + 1]);
+                    pf[0][n][i] = transpose8x8(hi);
+                    if (F32) {
+                        const float2 h2 = unpack_f16(hi);
+                        pf[PARTS - 1][n][i] = transpose8x8(pack_f16(pr[2 * i] - h2.x, pr[2 * i + 1] - h2.y));
+                    }
+                }
+            }
+            // ---- O^T += V^T P^T ----
+            uint32_t vw[4][D / 64];                 // tokens 4 cc .. 4 cc + 3, the thread's D / 8 dimensions
+            const uint32_t vb = st + Ti::V + (D == 128 ? r : r >> 1) * 128 + cc * 32;
+            const bool odd = r & 1;
+            {
+                // (odd r reads its two halves in the other order: no two threads of a phase meet in a bank)
+                const bool swap = D == 128 && odd;
+                const uint4 x0v = lds<uint4>(vb + (swap ? 16 : 0)), x1v = lds<uint4>(vb + (swap ? 0 : 16));
+                const uint4 v0 = swap ? x1v : x0v, v1 = swap ? x0v : x1v;
+                if (D == 128) {
+                    vw[0][0] = v0.x; vw[0][D / 64 - 1] = v0.y; vw[1][0] = v0.z; vw[1][D / 64 - 1] = v0.w;
+                    vw[2][0] = v1.x; vw[2][D / 64 - 1] = v1.y; vw[3][0] = v1.z; vw[3][D / 64 - 1] = v1.w;
+                } else {
+                    vw[0][0] = odd ? v0.y : v0.x; vw[1][0] = odd ? v0.w : v0.z;
+                    vw[2][0] = odd ? v1.y : v1.x; vw[3][0] = odd ? v1.w : v1.z;
+                }
+            }
+            uint32_t vs4 = lds<uint32_t>(st + Ti::VS + (D == 128 ? r : r >> 1) * 16 + cc * 4);
+            if (pos + 16 > cu.hi) {                 // tokens behind the last one: whatever the page holds there counts as zero
+                const int have = cu.hi - pos - 4 * cc;
+                vs4 &= have >= 4 ? 0xFFFFFFFFu : have <= 0 ? 0u : (1u << (8 * have)) - 1;
+            }
+            const uint32_t vs[2] = {e4m3_f16x2(vs4 & 0xFFFFu), e4m3_f16x2(vs4 >> 16)};
+#pragma unroll
+            for (int i4 = 0; i4 < D / 64; ++i4) {
+                uint32_t even[2], oddw[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t x = vw[2 * h][i4], y = vw[2 * h + 1][i4];
+                    even[h] = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u);
+                    oddw[h] = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t f0 = mul_f16(codes_f16x2(even[0] >> (8 * i)), vs[0]), f1 = mul_f16(codes_f16x2(oddw[0] >> (8 * i)), vs[0]);
+                    const uint32_t f2 = mul_f16(codes_f16x2(even[1] >> (8 * i)), vs[1]), f3 = mul_f16(codes_f16x2(oddw[1] >> (8 * i)), vs[1]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[0][n][0], pf[0][n][1]);
+                        if (F32) mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[PARTS - 1][n][0], pf[PARTS - 1][n][1]);
+                    }
+                }
+            }
+        }
+        __syncwarp();
+        if (++stage == AT_STAGES) stage = 0;
+
+        // ---- the end of an item, or of the run: the four warps' states become one ----
+        const bool item_ends = cu.u + 1 == cu.nu;
+        if (item_ends || x + 1 == x1) {
+            const int head = cu.sub / p.row_tiles, rt = cu.sub % p.row_tiles;
+            const bool whole = item_ends && seg_u0 == 0;
+            float* part = nullptr;
+            if (!whole) part = p.part_cta + (size_t)(2 * blockIdx.x + (seg_u0 == 0)) * state_floats<D>(8 * NT);
+            else if (p.part_item) part = p.part_item + ((size_t)cu.b * subs + cu.sub) * state_floats<D>(8 * NT);
+            const float vg = c.v_scale ? c.v_scale[head] : 1.f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float sum = l[n][h];
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+                    if (r == 0) { join_m[w][2 * cc + h] = m[n][h]; join_l[w][2 * cc + h] = sum; }
+#pragma unroll
+                    for (int i = 0; i < KS; ++i)
+                        *reinterpret_cast<float2*>(&join[w][2 * cc + h][r * (D / 8 + 2) + 2 * i]) = make_float2(o[n][i][h], o[n][i][2 + h]);
+                }
+                __syncthreads();
+                constexpr int PER = D / 16;         // dimensions of a thread; 16 threads a row
+                const int rw = tid >> 4, d0 = (tid & 15) * PER;
+                float f[AT_W], M = -INFINITY, L = 0.f, acc[PER];
+#pragma unroll
+                for (int i = 0; i < AT_W; ++i) M = fmaxf(M, join_m[i][rw]);
+#pragma unroll
+                for (int i = 0; i < AT_W; ++i) {
+                    f[i] = join_m[i][rw] == -INFINITY ? 0.f : ex2(join_m[i][rw] - M);
+                    L += f[i] * join_l[i][rw];
+                }
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    acc[e] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < AT_W; ++i) acc[e] += f[i] * join[i][rw][(d0 / (D / 8)) * (D / 8 + 2) + d0 % (D / 8) + e];
+                }
+                const int row = rt * 8 * NT + n * 8 + rw;
+                if (part) {
+                    float* at = part + (n * 8 + rw) * D + d0;
+#pragma unroll
+                    for (int e = 0; e < PER; e += 4) *reinterpret_cast<float4*>(at + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+                    if (d0 == 0) { part[8 * NT * D + n * 8 + rw] = M; part[8 * NT * (D + 1) + n * 8 + rw] = L; }
+                } else if (row < p.rows) {
+                    const float inv = L > 0.f ? vg / L : 0.f;
+                    const int ln = cu.b + row / (c.T * g), t = row / g % c.T;
+                    const size_t orow = ((size_t)ln * c.T + t) * a.q_heads + head * g + row % g;
+                    E* at = static_cast<E*>(a.out) + orow * D + d0;
+#pragma unroll
+                    for (int e = 0; e < PER; e += 2) {
+                        if constexpr (F32) *reinterpret_cast<float2*>(at + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
+                        else *reinterpret_cast<__nv_bfloat162*>(at + e) = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
+                    }
+                    if (a.lse && d0 == 0) a.lse[orow] = L > 0.f ? 0.693147180559945f * (M + log2f(L)) : -INFINITY;
+                }
+                __syncthreads();
+            }
+            fresh = true;
+        }
+        cu.step(c, p);
+    }
+}
+
+// The states of row (item, row within its tile) of a pass, joined into (M, L, acc[PER]) of a warp's
+// thread (PER = D / 32 neighbouring dimensions).  Returns false where the pass has written the output.
+template <int D>
+__device__ __forceinline__ bool gather_states(const CacheArgs& c, const PassArgs& p, int tile_rows, int b, int sub, int rw, int lane, float& M, float& L,
+                                              float (&acc)[D / 32]) {
+    constexpr int PER = D / 32;
+    const int subs = c.heads * p.row_tiles;
+    const int at = p.cum[b], nu = p.cum[b + 1] - at;
+    if (nu == 0) return true;
+    const long long U = (long long)p.cum[p.n] * subs, x0 = (long long)at * subs + (long long)sub * nu;
+    const int G = (int)min((long long)p.ctas, U);
+    const int c0 = cta_of(x0, U, G), c1 = cta_of(x0 + nu - 1, U, G);
+    if (c0 == c1 && !p.part_item) return false;
+    for (int k = c0; k <= c1; ++k) {
+        const float* s;
+        if (c0 == c1) s = p.part_item + ((size_t)b * subs + sub) * state_floats<D>(tile_rows);
+        else s = p.part_cta + (size_t)(2 * k + (U * k / G <= x0)) * state_floats<D>(tile_rows);
+        const float m2 = s[tile_rows * D + rw], l2 = s[tile_rows * (D + 1) + rw];
+        const float top = fmaxf(M, m2);
+        const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
+        L = L * f + l2 * f2;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) acc[e] = acc[e] * f + s[rw * D + lane * PER + e] * f2;
+        M = top;
+    }
+    return true;
+}
+
+// One warp per output row: joins the states of the rows that were split over CTAs or passes, in a
+// fixed order, and writes rows that saw nothing.
+template <int DT, int D>
+__global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs a, const PassArgs own, int own_rows, const PassArgs pre, int pre_rows) {
     constexpr int PER = D / 32;
     const CacheArgs& c = a.c;
-    const int l = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, g = a.q_heads / c.heads;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const long long rows = (long long)c.lanes * c.T * a.q_heads;
-    for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); r < rows; r += (long long)gridDim.x * 4) {
-        const int h = (int)(r % a.q_heads);
-        const long long row = r / a.q_heads;
-        const int lane = (int)(row / c.T), tok = (int)(row % c.T);
-        const int head = h / (a.q_heads / c.heads);
-        int len = c.len[lane];
-        if (len < 0 || len > ((long long)c.max_pages << c.page_shift)) { if (l == 0) flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG); len = 0; }
-        const int limit = len - c.T + 1 + tok;
-        const typename Io<DT>::type* q = reinterpret_cast<const typename Io<DT>::type*>(a.q) + row * a.q_ld + h * D + l * PER;
-        const float kg = c.k_scale ? c.k_scale[head] : 1.f, vg = c.v_scale ? c.v_scale[head] : 1.f;
-        float x[PER], o[PER], m = -INFINITY, sum = 0.f;
+    for (long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * 4) {
+        const int hq = (int)(i % a.q_heads), t = (int)(i / a.q_heads % c.T), ln = (int)(i / a.q_heads / c.T);
+        const int head = hq / g;
+        float M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) { x[e] = (float)q[e] * (a.scale * kg); o[e] = 0.f; }
-        const int b = l * PER / 16, inb = l * PER % 16;
-        for (int p = 0; p < limit; ++p) {
-            bool bad = false;
-            const char* tile = tile_of<D>(c, lane, head, p, bad);
-            if (bad) {
-                if (l == 0) flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG);
-                tile = c.pages + ((size_t)head * (1 << (c.page_shift - 4)) + ((p & ((1 << c.page_shift) - 1)) >> 4)) * Ti::BYTES;
-            }
-            const int t = p & 15;
-            const float ks = e4m3_value((uint8_t)tile[Ti::k_scale(t, b)]), vs = e4m3_value((uint8_t)tile[Ti::v_scale(t, b)]);
-            float s = 0.f, val[PER];
-#pragma unroll
-            for (int e = 0; e < PER; e += 2) {
-                const uint32_t kh = codes_f16x2((uint8_t)tile[Ti::k_code(t, b) + (inb + e) / 2]);
-                const uint32_t vh = codes_f16x2((uint8_t)tile[Ti::v_code(t, b) + (inb + e) / 2]);
-                const float2 kf = __half22float2(*reinterpret_cast<const __half2*>(&kh));
-                const float2 vf = __half22float2(*reinterpret_cast<const __half2*>(&vh));
-                s += x[e] * kf.x + x[e + 1] * kf.y;
-                val[e] = vf.x * vs; val[e + 1] = vf.y * vs;
-            }
-            s *= ks;
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-            const float m2 = fmaxf(m, s), f = __expf(m - m2), w = __expf(s - m2);
-            sum = sum * f + w;
-#pragma unroll
-            for (int e = 0; e < PER; ++e) o[e] = o[e] * f + w * val[e];
-            m = m2;
+        for (int e = 0; e < PER; ++e) acc[e] = 0.f;
+        if (pre.begin) {
+            const int row = ((ln % pre.N) * c.T + t) * g + hq % g;
+            gather_states<D>(c, pre, pre_rows, ln / pre.N, head * pre.row_tiles + row / pre_rows, row % pre_rows, lane, M, L, acc);
         }
-        const float inv = sum > 0.f ? vg / sum : 0.f;
-        typename Io<DT>::type* out = reinterpret_cast<typename Io<DT>::type*>(a.out) + r * D + l * PER;
+        const int row = t * g + hq % g;
+        if (!gather_states<D>(c, own, own_rows, ln, head * own.row_tiles + row / own_rows, row % own_rows, lane, M, L, acc)) continue;
+        const float inv = L > 0.f ? (c.v_scale ? c.v_scale[head] : 1.f) / L : 0.f;
+        typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + i * D + lane * PER;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) out[e] = o[e] * inv;
-        if (a.lse && l == 0) a.lse[r] = sum > 0.f ? m + logf(sum) : -INFINITY;
+        for (int e = 0; e < PER; ++e) out[e] = acc[e] * inv;
+        if (a.lse && lane == 0) a.lse[i] = L > 0.f ? 0.693147180559945f * (M + log2f(L)) : -INFINITY;
+    }
+}
+
+// One CTA per group: the shared beginning that can be used (0 where the caller's does not fit).
+__global__ void __launch_bounds__(128) attend_shared_kernel(const CacheArgs c, int N, const int* shared, int* begin) {
+    const int gr = blockIdx.x, s = shared[gr];
+    bool ok = s > 0 && (s & ((1 << c.page_shift) - 1)) == 0;
+    for (int j = threadIdx.x; j < N; j += 128) ok &= s <= lane_len(c, gr * N + j);
+    ok = __syncthreads_and(ok);
+    if (threadIdx.x == 0) begin[gr] = ok ? s : 0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// Lanes whose length is out of range.
+__global__ void __launch_bounds__(256) attend_status_kernel(const CacheArgs c) {
+    for (int j = blockIdx.x * 256 + threadIdx.x; j < c.lanes; j += gridDim.x * 256) {
+        bool bad;
+        lane_len(c, j, &bad);
+        c.lane_status[j] = bad ? AS_ERR_INVALID_ARG : AS_OK;
     }
 }
 

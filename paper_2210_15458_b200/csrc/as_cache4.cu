@@ -65,6 +65,106 @@ static void launch_load(const CacheArgs& a, void* k, void* v, cudaStream_t st) {
     load_kernel<DT, D><<<grid_of(n, C4_NT), C4_NT, 0, st>>>(a, static_cast<E*>(k), static_cast<E*>(v));
 }
 
+// ---------------------------------------------------------------------------
+// attention: passes and scratch
+// ---------------------------------------------------------------------------
+struct AttendPlan {
+    int own_nt, pre_nt;             // row tiles of 8 * nt rows, in the lanes' own pass and in that over shared beginnings
+    PassArgs own, pre;
+    int* begin;
+    size_t bytes;
+};
+
+static int rows_nt(int dtype, int rows) { return dtype == AS_F32 || rows <= 8 ? 1 : 2; }
+
+// The shapes of the passes and where their scratch lies in d_work (sizes alone if d_work is null).
+// Scratch for the pass over shared beginnings is there whenever N > 1.
+static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_heads, int D, int N, void* d_work) {
+    AttendPlan pl = {};
+    const int g = q_heads / heads;
+    char* base = static_cast<char*>(d_work);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char* q = base ? base + at : nullptr;
+        at += (bytes + 255) & ~(size_t)255;
+        return q;
+    };
+    pl.begin = reinterpret_cast<int*>(take(sizeof(int) * (size_t)(lanes / N)));
+    auto pass = [&](PassArgs& p, int& nt, int n, int group, bool prefix) {
+        p.n = n; p.group = group; p.prefix = prefix; p.N = N;
+        p.rows = group * T * g;
+        nt = rows_nt(dtype, p.rows);
+        p.row_tiles = (p.rows + 8 * nt - 1) / (8 * nt);
+        p.cum = reinterpret_cast<int*>(take(sizeof(int) * (size_t)(n + 1)));
+        const size_t state = sizeof(float) * 8 * (size_t)nt * (D + 2);
+        p.part_cta = reinterpret_cast<float*>(take(2 * AT_MAX_CTAS * state));
+        if (N > 1) p.part_item = reinterpret_cast<float*>(take((size_t)n * heads * p.row_tiles * state));
+    };
+    pass(pl.own, pl.own_nt, lanes, 1, false);
+    if (N > 1) pass(pl.pre, pl.pre_nt, lanes / N, N, true);
+    pl.bytes = at;
+    return pl;
+}
+
+template <class K, class... A>
+static cudaError_t launch_after(K kern, unsigned grid, unsigned block, cudaStream_t st, A... args) {
+    // the kernel waits for its predecessor's results itself (griddepcontrol.wait), so its launch may overlap it
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+template <int DT, int D, int NT>
+static cudaError_t launch_pass(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
+    static int per_sm[64] = {0};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    auto kern = attend_mma_kernel<DT, D, NT>;
+    if (per_sm[dev] == 0) {
+        int n = 0;
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, AT_NT, 0);
+        if (e != cudaSuccess) return e;
+        per_sm[dev] = n > 0 ? n : 1;
+    }
+    p.ctas = per_sm[dev] * sms < AT_MAX_CTAS ? per_sm[dev] * sms : AT_MAX_CTAS;
+    return launch_after(kern, p.ctas, AT_NT, st, a, p);
+}
+
+template <int DT, int D>
+static cudaError_t launch_pass(const AttendArgs& a, PassArgs& p, int nt, int sms, cudaStream_t st) {
+    if constexpr (DT == AS_BF16) {
+        if (nt == 2) return launch_pass<DT, D, 2>(a, p, sms, st);
+    }
+    return launch_pass<DT, D, 1>(a, p, sms, st);
+}
+
+template <int DT, int D>
+static int launch_attend(const AttendArgs& a, int N, const int* shared, void* work, int sms, cudaStream_t st) {
+    AttendPlan pl = plan_attend(DT, a.c.lanes, a.c.T, a.c.heads, a.q_heads, D, N, work);
+    cudaError_t e = cudaSuccess;
+    if (shared && N > 1) {
+        attend_shared_kernel<<<a.c.lanes / N, 128, 0, st>>>(a.c, N, shared, pl.begin);
+        pl.own.begin = pl.pre.begin = pl.begin;
+        e = launch_pass<DT, D>(a, pl.pre, pl.pre_nt, sms, st);
+        if (e != cudaSuccess) return cuda_fail(e, "attention kernel launch (shared beginnings)");
+    } else {
+        pl.own.part_item = nullptr;
+    }
+    e = launch_pass<DT, D>(a, pl.own, pl.own_nt, sms, st);
+    if (e != cudaSuccess) return cuda_fail(e, "attention kernel launch");
+    const long long rows = (long long)a.c.lanes * a.c.T * a.q_heads, want = (rows + 3) / 4;
+    const unsigned grid = (unsigned)(want < 64 * sms ? want : 64 * sms);
+    e = launch_after(attend_join_kernel<DT, D>, grid, 128, st, a, pl.own, 8 * pl.own_nt, pl.pre, 8 * pl.pre_nt);
+    return e == cudaSuccess ? AS_OK : cuda_fail(e, "attention join kernel launch");
+}
+
 }  // namespace asx
 
 using namespace asx;
@@ -130,8 +230,8 @@ int as_cache4_load(const as_cache4* cache, void* d_k, void* d_v, int dtype, int 
 }
 
 size_t as_cache4_attend_work_bytes(const as_cache4* cache, int dtype, int lanes, int T, int q_heads, int N) {
-    (void)cache; (void)dtype; (void)lanes; (void)T; (void)q_heads; (void)N;
-    return 256;
+    if (!cache || cache->heads < 1 || lanes < 0 || T < 1 || q_heads < cache->heads || N < 1) return 0;
+    return plan_attend(dtype, lanes, T, cache->heads, q_heads, cache->head_dim, N, nullptr).bytes;
 }
 
 int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, int dtype, int lanes, int T, int q_heads,
@@ -155,20 +255,12 @@ int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, in
     const DeviceInfo* di;
     if ((rc = device_info(&di)) != AS_OK) return rc;
     cudaStream_t st = (cudaStream_t)stream;
-    if ((rc = clear_status(d_lane_status, lanes, st)) != AS_OK) return rc;
     AttendArgs a;
     a.c = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
-    a.q = d_q; a.q_ld = q_ld; a.q_heads = q_heads; a.scale = (float)scale; a.N = N; a.shared = d_shared; a.out = d_out; a.lse = d_lse;
-    const unsigned grid = grid_of((long long)lanes * T * q_heads, 4);
-    if (dtype == AS_F32) {
-        if (cache->head_dim == 64) attend_rows_kernel<AS_F32, 64><<<grid, 128, 0, st>>>(a);
-        else attend_rows_kernel<AS_F32, 128><<<grid, 128, 0, st>>>(a);
-    } else {
-        if (cache->head_dim == 64) attend_rows_kernel<AS_BF16, 64><<<grid, 128, 0, st>>>(a);
-        else attend_rows_kernel<AS_BF16, 128><<<grid, 128, 0, st>>>(a);
-    }
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? AS_OK : cuda_fail(e, "attention kernel launch");
+    a.q = d_q; a.q_ld = q_ld; a.q_heads = q_heads; a.scale = (float)scale; a.out = d_out; a.lse = d_lse;
+    if (d_lane_status) attend_status_kernel<<<grid_of(lanes, 256), 256, 0, st>>>(a.c);
+    if (dtype == AS_F32) return cache->head_dim == 64 ? launch_attend<AS_F32, 64>(a, N, d_shared, d_work, di->sms, st) : launch_attend<AS_F32, 128>(a, N, d_shared, d_work, di->sms, st);
+    return cache->head_dim == 64 ? launch_attend<AS_BF16, 64>(a, N, d_shared, d_work, di->sms, st) : launch_attend<AS_BF16, 128>(a, N, d_shared, d_work, di->sms, st);
 }
 
 }  // extern "C"
