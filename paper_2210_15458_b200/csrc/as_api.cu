@@ -27,7 +27,7 @@ struct Tune {
 static Tune g_tune_path, g_tune_cluster, g_tune_ctas, g_tune_stages, g_tune_minb, g_tune_serial,
     g_tune_wait_kcycles, g_tune_no_copy, g_tune_radix_nucleus;
 
-static long long wait_cycles_now() {
+long long wait_cycles_now() {
     const int k = g_tune_wait_kcycles;
     return k > 0 ? (long long)k * 1000 : ST_WAIT_CYCLES;
 }

@@ -27,19 +27,21 @@ struct AttendArgs {
 
 // One pass over the cache.  An item is a set of query rows that read the same tokens of one head: the
 // rows of `group` lanes (1, or all N lanes of a group for their shared beginning) x T tokens x the
-// query heads of a key head, cut into row tiles of 8 * NT.  Items are ordered by lane (or group), then
-// head, then row tile; their units are dealt out to the CTAs in equal contiguous runs.
+// query heads of a key head, cut into row tiles of tile_rows.  Items are ordered by entry (lane or
+// group, row tile), then head; their units (`unit` tokens each) are dealt out to the CTAs in equal
+// contiguous runs.
 struct PassArgs {
     int n;                                  // lanes, or groups
     int group;                              // lanes of an item
     bool prefix;                            // tokens [0, begin[b]) of group b, else [begin[b / N], len) of lane b
     int N;
     const int* begin;                       // [lanes / N] usable shared lengths, or null (0)
-    int rows, row_tiles;
-    int* cum;                               // [n + 1] units of one (head, row tile) in front of lane b, written by CTA 0
+    int rows, tile_rows, row_tiles, unit;
+    int* cum;                               // [n * row_tiles + 1] units of one head in front of an entry, written by CTA 0
     float* part_item;                       // states of items that one CTA saw whole; null: it writes the output itself
-    float* part_cta;                        // [2 * gridDim] states of the others: a CTA's first and last item
-    int ctas;                               // gridDim of the pass
+    float* part_cta;                        // [2 * ctas] states of the others: a CTA's first and last item
+    int ctas;
+    long long wait_cycles;
 };
 
 __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad = nullptr) {
@@ -48,14 +50,102 @@ __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad 
     if (bad) *bad = b;
     return b ? 0 : len;
 }
-__device__ __forceinline__ void token_range(const CacheArgs& c, const PassArgs& p, int b, int& lo, int& hi) {
+// the tokens [lo, hi) that the rows of an entry read; behind a tile's last row nothing is seen
+__device__ __forceinline__ void token_range(const CacheArgs& c, const PassArgs& p, int g, int entry, int& lo, int& hi) {
+    const int b = p.row_tiles == 1 ? entry : entry / p.row_tiles;
     const int s = p.begin ? p.begin[p.prefix ? b : b / p.N] : 0;
     lo = p.prefix ? 0 : s;
     hi = p.prefix ? s : lane_len(c, b);
+    if (!p.prefix && c.T > 1) {
+        const int last = min(p.rows, (entry % p.row_tiles + 1) * p.tile_rows) - 1;
+        hi = max(lo, hi - c.T + 1 + last / g);
+    }
 }
-__device__ __forceinline__ int units_of(int lo, int hi) { return (hi - lo + 16 * AT_W - 1) / (16 * AT_W); }
+__device__ __forceinline__ int units_of(const PassArgs& p, int lo, int hi) { return (hi - lo + p.unit - 1) / p.unit; }
 // the CTA of `ctas` <= U whose run holds unit x of U
 __device__ __forceinline__ int cta_of(long long x, long long U, int ctas) { return (int)(((x + 1) * ctas - 1) / U); }
+
+// Where a CTA stands in its run of units.
+struct Cursor {
+    int entry, head, u, nu, lo, hi;
+    __device__ void enter(const CacheArgs& c, const PassArgs& p, int g) {
+        for (; entry < p.n * p.row_tiles; ++entry) {
+            token_range(c, p, g, entry, lo, hi);
+            nu = units_of(p, lo, hi);
+            if (nu > 0) return;
+        }
+    }
+    __device__ void next_item(const CacheArgs& c, const PassArgs& p, int g) {
+        u = 0;
+        if (++head < c.heads) return;
+        head = 0;
+        ++entry;
+        enter(c, p, g);
+    }
+    __device__ void step(const CacheArgs& c, const PassArgs& p, int g) {
+        if (++u == nu) next_item(c, p, g);
+    }
+    __device__ int row_of_table(const PassArgs& p) const { return p.prefix ? entry / p.row_tiles * p.N : entry / p.row_tiles; }
+};
+
+// The CTA's run [x0, x1) and where it starts; called by all NT threads.
+struct RunSmem {
+    int warp_sum[32];
+    int start[3];
+};
+template <int NT>
+__device__ bool find_run(const CacheArgs& c, const PassArgs& p, int g, RunSmem& sm, long long& x0, long long& x1, Cursor& cu) {
+    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, n = p.n * p.row_tiles;
+    const int per = (n + NT - 1) / NT, j0 = min(tid * per, n), j1 = min(j0 + per, n);
+    auto units = [&](int j) {
+        int lo, hi;
+        token_range(c, p, g, j, lo, hi);
+        return units_of(p, lo, hi);
+    };
+    int mine = 0;
+    for (int j = j0; j < j1; ++j) mine += units(j);
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) sm.warp_sum[w] = incl;
+    __syncthreads();
+    int before = incl - mine, total = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) {
+        if (i < w) before += sm.warp_sum[i];
+        total += sm.warp_sum[i];
+    }
+    const long long U = (long long)total * c.heads;
+    const int G = (int)min((long long)p.ctas, U);   // no run is empty
+    if (blockIdx.x == 0) {
+        int at = before;
+        for (int j = j0; j < j1; ++j) {
+            p.cum[j] = at;
+            at += units(j);
+        }
+        if (tid == 0) p.cum[n] = total;
+    }
+    if (blockIdx.x >= G) return false;
+    x0 = U * blockIdx.x / G;
+    x1 = U * (blockIdx.x + 1) / G;
+    long long at = (long long)before * c.heads;
+    for (int j = j0; j < j1; ++j) {
+        const int nu = units(j);
+        if (x0 >= at && x0 < at + (long long)nu * c.heads) {
+            sm.start[0] = j;
+            sm.start[1] = (int)((x0 - at) / nu);
+            sm.start[2] = (int)((x0 - at) % nu);
+        }
+        at += (long long)nu * c.heads;
+    }
+    __syncthreads();
+    cu.entry = sm.start[0]; cu.head = sm.start[1]; cu.u = sm.start[2];
+    cu.enter(c, p, g);
+    return true;
+}
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -119,27 +209,6 @@ template <> __device__ __forceinline__ unsigned char lds<unsigned char>(uint32_t
     return (unsigned char)v;
 }
 
-// Where a CTA stands in its run of units.
-struct Cursor {
-    int b, sub, u, nu, lo, hi;
-    __device__ void enter(const CacheArgs& c, const PassArgs& p) {
-        for (; b < p.n; ++b) {
-            token_range(c, p, b, lo, hi);
-            nu = units_of(lo, hi);
-            if (nu > 0) return;
-        }
-    }
-    __device__ void step(const CacheArgs& c, const PassArgs& p) {
-        if (++u < nu) return;
-        u = 0;
-        if (++sub < c.heads * p.row_tiles) return;
-        sub = 0;
-        ++b;
-        enter(c, p);
-    }
-};
-
-
 // A state as it is kept in scratch: rows x D sums, then m and l of each row.
 template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(int rows) { return rows * (D + 2); }
 
@@ -160,67 +229,16 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
     __shared__ __align__(16) char ring[AT_W][AT_STAGES][Ti::BYTES];
     __shared__ float join[AT_W][8][PITCH];
     __shared__ float join_m[AT_W][8], join_l[AT_W][8];
-    __shared__ int sh_start[3], sh_warp[AT_W];
+    __shared__ RunSmem run;
     const CacheArgs& c = a.c;
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, r = lane >> 2, cc = lane & 3;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---- the run: units [x0, x1) of all; the lane, head and row tile in which it starts ----
-    const int subs = c.heads * p.row_tiles;
-    const int per = (p.n + AT_NT - 1) / AT_NT, j0 = min(tid * per, p.n), j1 = min(j0 + per, p.n);
-    int mine = 0;
-    for (int j = j0; j < j1; ++j) {
-        int lo, hi;
-        token_range(c, p, j, lo, hi);
-        mine += units_of(lo, hi);
-    }
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane >= o) incl += v;
-    }
-    if (lane == 31) sh_warp[w] = incl;
-    __syncthreads();
-    int before = incl - mine, total = 0;
-#pragma unroll
-    for (int i = 0; i < AT_W; ++i) {
-        if (i < w) before += sh_warp[i];
-        total += sh_warp[i];
-    }
-    const long long U = (long long)total * subs;
-    const int G = (int)min((long long)p.ctas, U);   // no run is empty
-    const long long x0 = blockIdx.x < G ? U * blockIdx.x / G : 0, x1 = blockIdx.x < G ? U * (blockIdx.x + 1) / G : 0;
-    if (blockIdx.x == 0) {
-        int at = before;
-        for (int j = j0; j < j1; ++j) {
-            int lo, hi;
-            token_range(c, p, j, lo, hi);
-            p.cum[j] = at;
-            at += units_of(lo, hi);
-        }
-        if (tid == 0) p.cum[p.n] = total;
-    }
-    if (x0 >= x1) return;
-    {
-        long long at = (long long)before * subs;
-        for (int j = j0; j < j1; ++j) {
-            int lo, hi;
-            token_range(c, p, j, lo, hi);
-            const int nu = units_of(lo, hi);
-            if (x0 >= at && x0 < at + (long long)nu * subs) {
-                sh_start[0] = j;
-                sh_start[1] = (int)((x0 - at) / nu);
-                sh_start[2] = (int)((x0 - at) % nu);
-            }
-            at += (long long)nu * subs;
-        }
-    }
-    __syncthreads();
+    const int g = a.q_heads / c.heads;
+    long long x0, x1;
     Cursor cu, ahead;
-    cu.b = sh_start[0]; cu.sub = sh_start[1]; cu.u = sh_start[2];
-    cu.enter(c, p);
+    if (!find_run<AT_NT>(c, p, g, run, x0, x1, cu)) return;
     ahead = cu;
     const long long units = x1 - x0;
 
@@ -230,19 +248,19 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
     int page = 0;
     auto look = [&]() {                             // page id of the tile under `ahead`
         const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
-        if (pos < ahead.hi) page = c.table[(size_t)(p.prefix ? ahead.b * p.N : ahead.b) * c.max_pages + (pos >> c.page_shift)];
+        if (pos < ahead.hi) page = c.table[(size_t)ahead.row_of_table(p) * c.max_pages + (pos >> c.page_shift)];
     };
     auto issue = [&](int stage) {
         const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
         if (pos < ahead.hi) {
             if (page < 0 || page >= c.n_pages) {
                 if (lane == 0 && c.lane_status) {
-                    const int l0 = p.prefix ? ahead.b * p.N : ahead.b;
+                    const int l0 = ahead.row_of_table(p);
                     for (int j = 0; j < p.group; ++j) flag_lane(c.lane_status, l0 + j, AS_ERR_INVALID_ARG);
                 }
                 page = 0;
             }
-            const char* src = c.pages + (((size_t)page * c.heads + ahead.sub / p.row_tiles) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
+            const char* src = c.pages + (((size_t)page * c.heads + ahead.head) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
             const uint32_t dst = ring0 + stage * Ti::BYTES;
 #pragma unroll
             for (int i = 0; i < (Ti::BYTES / 16 + 31) / 32; ++i)
@@ -256,13 +274,12 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
         if (issued < units) {
             issue(s);
             ++issued;
-            ahead.step(c, p);
+            ahead.step(c, p, g);
             if (issued < units) look();
         }
         cp_commit();
     }
 
-    const int g = a.q_heads / c.heads;
     using E = typename Io<DT>::type;
     uint32_t qf[PARTS][NT][KS][2];
     float o[NT][KS][4], m[NT][2], mu[NT][2], l[NT][2], k2[NT][2];
@@ -273,7 +290,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
         if (fresh) {                                // ---- a new item: its query rows ----
             fresh = false;
             seg_u0 = cu.u;
-            const int head = cu.sub / p.row_tiles, row0 = (cu.sub % p.row_tiles) * 8 * NT;
+            const int head = cu.head, row0 = (cu.entry % p.row_tiles) * 8 * NT, lane0 = cu.row_of_table(p);
             const float kg = c.k_scale ? c.k_scale[head] : 1.f;
             const float to_log2 = a.scale * kg * 1.44269504088896f;
             lim_min = 0x7FFFFFFF;
@@ -284,7 +301,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
 #pragma unroll
                 for (int e = 0; e < D / 4; ++e) xq[e] = 0.f;
                 if (row < p.rows) {
-                    const int ln = (p.prefix ? cu.b * p.N : cu.b) + row / (c.T * g), t = row / g % c.T;
+                    const int ln = lane0 + row / (c.T * g), t = row / g % c.T;
                     const E* src = static_cast<const E*>(a.q) + ((long long)ln * c.T + t) * a.q_ld + (head * g + row % g) * D + cc * (D / 4);
                     const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
 #pragma unroll
@@ -313,7 +330,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
                 for (int h = 0; h < 2; ++h) {
                     const int rw = row0 + n * 8 + 2 * cc + h;
                     k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
-                    const int ln = (p.prefix ? cu.b * p.N : cu.b) + rw / (c.T * g);
+                    const int ln = lane0 + rw / (c.T * g);
                     lim[n][h] = rw < p.rows ? min(lane_len(c, ln) - c.T + 1 + rw / g % c.T, cu.hi) : 0;
                     if (rw < p.rows) lim_min = min(lim_min, lim[n][h]);
                     m[n][h] = -INFINITY; mu[n][h] = 0.f; l[n][h] = 0.f;
@@ -332,7 +349,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
             if (into >= AT_STAGES) into -= AT_STAGES;
             issue(into);
             ++issued;
-            ahead.step(c, p);
+            ahead.step(c, p, g);
             if (issued < units) look();
         }
         cp_commit();
@@ -476,11 +493,11 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
         // ---- the end of an item, or of the run: the four warps' states become one ----
         const bool item_ends = cu.u + 1 == cu.nu;
         if (item_ends || x + 1 == x1) {
-            const int head = cu.sub / p.row_tiles, rt = cu.sub % p.row_tiles;
+            const int head = cu.head, rt = cu.entry % p.row_tiles;
             const bool whole = item_ends && seg_u0 == 0;
             float* part = nullptr;
             if (!whole) part = p.part_cta + (size_t)(2 * blockIdx.x + (seg_u0 == 0)) * state_floats<D>(8 * NT);
-            else if (p.part_item) part = p.part_item + ((size_t)cu.b * subs + cu.sub) * state_floats<D>(8 * NT);
+            else if (p.part_item) part = p.part_item + ((size_t)cu.entry * c.heads + cu.head) * state_floats<D>(8 * NT);
             const float vg = c.v_scale ? c.v_scale[head] : 1.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -519,7 +536,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
                     if (d0 == 0) { part[8 * NT * D + n * 8 + rw] = M; part[8 * NT * (D + 1) + n * 8 + rw] = L; }
                 } else if (row < p.rows) {
                     const float inv = L > 0.f ? vg / L : 0.f;
-                    const int ln = cu.b + row / (c.T * g), t = row / g % c.T;
+                    const int ln = cu.row_of_table(p) + row / (c.T * g), t = row / g % c.T;
                     const size_t orow = ((size_t)ln * c.T + t) * a.q_heads + head * g + row % g;
                     E* at = static_cast<E*>(a.out) + orow * D + d0;
 #pragma unroll
@@ -533,28 +550,27 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
             }
             fresh = true;
         }
-        cu.step(c, p);
+        cu.step(c, p, g);
     }
 }
 
-// The states of row (item, row within its tile) of a pass, joined into (M, L, acc[PER]) of a warp's
-// thread (PER = D / 32 neighbouring dimensions).  Returns false where the pass has written the output.
+// The states of a row of a pass, joined into (M, L, acc[PER]) of a warp's thread (PER = D / 32
+// neighbouring dimensions).  Returns false where the pass has written the output.
 template <int D>
-__device__ __forceinline__ bool gather_states(const CacheArgs& c, const PassArgs& p, int tile_rows, int b, int sub, int rw, int lane, float& M, float& L,
-                                              float (&acc)[D / 32]) {
+__device__ __forceinline__ bool gather_states(const CacheArgs& c, const PassArgs& p, int b, int head, int row, int lane, float& M, float& L, float (&acc)[D / 32]) {
     constexpr int PER = D / 32;
-    const int subs = c.heads * p.row_tiles;
-    const int at = p.cum[b], nu = p.cum[b + 1] - at;
+    const int entry = b * p.row_tiles + row / p.tile_rows, rw = row % p.tile_rows;
+    const int at = p.cum[entry], nu = p.cum[entry + 1] - at;
     if (nu == 0) return true;
-    const long long U = (long long)p.cum[p.n] * subs, x0 = (long long)at * subs + (long long)sub * nu;
+    const long long U = (long long)p.cum[p.n * p.row_tiles] * c.heads, x0 = (long long)at * c.heads + (long long)head * nu;
     const int G = (int)min((long long)p.ctas, U);
     const int c0 = cta_of(x0, U, G), c1 = cta_of(x0 + nu - 1, U, G);
     if (c0 == c1 && !p.part_item) return false;
     for (int k = c0; k <= c1; ++k) {
         const float* s;
-        if (c0 == c1) s = p.part_item + ((size_t)b * subs + sub) * state_floats<D>(tile_rows);
-        else s = p.part_cta + (size_t)(2 * k + (U * k / G <= x0)) * state_floats<D>(tile_rows);
-        const float m2 = s[tile_rows * D + rw], l2 = s[tile_rows * (D + 1) + rw];
+        if (c0 == c1) s = p.part_item + ((size_t)entry * c.heads + head) * state_floats<D>(p.tile_rows);
+        else s = p.part_cta + (size_t)(2 * k + (U * k / G <= x0)) * state_floats<D>(p.tile_rows);
+        const float m2 = s[p.tile_rows * D + rw], l2 = s[p.tile_rows * (D + 1) + rw];
         const float top = fmaxf(M, m2);
         const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
         L = L * f + l2 * f2;
@@ -568,7 +584,7 @@ __device__ __forceinline__ bool gather_states(const CacheArgs& c, const PassArgs
 // One warp per output row: joins the states of the rows that were split over CTAs or passes, in a
 // fixed order, and writes rows that saw nothing.
 template <int DT, int D>
-__global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs a, const PassArgs own, int own_rows, const PassArgs pre, int pre_rows) {
+__global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs a, const PassArgs own, const PassArgs pre) {
     constexpr int PER = D / 32;
     const CacheArgs& c = a.c;
     const int lane = threadIdx.x & 31, g = a.q_heads / c.heads;
@@ -576,16 +592,12 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs a, co
     const long long rows = (long long)c.lanes * c.T * a.q_heads;
     for (long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * 4) {
         const int hq = (int)(i % a.q_heads), t = (int)(i / a.q_heads % c.T), ln = (int)(i / a.q_heads / c.T);
-        const int head = hq / g;
+        const int head = hq / g, row = t * g + hq % g;
         float M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
         for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-        if (pre.begin) {
-            const int row = ((ln % pre.N) * c.T + t) * g + hq % g;
-            gather_states<D>(c, pre, pre_rows, ln / pre.N, head * pre.row_tiles + row / pre_rows, row % pre_rows, lane, M, L, acc);
-        }
-        const int row = t * g + hq % g;
-        if (!gather_states<D>(c, own, own_rows, ln, head * own.row_tiles + row / own_rows, row % own_rows, lane, M, L, acc)) continue;
+        if (pre.begin) gather_states<D>(c, pre, ln / pre.N, head, (ln % pre.N) * c.T * g + row, lane, M, L, acc);
+        if (!gather_states<D>(c, own, ln, head, row, lane, M, L, acc)) continue;
         const float inv = L > 0.f ? (c.v_scale ? c.v_scale[head] : 1.f) / L : 0.f;
         typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + i * D + lane * PER;
 #pragma unroll

@@ -1,5 +1,6 @@
 // C-ABI entry points of the 4-bit cache and of attention over it.
 #include "as_attend.cuh"
+#include "as_attend_tc.cuh"
 #include "as_cache4.cuh"
 
 #include <cmath>
@@ -68,14 +69,19 @@ static void launch_load(const CacheArgs& a, void* k, void* v, cudaStream_t st) {
 // ---------------------------------------------------------------------------
 // attention: passes and scratch
 // ---------------------------------------------------------------------------
+enum Kernel { MMA_8, MMA_16, TC_128, TC_256 };      // rows of a tile and the kernel that takes it
+
 struct AttendPlan {
-    int own_nt, pre_nt;             // row tiles of 8 * nt rows, in the lanes' own pass and in that over shared beginnings
+    Kernel own_kernel, pre_kernel;  // of the lanes' own pass and of that over shared beginnings
     PassArgs own, pre;
     int* begin;
     size_t bytes;
 };
 
-static int rows_nt(int dtype, int rows) { return dtype == AS_F32 || rows <= 8 ? 1 : 2; }
+static Kernel kernel_for(int dtype, int rows) {
+    if (dtype == AS_F32) return MMA_8;
+    return rows <= 8 ? MMA_8 : rows <= 16 ? MMA_16 : rows <= 128 ? TC_128 : TC_256;
+}
 
 // The shapes of the passes and where their scratch lies in d_work (sizes alone if d_work is null).
 // Scratch for the pass over shared beginnings is there whenever N > 1.
@@ -90,28 +96,32 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
         return q;
     };
     pl.begin = reinterpret_cast<int*>(take(sizeof(int) * (size_t)(lanes / N)));
-    auto pass = [&](PassArgs& p, int& nt, int n, int group, bool prefix) {
+    auto pass = [&](PassArgs& p, Kernel& kernel, int n, int group, bool prefix) {
         p.n = n; p.group = group; p.prefix = prefix; p.N = N;
         p.rows = group * T * g;
-        nt = rows_nt(dtype, p.rows);
-        p.row_tiles = (p.rows + 8 * nt - 1) / (8 * nt);
-        p.cum = reinterpret_cast<int*>(take(sizeof(int) * (size_t)(n + 1)));
-        const size_t state = sizeof(float) * 8 * (size_t)nt * (D + 2);
-        p.part_cta = reinterpret_cast<float*>(take(2 * AT_MAX_CTAS * state));
+        kernel = kernel_for(dtype, p.rows);
+        const bool tc = kernel == TC_128 || kernel == TC_256;
+        p.tile_rows = kernel == MMA_8 ? 8 : kernel == MMA_16 ? 16 : kernel == TC_128 ? 128 : 256;
+        p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
+        p.unit = tc ? TC_KV : 16 * AT_W;
+        p.cum = reinterpret_cast<int*>(take(sizeof(int) * ((size_t)n * p.row_tiles + 1)));
+        const size_t state = sizeof(float) * (size_t)p.tile_rows * (D + 2);
+        p.part_cta = reinterpret_cast<float*>(take(2 * (size_t)(tc ? TC_MAX_CTAS : AT_MAX_CTAS) * state));
         if (N > 1) p.part_item = reinterpret_cast<float*>(take((size_t)n * heads * p.row_tiles * state));
     };
-    pass(pl.own, pl.own_nt, lanes, 1, false);
-    if (N > 1) pass(pl.pre, pl.pre_nt, lanes / N, N, true);
+    pass(pl.own, pl.own_kernel, lanes, 1, false);
+    if (N > 1) pass(pl.pre, pl.pre_kernel, lanes / N, N, true);
     pl.bytes = at;
     return pl;
 }
 
 template <class K, class... A>
-static cudaError_t launch_after(K kern, unsigned grid, unsigned block, cudaStream_t st, A... args) {
+static cudaError_t launch_after(K kern, unsigned grid, unsigned block, size_t smem, cudaStream_t st, A... args) {
     // the kernel waits for its predecessor's results itself (griddepcontrol.wait), so its launch may overlap it
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -122,7 +132,7 @@ static cudaError_t launch_after(K kern, unsigned grid, unsigned block, cudaStrea
 }
 
 template <int DT, int D, int NT>
-static cudaError_t launch_pass(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
+static cudaError_t launch_mma(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
     static int per_sm[64] = {0};
     int dev = 0;
     cudaGetDevice(&dev);
@@ -134,15 +144,33 @@ static cudaError_t launch_pass(const AttendArgs& a, PassArgs& p, int sms, cudaSt
         per_sm[dev] = n > 0 ? n : 1;
     }
     p.ctas = per_sm[dev] * sms < AT_MAX_CTAS ? per_sm[dev] * sms : AT_MAX_CTAS;
-    return launch_after(kern, p.ctas, AT_NT, st, a, p);
+    return launch_after(kern, p.ctas, AT_NT, 0, st, a, p);
+}
+
+template <int D, bool DUAL>
+static cudaError_t launch_tc(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
+    static bool attr_set[64] = {false};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    auto kern = attend_tc_kernel<D, DUAL>;
+    if (!attr_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_smem_bytes<D, DUAL>());
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    p.ctas = sms < TC_MAX_CTAS ? sms : TC_MAX_CTAS;
+    p.wait_cycles = wait_cycles_now();
+    return launch_after(kern, p.ctas, TC_NT, tc_smem_bytes<D, DUAL>(), st, a, p);
 }
 
 template <int DT, int D>
-static cudaError_t launch_pass(const AttendArgs& a, PassArgs& p, int nt, int sms, cudaStream_t st) {
+static cudaError_t launch_pass(const AttendArgs& a, PassArgs& p, Kernel kernel, int sms, cudaStream_t st) {
     if constexpr (DT == AS_BF16) {
-        if (nt == 2) return launch_pass<DT, D, 2>(a, p, sms, st);
+        if (kernel == TC_256) return launch_tc<D, true>(a, p, sms, st);
+        if (kernel == TC_128) return launch_tc<D, false>(a, p, sms, st);
+        if (kernel == MMA_16) return launch_mma<DT, D, 2>(a, p, sms, st);
     }
-    return launch_pass<DT, D, 1>(a, p, sms, st);
+    return launch_mma<DT, D, 1>(a, p, sms, st);
 }
 
 template <int DT, int D>
@@ -152,16 +180,16 @@ static int launch_attend(const AttendArgs& a, int N, const int* shared, void* wo
     if (shared && N > 1) {
         attend_shared_kernel<<<a.c.lanes / N, 128, 0, st>>>(a.c, N, shared, pl.begin);
         pl.own.begin = pl.pre.begin = pl.begin;
-        e = launch_pass<DT, D>(a, pl.pre, pl.pre_nt, sms, st);
+        e = launch_pass<DT, D>(a, pl.pre, pl.pre_kernel, sms, st);
         if (e != cudaSuccess) return cuda_fail(e, "attention kernel launch (shared beginnings)");
     } else {
         pl.own.part_item = nullptr;
     }
-    e = launch_pass<DT, D>(a, pl.own, pl.own_nt, sms, st);
+    e = launch_pass<DT, D>(a, pl.own, pl.own_kernel, sms, st);
     if (e != cudaSuccess) return cuda_fail(e, "attention kernel launch");
     const long long rows = (long long)a.c.lanes * a.c.T * a.q_heads, want = (rows + 3) / 4;
     const unsigned grid = (unsigned)(want < 64 * sms ? want : 64 * sms);
-    e = launch_after(attend_join_kernel<DT, D>, grid, 128, st, a, pl.own, 8 * pl.own_nt, pl.pre, 8 * pl.pre_nt);
+    e = launch_after(attend_join_kernel<DT, D>, grid, 128, 0, st, a, pl.own, pl.pre);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "attention join kernel launch");
 }
 

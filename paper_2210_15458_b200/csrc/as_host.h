@@ -15,6 +15,8 @@ struct DeviceInfo {
 };
 int device_info(const DeviceInfo** out);            // the current device's, looked up once
 
+long long wait_cycles_now();                        // bound on every on-device wait, in clock cycles (AS_TUNE_WAIT_KCYCLES)
+
 constexpr size_t SMEM_OPTIN_MAX = 232448;           // 227 KB per CTA on sm_100
 
 // Checked builds: each translation unit keeps its own record of out-of-range indices; these copy
