@@ -15,6 +15,19 @@ constexpr int AT_STAGES = 3;                // tiles that a warp has in flight o
 constexpr int AT_MAX_CTAS = 1024;
 constexpr float AT_LAZY = 8.f;              // the running maximum may lag by 8 (weights stay below 2^8, well within f16)
 
+// n / d for n < 2^31 by a multiplication (Granlund and Montgomery's round-up method)
+struct Divisor {
+    uint32_t d, mul, shift;
+    __host__ void set(uint32_t by) {
+        d = by;
+        shift = 0;
+        while ((1ull << shift) < by) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
+};
+
 struct AttendArgs {
     CacheArgs c;
     const void* q;
@@ -23,12 +36,13 @@ struct AttendArgs {
     float scale;
     void* out;
     float* lse;
+    Divisor by_g, by_Tg;                    // query heads of a key head, rows of a lane
 };
 
 // One pass over the cache.  An item is a set of query rows that read the same tokens of one head: the
 // rows of `group` lanes (1, or all N lanes of a group for their shared beginning) x T tokens x the
 // query heads of a key head, cut into row tiles of tile_rows.  Items are ordered by entry (lane or
-// group, row tile), then head; their units (`unit` tokens each) are dealt out to the CTAs in equal
+// group, row tile), then head; their units (2^unit_shift tokens each) are dealt out to the CTAs in equal
 // contiguous runs.
 struct PassArgs {
     int n;                                  // lanes, or groups
@@ -36,7 +50,8 @@ struct PassArgs {
     bool prefix;                            // tokens [0, begin[b]) of group b, else [begin[b / N], len) of lane b
     int N;
     const int* begin;                       // [lanes / N] usable shared lengths, or null (0)
-    int rows, tile_rows, row_tiles, unit;
+    int rows, tile_rows, row_tiles, unit_shift;
+    Divisor by_row_tiles, by_N;
     int* cum;                               // [n * row_tiles + 1] units of one head in front of an entry, written by CTA 0
     float* part_item;                       // states of items that one CTA saw whole; null: it writes the output itself
     float* part_cta;                        // [2 * ctas] states of the others: a CTA's first and last item
@@ -51,41 +66,82 @@ __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad 
     return b ? 0 : len;
 }
 // the tokens [lo, hi) that the rows of an entry read; behind a tile's last row nothing is seen
-__device__ __forceinline__ void token_range(const CacheArgs& c, const PassArgs& p, int g, int entry, int& lo, int& hi) {
-    const int b = p.row_tiles == 1 ? entry : entry / p.row_tiles;
-    const int s = p.begin ? p.begin[p.prefix ? b : b / p.N] : 0;
+__device__ __forceinline__ void token_range(const AttendArgs& a, const PassArgs& p, int entry, int b, int& lo, int& hi) {
+    const int s = p.begin ? p.begin[p.prefix ? b : p.by_N.div(b)] : 0;
     lo = p.prefix ? 0 : s;
-    hi = p.prefix ? s : lane_len(c, b);
-    if (!p.prefix && c.T > 1) {
-        const int last = min(p.rows, (entry % p.row_tiles + 1) * p.tile_rows) - 1;
-        hi = max(lo, hi - c.T + 1 + last / g);
+    hi = p.prefix ? s : lane_len(a.c, b);
+    if (!p.prefix && a.c.T > 1) {
+        const int last = min(p.rows, (entry - b * p.row_tiles + 1) * p.tile_rows) - 1;
+        hi = max(lo, hi - a.c.T + 1 + a.by_g.div(last));
     }
 }
-__device__ __forceinline__ int units_of(const PassArgs& p, int lo, int hi) { return (hi - lo + p.unit - 1) / p.unit; }
-// the CTA of `ctas` <= U whose run holds unit x of U
-__device__ __forceinline__ int cta_of(long long x, long long U, int ctas) { return (int)(((x + 1) * ctas - 1) / U); }
+__device__ __forceinline__ int units_of(const PassArgs& p, int lo, int hi) { return (hi - lo + (1 << p.unit_shift) - 1) >> p.unit_shift; }
+// The runs of G CTAs: CTA k has units [start(k), start(k + 1)) of U = q G + r, in equal shares.
+struct Runs {
+    long long q;
+    int r, G;
+    __device__ Runs(long long U, int ctas) {
+        G = U < ctas ? (int)U : ctas;               // no run is empty
+        q = G > 0 ? (long long)((double)U / G) : 0; // U is far below 2^53: at most one off
+        if (G > 0 && q * G > U) --q;
+        r = (int)(U - q * G);
+    }
+    __device__ long long start(int k) const { return q * k + (unsigned)r * (unsigned)k / (unsigned)G; }
+    // the CTA that has unit x
+    __device__ int of(long long x) const {
+        int k = (int)((double)x / ((double)q + (double)r / G));
+        k = min(max(k, 0), G - 1);
+#pragma unroll 1
+        while (k > 0 && start(k) > x) --k;
+#pragma unroll 1
+        while (k + 1 < G && start(k + 1) <= x) ++k;
+        return k;
+    }
+};
+
+// Positions that a row may see, and where its output goes.
+__device__ __forceinline__ int row_limit(const AttendArgs& a, int lane0, int row) {
+    const int ln = a.by_Tg.div(row), t = a.by_g.div(row) - ln * a.c.T;
+    return lane_len(a.c, lane0 + ln) - a.c.T + 1 + t;
+}
+__device__ __forceinline__ size_t out_row(const AttendArgs& a, int lane0, int head, int row) {
+    const int tok = a.by_g.div(row), g = (int)a.by_g.d;
+    return ((size_t)lane0 * a.c.T + tok) * a.q_heads + head * g + row - tok * g;
+}
+
+// The first entry from `entry` on that has tokens: (entry, lo, hi, lane or group).  A call: it is rare, and inlined it
+// would swell every loop that moves on through the units beyond the instruction caches.
+__device__ __noinline__ int4 find_entry(const AttendArgs& a, const PassArgs& p, int entry) {
+    int b = 0, lo = 0, hi = 0;
+#pragma unroll 1
+    for (; entry < p.n * p.row_tiles; ++entry) {
+        b = p.by_row_tiles.div(entry);
+        token_range(a, p, entry, b, lo, hi);
+        if (hi > lo) break;
+    }
+    return make_int4(entry, lo, hi, b);
+}
 
 // Where a CTA stands in its run of units.
 struct Cursor {
-    int entry, head, u, nu, lo, hi;
-    __device__ void enter(const CacheArgs& c, const PassArgs& p, int g) {
-        for (; entry < p.n * p.row_tiles; ++entry) {
-            token_range(c, p, g, entry, lo, hi);
-            nu = units_of(p, lo, hi);
-            if (nu > 0) return;
-        }
+    int entry, head, u, nu, lo, hi, lane0, row0;    // row0: the tile's first row
+    __device__ __forceinline__ void enter(const AttendArgs& a, const PassArgs& p) {
+        const int4 e = find_entry(a, p, entry);
+        entry = e.x; lo = e.y; hi = e.z;
+        nu = units_of(p, lo, hi);
+        lane0 = p.prefix ? e.w * p.N : e.w;
+        row0 = (entry - e.w * p.row_tiles) * p.tile_rows;
     }
-    __device__ void next_item(const CacheArgs& c, const PassArgs& p, int g) {
+    __device__ __forceinline__ void next_item(const AttendArgs& a, const PassArgs& p) {
         u = 0;
-        if (++head < c.heads) return;
+        if (++head < a.c.heads) return;
         head = 0;
         ++entry;
-        enter(c, p, g);
+        enter(a, p);
     }
-    __device__ void step(const CacheArgs& c, const PassArgs& p, int g) {
-        if (++u == nu) next_item(c, p, g);
+    __device__ __forceinline__ void step(const AttendArgs& a, const PassArgs& p) {
+        if (++u == nu) next_item(a, p);
     }
-    __device__ int row_of_table(const PassArgs& p) const { return p.prefix ? entry / p.row_tiles * p.N : entry / p.row_tiles; }
 };
 
 // The CTA's run [x0, x1) and where it starts; called by all NT threads.
@@ -94,15 +150,17 @@ struct RunSmem {
     int start[3];
 };
 template <int NT>
-__device__ bool find_run(const CacheArgs& c, const PassArgs& p, int g, RunSmem& sm, long long& x0, long long& x1, Cursor& cu) {
+__device__ __forceinline__ bool find_run(const AttendArgs& a, const PassArgs& p, RunSmem& sm, long long& x0, long long& x1, Cursor& cu) {
+    const CacheArgs& c = a.c;
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, n = p.n * p.row_tiles;
     const int per = (n + NT - 1) / NT, j0 = min(tid * per, n), j1 = min(j0 + per, n);
     auto units = [&](int j) {
         int lo, hi;
-        token_range(c, p, g, j, lo, hi);
+        token_range(a, p, j, p.by_row_tiles.div(j), lo, hi);
         return units_of(p, lo, hi);
     };
     int mine = 0;
+#pragma unroll 1
     for (int j = j0; j < j1; ++j) mine += units(j);
     int incl = mine;
 #pragma unroll
@@ -118,32 +176,34 @@ __device__ bool find_run(const CacheArgs& c, const PassArgs& p, int g, RunSmem& 
         if (i < w) before += sm.warp_sum[i];
         total += sm.warp_sum[i];
     }
-    const long long U = (long long)total * c.heads;
-    const int G = (int)min((long long)p.ctas, U);   // no run is empty
+    const Runs runs((long long)total * c.heads, p.ctas);
     if (blockIdx.x == 0) {
         int at = before;
+#pragma unroll 1
         for (int j = j0; j < j1; ++j) {
             p.cum[j] = at;
             at += units(j);
         }
         if (tid == 0) p.cum[n] = total;
     }
-    if (blockIdx.x >= G) return false;
-    x0 = U * blockIdx.x / G;
-    x1 = U * (blockIdx.x + 1) / G;
+    if (blockIdx.x >= runs.G) return false;
+    x0 = runs.start(blockIdx.x);
+    x1 = runs.start(blockIdx.x + 1);
     long long at = (long long)before * c.heads;
+#pragma unroll 1
     for (int j = j0; j < j1; ++j) {
         const int nu = units(j);
         if (x0 >= at && x0 < at + (long long)nu * c.heads) {
             sm.start[0] = j;
-            sm.start[1] = (int)((x0 - at) / nu);
-            sm.start[2] = (int)((x0 - at) % nu);
+            const unsigned in = (unsigned)(x0 - at);        // below nu x heads, which the host holds below 2^32
+            sm.start[1] = (int)(in / nu);
+            sm.start[2] = (int)(in % nu);
         }
         at += (long long)nu * c.heads;
     }
     __syncthreads();
     cu.entry = sm.start[0]; cu.head = sm.start[1]; cu.u = sm.start[2];
-    cu.enter(c, p, g);
+    cu.enter(a, p);
     return true;
 }
 
@@ -220,7 +280,7 @@ template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(
 // thread's keys are 16 neighbouring bytes and its values the 16 dimensions of one block, which share
 // their scale.  Token l of the products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
 template <int DT, int D, int NT>
-__global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, const PassArgs p) {
+__global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
     constexpr bool F32 = DT == AS_F32;
     constexpr int PARTS = F32 ? 2 : 1;
@@ -235,10 +295,10 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    const int g = a.q_heads / c.heads;
+    const int g = (int)a.by_g.d;
     long long x0, x1;
     Cursor cu, ahead;
-    if (!find_run<AT_NT>(c, p, g, run, x0, x1, cu)) return;
+    if (!find_run<AT_NT>(a, p, run, x0, x1, cu)) return;
     ahead = cu;
     const long long units = x1 - x0;
 
@@ -248,14 +308,15 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
     int page = 0;
     auto look = [&]() {                             // page id of the tile under `ahead`
         const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
-        if (pos < ahead.hi) page = c.table[(size_t)ahead.row_of_table(p) * c.max_pages + (pos >> c.page_shift)];
+        if (pos < ahead.hi) page = c.table[(size_t)ahead.lane0 * c.max_pages + (pos >> c.page_shift)];
     };
     auto issue = [&](int stage) {
         const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
         if (pos < ahead.hi) {
             if (page < 0 || page >= c.n_pages) {
                 if (lane == 0 && c.lane_status) {
-                    const int l0 = ahead.row_of_table(p);
+                    const int l0 = ahead.lane0;
+#pragma unroll 1
                     for (int j = 0; j < p.group; ++j) flag_lane(c.lane_status, l0 + j, AS_ERR_INVALID_ARG);
                 }
                 page = 0;
@@ -269,12 +330,12 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
     };
     long long issued = 0;
     look();
-#pragma unroll
+#pragma unroll 1
     for (int s = 0; s < AT_STAGES - 1; ++s) {
         if (issued < units) {
             issue(s);
             ++issued;
-            ahead.step(c, p, g);
+            ahead.step(a, p);
             if (issued < units) look();
         }
         cp_commit();
@@ -286,11 +347,12 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
     int lim[NT][2], lim_min = 0;
     int seg_u0 = 0, stage = 0;
     bool fresh = true;
+#pragma unroll 1
     for (long long x = x0; x < x1; ++x) {
         if (fresh) {                                // ---- a new item: its query rows ----
             fresh = false;
             seg_u0 = cu.u;
-            const int head = cu.head, row0 = (cu.entry % p.row_tiles) * 8 * NT, lane0 = cu.row_of_table(p);
+            const int head = cu.head, row0 = cu.row0, lane0 = cu.lane0;
             const float kg = c.k_scale ? c.k_scale[head] : 1.f;
             const float to_log2 = a.scale * kg * 1.44269504088896f;
             lim_min = 0x7FFFFFFF;
@@ -301,8 +363,9 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
 #pragma unroll
                 for (int e = 0; e < D / 4; ++e) xq[e] = 0.f;
                 if (row < p.rows) {
-                    const int ln = lane0 + row / (c.T * g), t = row / g % c.T;
-                    const E* src = static_cast<const E*>(a.q) + ((long long)ln * c.T + t) * a.q_ld + (head * g + row % g) * D + cc * (D / 4);
+                    // row = (lane of the group x T + token) x g + query head
+                    const int tok = a.by_g.div(row);
+                    const E* src = static_cast<const E*>(a.q) + ((long long)lane0 * c.T + tok) * a.q_ld + (head * g + row - tok * g) * D + cc * (D / 4);
                     const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
 #pragma unroll
                     for (int e = 0; e < D / 4; e += 16) Io<DT>::read16(src + e, vec, *reinterpret_cast<float(*)[16]>(&xq[e]));
@@ -330,8 +393,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
                 for (int h = 0; h < 2; ++h) {
                     const int rw = row0 + n * 8 + 2 * cc + h;
                     k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
-                    const int ln = lane0 + rw / (c.T * g);
-                    lim[n][h] = rw < p.rows ? min(lane_len(c, ln) - c.T + 1 + rw / g % c.T, cu.hi) : 0;
+                    lim[n][h] = rw < p.rows ? min(row_limit(a, lane0, rw), cu.hi) : 0;
                     if (rw < p.rows) lim_min = min(lim_min, lim[n][h]);
                     m[n][h] = -INFINITY; mu[n][h] = 0.f; l[n][h] = 0.f;
                 }
@@ -349,7 +411,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
             if (into >= AT_STAGES) into -= AT_STAGES;
             issue(into);
             ++issued;
-            ahead.step(c, p, g);
+            ahead.step(a, p);
             if (issued < units) look();
         }
         cp_commit();
@@ -493,7 +555,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
         // ---- the end of an item, or of the run: the four warps' states become one ----
         const bool item_ends = cu.u + 1 == cu.nu;
         if (item_ends || x + 1 == x1) {
-            const int head = cu.head, rt = cu.entry % p.row_tiles;
+            const int head = cu.head;
             const bool whole = item_ends && seg_u0 == 0;
             float* part = nullptr;
             if (!whole) part = p.part_cta + (size_t)(2 * blockIdx.x + (seg_u0 == 0)) * state_floats<D>(8 * NT);
@@ -528,7 +590,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
 #pragma unroll
                     for (int i = 0; i < AT_W; ++i) acc[e] += f[i] * join[i][rw][(d0 / (D / 8)) * (D / 8 + 2) + d0 % (D / 8) + e];
                 }
-                const int row = rt * 8 * NT + n * 8 + rw;
+                const int row = cu.row0 + n * 8 + rw;
                 if (part) {
                     float* at = part + (n * 8 + rw) * D + d0;
 #pragma unroll
@@ -536,8 +598,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
                     if (d0 == 0) { part[8 * NT * D + n * 8 + rw] = M; part[8 * NT * (D + 1) + n * 8 + rw] = L; }
                 } else if (row < p.rows) {
                     const float inv = L > 0.f ? vg / L : 0.f;
-                    const int ln = cu.row_of_table(p) + row / (c.T * g), t = row / g % c.T;
-                    const size_t orow = ((size_t)ln * c.T + t) * a.q_heads + head * g + row % g;
+                    const size_t orow = out_row(a, cu.lane0, head, row);
                     E* at = static_cast<E*>(a.out) + orow * D + d0;
 #pragma unroll
                     for (int e = 0; e < PER; e += 2) {
@@ -550,59 +611,84 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const AttendArgs a, c
             }
             fresh = true;
         }
-        cu.step(c, p, g);
+        cu.step(a, p);
     }
 }
 
-// The states of a row of a pass, joined into (M, L, acc[PER]) of a warp's thread (PER = D / 32
-// neighbouring dimensions).  Returns false where the pass has written the output.
-template <int D>
-__device__ __forceinline__ bool gather_states(const CacheArgs& c, const PassArgs& p, int b, int head, int row, int lane, float& M, float& L, float (&acc)[D / 32]) {
-    constexpr int PER = D / 32;
-    const int entry = b * p.row_tiles + row / p.tile_rows, rw = row % p.tile_rows;
-    const int at = p.cum[entry], nu = p.cum[entry + 1] - at;
-    if (nu == 0) return true;
-    const long long U = (long long)p.cum[p.n * p.row_tiles] * c.heads, x0 = (long long)at * c.heads + (long long)head * nu;
-    const int G = (int)min((long long)p.ctas, U);
-    const int c0 = cta_of(x0, U, G), c1 = cta_of(x0 + nu - 1, U, G);
-    if (c0 == c1 && !p.part_item) return false;
-    for (int k = c0; k <= c1; ++k) {
-        const float* s;
-        if (c0 == c1) s = p.part_item + ((size_t)entry * c.heads + head) * state_floats<D>(p.tile_rows);
-        else s = p.part_cta + (size_t)(2 * k + (U * k / G <= x0)) * state_floats<D>(p.tile_rows);
-        const float m2 = s[p.tile_rows * D + rw], l2 = s[p.tile_rows * (D + 1) + rw];
-        const float top = fmaxf(M, m2);
-        const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
-        L = L * f + l2 * f2;
+// Where the states of an item lie: item by item, or with the CTAs c0..c1 that shared it.
+struct ItemStates {
+    const float* whole;
+    const float* cta;
+    long long x0;
+    Runs runs;
+    int c0, c1, tile_rows;
+    bool none, written;                     // no tokens; the pass has written the output itself
+    __device__ ItemStates(const CacheArgs& c, const PassArgs& p, int D, int entry, int head)
+        : runs((long long)p.cum[p.n * p.row_tiles] * c.heads, p.ctas) {
+        const int at = p.cum[entry], nu = p.cum[entry + 1] - at;
+        tile_rows = p.tile_rows;
+        none = nu == 0;
+        written = false;
+        c0 = 0; c1 = -1;
+        if (none) return;
+        x0 = (long long)at * c.heads + (long long)head * nu;
+        c0 = runs.of(x0);
+        c1 = runs.of(x0 + nu - 1);
+        cta = p.part_cta;
+        whole = c0 == c1 && p.part_item ? p.part_item + ((size_t)entry * c.heads + head) * tile_rows * (D + 2) : nullptr;
+        written = c0 == c1 && !p.part_item;
+    }
+    // joins the item's states of row rw into (M, L, acc): a warp's thread has D / 32 neighbouring dimensions
+    template <int D> __device__ void join(int rw, int lane, float& M, float& L, float (&acc)[D / 32]) const {
+        constexpr int PER = D / 32;
+#pragma unroll 1
+        for (int k = c0; k <= c1; ++k) {
+            const float* s = whole ? whole : cta + (size_t)(2 * k + (runs.start(k) <= x0)) * state_floats<D>(tile_rows);
+            const float m2 = s[tile_rows * D + rw], l2 = s[tile_rows * (D + 1) + rw];
+            const float top = fmaxf(M, m2);
+            const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
+            L = L * f + l2 * f2;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) acc[e] = acc[e] * f + s[rw * D + lane * PER + e] * f2;
-        M = top;
+            for (int e = 0; e < PER; ++e) acc[e] = acc[e] * f + s[rw * D + lane * PER + e] * f2;
+            M = top;
+        }
     }
-    return true;
-}
+};
 
-// One warp per output row: joins the states of the rows that were split over CTAs or passes, in a
-// fixed order, and writes rows that saw nothing.
+// One CTA per item of the lanes' own pass: joins the states of rows that were split over CTAs or
+// passes, in a fixed order, and writes rows that saw nothing.
 template <int DT, int D>
-__global__ void __launch_bounds__(128) attend_join_kernel(const AttendArgs a, const PassArgs own, const PassArgs pre) {
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs own, const __grid_constant__ PassArgs pre) {
     constexpr int PER = D / 32;
     const CacheArgs& c = a.c;
-    const int lane = threadIdx.x & 31, g = a.q_heads / c.heads;
+    const int lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const long long rows = (long long)c.lanes * c.T * a.q_heads;
-    for (long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * 4) {
-        const int hq = (int)(i % a.q_heads), t = (int)(i / a.q_heads % c.T), ln = (int)(i / a.q_heads / c.T);
-        const int head = hq / g, row = t * g + hq % g;
-        float M = -INFINITY, L = 0.f, acc[PER];
+    const unsigned items = (unsigned)own.n * own.row_tiles * c.heads;       // (the host holds it below 2^31)
+#pragma unroll 1
+    for (unsigned i = blockIdx.x; i < items; i += gridDim.x) {
+        const int entry = (int)(i / c.heads), head = (int)(i % c.heads);
+        const ItemStates st(c, own, D, entry, head);
+        if (st.written) continue;
+        const int ln = own.by_row_tiles.div(entry), row0 = (entry - ln * own.row_tiles) * own.tile_rows;
+#pragma unroll 1
+        for (int rw = threadIdx.x >> 5; rw < own.tile_rows && row0 + rw < own.rows; rw += 4) {
+            const int row = row0 + rw;
+            float M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-        if (pre.begin) gather_states<D>(c, pre, ln / pre.N, head, (ln % pre.N) * c.T * g + row, lane, M, L, acc);
-        if (!gather_states<D>(c, own, ln, head, row, lane, M, L, acc)) continue;
-        const float inv = L > 0.f ? (c.v_scale ? c.v_scale[head] : 1.f) / L : 0.f;
-        typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + i * D + lane * PER;
+            for (int e = 0; e < PER; ++e) acc[e] = 0.f;
+            if (pre.begin) {
+                const int gr = pre.by_N.div(ln), prow = (ln - gr * pre.N) * own.rows + row, pt = prow / pre.tile_rows;
+                const ItemStates ps(c, pre, D, gr * pre.row_tiles + pt, head);
+                ps.join<D>(prow - pt * pre.tile_rows, lane, M, L, acc);
+            }
+            st.join<D>(rw, lane, M, L, acc);
+            const float inv = L > 0.f ? (c.v_scale ? c.v_scale[head] : 1.f) / L : 0.f;
+            const size_t orow = out_row(a, ln, head, row);
+            typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + orow * D + lane * PER;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) out[e] = acc[e] * inv;
-        if (a.lse && lane == 0) a.lse[i] = L > 0.f ? 0.693147180559945f * (M + log2f(L)) : -INFINITY;
+            for (int e = 0; e < PER; ++e) out[e] = acc[e] * inv;
+            if (a.lse && lane == 0) a.lse[orow] = L > 0.f ? 0.693147180559945f * (M + log2f(L)) : -INFINITY;
+        }
     }
 }
 

@@ -3,12 +3,16 @@
 #pragma once
 #include "as_attend.cuh"
 
+#include <type_traits>
+
 namespace asx {
 
 constexpr int TC_MAX_CTAS = 160;            // one on each SM
 constexpr int TC_KV = 128;                  // tokens of a tile
-constexpr int TC_SOFT = 256, TC_FILL = 128; // threads: two softmax groups, one filling group, one warp that issues
-constexpr int TC_NT = TC_SOFT + TC_FILL + 32;
+// Threads, in this order: a warp that issues (and three that are not used: a group's first warp reads the first lanes of
+// TMEM), a group of 128 that fills in keys (and queries), one that fills in values, two softmax groups.  Their loops run side by side on each quarter of the SM and together have to fit its instruction cache: they
+// are kept short, rare parts are calls (unrolled whole, the kernel was instruction-bound and half as fast).
+constexpr int TC_SOFT = 256, TC_FILL = 128, TC_FIRST = 128, TC_NT = TC_FIRST + 2 * TC_FILL + TC_SOFT;
 
 __device__ __forceinline__ void tc_bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void tc_bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
@@ -21,35 +25,72 @@ __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sy
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // A wait for a phase of a barrier, bounded: false when the bound has run out here or in another warp.
-__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, long long limit, volatile int* failed) {
-    long long start = 0;
-    for (int spin = 0;; ++spin) {
-        uint32_t ok;
-        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
+__device__ __forceinline__ bool tc_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
+__device__ __noinline__ bool tc_wait_long(uint32_t bar, uint32_t parity, long long limit, volatile int* failed) {
+    const long long start = clock64();
+#pragma unroll 1
+    while (!tc_try(bar, parity)) {
         if (*failed) return false;
-        if (spin == 0) start = clock64();
-        else if (clock64() - start > limit) { *failed = 1; return false; }
+        if (clock64() - start > limit) { *failed = 1; return false; }
     }
+    return true;
+}
+__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, long long limit, volatile int* failed) {
+    return tc_try(bar, parity) || tc_wait_long(bar, parity, limit, failed);
 }
 
 #define TC_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
 #define TC_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+__device__ __forceinline__ bool tc_elect() {
+    uint32_t e;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+    return e;
+}
 // 32 columns of the warp's 32 lanes of TMEM: thread = lane
 __device__ __forceinline__ void tc_ld32(uint32_t at, uint32_t (&r)[32]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
                  "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
                  : TC_R8(r, 0), TC_R8(r, 8), TC_R8(r, 16), TC_R8(r, 24) : "r"(at));
 }
-__device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t (&r)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-                 ::TC_W8(r, 0), TC_W8(r, 8), TC_W8(r, 16), TC_W8(r, 24), "r"(at) : "memory");
-}
-__device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t (&r)[16]) {
+template <int N> __device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t (&r)[N]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                  ::TC_W8(r, 0), TC_W8(r, 8), "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t at, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : TC_R8(r, 0), TC_R8(r, 8) : "r"(at));
+}
+// columns at .. at + 16 n of the warp's lanes, each thread's times f: 32-bit sums, or pairs of f16 weights
+__device__ __noinline__ void tc_scale_sums(uint32_t at, int n, float f) {
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        uint32_t o[16];
+        tc_ld16(at + 16 * i, o);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+        tc_st16(at + 16 * i, o);
+    }
+}
+__device__ __noinline__ void tc_scale_weights(uint32_t at, int n, float f) {
+    tc_wait_st();
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        uint32_t o[16];
+        tc_ld16(at + 16 * i, o);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float2 h = unpack_f16(o[e]);
+            o[e] = pack_f16(h.x * f, h.y * f);
+        }
+        tc_st16(at + 16 * i, o);
+    }
 }
 // D[tmem] (+)= A x B, f16 in, f32 accumulators; A from shared memory or from TMEM, B from shared memory
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
@@ -71,7 +112,7 @@ __host__ __device__ constexpr uint32_t tc_idesc(int M, int N, bool b_rows_are_k)
 __device__ __forceinline__ uint32_t tc_at(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }     // 16-byte piece of a block
 
 struct TcSmem {
-    unsigned long long k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], q_full, q_empty, o_full, o_empty, ml_full, fin;
+    unsigned long long k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], q_full[2], q_empty[2], o_full, o_empty, ml_full, fin;
     uint32_t tmem;
     int failed;
     RunSmem run;
@@ -79,25 +120,27 @@ struct TcSmem {
     float ml[2][2][2][128];                 // [parity][group][m, l][row]
 };
 
-template <int D, bool DUAL> constexpr size_t tc_smem_bytes() { return 1024 + (size_t)(DUAL ? 6 : 5) * TC_KV * D * 2 + sizeof(TcSmem); }
+template <int D, bool DUAL> constexpr size_t tc_smem_bytes() { return 1024 + (size_t)6 * TC_KV * D * 2 + (size_t)TC_KV * D + sizeof(TcSmem); }
 
 // An item's rows stand in one tile of 128 (DUAL: two).  Filling threads turn 128 tokens at a time into
 // f16 keys and values in shared memory, two buffers; the issuing thread runs S = Q K^T into TMEM and
 // O += P V with P taken from TMEM; two groups of 128 softmax threads, a thread to a row, turn S into P in
 // place.  DUAL: each group has a row tile and takes every tile of tokens; else the groups take the
-// tiles of tokens in turn, each with its own m, l and O, joined at the end.  Either way step i belongs to
+// tiles of tokens in turn, each with its own m, l and O, joined at the end, and the next item's queries have
+// a buffer of their own.  Either way step i belongs to
 // group i % 2, so that one group's products run while the other's weights are formed.
 template <int D, bool DUAL>
-__global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const AttendArgs a, const PassArgs p) {
+__global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
+    constexpr int FILL = TC_FIRST / 32, SOFT = FILL + 2 * TC_FILL / 32;     // first warps of the groups
     constexpr int MAT = TC_KV * D * 2, BLK = TC_KV * 128, CHUNKS = D / 8, KSTEPS = D / 16;
     extern __shared__ char raw[];
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(raw) + 1023) & ~1023u;
-    const uint32_t q_s = base, k_s = q_s + (DUAL ? 2 : 1) * MAT, v_s = k_s + 2 * MAT;
-    TcSmem& sm = *reinterpret_cast<TcSmem*>(raw + (v_s + 2 * MAT - (uint32_t)__cvta_generic_to_shared(raw)));
+    const uint32_t q_s = base, k_s = q_s + 2 * MAT, v_s = k_s + 2 * MAT, raw_s = v_s + 2 * MAT;
+    TcSmem& sm = *reinterpret_cast<TcSmem*>(raw + (raw_s + TC_KV * D - (uint32_t)__cvta_generic_to_shared(raw)));
     auto bar = [](const unsigned long long& b) { return (uint32_t)__cvta_generic_to_shared(&b); };
     const CacheArgs& c = a.c;
-    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g = a.q_heads / c.heads;
+    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g = (int)a.by_g.d;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) {
@@ -105,8 +148,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const AttendArgs a,
             tc_bar_init(bar(sm.k_full[i]), TC_FILL / 32); tc_bar_init(bar(sm.v_full[i]), TC_FILL / 32);
             tc_bar_init(bar(sm.k_empty[i]), 1); tc_bar_init(bar(sm.v_empty[i]), 1);
             tc_bar_init(bar(sm.s_full[i]), 1); tc_bar_init(bar(sm.p_full[i]), 4);
+            tc_bar_init(bar(sm.q_full[i]), TC_FILL / 32); tc_bar_init(bar(sm.q_empty[i]), 1 + TC_SOFT / 32);
         }
-        tc_bar_init(bar(sm.q_full), TC_FILL / 32); tc_bar_init(bar(sm.q_empty), 1 + TC_SOFT / 32);
         tc_bar_init(bar(sm.o_full), 1); tc_bar_init(bar(sm.o_empty), TC_SOFT / 32);
         tc_bar_init(bar(sm.ml_full), TC_SOFT / 32); tc_bar_init(bar(sm.fin), 1);
         sm.failed = 0;
@@ -114,103 +157,93 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const AttendArgs a,
     }
     long long x0, x1;
     Cursor cu;
-    if (!find_run<TC_NT>(c, p, g, sm.run, x0, x1, cu)) return;
-    if (w == TC_NT / 32 - 1) {
+    if (!find_run<TC_NT>(a, p, sm.run, x0, x1, cu)) return;
+    if (w == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&sm.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sm.tmem, s_t = tmem, o_t = tmem + 256;    // columns: S of group 0, 1 (P in its place), then O of group 0, 1
+    constexpr uint32_t s_t = 0, o_t = 256;      // TMEM columns: S of group 0, 1 (P in its place), then O of group 0, 1
+    const uint32_t tmem = sm.tmem;              // (all 512 columns: 0)
     const long long limit = p.wait_cycles;
     volatile int* failed = &sm.failed;
     bool ok = true;
     long long x = x0;
+    // the query buffer of an item, and how often it has been used before
+    auto q_buf = [](int item) { return DUAL ? 0 : item & 1; };
+    auto q_use = [](int item) { return (uint32_t)(DUAL ? item : item >> 1); };
     auto wait_warp = [&](const unsigned long long& b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, tc_wait(bar(b), parity, limit, failed)); };
 
-    if (w < TC_SOFT / 32) {
+    if (w >= SOFT) {
         // ------------------------------------------------ weights ------------------------------------------------
-        const int s = w >> 2, r = tid & 127;
+        const int s = (w - SOFT) >> 2, r = tid & 127;
         const uint32_t mine = (uint32_t)(w & 3) << 21;              // the warp's 32 lanes of TMEM
         const uint32_t st = s_t + 128 * s + mine, ot = o_t + 128 * s + mine;
         uint32_t steps = 0;                                         // of this group, ever
+#pragma unroll 1
         for (int item = 0; x < x1 && ok; ++item) {
             const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x);
-            const int row = (cu.entry % p.row_tiles) * p.tile_rows + (DUAL ? 128 * s : 0) + r;
-            const int lane0 = cu.row_of_table(p);
-            const int ln = lane0 + row / (c.T * g), t = row / g % c.T;
-            const int lim = row < p.rows ? min(lane_len(c, ln) - c.T + 1 + t, cu.hi) : 0;
+            const int row = cu.row0 + (DUAL ? 128 * s : 0) + r;
+            const int lim = row < p.rows ? min(row_limit(a, cu.lane0, row), cu.hi) : 0;
             const float vg = c.v_scale ? c.v_scale[cu.head] : 1.f;
-            ok = wait_warp(sm.q_full, item & 1);
+            ok = wait_warp(sm.q_full[q_buf(item)], q_use(item) & 1);
             if (!ok) break;
-            const float k2 = sm.up[item & 1][(DUAL ? 128 * s : 0) + r] * fabsf(a.scale) * (c.k_scale ? c.k_scale[cu.head] : 1.f) * 1.44269504088896f;
+            float k2 = sm.up[item & 1][(DUAL ? 128 * s : 0) + r] * fabsf(a.scale) * (c.k_scale ? c.k_scale[cu.head] : 1.f) * 1.44269504088896f;
+            k2 = fmaxf(k2, 1e-37f);         // (a scale of 0: -inf x k2 stays -inf)
             __syncwarp();
-            if (lane == 0) tc_bar_arrive(bar(sm.q_empty));          // (so that no group falls two items behind the filling)
+            if (lane == 0) tc_bar_arrive(bar(sm.q_empty[q_buf(item)]));          // (so that no group falls two items behind the filling)
             float m = -INFINITY, mu = 0.f, l = 0.f;
             bool first = true;
+#pragma unroll 1
             for (int j = DUAL ? 0 : s; j < tiles && ok; j += DUAL ? 1 : 2, ++steps) {
                 ok = wait_warp(sm.s_full[s], steps & 1);
                 if (!ok) break;
                 tc_fence_after();
                 const int left = lim - (cu.lo + (cu.u + j) * TC_KV);        // visible tokens of the tile
                 const bool cut = __any_sync(0xFFFFFFFFu, left < TC_KV);
-                float top = -INFINITY;
-#pragma unroll
+                // One pass over the row, 32 columns at a time.  The running maximum hardly ever rises after the first tiles;
+                // where it does, what was written with the old one is scaled.
+#pragma unroll 1
                 for (int ch = 0; ch < 4; ++ch) {
                     uint32_t v[32];
                     tc_ld32(st + 32 * ch, v);
                     tc_wait_ld();
                     if (cut) {
+                        const int have = left - 32 * ch;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * ch + e < left) top = fmaxf(top, __uint_as_float(v[e]));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(v[e]));
+                        for (int e = 0; e < 32; ++e) v[e] = e < have ? v[e] : 0xFF800000u;
                     }
-                }
-                top = top == -INFINITY ? top : top * k2;
-                const bool rise = top > m + AT_LAZY;
-                if (__any_sync(0xFFFFFFFFu, rise)) {
-                    float f = 1.f;
-                    if (rise) {
-                        f = ex2(m - top);
-                        m = mu = top;
-                        l *= f;
+                    float t0 = fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1])), t1 = fmaxf(__uint_as_float(v[2]), __uint_as_float(v[3]));
+#pragma unroll
+                    for (int e = 4; e < 32; e += 4) {
+                        t0 = fmaxf(fmaxf(t0, __uint_as_float(v[e])), __uint_as_float(v[e + 1]));
+                        t1 = fmaxf(fmaxf(t1, __uint_as_float(v[e + 2])), __uint_as_float(v[e + 3]));
                     }
-                    if (!first) {
-#pragma unroll
-                        for (int ch = 0; ch < D / 32; ++ch) {
-                            uint32_t v[32];
-                            tc_ld32(ot + 32 * ch, v);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
-                            tc_st32(ot + 32 * ch, v);
+                    const float top = fmaxf(t0, t1) * k2;
+                    const bool rise = top > m + AT_LAZY;
+                    if (__any_sync(0xFFFFFFFFu, rise)) {
+                        float f = 1.f;
+                        if (rise) {
+                            f = ex2(m - top);
+                            m = mu = top;
+                            l *= f;
                         }
+                        if (!first) tc_scale_sums(ot, D / 16, f);
+                        if (ch > 0) tc_scale_weights(st, ch, f);
                     }
-                }
-                first = false;
-#pragma unroll
-                for (int ch = 0; ch < 4; ++ch) {
-                    uint32_t v[32], pk[16];
-                    tc_ld32(st + 32 * ch, v);
-                    tc_wait_ld();
                     float l0 = 0.f, l1 = 0.f;
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        float p0 = ex2(fmaf(__uint_as_float(v[e]), k2, -mu)), p1 = ex2(fmaf(__uint_as_float(v[e + 1]), k2, -mu));
-                        if (cut) {
-                            if (32 * ch + e >= left) p0 = 0.f;
-                            if (32 * ch + e + 1 >= left) p1 = 0.f;
-                        }
+                        const float p0 = ex2(fmaf(__uint_as_float(v[e]), k2, -mu)), p1 = ex2(fmaf(__uint_as_float(v[e + 1]), k2, -mu));
                         l0 += p0; l1 += p1;
-                        pk[e / 2] = pack_f16(p0, p1);
+                        v[e / 2] = pack_f16(p0, p1);
                     }
                     l += l0 + l1;
-                    tc_st16(st + 16 * ch, pk);
+                    tc_st16(st + 16 * ch, v);
                 }
+                first = false;
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -243,9 +276,9 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const AttendArgs a,
                 L = f0 * sm.ml[item & 1][0][1][r] + f1 * sm.ml[item & 1][1][1][r];
             }
             const int tr = (DUAL ? 128 * s : 0) + r;
-            const size_t orow = ((size_t)ln * c.T + t) * a.q_heads + cu.head * g + row % g;
+            const size_t orow = row < p.rows ? out_row(a, cu.lane0, cu.head, row) : 0;
             const float inv = L > 0.f ? vg / L : 0.f;
-#pragma unroll
+#pragma unroll 1
             for (int ch = 0; ch < (DUAL ? D / 32 : D / 64); ++ch) {
                 const int col = (DUAL ? 0 : s * (D / 2)) + 32 * ch;
                 uint32_t v[32], u[32];
@@ -291,208 +324,226 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const AttendArgs a,
             if (lane == 0) tc_bar_arrive(bar(sm.o_empty));
             x += tiles;
             if (cu.u + tiles < cu.nu) cu.u += tiles;
-            else cu.next_item(c, p, g);
+            else cu.next_item(a, p);
         }
-    } else if (w < (TC_SOFT + TC_FILL) / 32) {
+    } else if (w >= FILL) {
         // ------------------------------------------------ filling ------------------------------------------------
-        const int r = tid - TC_SOFT;                                // token of a tile, row of a query tile
-        const int page_mask = (1 << c.page_shift) - 1, tiles_per_page = 1 << (c.page_shift - 4);
-        Cursor ahead = cu;
-        long long looked = x0;
-        bool real = false;
-        const char* src = nullptr;                                  // the thread's token under `ahead`
-        auto look = [&]() {
-            real = false;
-            if (looked >= x1) return;
-            const int pos = ahead.lo + ahead.u * TC_KV + r;
-            if (pos < ahead.hi) {
-                const int l0 = ahead.row_of_table(p);
-                int page = c.table[(size_t)l0 * c.max_pages + (pos >> c.page_shift)];
-                if (page < 0 || page >= c.n_pages) {
-                    for (int j = 0; j < p.group; ++j) flag_lane(c.lane_status, l0 + j, AS_ERR_INVALID_ARG);
+        auto fill = [&](auto which) {
+            constexpr bool keys = decltype(which)::value;
+            const int r = tid & 127, t = r & 15;                        // token of a tile of 128, row of a query tile
+            const int page_mask = (1 << c.page_shift) - 1, tiles_per_page = 1 << (c.page_shift - 4);
+            // Each thread takes its token's codes into registers a tile before they are widened, and the page's id a tile
+            // before that.  They are widened from the thread's own place in shared memory, by a loop.
+            Cursor ahead = cu;
+            long long looked = x0;
+            int page = 0, next_lane = 0;
+            uint4 code[D / 32];
+            uint2 scale = make_uint2(0, 0);                         // keys' scales; values' are bytes apart
+            uint32_t byte[KSTEPS];
+            bool next_real = false, real = false;
+            const char* next_base = c.pages;                        // the token's place within page 0 of its head
+            const uint32_t own = raw_s + (keys ? 0 : TC_KV * (D / 2)) + r * 16;
+            auto load = [&]() {
+                if (next_real && (page < 0 || page >= c.n_pages)) {
+#pragma unroll 1
+                    for (int j = 0; j < p.group; ++j) flag_lane(c.lane_status, next_lane + j, AS_ERR_INVALID_ARG);
                     page = 0;
                 }
-                src = c.pages + (((size_t)page * c.heads + ahead.head) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
-                real = true;
-            }
-            ++looked;
-            ahead.step(c, p, g);
-        };
-        uint32_t kc[CHUNKS], vc[CHUNKS], ksc[CHUNKS / 8 + (CHUNKS % 8 != 0)], vsc[KSTEPS];
-        const int t = r & 15;
-        auto load_k = [&]() {
+                // tokens behind the last one count as zeros: their scales do (any code is finite)
+                const char* src = next_real ? next_base + (size_t)page * c.heads * tiles_per_page * Ti::BYTES : c.pages;
+                if constexpr (keys) {
 #pragma unroll
-            for (int i = 0; i < CHUNKS; i += 4) {
-                const uint4 q = real ? *reinterpret_cast<const uint4*>(src + Ti::k_code(t, 0) + 4 * i) : make_uint4(0, 0, 0, 0);
-                kc[i] = q.x; kc[i + 1] = q.y; kc[i + 2] = q.z; kc[i + 3] = q.w;
-            }
+                    for (int i = 0; i < D / 32; ++i) code[i] = __ldg(reinterpret_cast<const uint4*>(src + Ti::k_code(t, 2 * i)));
+                    if constexpr (D == 128) scale = __ldg(reinterpret_cast<const uint2*>(src + Ti::k_scale(t, 0)));
+                    else scale.x = __ldg(reinterpret_cast<const uint32_t*>(src + Ti::k_scale(t, 0)));
+                } else {
+                    uint32_t b1[KSTEPS];
 #pragma unroll
-            for (int i = 0; i < KSTEPS / 4; ++i) ksc[i] = real ? *reinterpret_cast<const uint32_t*>(src + Ti::k_scale(t, 4 * i)) : 0u;
-        };
-        auto load_v = [&]() {
-#pragma unroll
-            for (int b = 0; b < KSTEPS; ++b) {
-                const uint2 q = real ? *reinterpret_cast<const uint2*>(src + Ti::v_code(t, b)) : make_uint2(0, 0);
-                vc[2 * b] = q.x; vc[2 * b + 1] = q.y;
-                vsc[b] = real ? (uint32_t)(uint8_t)src[Ti::v_scale(t, b)] : 0u;
-            }
-        };
-        // 8 codes x scale -> 16 bytes of f16
-        auto widen = [](uint32_t codes, uint32_t scale2) {
-            return make_uint4(mul_f16(codes_f16x2(codes), scale2), mul_f16(codes_f16x2(codes >> 8), scale2), mul_f16(codes_f16x2(codes >> 16), scale2),
-                              mul_f16(codes_f16x2(codes >> 24), scale2));
-        };
-        auto put = [](uint32_t at, const uint4& v) { asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); };
-        auto filled = [&](uint32_t b) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) tc_bar_arrive(b);
-        };
-        look();
-        load_k();
-        load_v();
-        uint32_t n = 0;                                             // tiles filled
-        for (int item = 0; x < x1 && ok; ++item) {
-            const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x);
-            // ---- the item's queries, scaled by a power of two into f16's range; a negative scale goes in here ----
-            if (item > 0) ok = wait_warp(sm.q_empty, (item - 1) & 1);
-            if (!ok) break;
-#pragma unroll
-            for (int h = 0; h < (DUAL ? 2 : 1); ++h) {
-                const int row = (cu.entry % p.row_tiles) * p.tile_rows + 128 * h + r;
-                uint4 q[CHUNKS];
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) q[i] = make_uint4(0, 0, 0, 0);
-                if (row < p.rows) {
-                    const int ln = cu.row_of_table(p) + row / (c.T * g), tt = row / g % c.T;
-                    const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + ((long long)ln * c.T + tt) * a.q_ld + (cu.head * g + row % g) * D;
-                    if ((reinterpret_cast<uintptr_t>(from) & 15) == 0) {
-#pragma unroll
-                        for (int i = 0; i < CHUNKS; ++i) q[i] = reinterpret_cast<const uint4*>(from)[i];
-                    } else {
-                        const uint16_t* e = reinterpret_cast<const uint16_t*>(from);
-#pragma unroll
-                        for (int i = 0; i < CHUNKS; ++i)
-                            q[i] = make_uint4(e[8 * i] | (uint32_t)e[8 * i + 1] << 16, e[8 * i + 2] | (uint32_t)e[8 * i + 3] << 16,
-                                              e[8 * i + 4] | (uint32_t)e[8 * i + 5] << 16, e[8 * i + 6] | (uint32_t)e[8 * i + 7] << 16);
+                    for (int i = 0; i < KSTEPS; ++i) {
+                        const uint2 q = __ldg(reinterpret_cast<const uint2*>(src + Ti::v_code(t, i)));
+                        if (i & 1) { code[i / 2].z = q.x; code[i / 2].w = q.y; }
+                        else { code[i / 2].x = q.x; code[i / 2].y = q.y; }
+                        b1[i] = __ldg(reinterpret_cast<const unsigned char*>(src + Ti::v_scale(t, i)));
                     }
+#pragma unroll
+                    for (int i = 0; i < KSTEPS; ++i) byte[i] = b1[i];
                 }
-                uint32_t top = 0;                                   // largest magnitude's bits
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) {
-                    const uint32_t z[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top = max(top, max(z[e] & 0x7FFFu, z[e] >> 16 & 0x7FFFu));
+                real = next_real;
+                next_real = false;
+                if (looked < x1) {
+                    const int pos = ahead.lo + ahead.u * TC_KV + r;
+                    if (pos < ahead.hi) {
+                        page = c.table[(size_t)ahead.lane0 * c.max_pages + (pos >> c.page_shift)];
+                        next_base = c.pages + ((size_t)ahead.head * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
+                        next_lane = ahead.lane0;
+                        next_real = true;
+                    }
+                    ++looked;
+                    ahead.step(a, p);
                 }
-                int ex = (int)(top >> 7) - 127;
-                ex = ex > 126 ? 126 : ex < -126 ? -126 : ex;
-                const float down = __uint_as_float((uint32_t)(127 - ex) << 23 | (a.scale < 0.f ? 0x80000000u : 0u));
-                sm.up[item & 1][128 * h + r] = __uint_as_float((uint32_t)(127 + ex) << 23);
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) {
-                    const uint32_t z[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
-                    uint32_t f[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) f[e] = pack_f16(__uint_as_float(z[e] << 16) * down, __uint_as_float(z[e] & 0xFFFF0000u) * down);
-                    put(q_s + h * MAT + (i / 8) * BLK + tc_at(r, i % 8), make_uint4(f[0], f[1], f[2], f[3]));
+            };
+            // 8 codes x scale -> 16 bytes of f16
+            auto widen = [](uint32_t codes, uint32_t scale2) {
+                return make_uint4(mul_f16(codes_f16x2(codes), scale2), mul_f16(codes_f16x2(codes >> 8), scale2), mul_f16(codes_f16x2(codes >> 16), scale2),
+                                  mul_f16(codes_f16x2(codes >> 24), scale2));
+            };
+            auto put = [](uint32_t at, const uint4& v) { asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); };
+            auto filled = [&](uint32_t b) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) tc_bar_arrive(b);
+            };
+#pragma unroll 1
+            for (int i = 0; i < 2; ++i) load();                         // (the first time round only the page id is fetched)
+            uint32_t n = 0;                                             // tiles filled
+#pragma unroll 1
+            for (int item = 0; x < x1 && ok; ++item) {
+                const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x);
+                if constexpr (keys) {
+                    // ---- the item's queries, scaled by a power of two into f16's range; a negative scale goes in here ----
+                    if (q_use(item) > 0) ok = wait_warp(sm.q_empty[q_buf(item)], (q_use(item) - 1) & 1);
+                    if (!ok) break;
+#pragma unroll 1
+                    for (int h = 0; h < (DUAL ? 2 : 1); ++h) {
+                        const int row = cu.row0 + 128 * h + r, tok = a.by_g.div(row);
+                        const uint16_t* from = static_cast<const uint16_t*>(a.q) + ((long long)cu.lane0 * c.T + tok) * a.q_ld + (cu.head * g + row - tok * g) * D;
+                        const bool there = row < p.rows, wide = (reinterpret_cast<uintptr_t>(from) & 15) == 0;
+                        auto piece = [&](int i) {                       // 8 of the row's elements
+                            if (!there) return make_uint4(0, 0, 0, 0);
+                            if (wide) return reinterpret_cast<const uint4*>(from)[i];
+                            const uint16_t* e = from + 8 * i;
+                            return make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+                        };
+                        uint32_t top = 0;                               // largest magnitude's bits
+#pragma unroll 4
+                        for (int i = 0; i < CHUNKS; ++i) {
+                            const uint4 q = piece(i);
+                            top = max(max(max(q.x & 0x7FFFu, q.x >> 16 & 0x7FFFu), max(q.y & 0x7FFFu, q.y >> 16 & 0x7FFFu)),
+                                      max(max(max(q.z & 0x7FFFu, q.z >> 16 & 0x7FFFu), max(q.w & 0x7FFFu, q.w >> 16 & 0x7FFFu)), top));
+                        }
+                        int ex = (int)(top >> 7) - 127;
+                        ex = ex > 126 ? 126 : ex < -126 ? -126 : ex;
+                        const float down = __uint_as_float((uint32_t)(127 - ex) << 23 | (a.scale < 0.f ? 0x80000000u : 0u));
+                        sm.up[item & 1][128 * h + r] = __uint_as_float((uint32_t)(127 + ex) << 23);
+                        const uint32_t to = q_s + (DUAL ? h : q_buf(item)) * MAT;
+                        auto both = [&](uint32_t z) { return pack_f16(__uint_as_float(z << 16) * down, __uint_as_float(z & 0xFFFF0000u) * down); };
+#pragma unroll 4
+                        for (int i = 0; i < CHUNKS; ++i) {
+                            const uint4 q = piece(i);
+                            put(to + (i / 8) * BLK + tc_at(r, i % 8), make_uint4(both(q.x), both(q.y), both(q.z), both(q.w)));
+                        }
+                    }
+                    filled(bar(sm.q_full[q_buf(item)]));
                 }
+                // ---- its keys or values ----
+                const uint32_t to = (keys ? k_s : v_s) + r * 128;
+#pragma unroll 1
+                for (int j = 0; j < tiles && ok; ++j, ++n) {
+                    const int b = n & 1;
+                    if (n >= 2) ok = wait_warp(keys ? sm.k_empty[b] : sm.v_empty[b], ((n >> 1) & 1) ^ 1);
+                    if (!ok) break;
+                    // piece i of a token's codes lies TC_KV * 16 bytes behind piece i - 1: threads side by side, 16 bytes each
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) put(own + i * (TC_KV * 16), code[i]);
+                    if constexpr (!keys) {
+                        scale.x = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
+                        if constexpr (D == 128) scale.y = byte[KSTEPS - 4] | byte[KSTEPS - 3] << 8 | byte[KSTEPS - 2] << 16 | byte[KSTEPS - 1] << 24;
+                    }
+                    const uint32_t sc_lo = real ? scale.x : 0u, sc_hi = real ? scale.y : 0u;
+                    load();
+#pragma unroll 1
+                    for (int i = 0; i < D / 32; ++i) {
+                        const uint4 q = lds<uint4>(own + i * (TC_KV * 16));
+                        const uint32_t two = e4m3_f16x2(((D == 128 && i >= 2 ? sc_hi : sc_lo) >> (16 * (i & 1))) & 0xFFFFu);
+                        const uint32_t sa = __byte_perm(two, two, 0x1010), sb = __byte_perm(two, two, 0x3232);
+                        const uint32_t at = to + b * MAT + (i >> 1) * BLK;
+                        const int cx = (4 * (i & 1)) ^ (r & 7);
+                        put(at + ((cx ^ 0) << 4), widen(q.x, sa));
+                        put(at + ((cx ^ 1) << 4), widen(q.y, sa));
+                        put(at + ((cx ^ 2) << 4), widen(q.z, sb));
+                        put(at + ((cx ^ 3) << 4), widen(q.w, sb));
+                    }
+                    filled(bar(keys ? sm.k_full[b] : sm.v_full[b]));
+                }
+                x += tiles;
+                if (cu.u + tiles < cu.nu) cu.u += tiles;
+                else cu.next_item(a, p);
             }
-            filled(bar(sm.q_full));
-            // ---- its keys and values ----
-            for (int j = 0; j < tiles && ok; ++j, ++n) {
-                const int b = n & 1;
-                const uint32_t turn = (n >> 1) & 1;
-                if (n >= 2) ok = wait_warp(sm.k_empty[b], turn ^ 1);
-                if (!ok) break;
-                uint32_t sc[KSTEPS];
-#pragma unroll
-                for (int i = 0; i < KSTEPS; i += 2) {
-                    const uint32_t two = e4m3_f16x2(ksc[i / 4] >> (8 * (i & 2)) & 0xFFFFu);
-                    sc[i] = __byte_perm(two, two, 0x1010);
-                    sc[i + 1] = __byte_perm(two, two, 0x3232);
-                }
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) put(k_s + b * MAT + (i / 8) * BLK + tc_at(r, i % 8), widen(kc[i], sc[i / 2]));
-                filled(bar(sm.k_full[b]));
-                if (n >= 2) ok = wait_warp(sm.v_empty[b], turn ^ 1);
-                if (!ok) break;
-#pragma unroll
-                for (int i = 0; i < KSTEPS; ++i) {
-                    const uint32_t one = e4m3_f16x2(vsc[i]);
-                    sc[i] = __byte_perm(one, one, 0x1010);
-                }
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) put(v_s + b * MAT + (i / 8) * BLK + tc_at(r, i % 8), widen(vc[i], sc[i / 2]));
-                filled(bar(sm.v_full[b]));
-                look();
-                load_k();
-                load_v();
-            }
-            x += tiles;
-            if (cu.u + tiles < cu.nu) cu.u += tiles;
-            else cu.next_item(c, p, g);
-        }
-    } else if (lane == 0) {
+        };
+        if (w < FILL + TC_FILL / 32) fill(std::true_type{});
+        else fill(std::false_type{});
+    } else {
         // ------------------------------------------------ issuing ------------------------------------------------
-        constexpr uint32_t ID_S = tc_idesc(128, TC_KV, false), ID_O = tc_idesc(128, D, true);
-        uint32_t n0 = 0, p_seen[2] = {0, 0};                        // tiles before this item; weights taken, by group
-        for (int item = 0; x < x1 && ok; ++item) {
-            const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x), steps = DUAL ? 2 * tiles : tiles;
-            ok = tc_wait(bar(sm.q_full), item & 1, limit, failed);
-            if (!ok) break;
-            for (int i = 0; i <= steps && ok; ++i) {
-                if (i < steps) {
-                    const int j = DUAL ? i >> 1 : i, s = i & 1;
-                    const uint32_t n = n0 + j, b = n & 1;
-                    if (!DUAL || s == 0) ok = tc_wait(bar(sm.k_full[b]), (n >> 1) & 1, limit, failed);
-                    if (!ok) break;
-                    tc_fence_after();
+        if (w == 0 && tc_elect()) {
+            // One thread walks the steps.  (Chosen by elect.sync, not by its number: the compiler then keeps operands in uniform
+            // registers, where each product otherwise costs a dozen instructions that wait their turn behind the other
+            // groups'.  TMEM, allocated whole, starts at 0.)
+            constexpr uint32_t ID_S = tc_idesc(128, TC_KV, false), ID_O = tc_idesc(128, D, true);
+            const uint64_t q_d = tc_desc(q_s, 0), k_d = tc_desc(k_s, 0), v_d = tc_desc(v_s, BLK);
+            uint32_t n0 = 0, p_seen0 = 0, p_seen1 = 0;              // tiles before this item; weights taken, by group
+#pragma unroll 1
+            for (int item = 0; x < x1 && ok; ++item) {
+                const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x), steps = DUAL ? 2 * tiles : tiles;
+                ok = tc_wait(bar(sm.q_full[q_buf(item)]), q_use(item) & 1, limit, failed);
+                if (!ok) break;
+#pragma unroll 1
+                for (int i = 0; i <= steps; ++i) {
+                    if (i < steps) {
+                        const int j = DUAL ? i >> 1 : i, s = i & 1;
+                        const uint32_t n = n0 + j, b = n & 1;
+                        if (!DUAL || s == 0) ok = tc_wait(bar(sm.k_full[b]), (n >> 1) & 1, limit, failed);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t qa = q_d + (DUAL ? s : q_buf(item)) * (MAT >> 4), ka = k_d + b * (MAT >> 4);
 #pragma unroll
-                    for (int k = 0; k < KSTEPS; ++k) {
-                        const uint32_t at = (k / 4) * BLK + (k % 4) * 32;
-                        tc_mma_ss(s_t + 128 * s, tc_desc(q_s + (DUAL ? s * MAT : 0) + at, 0), tc_desc(k_s + b * MAT + at, 0), ID_S, k > 0);
+                        for (int k = 0; k < KSTEPS; ++k) {
+                            const uint32_t at = (k / 4) * (BLK >> 4) + (k % 4) * 2;
+                            tc_mma_ss(s_t + 128 * s, qa + at, ka + at, ID_S, k > 0);
+                        }
+                        tc_commit(bar(sm.s_full[s]));
+                        if (!DUAL || s == 1) tc_commit(bar(sm.k_empty[b]));
+                        if (i + 1 == steps) tc_commit(bar(sm.q_empty[q_buf(item)]));
                     }
-                    tc_commit(bar(sm.s_full[s]));
-                    if (!DUAL || s == 1) tc_commit(bar(sm.k_empty[b]));
-                    if (i + 1 == steps) tc_commit(bar(sm.q_empty));
-                }
-                if (i > 0) {
-                    const int i2 = i - 1, j = DUAL ? i2 >> 1 : i2, s = i2 & 1;
-                    const uint32_t n = n0 + j, b = n & 1;
-                    if (i2 == 0 && item > 0) ok = tc_wait(bar(sm.o_empty), (item - 1) & 1, limit, failed);
-                    if (ok && (!DUAL || s == 0)) ok = tc_wait(bar(sm.v_full[b]), (n >> 1) & 1, limit, failed);
-                    if (ok) ok = tc_wait(bar(sm.p_full[s]), p_seen[s] & 1, limit, failed);
-                    if (!ok) break;
-                    ++p_seen[s];
-                    tc_fence_after();
+                    if (i > 0) {
+                        const int i2 = i - 1, j = DUAL ? i2 >> 1 : i2, s = i2 & 1;
+                        const uint32_t n = n0 + j, b = n & 1;
+                        if (i2 == 0 && item > 0) ok = tc_wait(bar(sm.o_empty), (item - 1) & 1, limit, failed);
+                        if (ok && (!DUAL || s == 0)) ok = tc_wait(bar(sm.v_full[b]), (n >> 1) & 1, limit, failed);
+                        if (ok) ok = tc_wait(bar(sm.p_full[s]), (s ? p_seen1 : p_seen0) & 1, limit, failed);
+                        if (!ok) break;
+                        if (s) ++p_seen1;
+                        else ++p_seen0;
+                        tc_fence_after();
+                        const uint64_t va = v_d + b * (MAT >> 4);
+                        const bool add = DUAL ? j > 0 : j > 1;
 #pragma unroll
-                    for (int k = 0; k < TC_KV / 16; ++k)
-                        tc_mma_ts(o_t + 128 * s, s_t + 128 * s + 8 * k, tc_desc(v_s + b * MAT + k * 2048, BLK), ID_O, k > 0 || (DUAL ? j > 0 : j > 1));
-                    if (!DUAL || s == 1) tc_commit(bar(sm.v_empty[b]));
+                        for (int k = 0; k < TC_KV / 16; ++k)
+                            tc_mma_ts(o_t + 128 * s, s_t + 128 * s + 8 * k, va + k * (2048 >> 4), ID_O, k > 0 || add);
+                        if (!DUAL || s == 1) tc_commit(bar(sm.v_empty[b]));
+                        if (i == steps) tc_commit(bar(sm.o_full));
+                    }
                 }
+                if (!ok) break;
+                n0 += tiles;
+                x += tiles;
+                if (cu.u + tiles < cu.nu) cu.u += tiles;
+                else cu.next_item(a, p);
             }
-            if (!ok) break;
-            tc_commit(bar(sm.o_full));
-            n0 += tiles;
-            x += tiles;
-            if (cu.u + tiles < cu.nu) cu.u += tiles;
-            else cu.next_item(c, p, g);
-        }
-        // whatever is still in flight ends before TMEM is freed
-        tc_commit(bar(sm.fin));
-        for (long long start = clock64(); clock64() - start < limit;) {
-            uint32_t done;
-            asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], 0;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar(sm.fin)) : "memory");
-            if (done) break;
+            // whatever is still in flight ends before TMEM is freed
+            tc_commit(bar(sm.fin));
+            const long long start = clock64();
+#pragma unroll 1
+            while (!tc_try(bar(sm.fin), 0) && clock64() - start < limit) {}
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (sm.failed && tid == 0) {
+#pragma unroll 1
         for (int j = 0; j < c.lanes; ++j) flag_lane(c.lane_status, j, AS_ERR_TIMEOUT);
     }
-    if (w == TC_NT / 32 - 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if (w == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 }  // namespace asx

@@ -50,7 +50,7 @@ static int clear_status(int* status, int lanes, cudaStream_t st) {
 
 static unsigned grid_of(long long threads, int nt) {
     const long long n = (threads + nt - 1) / nt;
-    return (unsigned)(n < (1 << 30) ? n : (1 << 30));
+    return (unsigned)(n < (1 << 14) ? n : (1 << 14));       // (the kernels loop)
 }
 
 template <int DT, int D>
@@ -103,7 +103,9 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
         const bool tc = kernel == TC_128 || kernel == TC_256;
         p.tile_rows = kernel == MMA_8 ? 8 : kernel == MMA_16 ? 16 : kernel == TC_128 ? 128 : 256;
         p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
-        p.unit = tc ? TC_KV : 16 * AT_W;
+        p.by_row_tiles.set(p.row_tiles);
+        p.by_N.set(N);
+        p.unit_shift = tc ? 7 : 6;     // TC_KV, 16 * AT_W tokens
         p.cum = reinterpret_cast<int*>(take(sizeof(int) * ((size_t)n * p.row_tiles + 1)));
         const size_t state = sizeof(float) * (size_t)p.tile_rows * (D + 2);
         p.part_cta = reinterpret_cast<float*>(take(2 * (size_t)(tc ? TC_MAX_CTAS : AT_MAX_CTAS) * state));
@@ -187,8 +189,8 @@ static int launch_attend(const AttendArgs& a, int N, const int* shared, void* wo
     }
     e = launch_pass<DT, D>(a, pl.own, pl.own_kernel, sms, st);
     if (e != cudaSuccess) return cuda_fail(e, "attention kernel launch");
-    const long long rows = (long long)a.c.lanes * a.c.T * a.q_heads, want = (rows + 3) / 4;
-    const unsigned grid = (unsigned)(want < 64 * sms ? want : 64 * sms);
+    const long long items = (long long)pl.own.n * pl.own.row_tiles * a.c.heads;
+    const unsigned grid = (unsigned)(items < 64 * sms ? items : 64 * sms);
     e = launch_after(attend_join_kernel<DT, D>, grid, 128, 0, st, a, pl.own, pl.pre);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "attention join kernel launch");
 }
@@ -272,6 +274,8 @@ int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, in
     if (q_ld < (long long)q_heads * cache->head_dim) return set_err(AS_ERR_INVALID_ARG, "q_ld = %lld is smaller than q_heads * head_dim", q_ld);
     if (!std::isfinite(scale)) return set_err(AS_ERR_INVALID_ARG, "scale must be finite");
     if (N < 1 || lanes % N) return set_err(AS_ERR_INVALID_ARG, "N = %d must be >= 1 and divide lanes = %d", N, lanes);
+    if (cache->heads > 128 || (long long)lanes * T * q_heads > (1LL << 31) - 1)
+        return set_err(AS_ERR_UNSUPPORTED, "heads = %d must not exceed 128, lanes * T * q_heads not 2^31 - 1", cache->heads);
     if (lanes == 0) return AS_OK;
     if (!d_q || !d_out) return set_err(AS_ERR_INVALID_ARG, "d_q or d_out is NULL");
     const int es = dtype == AS_F32 ? 4 : 2;
@@ -286,6 +290,8 @@ int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, in
     AttendArgs a;
     a.c = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
     a.q = d_q; a.q_ld = q_ld; a.q_heads = q_heads; a.scale = (float)scale; a.out = d_out; a.lse = d_lse;
+    a.by_g.set(q_heads / cache->heads);
+    a.by_Tg.set(T * (q_heads / cache->heads));
     if (d_lane_status) attend_status_kernel<<<grid_of(lanes, 256), 256, 0, st>>>(a.c);
     if (dtype == AS_F32) return cache->head_dim == 64 ? launch_attend<AS_F32, 64>(a, N, d_shared, d_work, di->sms, st) : launch_attend<AS_F32, 128>(a, N, d_shared, d_work, di->sms, st);
     return cache->head_dim == 64 ? launch_attend<AS_BF16, 64>(a, N, d_shared, d_work, di->sms, st) : launch_attend<AS_BF16, 128>(a, N, d_shared, d_work, di->sms, st);

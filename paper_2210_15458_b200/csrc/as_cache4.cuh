@@ -129,13 +129,16 @@ __global__ void __launch_bounds__(C4_NT)
 append_kernel(const CacheArgs c, const typename Io<DT>::type* __restrict__ k, long long k_ld,
               const typename Io<DT>::type* __restrict__ v, long long v_ld, bool vec) {
     using Ti = Tile4<D>;
-    const long long n = (long long)c.lanes * c.T * 2 * c.heads * Ti::NB;
-    for (long long i = (long long)blockIdx.x * C4_NT + threadIdx.x; i < n; i += (long long)gridDim.x * C4_NT) {
-        const int b = (int)(i % Ti::NB);
-        long long r = i / Ti::NB;
-        const int head = (int)(r % c.heads); r /= c.heads;
-        const bool is_v = r & 1; r >>= 1;
-        const int lane = (int)(r / c.T), tok = (int)(r % c.T);
+    // (lanes x T is at most 2^30, heads at most 128: pieces of a row are counted in 32 bits, rows in 32 bits)
+    const unsigned per_row = 2 * c.heads * Ti::NB;
+    const unsigned step = gridDim.x * C4_NT, first = blockIdx.x * C4_NT + threadIdx.x;
+    const unsigned row_step = step / per_row, piece_step = step % per_row;
+    unsigned row = first / per_row, piece = first % per_row;
+    for (; row < (unsigned)c.lanes * c.T; row += row_step, piece += piece_step) {
+        if (piece >= per_row) { piece -= per_row; if (++row >= (unsigned)c.lanes * c.T) break; }
+        const int b = piece % Ti::NB, head = piece / Ti::NB % c.heads;
+        const bool is_v = piece >= per_row / 2;
+        const int lane = (int)(row / c.T), tok = (int)(row % c.T);
         const int len = c.len[lane];
         if (len < 0 || len > ((long long)c.max_pages << c.page_shift)) { flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG); continue; }
         const int p = len - c.T + tok;
@@ -144,8 +147,7 @@ append_kernel(const CacheArgs c, const typename Io<DT>::type* __restrict__ k, lo
         char* tile = tile_of<D>(c, lane, head, p, bad);
         if (bad) { flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG); continue; }
         float x[16];
-        const long long row = (long long)lane * c.T + tok;
-        Io<DT>::read16((is_v ? v + row * v_ld : k + row * k_ld) + head * D + b * 16, vec, x);
+        Io<DT>::read16((is_v ? v + (long long)row * v_ld : k + (long long)row * k_ld) + head * D + b * 16, vec, x);
         const float* hs = is_v ? c.v_scale : c.k_scale;
         const float inv = hs ? __frcp_rn(hs[head]) : 1.f;
         float top = 0.f;
@@ -177,13 +179,14 @@ template <int DT, int D>
 __global__ void __launch_bounds__(C4_NT)
 load_kernel(const CacheArgs c, typename Io<DT>::type* __restrict__ k, typename Io<DT>::type* __restrict__ v) {
     using Ti = Tile4<D>;
-    const long long n = (long long)c.lanes * c.T * 2 * c.heads * Ti::NB;
-    for (long long i = (long long)blockIdx.x * C4_NT + threadIdx.x; i < n; i += (long long)gridDim.x * C4_NT) {
-        const int b = (int)(i % Ti::NB);
-        long long r = i / Ti::NB;
-        const int head = (int)(r % c.heads); r /= c.heads;
-        const long long row = r % ((long long)c.lanes * c.T);
-        const bool is_v = r >= (long long)c.lanes * c.T;
+    const unsigned per_row = 2 * c.heads * Ti::NB;
+    const unsigned step = gridDim.x * C4_NT, first = blockIdx.x * C4_NT + threadIdx.x;
+    const unsigned row_step = step / per_row, piece_step = step % per_row;
+    unsigned row = first / per_row, piece = first % per_row;
+    for (; row < (unsigned)c.lanes * c.T; row += row_step, piece += piece_step) {
+        if (piece >= per_row) { piece -= per_row; if (++row >= (unsigned)c.lanes * c.T) break; }
+        const int b = piece % Ti::NB, head = piece / Ti::NB % c.heads;
+        const bool is_v = piece >= per_row / 2;
         const int lane = (int)(row / c.T), tok = (int)(row % c.T);
         const int len = c.len[lane];
         float x[16];
@@ -209,7 +212,7 @@ load_kernel(const CacheArgs c, typename Io<DT>::type* __restrict__ k, typename I
             }
         }
         if (bad) flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG);
-        Io<DT>::write16((is_v ? v : k) + row * c.heads * D + head * D + b * 16, x);
+        Io<DT>::write16((is_v ? v : k) + (size_t)row * c.heads * D + head * D + b * 16, x);
     }
 }
 
