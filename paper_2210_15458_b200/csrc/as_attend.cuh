@@ -655,8 +655,9 @@ struct ItemStates {
     }
 };
 
-// One CTA per item of the lanes' own pass: joins the states of rows that were split over CTAs or
-// passes, in a fixed order, and writes rows that saw nothing.
+// One CTA per item of the lanes' own pass and 32 of its rows, a warp to a row: joins the states of rows that were split
+// over CTAs or passes, in a fixed order, and writes rows that saw nothing.
+constexpr int JOIN_ROWS = 32;
 template <int DT, int D>
 __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs own, const __grid_constant__ PassArgs pre) {
     constexpr int PER = D / 32;
@@ -664,20 +665,23 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     const int lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const unsigned items = (unsigned)own.n * own.row_tiles * c.heads;       // (the host holds it below 2^31)
+    const int first = blockIdx.y * JOIN_ROWS + (threadIdx.x >> 5);
 #pragma unroll 1
     for (unsigned i = blockIdx.x; i < items; i += gridDim.x) {
         const int entry = (int)(i / c.heads), head = (int)(i % c.heads);
         const ItemStates st(c, own, D, entry, head);
         if (st.written) continue;
         const int ln = own.by_row_tiles.div(entry), row0 = (entry - ln * own.row_tiles) * own.tile_rows;
+        const int end = min(min(own.tile_rows, own.rows - row0), (int)(blockIdx.y + 1) * JOIN_ROWS);
+        const int gr = pre.begin ? pre.by_N.div(ln) : 0;
 #pragma unroll 1
-        for (int rw = threadIdx.x >> 5; rw < own.tile_rows && row0 + rw < own.rows; rw += 4) {
+        for (int rw = first; rw < end; rw += 4) {
             const int row = row0 + rw;
             float M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
             for (int e = 0; e < PER; ++e) acc[e] = 0.f;
             if (pre.begin) {
-                const int gr = pre.by_N.div(ln), prow = (ln - gr * pre.N) * own.rows + row, pt = prow / pre.tile_rows;
+                const int prow = (ln - gr * pre.N) * own.rows + row, pt = prow / pre.tile_rows;
                 const ItemStates ps(c, pre, D, gr * pre.row_tiles + pt, head);
                 ps.join<D>(prow - pt * pre.tile_rows, lane, M, L, acc);
             }

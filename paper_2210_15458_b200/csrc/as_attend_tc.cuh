@@ -57,13 +57,34 @@ __device__ __forceinline__ void tc_ld32(uint32_t at, uint32_t (&r)[32]) {
                  "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
                  : TC_R8(r, 0), TC_R8(r, 8), TC_R8(r, 16), TC_R8(r, 24) : "r"(at));
 }
-template <int N> __device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t (&r)[N]) {
+__device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t (&r)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                  ::TC_W8(r, 0), TC_W8(r, 8), "r"(at) : "memory");
 }
 __device__ __forceinline__ void tc_ld16(uint32_t at, uint32_t (&r)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : TC_R8(r, 0), TC_R8(r, 8) : "r"(at));
+}
+// two floats side by side in a 64-bit register, and arithmetic on both
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ float2 unpair(uint64_t x) {
+    float2 d;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(x));
+    return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
 }
 // columns at .. at + 16 n of the warp's lanes, each thread's times f: 32-bit sums, or pairs of f16 weights
 __device__ __noinline__ void tc_scale_sums(uint32_t at, int n, float f) {
@@ -148,7 +169,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             tc_bar_init(bar(sm.k_full[i]), TC_FILL / 32); tc_bar_init(bar(sm.v_full[i]), TC_FILL / 32);
             tc_bar_init(bar(sm.k_empty[i]), 1); tc_bar_init(bar(sm.v_empty[i]), 1);
             tc_bar_init(bar(sm.s_full[i]), 1); tc_bar_init(bar(sm.p_full[i]), 4);
-            tc_bar_init(bar(sm.q_full[i]), TC_FILL / 32); tc_bar_init(bar(sm.q_empty[i]), 1 + TC_SOFT / 32);
+            tc_bar_init(bar(sm.q_full[i]), (DUAL ? 2 : 1) * TC_FILL / 32); tc_bar_init(bar(sm.q_empty[i]), 1 + TC_SOFT / 32);
         }
         tc_bar_init(bar(sm.o_full), 1); tc_bar_init(bar(sm.o_empty), TC_SOFT / 32);
         tc_bar_init(bar(sm.ml_full), TC_SOFT / 32); tc_bar_init(bar(sm.fin), 1);
@@ -215,13 +236,14 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = e < have ? v[e] : 0xFF800000u;
                     }
-                    float t0 = fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1])), t1 = fmaxf(__uint_as_float(v[2]), __uint_as_float(v[3]));
+                    float tops[4];
 #pragma unroll
-                    for (int e = 4; e < 32; e += 4) {
-                        t0 = fmaxf(fmaxf(t0, __uint_as_float(v[e])), __uint_as_float(v[e + 1]));
-                        t1 = fmaxf(fmaxf(t1, __uint_as_float(v[e + 2])), __uint_as_float(v[e + 3]));
+                    for (int i = 0; i < 4; ++i) {
+                        tops[i] = fmaxf(__uint_as_float(v[8 * i]), __uint_as_float(v[8 * i + 1]));
+#pragma unroll
+                        for (int e = 2; e < 8; e += 2) tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(v[8 * i + e])), __uint_as_float(v[8 * i + e + 1]));
                     }
-                    const float top = fmaxf(t0, t1) * k2;
+                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * k2;
                     const bool rise = top > m + AT_LAZY;
                     if (__any_sync(0xFFFFFFFFu, rise)) {
                         float f = 1.f;
@@ -233,15 +255,19 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         if (!first) tc_scale_sums(ot, D / 16, f);
                         if (ch > 0) tc_scale_weights(st, ch, f);
                     }
-                    float l0 = 0.f, l1 = 0.f;
+                    const uint64_t kk = pair(k2, k2), mm = pair(-mu, -mu);
+                    uint64_t sum[2] = {0, 0};
+                    uint32_t pk[16];
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
-                        const float p0 = ex2(fmaf(__uint_as_float(v[e]), k2, -mu)), p1 = ex2(fmaf(__uint_as_float(v[e + 1]), k2, -mu));
-                        l0 += p0; l1 += p1;
-                        v[e / 2] = pack_f16(p0, p1);
+                        float2 w = unpair(fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), kk, mm));
+                        w = make_float2(ex2(w.x), ex2(w.y));
+                        sum[e / 2 & 1] = add2(sum[e / 2 & 1], pair(w.x, w.y));
+                        pk[e / 2] = pack_f16(w.x, w.y);
                     }
-                    l += l0 + l1;
-                    tc_st16(st + 16 * ch, v);
+                    const float2 total = unpair(add2(sum[0], sum[1]));
+                    l += total.x + total.y;
+                    tc_st16(st + 16 * ch, pk);
                 }
                 first = false;
                 tc_wait_st();
@@ -399,12 +425,12 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
 #pragma unroll 1
             for (int item = 0; x < x1 && ok; ++item) {
                 const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x);
-                if constexpr (keys) {
+                if constexpr (keys || DUAL) {
                     // ---- the item's queries, scaled by a power of two into f16's range; a negative scale goes in here ----
                     if (q_use(item) > 0) ok = wait_warp(sm.q_empty[q_buf(item)], (q_use(item) - 1) & 1);
                     if (!ok) break;
-#pragma unroll 1
-                    for (int h = 0; h < (DUAL ? 2 : 1); ++h) {
+                    {
+                        constexpr int h = keys ? 0 : 1;             // (the values' group takes the second row tile)
                         const int row = cu.row0 + 128 * h + r, tok = a.by_g.div(row);
                         const uint16_t* from = static_cast<const uint16_t*>(a.q) + ((long long)cu.lane0 * c.T + tok) * a.q_ld + (cu.head * g + row - tok * g) * D;
                         const bool there = row < p.rows, wide = (reinterpret_cast<uintptr_t>(from) & 15) == 0;
@@ -415,7 +441,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                             return make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
                         };
                         uint32_t top = 0;                               // largest magnitude's bits
-#pragma unroll 4
+#pragma unroll 8
                         for (int i = 0; i < CHUNKS; ++i) {
                             const uint4 q = piece(i);
                             top = max(max(max(q.x & 0x7FFFu, q.x >> 16 & 0x7FFFu), max(q.y & 0x7FFFu, q.y >> 16 & 0x7FFFu)),
@@ -427,7 +453,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         sm.up[item & 1][128 * h + r] = __uint_as_float((uint32_t)(127 + ex) << 23);
                         const uint32_t to = q_s + (DUAL ? h : q_buf(item)) * MAT;
                         auto both = [&](uint32_t z) { return pack_f16(__uint_as_float(z << 16) * down, __uint_as_float(z & 0xFFFF0000u) * down); };
-#pragma unroll 4
+#pragma unroll 8
                         for (int i = 0; i < CHUNKS; ++i) {
                             const uint4 q = piece(i);
                             put(to + (i / 8) * BLK + tc_at(r, i % 8), make_uint4(both(q.x), both(q.y), both(q.z), both(q.w)));

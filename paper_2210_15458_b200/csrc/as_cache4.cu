@@ -118,10 +118,10 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
 }
 
 template <class K, class... A>
-static cudaError_t launch_after(K kern, unsigned grid, unsigned block, size_t smem, cudaStream_t st, A... args) {
+static cudaError_t launch_after(K kern, dim3 grid, unsigned block, size_t smem, cudaStream_t st, A... args) {
     // the kernel waits for its predecessor's results itself (griddepcontrol.wait), so its launch may overlap it
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -190,7 +190,7 @@ static int launch_attend(const AttendArgs& a, int N, const int* shared, void* wo
     e = launch_pass<DT, D>(a, pl.own, pl.own_kernel, sms, st);
     if (e != cudaSuccess) return cuda_fail(e, "attention kernel launch");
     const long long items = (long long)pl.own.n * pl.own.row_tiles * a.c.heads;
-    const unsigned grid = (unsigned)(items < 64 * sms ? items : 64 * sms);
+    const dim3 grid((unsigned)(items < 64 * sms ? items : 64 * sms), (pl.own.tile_rows + JOIN_ROWS - 1) / JOIN_ROWS);
     e = launch_after(attend_join_kernel<DT, D>, grid, 128, 0, st, a, pl.own, pl.pre);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "attention join kernel launch");
 }
