@@ -443,18 +443,21 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
 #pragma unroll
-            for (int j = 0; j < KS; ++j) {
-                uint32_t f[4];
+            for (int j = 0; j < KS; j += 2) {               // a word of each token is two steps of 16 dimensions
+                uint32_t f[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) codes_f16x2(kw[i][j / 2], f[i]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[i][e] = mul_f16(f[i][e], ks[i][j / 4]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        f[2 * h + i] = mul_f16(codes_f16x2(kw[i][j / 2] >> (16 * (j & 1) + 8 * h)), ks[i][j / 4]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    mma_f16(s[n], f[0], f[1], f[2], f[3], qf[0][n][j][0], qf[0][n][j][1]);
-                    if (F32) mma_f16(s[n], f[0], f[1], f[2], f[3], qf[PARTS - 1][n][j][0], qf[PARTS - 1][n][j][1]);
-                }
+                    for (int n = 0; n < NT; ++n) {
+                        mma_f16(s[n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[0][n][j + h][0], qf[0][n][j + h][1]);
+                        if (F32) mma_f16(s[n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[PARTS - 1][n][j + h][0], qf[PARTS - 1][n][j + h][1]);
+                    }
             }
             // ---- weights ----
             bool rise = false;
@@ -537,10 +540,14 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     even[h] = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u);
                     oddw[h] = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
                 }
+                uint32_t f[4][4];
+                codes_f16x2(even[0], f[0]);
+                codes_f16x2(oddw[0], f[1]);
+                codes_f16x2(even[1], f[2]);
+                codes_f16x2(oddw[1], f[3]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t f0 = mul_f16(codes_f16x2(even[0] >> (8 * i)), vs[0]), f1 = mul_f16(codes_f16x2(oddw[0] >> (8 * i)), vs[0]);
-                    const uint32_t f2 = mul_f16(codes_f16x2(even[1] >> (8 * i)), vs[1]), f3 = mul_f16(codes_f16x2(oddw[1] >> (8 * i)), vs[1]);
+                    const uint32_t f0 = mul_f16(f[0][i], vs[0]), f1 = mul_f16(f[1][i], vs[0]), f2 = mul_f16(f[2][i], vs[1]), f3 = mul_f16(f[3][i], vs[1]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[0][n][0], pf[0][n][1]);

@@ -410,8 +410,9 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             };
             // 8 codes x scale -> 16 bytes of f16
             auto widen = [](uint32_t codes, uint32_t scale2) {
-                return make_uint4(mul_f16(codes_f16x2(codes), scale2), mul_f16(codes_f16x2(codes >> 8), scale2), mul_f16(codes_f16x2(codes >> 16), scale2),
-                                  mul_f16(codes_f16x2(codes >> 24), scale2));
+                uint32_t f[4];
+                codes_f16x2(codes, f);
+                return make_uint4(mul_f16(f[0], scale2), mul_f16(f[1], scale2), mul_f16(f[2], scale2), mul_f16(f[3], scale2));
             };
             auto put = [](uint32_t at, const uint4& v) { asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); };
             auto filled = [&](uint32_t b) {

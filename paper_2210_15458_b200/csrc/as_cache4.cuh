@@ -55,6 +55,12 @@ __device__ __forceinline__ uint32_t codes_f16x2(uint32_t byte) {
     return d;
 }
 
+// the four bytes of a word at once (the conversion picks its byte itself: no shifts)
+__device__ __forceinline__ void codes_f16x2(uint32_t word, uint32_t (&d)[4]) {
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}" : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "r"(word));
+}
+
 template <int DT> struct Io;
 template <> struct Io<AS_F32> {
     using type = float;
