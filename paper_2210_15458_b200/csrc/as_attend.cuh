@@ -9,9 +9,9 @@
 
 namespace asx {
 
-constexpr int AT_W = 4;                     // warps of a CTA; a unit of work is a tile of 16 tokens for each
+constexpr int AT_W = 4;                     // warps of a CTA; a unit of work is 2 tiles of 16 tokens for each
 constexpr int AT_NT = 32 * AT_W;
-constexpr int AT_STAGES = 3;                // tiles that a warp has in flight or in use
+constexpr int AT_STAGES = 2;                // pairs of tiles that a warp has in flight or in use
 constexpr int AT_MAX_CTAS = 1024;
 constexpr float AT_LAZY = 8.f;              // the running maximum may lag by 8 (weights stay below 2^8, well within f16)
 
@@ -269,10 +269,17 @@ template <> __device__ __forceinline__ unsigned char lds<unsigned char>(uint32_t
     return (unsigned char)v;
 }
 
+template <int D> struct AttendSmem {
+    char ring[AT_W][AT_STAGES][2 * Tile4<D>::BYTES];
+    float join[AT_W][8][D + 20];            // the warps' sums (the pitch spreads rows over the banks)
+    float join_m[AT_W][8], join_l[AT_W][8];
+    RunSmem run;
+};
+
 // A state as it is kept in scratch: rows x D sums, then m and l of each row.
 template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(int rows) { return rows * (D + 2); }
 
-// Each warp takes every fourth tile of the CTA's run.  Scores are formed transposed, S^T = K q^T (tokens
+// Each warp takes every fourth pair of tiles of the CTA's run.  Scores are formed transposed, S^T = K q^T (tokens
 // x rows, so that 16 x 16 keys go through one instruction whatever the number of rows up to 8), and
 // so is the output, O^T = V^T P^T.  Keys and values become f16 in registers: code x scale is exact
 // there; queries are scaled by a power of two to lie in f16's range (bf16: exact) or split in two f16
@@ -285,11 +292,8 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     constexpr bool F32 = DT == AS_F32;
     constexpr int PARTS = F32 ? 2 : 1;
     constexpr int KS = D / 16;                      // steps of 16 dimensions
-    constexpr int PITCH = D + 20;                   // floats of a row in the joining buffer
-    __shared__ __align__(16) char ring[AT_W][AT_STAGES][Ti::BYTES];
-    __shared__ float join[AT_W][8][PITCH];
-    __shared__ float join_m[AT_W][8], join_l[AT_W][8];
-    __shared__ RunSmem run;
+    extern __shared__ __align__(16) char at_smem[];
+    AttendSmem<D>& sm = *reinterpret_cast<AttendSmem<D>*>(at_smem);
     const CacheArgs& c = a.c;
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, r = lane >> 2, cc = lane & 3;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -298,48 +302,43 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     const int g = (int)a.by_g.d;
     long long x0, x1;
     Cursor cu, ahead;
-    if (!find_run<AT_NT>(a, p, run, x0, x1, cu)) return;
+    if (!find_run<AT_NT>(a, p, sm.run, x0, x1, cu)) return;
     ahead = cu;
-    const long long units = x1 - x0;
+    int left = (int)min(x1 - x0, 0x7FFFFFFFLL), to_issue = left;   // (a CTA's share of units fits 31 bits)
 
-    // ---- copies: tile `w` of a unit into the warp's ring, the page id fetched one unit before ----
-    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(&ring[w][0][0]);
+    // ---- copies: half a warp brings in one of its two tiles; the page id is fetched a unit before ----
+    const int half = lane >> 4, hl = lane & 15;
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(&sm.ring[w][0][0]);
     const int page_mask = (1 << c.page_shift) - 1, tiles_per_page = 1 << (c.page_shift - 4);
     int page = 0;
-    auto look = [&]() {                             // page id of the tile under `ahead`
-        const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
+    auto look = [&]() {                             // page id of the half-warp's tile under `ahead`
+        const int pos = ahead.lo + ((ahead.u * AT_W + w) * 2 + half) * 16;
         if (pos < ahead.hi) page = c.table[(size_t)ahead.lane0 * c.max_pages + (pos >> c.page_shift)];
     };
     auto issue = [&](int stage) {
-        const int pos = ahead.lo + (ahead.u * AT_W + w) * 16;
+        const int pos = ahead.lo + ((ahead.u * AT_W + w) * 2 + half) * 16;
         if (pos < ahead.hi) {
             if (page < 0 || page >= c.n_pages) {
-                if (lane == 0 && c.lane_status) {
-                    const int l0 = ahead.lane0;
+                if (hl == 0) {
 #pragma unroll 1
-                    for (int j = 0; j < p.group; ++j) flag_lane(c.lane_status, l0 + j, AS_ERR_INVALID_ARG);
+                    for (int j = 0; j < p.group; ++j) flag_lane(c.lane_status, ahead.lane0 + j, AS_ERR_INVALID_ARG);
                 }
                 page = 0;
             }
-            const char* src = c.pages + (((size_t)page * c.heads + ahead.head) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
-            const uint32_t dst = ring0 + stage * Ti::BYTES;
+            const char* src = c.pages + (((size_t)page * c.heads + ahead.head) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES + hl * 16;
+            const uint32_t dst = ring0 + (stage * 2 + half) * Ti::BYTES + hl * 16;
 #pragma unroll
-            for (int i = 0; i < (Ti::BYTES / 16 + 31) / 32; ++i)
-                if (i * 32 + lane < Ti::BYTES / 16) cp_async16(dst + (i * 32 + lane) * 16, src + (i * 32 + lane) * 16);
+            for (int i = 0; i < (Ti::BYTES / 16 + 15) / 16; ++i)
+                if (i * 16 + 16 <= Ti::BYTES / 16 || i * 16 + hl < Ti::BYTES / 16) cp_async16(dst + i * 256, src + i * 256);
+        }
+        if (--to_issue > 0) {
+            ahead.step(a, p);
+            look();
         }
     };
-    long long issued = 0;
     look();
-#pragma unroll 1
-    for (int s = 0; s < AT_STAGES - 1; ++s) {
-        if (issued < units) {
-            issue(s);
-            ++issued;
-            ahead.step(a, p);
-            if (issued < units) look();
-        }
-        cp_commit();
-    }
+    issue(0);
+    cp_commit();
 
     using E = typename Io<DT>::type;
     uint32_t qf[PARTS][NT][KS][2];
@@ -348,7 +347,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     int seg_u0 = 0, stage = 0;
     bool fresh = true;
 #pragma unroll 1
-    for (long long x = x0; x < x1; ++x) {
+    for (; left > 0; --left) {
         if (fresh) {                                // ---- a new item: its query rows ----
             fresh = false;
             seg_u0 = cu.u;
@@ -404,81 +403,82 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
             }
             lim_min = __reduce_min_sync(0xFFFFFFFFu, lim_min);
         }
-        cp_wait<AT_STAGES - 2>();
+        cp_wait<0>();
         __syncwarp();
-        if (issued < units) {
-            int into = stage + AT_STAGES - 1;
-            if (into >= AT_STAGES) into -= AT_STAGES;
-            issue(into);
-            ++issued;
-            ahead.step(a, p);
-            if (issued < units) look();
-        }
+        if (to_issue > 0) issue(stage ^ 1);
         cp_commit();
-        const int pos = cu.lo + (cu.u * AT_W + w) * 16;
+        const int pos = cu.lo + (cu.u * AT_W + w) * 32;
         if (pos < cu.hi) {
-            const uint32_t st = ring0 + stage * Ti::BYTES;
+            const uint32_t st = ring0 + stage * 2 * Ti::BYTES;
+            const bool two = pos + 16 < cu.hi;              // (the second tile may lie behind the last token: nothing was copied)
             // ---- S^T = K q^T ----
-            const int t0 = 4 * (r >> 1) + (r & 1);      // the thread's tokens: t0 and t0 + 2
-            uint32_t kw[2][D / 32], ks[2][D / 64];
+            const int t0 = 4 * (r >> 1) + (r & 1);      // the thread's tokens of a tile: t0 and t0 + 2
+            float s[2][NT][4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int t = t0 + 2 * i;
-                if (D == 128) {
-                    const uint4 v = lds<uint4>(st + Ti::K + t * (D / 2) + cc * 16);
-                    kw[i][0] = v.x; kw[i][1] = v.y; kw[i][D / 32 - 2] = v.z; kw[i][D / 32 - 1] = v.w;
-                    const uint32_t s2 = e4m3_f16x2(lds<unsigned short>(st + Ti::KS + t * Ti::NB + 2 * cc));
-                    ks[i][0] = __byte_perm(s2, s2, 0x1010);
-                    ks[i][D / 64 - 1] = __byte_perm(s2, s2, 0x3232);
-                } else {
-                    const uint2 v = lds<uint2>(st + Ti::K + t * (D / 2) + cc * 8);
-                    kw[i][0] = v.x; kw[i][1] = v.y;
-                    const uint32_t s2 = e4m3_f16x2(lds<unsigned char>(st + Ti::KS + t * Ti::NB + cc));
-                    ks[i][0] = __byte_perm(s2, s2, 0x1010);
-                }
-            }
-            float s[NT][4];
+            for (int b = 0; b < 2; ++b) {
+                const uint32_t sb = st + b * Ti::BYTES;
+                uint32_t kw[2][D / 32], ks[2][D / 64];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-#pragma unroll
-            for (int j = 0; j < KS; j += 2) {               // a word of each token is two steps of 16 dimensions
-                uint32_t f[2][4];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) codes_f16x2(kw[i][j / 2], f[i]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) f[i][e] = mul_f16(f[i][e], ks[i][j / 4]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma_f16(s[n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[0][n][j + h][0], qf[0][n][j + h][1]);
-                        if (F32) mma_f16(s[n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[PARTS - 1][n][j + h][0], qf[PARTS - 1][n][j + h][1]);
+                for (int i = 0; i < 2; ++i) {
+                    const int t = t0 + 2 * i;
+                    if (D == 128) {
+                        const uint4 v = lds<uint4>(sb + Ti::K + t * (D / 2) + cc * 16);
+                        kw[i][0] = v.x; kw[i][1] = v.y; kw[i][D / 32 - 2] = v.z; kw[i][D / 32 - 1] = v.w;
+                        const uint32_t s2 = e4m3_f16x2(lds<unsigned short>(sb + Ti::KS + t * Ti::NB + 2 * cc));
+                        ks[i][0] = __byte_perm(s2, s2, 0x1010);
+                        ks[i][D / 64 - 1] = __byte_perm(s2, s2, 0x3232);
+                    } else {
+                        const uint2 v = lds<uint2>(sb + Ti::K + t * (D / 2) + cc * 8);
+                        kw[i][0] = v.x; kw[i][1] = v.y;
+                        const uint32_t s2 = e4m3_f16x2(lds<unsigned char>(sb + Ti::KS + t * Ti::NB + cc));
+                        ks[i][0] = __byte_perm(s2, s2, 0x1010);
                     }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][n][e] = 0.f;
+#pragma unroll
+                for (int j = 0; j < KS; j += 2) {           // a word of each token is two steps of 16 dimensions
+                    uint32_t f[2][4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) codes_f16x2(kw[i][j / 2], f[i]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) f[i][e] = mul_f16(f[i][e], ks[i][j / 4]);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma_f16(s[b][n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[0][n][j + h][0], qf[0][n][j + h][1]);
+                            if (F32) mma_f16(s[b][n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[PARTS - 1][n][j + h][0], qf[PARTS - 1][n][j + h][1]);
+                        }
+                }
             }
             // ---- weights ----
             bool rise = false;
+            const bool cut = pos + 32 > lim_min;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    s[n][h] *= k2[n][h];
-                    s[n][2 + h] *= k2[n][h];
-                    if (pos + 16 > lim_min) {
-                        if (pos + t0 >= lim[n][h]) s[n][h] = -INFINITY;
-                        if (pos + t0 + 2 >= lim[n][h]) s[n][2 + h] = -INFINITY;
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {           // tokens t0, t0 + 2 of the first tile, then of the second
+                        float& x = s[e >> 1][n][2 * (e & 1) + h];
+                        x *= k2[n][h];
+                        if (cut && pos + 16 * (e >> 1) + t0 + 2 * (e & 1) >= lim[n][h]) x = -INFINITY;
+                        top = fmaxf(top, x);
                     }
-                    rise |= fmaxf(s[n][h], s[n][2 + h]) > m[n][h] + AT_LAZY;
+                    rise |= top > m[n][h] + AT_LAZY;
                 }
             if (__any_sync(0xFFFFFFFFu, rise)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float top = fmaxf(s[n][h], s[n][2 + h]);
+                        float top = fmaxf(fmaxf(s[0][n][h], s[0][n][2 + h]), fmaxf(s[1][n][h], s[1][n][2 + h]));
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
                         top = fmaxf(top, m[n][h]);
@@ -490,78 +490,85 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                         for (int i = 0; i < KS; ++i) { o[n][i][h] *= f; o[n][i][2 + h] *= f; }
                     }
             }
-            uint32_t pf[PARTS][NT][2];
+            uint32_t pf[2][PARTS][NT][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float pr[4];
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) pr[e] = ex2(s[n][e] - mu[n][e & 1]);
-                l[n][0] += pr[0] + pr[2];
-                l[n][1] += pr[1] + pr[3];
+                for (int n = 0; n < NT; ++n) {
+                    float pr[4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t hi = pack_f16(pr[2 * i], pr[2 * i + 1]);
-                    pf[0][n][i] = transpose8x8(hi);
-                    if (F32) {
-                        const float2 h2 = unpack_f16(hi);
-                        pf[PARTS - 1][n][i] = transpose8x8(pack_f16(pr[2 * i] - h2.x, pr[2 * i + 1] - h2.y));
+                    for (int e = 0; e < 4; ++e) pr[e] = ex2(s[b][n][e] - mu[n][e & 1]);
+                    l[n][0] += pr[0] + pr[2];
+                    l[n][1] += pr[1] + pr[3];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t hi = pack_f16(pr[2 * i], pr[2 * i + 1]);
+                        pf[b][0][n][i] = transpose8x8(hi);
+                        if (F32) {
+                            const float2 h2 = unpack_f16(hi);
+                            pf[b][PARTS - 1][n][i] = transpose8x8(pack_f16(pr[2 * i] - h2.x, pr[2 * i + 1] - h2.y));
+                        }
                     }
                 }
-            }
             // ---- O^T += V^T P^T ----
-            uint32_t vw[4][D / 64];                 // tokens 4 cc .. 4 cc + 3, the thread's D / 8 dimensions
-            const uint32_t vb = st + Ti::V + (D == 128 ? r : r >> 1) * 128 + cc * 32;
-            const bool odd = r & 1;
-            {
-                // (odd r reads its two halves in the other order: no two threads of a phase meet in a bank)
-                const bool swap = D == 128 && odd;
-                const uint4 x0v = lds<uint4>(vb + (swap ? 16 : 0)), x1v = lds<uint4>(vb + (swap ? 0 : 16));
-                const uint4 v0 = swap ? x1v : x0v, v1 = swap ? x0v : x1v;
-                if (D == 128) {
-                    vw[0][0] = v0.x; vw[0][D / 64 - 1] = v0.y; vw[1][0] = v0.z; vw[1][D / 64 - 1] = v0.w;
-                    vw[2][0] = v1.x; vw[2][D / 64 - 1] = v1.y; vw[3][0] = v1.z; vw[3][D / 64 - 1] = v1.w;
-                } else {
-                    vw[0][0] = odd ? v0.y : v0.x; vw[1][0] = odd ? v0.w : v0.z;
-                    vw[2][0] = odd ? v1.y : v1.x; vw[3][0] = odd ? v1.w : v1.z;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                if (b == 1 && !two) break;
+                const uint32_t sb = st + b * Ti::BYTES;
+                uint32_t vw[4][D / 64];             // tokens 4 cc .. 4 cc + 3, the thread's D / 8 dimensions
+                const uint32_t vb = sb + Ti::V + (D == 128 ? r : r >> 1) * 128 + cc * 32;
+                const bool odd = r & 1;
+                {
+                    // (odd r reads its two halves in the other order: no two threads of a phase meet in a bank)
+                    const bool swap = D == 128 && odd;
+                    const uint4 x0v = lds<uint4>(vb + (swap ? 16 : 0)), x1v = lds<uint4>(vb + (swap ? 0 : 16));
+                    const uint4 v0 = swap ? x1v : x0v, v1 = swap ? x0v : x1v;
+                    if (D == 128) {
+                        vw[0][0] = v0.x; vw[0][D / 64 - 1] = v0.y; vw[1][0] = v0.z; vw[1][D / 64 - 1] = v0.w;
+                        vw[2][0] = v1.x; vw[2][D / 64 - 1] = v1.y; vw[3][0] = v1.z; vw[3][D / 64 - 1] = v1.w;
+                    } else {
+                        vw[0][0] = odd ? v0.y : v0.x; vw[1][0] = odd ? v0.w : v0.z;
+                        vw[2][0] = odd ? v1.y : v1.x; vw[3][0] = odd ? v1.w : v1.z;
+                    }
                 }
-            }
-            uint32_t vs4 = lds<uint32_t>(st + Ti::VS + (D == 128 ? r : r >> 1) * 16 + cc * 4);
-            if (pos + 16 > cu.hi) {                 // tokens behind the last one: whatever the page holds there counts as zero
-                const int have = cu.hi - pos - 4 * cc;
-                vs4 &= have >= 4 ? 0xFFFFFFFFu : have <= 0 ? 0u : (1u << (8 * have)) - 1;
-            }
-            const uint32_t vs[2] = {e4m3_f16x2(vs4 & 0xFFFFu), e4m3_f16x2(vs4 >> 16)};
-#pragma unroll
-            for (int i4 = 0; i4 < D / 64; ++i4) {
-                uint32_t even[2], oddw[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t x = vw[2 * h][i4], y = vw[2 * h + 1][i4];
-                    even[h] = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u);
-                    oddw[h] = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+                uint32_t vs4 = lds<uint32_t>(sb + Ti::VS + (D == 128 ? r : r >> 1) * 16 + cc * 4);
+                if (pos + 32 > cu.hi) {             // tokens behind the last one: whatever the page holds there counts as zero
+                    const int have = cu.hi - pos - 16 * b - 4 * cc;
+                    vs4 &= have >= 4 ? 0xFFFFFFFFu : have <= 0 ? 0u : (1u << (8 * have)) - 1;
                 }
-                uint32_t f[4][4];
-                codes_f16x2(even[0], f[0]);
-                codes_f16x2(oddw[0], f[1]);
-                codes_f16x2(even[1], f[2]);
-                codes_f16x2(oddw[1], f[3]);
+                const uint32_t vs[2] = {e4m3_f16x2(vs4 & 0xFFFFu), e4m3_f16x2(vs4 >> 16)};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t f0 = mul_f16(f[0][i], vs[0]), f1 = mul_f16(f[1][i], vs[0]), f2 = mul_f16(f[2][i], vs[1]), f3 = mul_f16(f[3][i], vs[1]);
+                for (int i4 = 0; i4 < D / 64; ++i4) {
+                    uint32_t even[2], oddw[2];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[0][n][0], pf[0][n][1]);
-                        if (F32) mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[PARTS - 1][n][0], pf[PARTS - 1][n][1]);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t x = vw[2 * h][i4], y = vw[2 * h + 1][i4];
+                        even[h] = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u);
+                        oddw[h] = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+                    }
+                    uint32_t f[4][4];
+                    codes_f16x2(even[0], f[0]);
+                    codes_f16x2(oddw[0], f[1]);
+                    codes_f16x2(even[1], f[2]);
+                    codes_f16x2(oddw[1], f[3]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t f0 = mul_f16(f[0][i], vs[0]), f1 = mul_f16(f[1][i], vs[0]), f2 = mul_f16(f[2][i], vs[1]), f3 = mul_f16(f[3][i], vs[1]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[b][0][n][0], pf[b][0][n][1]);
+                            if (F32) mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[b][PARTS - 1][n][0], pf[b][PARTS - 1][n][1]);
+                        }
                     }
                 }
             }
         }
         __syncwarp();
-        if (++stage == AT_STAGES) stage = 0;
+        stage ^= 1;
 
         // ---- the end of an item, or of the run: the four warps' states become one ----
         const bool item_ends = cu.u + 1 == cu.nu;
-        if (item_ends || x + 1 == x1) {
+        if (item_ends || left == 1) {
             const int head = cu.head;
             const bool whole = item_ends && seg_u0 == 0;
             float* part = nullptr;
@@ -575,27 +582,27 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     float sum = l[n][h];
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-                    if (r == 0) { join_m[w][2 * cc + h] = m[n][h]; join_l[w][2 * cc + h] = sum; }
+                    if (r == 0) { sm.join_m[w][2 * cc + h] = m[n][h]; sm.join_l[w][2 * cc + h] = sum; }
 #pragma unroll
                     for (int i = 0; i < KS; ++i)
-                        *reinterpret_cast<float2*>(&join[w][2 * cc + h][r * (D / 8 + 2) + 2 * i]) = make_float2(o[n][i][h], o[n][i][2 + h]);
+                        *reinterpret_cast<float2*>(&sm.join[w][2 * cc + h][r * (D / 8 + 2) + 2 * i]) = make_float2(o[n][i][h], o[n][i][2 + h]);
                 }
                 __syncthreads();
                 constexpr int PER = D / 16;         // dimensions of a thread; 16 threads a row
                 const int rw = tid >> 4, d0 = (tid & 15) * PER;
                 float f[AT_W], M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
-                for (int i = 0; i < AT_W; ++i) M = fmaxf(M, join_m[i][rw]);
+                for (int i = 0; i < AT_W; ++i) M = fmaxf(M, sm.join_m[i][rw]);
 #pragma unroll
                 for (int i = 0; i < AT_W; ++i) {
-                    f[i] = join_m[i][rw] == -INFINITY ? 0.f : ex2(join_m[i][rw] - M);
-                    L += f[i] * join_l[i][rw];
+                    f[i] = sm.join_m[i][rw] == -INFINITY ? 0.f : ex2(sm.join_m[i][rw] - M);
+                    L += f[i] * sm.join_l[i][rw];
                 }
 #pragma unroll
                 for (int e = 0; e < PER; ++e) {
                     acc[e] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < AT_W; ++i) acc[e] += f[i] * join[i][rw][(d0 / (D / 8)) * (D / 8 + 2) + d0 % (D / 8) + e];
+                    for (int i = 0; i < AT_W; ++i) acc[e] += f[i] * sm.join[i][rw][(d0 / (D / 8)) * (D / 8 + 2) + d0 % (D / 8) + e];
                 }
                 const int row = cu.row0 + n * 8 + rw;
                 if (part) {

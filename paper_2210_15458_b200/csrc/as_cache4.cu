@@ -105,7 +105,7 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
         p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
         p.by_row_tiles.set(p.row_tiles);
         p.by_N.set(N);
-        p.unit_shift = tc ? 7 : 6;     // TC_KV, 16 * AT_W tokens
+        p.unit_shift = 7;               // TC_KV = 32 * AT_W tokens
         p.cum = reinterpret_cast<int*>(take(sizeof(int) * ((size_t)n * p.row_tiles + 1)));
         const size_t state = sizeof(float) * (size_t)p.tile_rows * (D + 2);
         p.part_cta = reinterpret_cast<float*>(take(2 * (size_t)(tc ? TC_MAX_CTAS : AT_MAX_CTAS) * state));
@@ -141,12 +141,13 @@ static cudaError_t launch_mma(const AttendArgs& a, PassArgs& p, int sms, cudaStr
     auto kern = attend_mma_kernel<DT, D, NT>;
     if (per_sm[dev] == 0) {
         int n = 0;
-        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, AT_NT, 0);
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(AttendSmem<D>));
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, AT_NT, sizeof(AttendSmem<D>));
         if (e != cudaSuccess) return e;
         per_sm[dev] = n > 0 ? n : 1;
     }
     p.ctas = per_sm[dev] * sms < AT_MAX_CTAS ? per_sm[dev] * sms : AT_MAX_CTAS;
-    return launch_after(kern, p.ctas, AT_NT, 0, st, a, p);
+    return launch_after(kern, p.ctas, AT_NT, sizeof(AttendSmem<D>), st, a, p);
 }
 
 template <int D, bool DUAL>
