@@ -162,7 +162,8 @@ def _check(rc: int) -> None:
 
 def _stream(stream) -> int:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # the current device's current stream, without building a Stream object around it (0.3 us instead of 4.8)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -456,7 +457,7 @@ def as_logits_edit(logits: torch.Tensor, seq: Optional[torch.Tensor] = None, len
     lanes, width, ld = _logits_layout(logits)
     V = width if V is None else V
     if out is None:
-        out = torch.empty((lanes, V), dtype=logits.dtype, device=logits.device)
+        out = logits.new_empty((lanes, V))
     elif out.dtype != logits.dtype or out.dim() != 2 or out.shape[0] != lanes or out.shape[1] < V:
         raise ValueError("out must have the logits' dtype and a row of at least V for each lane")
     e = as_logit_edits()
@@ -541,7 +542,7 @@ def as_cache4_load(pages: torch.Tensor, table: torch.Tensor, length: torch.Tenso
     """(k, v) [lanes, T, heads, D]: what is stored for the last T tokens of each lane (zeros where there is none)."""
     c = _cache4(pages, k_scale, v_scale)
     lanes = length.numel()
-    k = torch.empty((lanes, T, c.heads, c.head_dim), dtype=dtype, device=pages.device)
+    k = pages.new_empty((lanes, T, c.heads, c.head_dim), dtype=dtype)
     v = torch.empty_like(k)
     tp, max_pages, lp = _table(table, length, lanes)
     _check(lib().as_cache4_load(ctypes.byref(c), k.data_ptr(), v.data_ptr(), _logits_dtype(k), lanes, T, tp, max_pages, lp,
@@ -563,7 +564,7 @@ def as_cache4_attend(pages: torch.Tensor, q: torch.Tensor, table: torch.Tensor, 
     c = _cache4(pages, k_scale, v_scale)
     lanes, T, heads, q_ld = _tokens(q, c.head_dim, "q")
     if out is None:
-        out = torch.empty((lanes, T, heads, c.head_dim), dtype=q.dtype, device=q.device)
+        out = q.new_empty((lanes, T, heads, c.head_dim))
     elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
         raise ValueError("out must be contiguous, with the shape and dtype of q")
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() != lanes * T * heads or not lse.is_contiguous()):
@@ -572,7 +573,7 @@ def as_cache4_attend(pages: torch.Tensor, q: torch.Tensor, table: torch.Tensor, 
     dt = _logits_dtype(q)
     need = L.as_cache4_attend_work_bytes(ctypes.byref(c), dt, lanes, T, heads, N)
     if work is None:
-        work = torch.empty(need, dtype=torch.uint8, device=q.device)
+        work = length.new_empty((need + 3) // 4)
     tp, max_pages, lp = _table(table, length, lanes)
     _check(L.as_cache4_attend(ctypes.byref(c), q.data_ptr(), q_ld, dt, lanes, T, heads, tp, max_pages, lp, scale, N,
                               _int32(shared, "shared", lanes // N if N > 0 else None), out.data_ptr(), _ptr(lse),
@@ -595,9 +596,9 @@ def _pool(pool: Optional[torch.Tensor], n_pages: int):
     return pool.data_ptr(), pool.shape[0], pool.stride(0) * e, pool.stride(1) * e
 
 
-def _pages_work(work: Optional[torch.Tensor], lanes_in: int, lanes_out: int, n_pages: int, device):
+def _pages_work(work: Optional[torch.Tensor], lanes_in: int, lanes_out: int, n_pages: int, like: torch.Tensor):
     if work is None:
-        work = torch.empty(lib().as_pages_work_bytes(lanes_in, lanes_out, n_pages), dtype=torch.uint8, device=device)
+        work = like.new_empty((lib().as_pages_work_bytes(lanes_in, lanes_out, n_pages) + 3) // 4)
     return work, work.numel() * work.element_size()
 
 
@@ -610,13 +611,13 @@ def as_pages_fork(parent: torch.Tensor, table: torch.Tensor, length: torch.Tenso
     lanes, max_pages = table.shape
     n = parent.numel()
     if table_out is None:
-        table_out = torch.empty((n, max_pages), dtype=torch.int32, device=table.device)
+        table_out = table.new_empty((n, max_pages))
     if length_out is None:
-        length_out = torch.empty(n, dtype=torch.int32, device=table.device)
+        length_out = table.new_empty(n)
     if ref_out is None:
         ref_out = torch.empty_like(ref)
     data, planes, stride, page_bytes = _pool(pool, ref.numel())
-    work, nbytes = _pages_work(work, lanes, n, ref.numel(), table.device)
+    work, nbytes = _pages_work(work, lanes, n, ref.numel(), ref)
     _check(lib().as_pages_fork(_int32(parent, "parent"), lanes, n, max_pages, page_size, ref.numel(), _int32(table, "table"),
                                _int32(length, "length", lanes), _int32(ref, "ref"),
                                _int32(table_out, "table_out", n * max_pages), _int32(length_out, "length_out", n),
@@ -629,7 +630,7 @@ def as_pages_grow(add: torch.Tensor, table: torch.Tensor, length: torch.Tensor, 
                   lane_status: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None, stream=None) -> None:
     """Give every lane the pages for add[lane] more tokens; table, length and ref are updated in place."""
     lanes, max_pages = table.shape
-    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), table.device)
+    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), ref)
     _check(lib().as_pages_grow(_int32(add, "add", lanes), lanes, max_pages, page_size, ref.numel(), _int32(table, "table"),
                                _int32(length, "length", lanes), _int32(ref, "ref"),
                                _int32(lane_status, "lane_status", lanes), work.data_ptr(), nbytes, _stream(stream)))
@@ -644,9 +645,9 @@ def as_pages_compact(table: torch.Tensor, ref: torch.Tensor, pool: Optional[torc
     table_out = table if table_out is None else table_out
     ref_out = ref if ref_out is None else ref_out
     if used is None:
-        used = torch.empty((), dtype=torch.int32, device=table.device)
+        used = table.new_empty(())
     data, planes, stride, page_bytes = _pool(pool, ref.numel())
-    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), table.device)
+    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), ref)
     _check(lib().as_pages_compact(lanes, max_pages, ref.numel(), _int32(table, "table"), _int32(ref, "ref"),
                                   _int32(table_out, "table_out", table.numel()), _int32(ref_out, "ref_out", ref.numel()),
                                   _int32(used, "used", 1), data, planes, stride, page_bytes, work.data_ptr(), nbytes,
