@@ -15,19 +15,6 @@ constexpr int AT_STAGES = 2;                // pairs of tiles that a warp has in
 constexpr int AT_MAX_CTAS = 1024;
 constexpr float AT_LAZY = 8.f;              // the running maximum may lag by 8 (weights stay below 2^8, well within f16)
 
-// n / d for n < 2^31 by a multiplication (Granlund and Montgomery's round-up method)
-struct Divisor {
-    uint32_t d, mul, shift;
-    __host__ void set(uint32_t by) {
-        d = by;
-        shift = 0;
-        while ((1ull << shift) < by) ++shift;
-        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
-    }
-    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
-    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
-};
-
 struct AttendArgs {
     CacheArgs c;
     const void* q;

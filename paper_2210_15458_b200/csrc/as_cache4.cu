@@ -39,6 +39,8 @@ static CacheArgs cache_args(const as_cache4* c, int lanes, int T, const int* tab
     a.k_scale = c->d_k_scale; a.v_scale = c->d_v_scale;
     a.table = table; a.max_pages = max_pages; a.len = len; a.lane_status = status;
     a.lanes = lanes; a.T = T;
+    a.by_T.set(T);
+    a.by_heads.set(c->heads);
     return a;
 }
 
@@ -53,17 +55,26 @@ static unsigned grid_of(long long threads, int nt) {
     return (unsigned)(n < (1 << 14) ? n : (1 << 14));       // (the kernels loop)
 }
 
+// (blocks by tiles from 16 tokens a lane on: below, most of a tile's threads would have nothing to do)
+static bool by_tiles(const CacheArgs& a) { return a.T >= 16 && (long long)a.lanes * ((a.T + 15) / 16 + 1) * a.heads < (1LL << 31); }
+static unsigned block_grid(const CacheArgs& a, int D, bool tiles) {
+    const long long tokens = tiles ? (long long)a.lanes * (((a.T + 15) / 16 + C4_U) / C4_U) * 16 : (long long)a.lanes * a.T;
+    return grid_of(tokens * 2 * a.heads * (D / 16), C4_NT);
+}
 template <int DT, int D>
 static void launch_append(const CacheArgs& a, const void* k, long long k_ld, const void* v, long long v_ld, bool vec, cudaStream_t st) {
     using E = typename Io<DT>::type;
-    const long long n = (long long)a.lanes * a.T * 2 * a.heads * (D / 16);
-    append_kernel<DT, D><<<grid_of(n, C4_NT), C4_NT, 0, st>>>(a, static_cast<const E*>(k), k_ld, static_cast<const E*>(v), v_ld, vec);
+    const bool tiles = by_tiles(a);
+    auto kern = tiles ? (vec ? append_kernel<DT, D, true, true> : append_kernel<DT, D, true, false>)
+                      : (vec ? append_kernel<DT, D, false, true> : append_kernel<DT, D, false, false>);
+    kern<<<block_grid(a, D, tiles), C4_NT, 0, st>>>(a, static_cast<const E*>(k), k_ld, static_cast<const E*>(v), v_ld);
 }
 template <int DT, int D>
 static void launch_load(const CacheArgs& a, void* k, void* v, cudaStream_t st) {
     using E = typename Io<DT>::type;
-    const long long n = (long long)a.lanes * a.T * 2 * a.heads * (D / 16);
-    load_kernel<DT, D><<<grid_of(n, C4_NT), C4_NT, 0, st>>>(a, static_cast<E*>(k), static_cast<E*>(v));
+    const bool tiles = by_tiles(a);
+    auto kern = tiles ? load_kernel<DT, D, true> : load_kernel<DT, D, false>;
+    kern<<<block_grid(a, D, tiles), C4_NT, 0, st>>>(a, static_cast<E*>(k), static_cast<E*>(v));
 }
 
 // ---------------------------------------------------------------------------

@@ -7,6 +7,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 namespace asx {
 
 // A tile: 16 tokens of one head (see as_cache4 in the header).
@@ -19,6 +21,19 @@ template <int D> struct Tile4 {
     __device__ static int v_scale(int t, int b) { return VS + b * 16 + t; }
 };
 
+// n / d for n < 2^31 by a multiplication (Granlund and Montgomery's round-up method)
+struct Divisor {
+    uint32_t d, mul, shift;
+    __host__ void set(uint32_t by) {
+        d = by;
+        shift = 0;
+        while ((1ull << shift) < by) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
+};
+
 struct CacheArgs {
     char* pages;
     int n_pages, heads, page_shift;                 // page size = 1 << page_shift tokens
@@ -28,6 +43,7 @@ struct CacheArgs {
     const int* len;
     int* lane_status;
     int lanes, T;
+    Divisor by_T, by_heads;
 };
 
 // e4m3 bits -> value
@@ -64,18 +80,18 @@ __device__ __forceinline__ void codes_f16x2(uint32_t word, uint32_t (&d)[4]) {
 template <int DT> struct Io;
 template <> struct Io<AS_F32> {
     using type = float;
-    __device__ static void read16(const float* p, bool vec, float (&x)[16]) {
-        if (vec) {
+    struct raw16 { float4 q[4]; };                      // 16 elements as they are
+    __device__ static raw16 load16(const float* p, bool vec) {
+        raw16 r;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 q = reinterpret_cast<const float4*>(p)[i];
-                x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = p[i];
-        }
+        for (int i = 0; i < 4; ++i) r.q[i] = vec ? __ldcs(reinterpret_cast<const float4*>(p) + i) : make_float4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
+        return r;
     }
+    __device__ static void widen16(const raw16& r, float (&x)[16]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[4 * i] = r.q[i].x; x[4 * i + 1] = r.q[i].y; x[4 * i + 2] = r.q[i].z; x[4 * i + 3] = r.q[i].w; }
+    }
+    __device__ static void read16(const float* p, bool vec, float (&x)[16]) { widen16(load16(p, vec), x); }
     __device__ static void write16(float* p, const float (&x)[16]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
@@ -83,23 +99,24 @@ template <> struct Io<AS_F32> {
 };
 template <> struct Io<AS_BF16> {
     using type = __nv_bfloat16;
-    __device__ static void read16(const __nv_bfloat16* p, bool vec, float (&x)[16]) {
+    struct raw16 { uint32_t w[8]; };
+    __device__ static raw16 load16(const __nv_bfloat16* p, bool vec) {
+        raw16 r;
         if (vec) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint4 q = reinterpret_cast<const uint4*>(p)[i];
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-                    x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-                }
-            }
+            const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+            r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w; r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
         } else {
+            const uint16_t* e = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = __bfloat162float(p[i]);
+            for (int i = 0; i < 8; ++i) r.w[i] = e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
         }
+        return r;
     }
+    __device__ static void widen16(const raw16& r, float (&x)[16]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { x[2 * i] = __uint_as_float(r.w[i] << 16); x[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u); }
+    }
+    __device__ static void read16(const __nv_bfloat16* p, bool vec, float (&x)[16]) { widen16(load16(p, vec), x); }
     __device__ static void write16(__nv_bfloat16* p, const float (&x)[16]) {
         uint32_t w[8];
 #pragma unroll
@@ -112,114 +129,186 @@ template <> struct Io<AS_BF16> {
     }
 };
 
-// Where position p of a lane's head lies: the tile's address, or null for a page id out of range.
-template <int D>
-__device__ __forceinline__ char* tile_of(const CacheArgs& c, int lane, int head, int p, bool& bad) {
-    const int page = c.table[(size_t)lane * c.max_pages + (p >> c.page_shift)];
-    if (page < 0 || page >= c.n_pages) { bad = true; return nullptr; }
-    const int tiles = 1 << (c.page_shift - 4), tile = (p & ((1 << c.page_shift) - 1)) >> 4;
-    return c.pages + (((size_t)page * c.heads + head) * tiles + tile) * Tile4<D>::BYTES;
-}
-
 __device__ __forceinline__ void flag_lane(int* lane_status, int lane, int code) {
     if (lane_status) atomicMin(&lane_status[lane], code);
 }
 
-// One thread stores one block of 16 dimensions of one token: it reads 16 elements, finds their
-// largest magnitude, and writes 8 bytes of codes and a scale.  Blocks run fastest over the threads:
-// a warp reads whole 32-byte sectors side by side.
+// Storing and reading back work on blocks: 16 dimensions of one token, which are 8 bytes of codes and a scale.  A thread
+// has U of them at a time, 16 tokens apart, so that their loads are in flight together.
+struct Block {
+    int lane, len, tok, head, b;                    // tok: the first token within the call (one outside 0 .. T - 1 is none)
+    bool is_v;
+};
+constexpr int C4_U = 4;
+
 constexpr int C4_NT = 256;
 
-template <int DT, int D>
-__global__ void __launch_bounds__(C4_NT)
-append_kernel(const CacheArgs c, const typename Io<DT>::type* __restrict__ k, long long k_ld,
-              const typename Io<DT>::type* __restrict__ v, long long v_ld, bool vec) {
-    using Ti = Tile4<D>;
-    // (lanes x T is at most 2^30, heads at most 128: pieces of a row are counted in 32 bits, rows in 32 bits)
-    const unsigned per_row = 2 * c.heads * Ti::NB;
+// Few tokens a lane (T < 16): blocks side by side in the caller's tensors run along the threads.  Tokens are rows
+// (at most 2^30), a row has 2 x heads x D / 16 blocks.
+template <int D, class F>
+__device__ __forceinline__ void each_block_by_rows(const CacheArgs& c, F&& f) {
+    constexpr int NB = D / 16;
+    const unsigned per_row = 2 * c.heads * NB, rows = (unsigned)c.lanes * c.T;
     const unsigned step = gridDim.x * C4_NT, first = blockIdx.x * C4_NT + threadIdx.x;
     const unsigned row_step = step / per_row, piece_step = step % per_row;
     unsigned row = first / per_row, piece = first % per_row;
-    for (; row < (unsigned)c.lanes * c.T; row += row_step, piece += piece_step) {
-        if (piece >= per_row) { piece -= per_row; if (++row >= (unsigned)c.lanes * c.T) break; }
-        const int b = piece % Ti::NB, head = piece / Ti::NB % c.heads;
-        const bool is_v = piece >= per_row / 2;
-        const int lane = (int)(row / c.T), tok = (int)(row % c.T);
-        const int len = c.len[lane];
-        if (len < 0 || len > ((long long)c.max_pages << c.page_shift)) { flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG); continue; }
-        const int p = len - c.T + tok;
-        if (p < 0) continue;
-        bool bad = false;
-        char* tile = tile_of<D>(c, lane, head, p, bad);
-        if (bad) { flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG); continue; }
-        float x[16];
-        Io<DT>::read16((is_v ? v + (long long)row * v_ld : k + (long long)row * k_ld) + head * D + b * 16, vec, x);
-        const float* hs = is_v ? c.v_scale : c.k_scale;
-        const float inv = hs ? __frcp_rn(hs[head]) : 1.f;
-        float top = 0.f;
-        bool odd = false;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            x[e] = __fmul_rn(x[e], inv);
-            odd |= !(fabsf(x[e]) <= 3.402823466e38f);
-            if (x[e] != x[e]) x[e] = 0.f;
-            top = fmaxf(top, fabsf(x[e]));
-        }
-        if (odd) flag_lane(c.lane_status, lane, AS_ERR_NUMERIC);
-        const uint32_t s8 = to_e4m3(__fmul_rn(top, 1.f / 6.f));
-        const float s = e4m3_value(s8);
-        const float rs = s > 0.f ? __frcp_rn(s) : 0.f;
-        uint32_t w[2] = {0, 0};
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            // (an infinite value with a zero factor cannot occur: its block's scale is the largest)
-            w[e >> 3] |= to_codes(__fmul_rn(x[e], rs), __fmul_rn(x[e + 1], rs)) << (4 * (e & 7));
-        }
-        const int t = p & 15;
-        *reinterpret_cast<uint2*>(tile + (is_v ? Ti::v_code(t, b) : Ti::k_code(t, b))) = make_uint2(w[0], w[1]);
-        tile[is_v ? Ti::v_scale(t, b) : Ti::k_scale(t, b)] = (char)s8;
+#pragma unroll 1
+    for (; row < rows; row += row_step, piece += piece_step) {
+        if (piece >= per_row) { piece -= per_row; if (++row >= rows) break; }
+        Block k;
+        k.is_v = piece >= per_row / 2;
+        const unsigned r = piece - (k.is_v ? per_row / 2 : 0);
+        k.b = r % NB;
+        k.head = r / NB;
+        k.lane = c.by_T.div(row);
+        k.tok = row - k.lane * c.T;
+        k.len = c.len[k.lane];
+        f(k, std::integral_constant<int, 1>{});
     }
 }
 
-template <int DT, int D>
+// Many tokens a lane: a group of 2 x D threads takes a tile of 16 positions of one head, keys in the order of their
+// codes (blocks of a token side by side), values in the order of theirs (tokens of a block side by side): every 32-byte
+// sector of the caller's tensors and of the cache is moved once and whole.
+template <int D, class F>
+__device__ __forceinline__ void each_block_by_tiles(const CacheArgs& c, F&& f) {
+    constexpr int NB = D / 16, GROUP = 32 * NB;
+    const int groups = ((c.T + 15) / 16 + 1 + C4_U - 1) / C4_U;     // sets of U tiles that T positions can touch
+    const unsigned r = threadIdx.x % GROUP;
+    const unsigned n = (unsigned)c.lanes * groups * c.heads, step = gridDim.x * (C4_NT / GROUP);
+#pragma unroll 1
+    for (unsigned i = blockIdx.x * (C4_NT / GROUP) + threadIdx.x / GROUP; i < n; i += step) {
+        Block k;
+        const unsigned j = c.by_heads.div(i), lane = j / groups;
+        k.head = i - j * c.heads;
+        k.lane = lane;
+        k.is_v = r >= 16 * NB;
+        const unsigned q = r % (16 * NB);
+        const int t = k.is_v ? q % 16 : q / NB;
+        k.b = k.is_v ? q / 16 : q % NB;
+        k.len = c.len[lane];
+        const int start = k.len - c.T, tile0 = start >> 4;          // (the first position may lie below 0)
+        k.tok = (tile0 + (int)(j - lane * groups) * C4_U) * 16 + t - start;
+        f(k, std::integral_constant<int, C4_U>{});
+    }
+}
+
+// The tiles of a thread's U tokens: null for one that is outside the call, in front of the first position or in no page.
+template <int D, int U>
+__device__ __forceinline__ void tiles_of(const CacheArgs& c, const Block& at, char* (&tile)[U]) {
+    const int p0 = at.len - c.T + at.tok, mask = (1 << c.page_shift) - 1;
+    const bool len_ok = at.len >= 0 && at.len <= ((long long)c.max_pages << c.page_shift);
+    int page[U];
+    bool real[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int tok = at.tok + 16 * u, p = p0 + 16 * u;
+        real[u] = len_ok && tok >= 0 && tok < c.T && p >= 0;
+        page[u] = real[u] ? c.table[(size_t)at.lane * c.max_pages + (p >> c.page_shift)] : 0;
+    }
+    bool bad = !len_ok;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const bool in = page[u] >= 0 && page[u] < c.n_pages;
+        bad |= !in;
+        tile[u] = real[u] && in ? c.pages + (((size_t)page[u] * c.heads + at.head) * (mask + 1 >> 4) + (((p0 + 16 * u) & mask) >> 4)) * Tile4<D>::BYTES : nullptr;
+    }
+    if (bad) flag_lane(c.lane_status, at.lane, AS_ERR_INVALID_ARG);
+}
+
+template <int DT, int D, bool TILES, bool VEC>
 __global__ void __launch_bounds__(C4_NT)
-load_kernel(const CacheArgs c, typename Io<DT>::type* __restrict__ k, typename Io<DT>::type* __restrict__ v) {
+append_kernel(const __grid_constant__ CacheArgs c, const typename Io<DT>::type* __restrict__ k, long long k_ld,
+              const typename Io<DT>::type* __restrict__ v, long long v_ld) {
     using Ti = Tile4<D>;
-    const unsigned per_row = 2 * c.heads * Ti::NB;
-    const unsigned step = gridDim.x * C4_NT, first = blockIdx.x * C4_NT + threadIdx.x;
-    const unsigned row_step = step / per_row, piece_step = step % per_row;
-    unsigned row = first / per_row, piece = first % per_row;
-    for (; row < (unsigned)c.lanes * c.T; row += row_step, piece += piece_step) {
-        if (piece >= per_row) { piece -= per_row; if (++row >= (unsigned)c.lanes * c.T) break; }
-        const int b = piece % Ti::NB, head = piece / Ti::NB % c.heads;
-        const bool is_v = piece >= per_row / 2;
-        const int lane = (int)(row / c.T), tok = (int)(row % c.T);
-        const int len = c.len[lane];
-        float x[16];
+    auto store = [&](const Block& at, auto many) {
+        constexpr int U = decltype(many)::value;
+        char* tile[U];
+        typename Io<DT>::raw16 raw[U];
+        const long long ld = at.is_v ? v_ld : k_ld;
+        const typename Io<DT>::type* src = (at.is_v ? v : k) + ((long long)at.lane * c.T + at.tok) * ld + at.head * D + at.b * 16;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = 0.f;
-        bool bad = len < 0 || len > ((long long)c.max_pages << c.page_shift);
-        const int p = len - c.T + tok;
-        if (!bad && p >= 0) {
-            const char* tile = tile_of<D>(c, lane, head, p, bad);
-            if (!bad) {
-                const int t = p & 15;
-                const uint2 q = *reinterpret_cast<const uint2*>(tile + (is_v ? Ti::v_code(t, b) : Ti::k_code(t, b)));
-                const float s = e4m3_value((uint8_t)tile[is_v ? Ti::v_scale(t, b) : Ti::k_scale(t, b)]);
-                const float* hs = is_v ? c.v_scale : c.k_scale;
-                const float g = hs ? hs[head] : 1.f;
+        for (int u = 0; u < U; ++u)
+            if (at.tok + 16 * u >= 0 && at.tok + 16 * u < c.T) raw[u] = Io<DT>::load16(src + 16 * u * ld, VEC);
+        tiles_of<D, U>(c, at, tile);
+        const float* hs = at.is_v ? c.v_scale : c.k_scale;
+        const float inv = hs ? __frcp_rn(hs[at.head]) : 1.f;
+        const int t = (at.len - c.T + at.tok) & 15;
 #pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                    const uint32_t h2 = codes_f16x2((e < 8 ? q.x : q.y) >> (4 * (e & 7)));
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
-                    x[e] = f.x * s * g;                 // code * scale is exact, one rounding
-                    x[e + 1] = f.y * s * g;
-                }
+        for (int u = 0; u < U; ++u) {
+            if (!tile[u]) continue;
+            float x[16], top = 0.f;
+            Io<DT>::widen16(raw[u], x);
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                x[e] = __fmul_rn(x[e], inv);
+                odd |= !(fabsf(x[e]) <= 3.402823466e38f);
+                x[e] = x[e] == x[e] ? x[e] : 0.f;
+                top = fmaxf(top, fabsf(x[e]));
+            }
+            if (odd) flag_lane(c.lane_status, at.lane, AS_ERR_NUMERIC);
+            const uint32_t s8 = to_e4m3(__fmul_rn(top, 1.f / 6.f));
+            const float s = e4m3_value(s8);
+            const float rs = s > 0.f ? __frcp_rn(s) : 0.f;
+            uint32_t w[2] = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                // (an infinite value with a zero factor cannot occur: its block's scale is the largest)
+                w[e >> 3] |= to_codes(__fmul_rn(x[e], rs), __fmul_rn(x[e + 1], rs)) << (4 * (e & 7));
+            }
+            *reinterpret_cast<uint2*>(tile[u] + (at.is_v ? Ti::v_code(t, at.b) : Ti::k_code(t, at.b))) = make_uint2(w[0], w[1]);
+            tile[u][at.is_v ? Ti::v_scale(t, at.b) : Ti::k_scale(t, at.b)] = (char)s8;
+        }
+    };
+    if constexpr (TILES) each_block_by_tiles<D>(c, store);
+    else each_block_by_rows<D>(c, store);
+}
+
+template <int DT, int D, bool TILES>
+__global__ void __launch_bounds__(C4_NT)
+load_kernel(const __grid_constant__ CacheArgs c, typename Io<DT>::type* __restrict__ k, typename Io<DT>::type* __restrict__ v) {
+    using Ti = Tile4<D>;
+    auto read = [&](const Block& at, auto many) {
+        constexpr int U = decltype(many)::value;
+        char* tile[U];
+        tiles_of<D, U>(c, at, tile);
+        const float* hs = at.is_v ? c.v_scale : c.k_scale;
+        const float g = hs ? hs[at.head] : 1.f;
+        const int t = (at.len - c.T + at.tok) & 15;
+        uint2 q[U];
+        uint32_t s8[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            q[u] = make_uint2(0, 0);
+            s8[u] = 0;                                  // zeros where there is no token
+            if (tile[u]) {
+                q[u] = *reinterpret_cast<const uint2*>(tile[u] + (at.is_v ? Ti::v_code(t, at.b) : Ti::k_code(t, at.b)));
+                s8[u] = (uint8_t)tile[u][at.is_v ? Ti::v_scale(t, at.b) : Ti::k_scale(t, at.b)];
             }
         }
-        if (bad) flag_lane(c.lane_status, lane, AS_ERR_INVALID_ARG);
-        Io<DT>::write16((is_v ? v : k) + (size_t)row * c.heads * D + head * D + b * 16, x);
-    }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int tok = at.tok + 16 * u;
+            if (tok < 0 || tok >= c.T) continue;
+            const float s = e4m3_value(s8[u]);
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t h[4];
+                codes_f16x2(i ? q[u].y : q[u].x, h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
+                    x[8 * i + 2 * e] = f.x * s * g;     // code * scale is exact, one rounding
+                    x[8 * i + 2 * e + 1] = f.y * s * g;
+                }
+            }
+            Io<DT>::write16((at.is_v ? v : k) + ((size_t)at.lane * c.T + tok) * c.heads * D + at.head * D + at.b * 16, x);
+        }
+    };
+    if constexpr (TILES) each_block_by_tiles<D>(c, read);
+    else each_block_by_rows<D>(c, read);
 }
 
 }  // namespace asx
