@@ -30,7 +30,7 @@ struct AttendArgs {
 // rows of `group` lanes (1, or all N lanes of a group for their shared beginning) x T tokens x the
 // query heads of a key head, cut into row tiles of tile_rows.  Items are ordered by entry (lane or
 // group, row tile), then head; their units (2^unit_shift tokens each) are dealt out to the CTAs in equal
-// contiguous runs.
+// contiguous runs.  (The host holds the number of units below 2^31.)
 struct PassArgs {
     int n;                                  // lanes, or groups
     int group;                              // lanes of an item
@@ -39,7 +39,7 @@ struct PassArgs {
     const int* begin;                       // [lanes / N] usable shared lengths, or null (0)
     int rows, tile_rows, row_tiles, unit_shift;
     Divisor by_row_tiles, by_N;
-    int* cum;                               // [n * row_tiles + 1] units of one head in front of an entry, written by CTA 0
+    int *first_cta, *last_cta;              // [items] the CTAs that have an item's first and last units, written by them
     float* part_item;                       // states of items that one CTA saw whole; null: it writes the output itself
     float* part_cta;                        // [2 * ctas] states of the others: a CTA's first and last item
     int ctas;
@@ -63,29 +63,6 @@ __device__ __forceinline__ void token_range(const AttendArgs& a, const PassArgs&
     }
 }
 __device__ __forceinline__ int units_of(const PassArgs& p, int lo, int hi) { return (hi - lo + (1 << p.unit_shift) - 1) >> p.unit_shift; }
-// The runs of G CTAs: CTA k has units [start(k), start(k + 1)) of U = q G + r, in equal shares.
-struct Runs {
-    long long q;
-    int r, G;
-    __device__ Runs(long long U, int ctas) {
-        G = U < ctas ? (int)U : ctas;               // no run is empty
-        q = G > 0 ? (long long)((double)U / G) : 0; // U is far below 2^53: at most one off
-        if (G > 0 && q * G > U) --q;
-        r = (int)(U - q * G);
-    }
-    __device__ long long start(int k) const { return q * k + (unsigned)r * (unsigned)k / (unsigned)G; }
-    // the CTA that has unit x
-    __device__ int of(long long x) const {
-        int k = (int)((double)x / ((double)q + (double)r / G));
-        k = min(max(k, 0), G - 1);
-#pragma unroll 1
-        while (k > 0 && start(k) > x) --k;
-#pragma unroll 1
-        while (k + 1 < G && start(k + 1) <= x) ++k;
-        return k;
-    }
-};
-
 // Positions that a row may see, and where its output goes.
 __device__ __forceinline__ int row_limit(const AttendArgs& a, int lane0, int row) {
     const int ln = a.by_Tg.div(row), t = a.by_g.div(row) - ln * a.c.T;
@@ -131,26 +108,25 @@ struct Cursor {
     }
 };
 
-// The CTA's run [x0, x1) and where it starts; called by all NT threads.
+// The CTA's run: how many units it has, and where it starts; called by all NT threads.  0: it has none.
 struct RunSmem {
     int warp_sum[32];
     int start[3];
 };
+__device__ __noinline__ int entry_units(const AttendArgs& a, const PassArgs& p, int entry) {
+    int lo, hi;
+    token_range(a, p, entry, p.by_row_tiles.div(entry), lo, hi);
+    return units_of(p, lo, hi);
+}
 template <int NT>
-__device__ __forceinline__ bool find_run(const AttendArgs& a, const PassArgs& p, RunSmem& sm, long long& x0, long long& x1, Cursor& cu) {
-    const CacheArgs& c = a.c;
+__device__ __forceinline__ int find_run(const AttendArgs& a, const PassArgs& p, RunSmem& sm, Cursor& cu) {
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, n = p.n * p.row_tiles;
     const int per = (n + NT - 1) / NT, j0 = min(tid * per, n), j1 = min(j0 + per, n);
-    auto units = [&](int j) {
-        int lo, hi;
-        token_range(a, p, j, p.by_row_tiles.div(j), lo, hi);
-        return units_of(p, lo, hi);
-    };
     int mine = 0;
 #pragma unroll 1
-    for (int j = j0; j < j1; ++j) mine += units(j);
+    for (int j = j0; j < j1; ++j) mine += entry_units(a, p, j);
     int incl = mine;
-#pragma unroll
+#pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
         const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
         if (lane >= o) incl += v;
@@ -158,40 +134,35 @@ __device__ __forceinline__ bool find_run(const AttendArgs& a, const PassArgs& p,
     if (lane == 31) sm.warp_sum[w] = incl;
     __syncthreads();
     int before = incl - mine, total = 0;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < NT / 32; ++i) {
-        if (i < w) before += sm.warp_sum[i];
-        total += sm.warp_sum[i];
+        const int v = sm.warp_sum[i];
+        before += i < w ? v : 0;
+        total += v;
     }
-    const Runs runs((long long)total * c.heads, p.ctas);
-    if (blockIdx.x == 0) {
-        int at = before;
+    // U = q G + r units in G equal shares, none of them empty
+    const unsigned U = (unsigned)total * a.c.heads, G = min((unsigned)p.ctas, U);
+    if (blockIdx.x >= G) return 0;
+    const unsigned q = U / G, r = U - q * G;
+    const unsigned x0 = q * blockIdx.x + r * blockIdx.x / G, x1 = q * (blockIdx.x + 1) + r * (blockIdx.x + 1) / G;
+    unsigned at = (unsigned)before * a.c.heads;
+    const unsigned end = at + (unsigned)mine * a.c.heads;
+    if (x0 >= at && x0 < end) {
 #pragma unroll 1
         for (int j = j0; j < j1; ++j) {
-            p.cum[j] = at;
-            at += units(j);
+            const unsigned nu = entry_units(a, p, j), all = nu * a.c.heads;
+            if (x0 >= at && x0 < at + all) {
+                sm.start[0] = j;
+                sm.start[1] = (int)((x0 - at) / nu);
+                sm.start[2] = (int)((x0 - at) % nu);
+            }
+            at += all;
         }
-        if (tid == 0) p.cum[n] = total;
-    }
-    if (blockIdx.x >= runs.G) return false;
-    x0 = runs.start(blockIdx.x);
-    x1 = runs.start(blockIdx.x + 1);
-    long long at = (long long)before * c.heads;
-#pragma unroll 1
-    for (int j = j0; j < j1; ++j) {
-        const int nu = units(j);
-        if (x0 >= at && x0 < at + (long long)nu * c.heads) {
-            sm.start[0] = j;
-            const unsigned in = (unsigned)(x0 - at);        // below nu x heads, which the host holds below 2^32
-            sm.start[1] = (int)(in / nu);
-            sm.start[2] = (int)(in % nu);
-        }
-        at += (long long)nu * c.heads;
     }
     __syncthreads();
     cu.entry = sm.start[0]; cu.head = sm.start[1]; cu.u = sm.start[2];
     cu.enter(a, p);
-    return true;
+    return (int)(x1 - x0);
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -287,11 +258,10 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     const int g = (int)a.by_g.d;
-    long long x0, x1;
     Cursor cu, ahead;
-    if (!find_run<AT_NT>(a, p, sm.run, x0, x1, cu)) return;
+    int left = find_run<AT_NT>(a, p, sm.run, cu), to_issue = left;
+    if (left == 0) return;
     ahead = cu;
-    int left = (int)min(x1 - x0, 0x7FFFFFFFLL), to_issue = left;   // (a CTA's share of units fits 31 bits)
 
     // ---- copies: half a warp brings in one of its two tiles; the page id is fetched a unit before ----
     const int half = lane >> 4, hl = lane & 15;
@@ -558,9 +528,14 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
         if (item_ends || left == 1) {
             const int head = cu.head;
             const bool whole = item_ends && seg_u0 == 0;
+            const size_t item = (size_t)cu.entry * c.heads + cu.head;
+            if (tid == 0) {
+                if (seg_u0 == 0) p.first_cta[item] = blockIdx.x;
+                if (item_ends) p.last_cta[item] = blockIdx.x;
+            }
             float* part = nullptr;
             if (!whole) part = p.part_cta + (size_t)(2 * blockIdx.x + (seg_u0 == 0)) * state_floats<D>(8 * NT);
-            else if (p.part_item) part = p.part_item + ((size_t)cu.entry * c.heads + cu.head) * state_floats<D>(8 * NT);
+            else if (p.part_item) part = p.part_item + item * state_floats<D>(8 * NT);
             const float vg = c.v_scale ? c.v_scale[head] : 1.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -616,45 +591,27 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     }
 }
 
-// Where the states of an item lie: item by item, or with the CTAs c0..c1 that shared it.
-struct ItemStates {
-    const float* whole;
-    const float* cta;
-    long long x0;
-    Runs runs;
-    int c0, c1, tile_rows;
-    bool none, written;                     // no tokens; the pass has written the output itself
-    __device__ ItemStates(const CacheArgs& c, const PassArgs& p, int D, int entry, int head)
-        : runs((long long)p.cum[p.n * p.row_tiles] * c.heads, p.ctas) {
-        const int at = p.cum[entry], nu = p.cum[entry + 1] - at;
-        tile_rows = p.tile_rows;
-        none = nu == 0;
-        written = false;
-        c0 = 0; c1 = -1;
-        if (none) return;
-        x0 = (long long)at * c.heads + (long long)head * nu;
-        c0 = runs.of(x0);
-        c1 = runs.of(x0 + nu - 1);
-        cta = p.part_cta;
-        whole = c0 == c1 && p.part_item ? p.part_item + ((size_t)entry * c.heads + head) * tile_rows * (D + 2) : nullptr;
-        written = c0 == c1 && !p.part_item;
-    }
-    // joins the item's states of row rw into (M, L, acc): a warp's thread has D / 32 neighbouring dimensions
-    template <int D> __device__ void join(int rw, int lane, float& M, float& L, float (&acc)[D / 32]) const {
-        constexpr int PER = D / 32;
+// Joins the states of row rw of an item into (M, L, acc), a warp's thread having D / 32 neighbouring dimensions.
+// The item was shared by CTAs c0 .. c1: the first kept its state in its second slot (that item was its last),
+// the others in their first; one that a CTA saw whole has a state of its own.
+template <int D>
+__device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int c0, int c1, int rw, int lane, float& M, float& L, float (&acc)[D / 32]) {
+    constexpr int PER = D / 32;
 #pragma unroll 1
-        for (int k = c0; k <= c1; ++k) {
-            const float* s = whole ? whole : cta + (size_t)(2 * k + (runs.start(k) <= x0)) * state_floats<D>(tile_rows);
-            const float m2 = s[tile_rows * D + rw], l2 = s[tile_rows * (D + 1) + rw];
-            const float top = fmaxf(M, m2);
-            const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
-            L = L * f + l2 * f2;
+    for (int k = c0; k <= c1; ++k) {
+        const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_cta + (size_t)(2 * k + (k == c0)) * state_floats<D>(p.tile_rows);
+        const float m2 = s[p.tile_rows * D + rw], l2 = s[p.tile_rows * (D + 1) + rw];
+        float x[PER];
 #pragma unroll
-            for (int e = 0; e < PER; ++e) acc[e] = acc[e] * f + s[rw * D + lane * PER + e] * f2;
-            M = top;
-        }
+        for (int e = 0; e < PER; ++e) x[e] = s[rw * D + lane * PER + e];
+        const float top = fmaxf(M, m2);
+        const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
+        L = L * f + l2 * f2;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) acc[e] = acc[e] * f + x[e] * f2;
+        M = top;
     }
-};
+}
 
 // One CTA per item of the lanes' own pass and 32 of its rows, a warp to a row: joins the states of rows that were split
 // over CTAs or passes, in a fixed order, and writes rows that saw nothing.
@@ -669,10 +626,11 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     const int first = blockIdx.y * JOIN_ROWS + (threadIdx.x >> 5);
 #pragma unroll 1
     for (unsigned i = blockIdx.x; i < items; i += gridDim.x) {
-        const int entry = (int)(i / c.heads), head = (int)(i % c.heads);
-        const ItemStates st(c, own, D, entry, head);
-        if (st.written) continue;
-        const int ln = own.by_row_tiles.div(entry), row0 = (entry - ln * own.row_tiles) * own.tile_rows;
+        const int entry = c.by_heads.div(i), head = (int)i - entry * c.heads, ln = own.by_row_tiles.div(entry);
+        const bool none = entry_units(a, own, entry) == 0;
+        const int c0 = none ? 0 : own.first_cta[i], c1 = none ? -1 : own.last_cta[i];
+        if (!none && c0 == c1 && !own.part_item) continue;                  // the pass has written the output itself
+        const int row0 = (entry - ln * own.row_tiles) * own.tile_rows;
         const int end = min(min(own.tile_rows, own.rows - row0), (int)(blockIdx.y + 1) * JOIN_ROWS);
         const int gr = pre.begin ? pre.by_N.div(ln) : 0;
 #pragma unroll 1
@@ -681,12 +639,12 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
             float M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
             for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-            if (pre.begin) {
+            if (pre.begin && pre.begin[gr] > 0) {
                 const int prow = (ln - gr * pre.N) * own.rows + row, pt = prow / pre.tile_rows;
-                const ItemStates ps(c, pre, D, gr * pre.row_tiles + pt, head);
-                ps.join<D>(prow - pt * pre.tile_rows, lane, M, L, acc);
+                const size_t item = ((size_t)gr * pre.row_tiles + pt) * c.heads + head;
+                join_states<D>(pre, item, pre.first_cta[item], pre.last_cta[item], prow - pt * pre.tile_rows, lane, M, L, acc);
             }
-            st.join<D>(rw, lane, M, L, acc);
+            join_states<D>(own, i, c0, c1, rw, lane, M, L, acc);
             const float inv = L > 0.f ? (c.v_scale ? c.v_scale[head] : 1.f) / L : 0.f;
             const size_t orow = out_row(a, ln, head, row);
             typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + orow * D + lane * PER;

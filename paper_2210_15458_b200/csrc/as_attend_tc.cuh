@@ -132,6 +132,20 @@ __host__ __device__ constexpr uint32_t tc_idesc(int M, int N, bool b_rows_are_k)
 }
 __device__ __forceinline__ uint32_t tc_at(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }     // 16-byte piece of a block
 
+// 32 elements of a query row, which may start off a 16-byte boundary or not be there
+__device__ __forceinline__ void tc_read_row(const uint16_t* from, bool there, bool wide, uint4 (&q)[4]) {
+    if (there && wide) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = reinterpret_cast<const uint4*>(from)[i];
+        return;
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = there ? from[2 * i] | (uint32_t)from[2 * i + 1] << 16 : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+
 struct TcSmem {
     unsigned long long k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], q_full[2], q_empty[2], o_full, o_empty, ml_full, fin;
     uint32_t tmem;
@@ -176,9 +190,9 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
         sm.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    long long x0, x1;
     Cursor cu;
-    if (!find_run<TC_NT>(a, p, sm.run, x0, x1, cu)) return;
+    const int run = find_run<TC_NT>(a, p, sm.run, cu);      // units of the CTA
+    if (run == 0) return;
     if (w == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&sm.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -191,7 +205,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
     const long long limit = p.wait_cycles;
     volatile int* failed = &sm.failed;
     bool ok = true;
-    long long x = x0;
+    int x = 0;                                  // units behind
     // the query buffer of an item, and how often it has been used before
     auto q_buf = [](int item) { return DUAL ? 0 : item & 1; };
     auto q_use = [](int item) { return (uint32_t)(DUAL ? item : item >> 1); };
@@ -204,8 +218,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
         const uint32_t st = s_t + 128 * s + mine, ot = o_t + 128 * s + mine;
         uint32_t steps = 0;                                         // of this group, ever
 #pragma unroll 1
-        for (int item = 0; x < x1 && ok; ++item) {
-            const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x);
+        for (int item = 0; x < run && ok; ++item) {
+            const int tiles = min(cu.nu - cu.u, run - x);
             const int row = cu.row0 + (DUAL ? 128 * s : 0) + r;
             const int lim = row < p.rows ? min(row_limit(a, cu.lane0, row), cu.hi) : 0;
             const float vg = c.v_scale ? c.v_scale[cu.head] : 1.f;
@@ -289,9 +303,14 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             if (!ok) break;
             tc_fence_after();
             const bool whole = cu.u == 0 && tiles == cu.nu;
+            const size_t at_item = (size_t)cu.entry * c.heads + cu.head;
+            if (tid == TC_NT - 1) {
+                if (cu.u == 0) p.first_cta[at_item] = blockIdx.x;
+                if (cu.u + tiles == cu.nu) p.last_cta[at_item] = blockIdx.x;
+            }
             float* part = nullptr;
             if (!whole) part = p.part_cta + (size_t)(2 * blockIdx.x + (cu.u == 0)) * state_floats<D>(p.tile_rows);
-            else if (p.part_item) part = p.part_item + ((size_t)cu.entry * c.heads + cu.head) * state_floats<D>(p.tile_rows);
+            else if (p.part_item) part = p.part_item + at_item * state_floats<D>(p.tile_rows);
             // DUAL: a thread writes its row; else the two groups' states of a row join, and each group writes half of it
             float M = m, L = l, f0 = 1.f, f1 = 0.f;
             if (!DUAL) {
@@ -361,7 +380,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             // Each thread takes its token's codes into registers a tile before they are widened, and the page's id a tile
             // before that.  They are widened from the thread's own place in shared memory, by a loop.
             Cursor ahead = cu;
-            long long looked = x0;
+            int looked = 0;
             int page = 0, next_lane = 0;
             uint4 code[D / 32];
             uint2 scale = make_uint2(0, 0);                         // keys' scales; values' are bytes apart
@@ -396,7 +415,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                 }
                 real = next_real;
                 next_real = false;
-                if (looked < x1) {
+                if (looked < run) {
                     const int pos = ahead.lo + ahead.u * TC_KV + r;
                     if (pos < ahead.hi) {
                         page = c.table[(size_t)ahead.lane0 * c.max_pages + (pos >> c.page_shift)];
@@ -424,8 +443,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             for (int i = 0; i < 2; ++i) load();                         // (the first time round only the page id is fetched)
             uint32_t n = 0;                                             // tiles filled
 #pragma unroll 1
-            for (int item = 0; x < x1 && ok; ++item) {
-                const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x);
+            for (int item = 0; x < run && ok; ++item) {
+                const int tiles = min(cu.nu - cu.u, run - x);
                 if constexpr (keys || DUAL) {
                     // ---- the item's queries, scaled by a power of two into f16's range; a negative scale goes in here ----
                     if (q_use(item) > 0) ok = wait_warp(sm.q_empty[q_buf(item)], (q_use(item) - 1) & 1);
@@ -435,29 +454,31 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         const int row = cu.row0 + 128 * h + r, tok = a.by_g.div(row);
                         const uint16_t* from = static_cast<const uint16_t*>(a.q) + ((long long)cu.lane0 * c.T + tok) * a.q_ld + (cu.head * g + row - tok * g) * D;
                         const bool there = row < p.rows, wide = (reinterpret_cast<uintptr_t>(from) & 15) == 0;
-                        auto piece = [&](int i) {                       // 8 of the row's elements
-                            if (!there) return make_uint4(0, 0, 0, 0);
-                            if (wide) return reinterpret_cast<const uint4*>(from)[i];
-                            const uint16_t* e = from + 8 * i;
-                            return make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
-                        };
                         uint32_t top = 0;                               // largest magnitude's bits
-#pragma unroll 8
-                        for (int i = 0; i < CHUNKS; ++i) {
-                            const uint4 q = piece(i);
-                            top = max(max(max(q.x & 0x7FFFu, q.x >> 16 & 0x7FFFu), max(q.y & 0x7FFFu, q.y >> 16 & 0x7FFFu)),
-                                      max(max(max(q.z & 0x7FFFu, q.z >> 16 & 0x7FFFu), max(q.w & 0x7FFFu, q.w >> 16 & 0x7FFFu)), top));
+                        // (twice over the row, 4 pieces of 8 elements at a time: code that runs once an item is fetched anew each
+                        // time, so that a short loop is faster than straight code)
+#pragma unroll 1
+                        for (int i = 0; i < CHUNKS; i += 4) {
+                            uint4 q[4];
+                            tc_read_row(from + 8 * i, there, wide, q);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                top = max(max(max(q[e].x & 0x7FFFu, q[e].x >> 16 & 0x7FFFu), max(q[e].y & 0x7FFFu, q[e].y >> 16 & 0x7FFFu)),
+                                          max(max(max(q[e].z & 0x7FFFu, q[e].z >> 16 & 0x7FFFu), max(q[e].w & 0x7FFFu, q[e].w >> 16 & 0x7FFFu)), top));
                         }
                         int ex = (int)(top >> 7) - 127;
                         ex = ex > 126 ? 126 : ex < -126 ? -126 : ex;
                         const float down = __uint_as_float((uint32_t)(127 - ex) << 23 | (a.scale < 0.f ? 0x80000000u : 0u));
                         sm.up[item & 1][128 * h + r] = __uint_as_float((uint32_t)(127 + ex) << 23);
-                        const uint32_t to = q_s + (DUAL ? h : q_buf(item)) * MAT;
+                        const uint32_t to_q = q_s + (DUAL ? h : q_buf(item)) * MAT;
                         auto both = [&](uint32_t z) { return pack_f16(__uint_as_float(z << 16) * down, __uint_as_float(z & 0xFFFF0000u) * down); };
-#pragma unroll 8
-                        for (int i = 0; i < CHUNKS; ++i) {
-                            const uint4 q = piece(i);
-                            put(to + (i / 8) * BLK + tc_at(r, i % 8), make_uint4(both(q.x), both(q.y), both(q.z), both(q.w)));
+#pragma unroll 1
+                        for (int i = 0; i < CHUNKS; i += 4) {
+                            uint4 q[4];
+                            tc_read_row(from + 8 * i, there, wide, q);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                put(to_q + (i / 8) * BLK + tc_at(r, (i & 4) + e), make_uint4(both(q[e].x), both(q[e].y), both(q[e].z), both(q[e].w)));
                         }
                     }
                     filled(bar(sm.q_full[q_buf(item)]));
@@ -509,8 +530,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             const uint64_t q_d = tc_desc(q_s, 0), k_d = tc_desc(k_s, 0), v_d = tc_desc(v_s, BLK);
             uint32_t n0 = 0, p_seen0 = 0, p_seen1 = 0;              // tiles before this item; weights taken, by group
 #pragma unroll 1
-            for (int item = 0; x < x1 && ok; ++item) {
-                const int tiles = (int)min((long long)(cu.nu - cu.u), x1 - x), steps = DUAL ? 2 * tiles : tiles;
+            for (int item = 0; x < run && ok; ++item) {
+                const int tiles = min(cu.nu - cu.u, run - x), steps = DUAL ? 2 * tiles : tiles;
                 ok = tc_wait(bar(sm.q_full[q_buf(item)]), q_use(item) & 1, limit, failed);
                 if (!ok) break;
 #pragma unroll 1

@@ -117,10 +117,12 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
         p.by_row_tiles.set(p.row_tiles);
         p.by_N.set(N);
         p.unit_shift = 7;               // TC_KV = 32 * AT_W tokens
-        p.cum = reinterpret_cast<int*>(take(sizeof(int) * ((size_t)n * p.row_tiles + 1)));
+        const size_t items = (size_t)n * heads * p.row_tiles;
+        p.first_cta = reinterpret_cast<int*>(take(sizeof(int) * items));
+        p.last_cta = reinterpret_cast<int*>(take(sizeof(int) * items));
         const size_t state = sizeof(float) * (size_t)p.tile_rows * (D + 2);
         p.part_cta = reinterpret_cast<float*>(take(2 * (size_t)(tc ? TC_MAX_CTAS : AT_MAX_CTAS) * state));
-        if (N > 1) p.part_item = reinterpret_cast<float*>(take((size_t)n * heads * p.row_tiles * state));
+        if (N > 1) p.part_item = reinterpret_cast<float*>(take(items * state));
     };
     pass(pl.own, pl.own_kernel, lanes, 1, false);
     if (N > 1) pass(pl.pre, pl.pre_kernel, lanes / N, N, true);
@@ -286,8 +288,10 @@ int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, in
     if (q_ld < (long long)q_heads * cache->head_dim) return set_err(AS_ERR_INVALID_ARG, "q_ld = %lld is smaller than q_heads * head_dim", q_ld);
     if (!std::isfinite(scale)) return set_err(AS_ERR_INVALID_ARG, "scale must be finite");
     if (N < 1 || lanes % N) return set_err(AS_ERR_INVALID_ARG, "N = %d must be >= 1 and divide lanes = %d", N, lanes);
-    if (cache->heads > 128 || (long long)lanes * T * q_heads > (1LL << 31) - 1)
-        return set_err(AS_ERR_UNSUPPORTED, "heads = %d must not exceed 128, lanes * T * q_heads not 2^31 - 1", cache->heads);
+    // units of 128 tokens over all lanes, heads and tiles of 8 rows, and rows, are counted in 31 bits
+    const long long tiles = ((long long)T * (q_heads / cache->heads) + 7) / 8, units = ((long long)max_pages * cache->page_size + 127) / 128;
+    if ((long long)lanes * T * q_heads > 0x7FFFFFFFLL || (double)lanes * cache->heads * tiles * units > 2147483647.0)
+        return set_err(AS_ERR_UNSUPPORTED, "lanes, T, q_heads and max_pages * page_size make more than 2^31 rows or units of work");
     if (lanes == 0) return AS_OK;
     if (!d_q || !d_out) return set_err(AS_ERR_INVALID_ARG, "d_q or d_out is NULL");
     const int es = dtype == AS_F32 ? 4 : 2;
