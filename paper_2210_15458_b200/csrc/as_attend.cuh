@@ -38,7 +38,7 @@ struct PassArgs {
     int N;
     const int* begin;                       // [lanes / N] usable shared lengths, or null (0)
     int rows, tile_rows, row_tiles, unit_shift;
-    Divisor by_row_tiles, by_N;
+    Divisor by_row_tiles, by_tile_rows, by_N;
     int *first_cta, *last_cta;              // [items] the CTAs that have an item's first and last units, written by them
     float* part_item;                       // states of items that one CTA saw whole; null: it writes the output itself
     float* part_cta;                        // [2 * ctas] states of the others: a CTA's first and last item
@@ -227,6 +227,13 @@ template <> __device__ __forceinline__ unsigned char lds<unsigned char>(uint32_t
     return (unsigned char)v;
 }
 
+// row = (lane of the group x T + token) x g + query head
+template <int DT, int D>
+__device__ __forceinline__ const typename Io<DT>::type* query_row(const AttendArgs& a, int lane0, int head, int row) {
+    const int tok = a.by_g.div(row), g = (int)a.by_g.d;
+    return static_cast<const typename Io<DT>::type*>(a.q) + ((long long)lane0 * a.c.T + tok) * a.q_ld + (head * g + row - tok * g) * D;
+}
+
 template <int D> struct AttendSmem {
     char ring[AT_W][AT_STAGES][2 * Tile4<D>::BYTES];
     float join[AT_W][8][D + 20];            // the warps' sums (the pitch spreads rows over the banks)
@@ -257,7 +264,6 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    const int g = (int)a.by_g.d;
     Cursor cu, ahead;
     int left = find_run<AT_NT>(a, p, sm.run, cu), to_issue = left;
     if (left == 0) return;
@@ -291,6 +297,10 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
         if (--to_issue > 0) {
             ahead.step(a, p);
             look();
+            if (ahead.u == 0) {                     // the next item's queries: into L1 meanwhile
+                const int row = ahead.row0 + r;
+                if (row < p.rows) asm volatile("prefetch.global.L1 [%0];" ::"l"(query_row<DT, D>(a, ahead.lane0, ahead.head, row) + cc * (D / 4)));
+            }
         }
     };
     look();
@@ -319,9 +329,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
 #pragma unroll
                 for (int e = 0; e < D / 4; ++e) xq[e] = 0.f;
                 if (row < p.rows) {
-                    // row = (lane of the group x T + token) x g + query head
-                    const int tok = a.by_g.div(row);
-                    const E* src = static_cast<const E*>(a.q) + ((long long)lane0 * c.T + tok) * a.q_ld + (head * g + row - tok * g) * D + cc * (D / 4);
+                    const E* src = query_row<DT, D>(a, lane0, head, row) + cc * (D / 4);
                     const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
 #pragma unroll
                     for (int e = 0; e < D / 4; e += 16) Io<DT>::read16(src + e, vec, *reinterpret_cast<float(*)[16]>(&xq[e]));
@@ -591,19 +599,18 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     }
 }
 
-// Joins the states of row rw of an item into (M, L, acc), a warp's thread having D / 32 neighbouring dimensions.
-// The item was shared by CTAs c0 .. c1: the first kept its state in its second slot (that item was its last),
-// the others in their first; one that a CTA saw whole has a state of its own.
-template <int D>
-__device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int c0, int c1, int rw, int lane, float& M, float& L, float (&acc)[D / 32]) {
-    constexpr int PER = D / 32;
+// Joins the states of row rw of an item into (M, L, acc): dimensions d0 .. d0 + PER - 1.  The item was shared by CTAs
+// c0 .. c1: the first kept its state in its second slot (that item was its last), the others in their first; one
+// that a CTA saw whole has a state of its own.
+template <int D, int PER>
+__device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int c0, int c1, int rw, int d0, float& M, float& L, float (&acc)[PER]) {
 #pragma unroll 1
     for (int k = c0; k <= c1; ++k) {
         const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_cta + (size_t)(2 * k + (k == c0)) * state_floats<D>(p.tile_rows);
         const float m2 = s[p.tile_rows * D + rw], l2 = s[p.tile_rows * (D + 1) + rw];
         float x[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) x[e] = s[rw * D + lane * PER + e];
+        for (int e = 0; e < PER; ++e) x[e] = s[rw * D + d0 + e];
         const float top = fmaxf(M, m2);
         const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
         L = L * f + l2 * f2;
@@ -611,6 +618,15 @@ __device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int 
         for (int e = 0; e < PER; ++e) acc[e] = acc[e] * f + x[e] * f2;
         M = top;
     }
+}
+// the same for what the pass over shared beginnings has left for a row of a lane
+template <int D, int PER>
+__device__ __forceinline__ void join_shared(const AttendArgs& a, const PassArgs& pre, int lane, int row, int rows, int head, int d0, float& M, float& L, float (&acc)[PER]) {
+    const int gr = pre.by_N.div(lane);
+    if (pre.begin[gr] == 0) return;
+    const int prow = (lane - gr * pre.N) * rows + row, pt = pre.by_tile_rows.div(prow);
+    const size_t item = ((size_t)gr * pre.row_tiles + pt) * a.c.heads + head;
+    join_states<D>(pre, item, pre.first_cta[item], pre.last_cta[item], prow - pt * pre.tile_rows, d0, M, L, acc);
 }
 
 // One CTA per item of the lanes' own pass and 32 of its rows, a warp to a row: joins the states of rows that were split
@@ -632,19 +648,14 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
         if (!none && c0 == c1 && !own.part_item) continue;                  // the pass has written the output itself
         const int row0 = (entry - ln * own.row_tiles) * own.tile_rows;
         const int end = min(min(own.tile_rows, own.rows - row0), (int)(blockIdx.y + 1) * JOIN_ROWS);
-        const int gr = pre.begin ? pre.by_N.div(ln) : 0;
 #pragma unroll 1
         for (int rw = first; rw < end; rw += 4) {
             const int row = row0 + rw;
             float M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
             for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-            if (pre.begin && pre.begin[gr] > 0) {
-                const int prow = (ln - gr * pre.N) * own.rows + row, pt = prow / pre.tile_rows;
-                const size_t item = ((size_t)gr * pre.row_tiles + pt) * c.heads + head;
-                join_states<D>(pre, item, pre.first_cta[item], pre.last_cta[item], prow - pt * pre.tile_rows, lane, M, L, acc);
-            }
-            join_states<D>(own, i, c0, c1, rw, lane, M, L, acc);
+            if (pre.begin) join_shared<D>(a, pre, ln, row, own.rows, head, lane * PER, M, L, acc);
+            join_states<D>(own, i, c0, c1, rw, lane * PER, M, L, acc);
             const float inv = L > 0.f ? (c.v_scale ? c.v_scale[head] : 1.f) / L : 0.f;
             const size_t orow = out_row(a, ln, head, row);
             typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + orow * D + lane * PER;

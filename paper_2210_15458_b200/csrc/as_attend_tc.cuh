@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
     TcSmem& sm = *reinterpret_cast<TcSmem*>(raw + (raw_s + TC_KV * D - (uint32_t)__cvta_generic_to_shared(raw)));
     auto bar = [](const unsigned long long& b) { return (uint32_t)__cvta_generic_to_shared(&b); };
     const CacheArgs& c = a.c;
-    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, g = (int)a.by_g.d;
+    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) {
@@ -445,14 +445,16 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
 #pragma unroll 1
             for (int item = 0; x < run && ok; ++item) {
                 const int tiles = min(cu.nu - cu.u, run - x);
+                Cursor next = cu;
+                if (x + tiles < run) next.next_item(a, p);
                 if constexpr (keys || DUAL) {
                     // ---- the item's queries, scaled by a power of two into f16's range; a negative scale goes in here ----
                     if (q_use(item) > 0) ok = wait_warp(sm.q_empty[q_buf(item)], (q_use(item) - 1) & 1);
                     if (!ok) break;
                     {
                         constexpr int h = keys ? 0 : 1;             // (the values' group takes the second row tile)
-                        const int row = cu.row0 + 128 * h + r, tok = a.by_g.div(row);
-                        const uint16_t* from = static_cast<const uint16_t*>(a.q) + ((long long)cu.lane0 * c.T + tok) * a.q_ld + (cu.head * g + row - tok * g) * D;
+                        const int row = cu.row0 + 128 * h + r;
+                        const uint16_t* from = reinterpret_cast<const uint16_t*>(query_row<AS_BF16, D>(a, cu.lane0, cu.head, row));
                         const bool there = row < p.rows, wide = (reinterpret_cast<uintptr_t>(from) & 15) == 0;
                         uint32_t top = 0;                               // largest magnitude's bits
                         // (twice over the row, 4 pieces of 8 elements at a time: code that runs once an item is fetched anew each
@@ -482,6 +484,13 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         }
                     }
                     filled(bar(sm.q_full[q_buf(item)]));
+                    // the next item's, into L1 meanwhile
+                    const int row = next.row0 + 128 * (keys ? 0 : 1) + r;
+                    if (x + tiles < run && row < p.rows) {
+                        const __nv_bfloat16* from = query_row<AS_BF16, D>(a, next.lane0, next.head, row);
+                        asm volatile("prefetch.global.L1 [%0];" ::"l"(from));
+                        if (D == 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(from + 64));
+                    }
                 }
                 // ---- its keys or values ----
                 const uint32_t to = (keys ? k_s : v_s) + r * 128;
@@ -514,8 +523,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     filled(bar(keys ? sm.k_full[b] : sm.v_full[b]));
                 }
                 x += tiles;
-                if (cu.u + tiles < cu.nu) cu.u += tiles;
-                else cu.next_item(a, p);
+                cu = next;                                          // (an item ends, or the run does)
             }
         };
         if (w < FILL + TC_FILL / 32) fill(std::true_type{});

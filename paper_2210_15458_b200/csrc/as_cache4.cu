@@ -115,6 +115,7 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
         p.tile_rows = kernel == MMA_8 ? 8 : kernel == MMA_16 ? 16 : kernel == TC_128 ? 128 : 256;
         p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
         p.by_row_tiles.set(p.row_tiles);
+        p.by_tile_rows.set(p.tile_rows);
         p.by_N.set(N);
         p.unit_shift = 7;               // TC_KV = 32 * AT_W tokens
         const size_t items = (size_t)n * heads * p.row_tiles;
