@@ -456,12 +456,14 @@ def as_logits_edit(logits: torch.Tensor, seq: Optional[torch.Tensor] = None, len
     (bit set = allowed) with mask_row [lanes] (-1 = none).  out=logits edits in place."""
     lanes, width, ld = _logits_layout(logits)
     V = width if V is None else V
+    out_ld = V
     if out is None:
         out = logits.new_empty((lanes, V))
     elif out.dtype != logits.dtype or out.dim() != 2 or out.shape[0] != lanes or out.shape[1] < V:
         raise ValueError("out must have the logits' dtype and a row of at least V for each lane")
-    e = as_logit_edits()
-    e.repetition, e.presence, e.frequency = repetition, presence, frequency
+    else:
+        out_ld = _logits_layout(out)[2]
+    e = as_logit_edits(None, 0, None, None, repetition, presence, frequency)
     if seq is not None:
         if seq.dim() != 2 or seq.shape[0] != lanes or length is None:
             raise ValueError("seq must be [lanes, T] and comes with a length for each lane")
@@ -478,7 +480,7 @@ def as_logits_edit(logits: torch.Tensor, seq: Optional[torch.Tensor] = None, len
         e.mask_ld = mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
         e.d_mask_row = _int32(mask_row, "mask_row", lanes)
     _check(lib().as_logits_edit(logits.data_ptr(), _logits_dtype(logits), lanes, V, ld, ctypes.byref(e), out.data_ptr(),
-                                _logits_layout(out)[2], _int32(lane_status, "lane_status", lanes), _stream(stream)))
+                                out_ld, _int32(lane_status, "lane_status", lanes), _stream(stream)))
     return out
 
 

@@ -131,22 +131,6 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
     return pl;
 }
 
-template <class K, class... A>
-static cudaError_t launch_after(K kern, dim3 grid, unsigned block, size_t smem, cudaStream_t st, A... args) {
-    // the kernel waits for its predecessor's results itself (griddepcontrol.wait), so its launch may overlap it
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(block);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, args...);
-}
-
 template <int DT, int D, int NT>
 static cudaError_t launch_mma(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
     static int per_sm[64] = {0};

@@ -19,6 +19,23 @@ long long wait_cycles_now();                        // bound on every on-device 
 
 constexpr size_t SMEM_OPTIN_MAX = 232448;           // 227 KB per CTA on sm_100
 
+// Launches a kernel that may be set up while the one before it on the stream drains: it waits for that one's completion
+// itself (griddepcontrol.wait) before it touches global memory.
+template <class K, class... A>
+inline cudaError_t launch_after(K kern, dim3 grid, unsigned block, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 // Checked builds: each translation unit keeps its own record of out-of-range indices; these copy
 // it out (failures, first site, index, bound) and reset it.
 #ifdef AS_BOUNDS_CHECK

@@ -48,6 +48,8 @@ __device__ __forceinline__ int pages_of(int len, int page_size) { return (len + 
 // CTA j: how many lanes continue lane j and which is the first; whether its row is usable; its
 // share of the copy of the reference counts.
 __global__ void __launch_bounds__(PG_NT) fork_count_kernel(const ForkArgs a, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x;
     if (a.ref_out != a.ref)
         for (int i = blockIdx.x * PG_NT + tid; i < a.n_pages; i += gridDim.x * PG_NT) a.ref_out[i] = a.ref[i];
@@ -74,6 +76,8 @@ __global__ void __launch_bounds__(PG_NT) fork_count_kernel(const ForkArgs a, con
 
 // CTA j: the change of the reference counts of lane j's pages, and row j of the new table.
 __global__ void __launch_bounds__(PG_NT) fork_table_kernel(const ForkArgs a, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x;
     const int n = max(a.lanes_in, a.lanes_out);
     for (int j = blockIdx.x; j < n; j += gridDim.x) {
@@ -144,6 +148,8 @@ __device__ int collect(const int* ref, int lo, int hi, bool used, int want, int*
 
 // One CTA: which lanes need a page for a copy, and which page each gets.
 __global__ void __launch_bounds__(PL_NT) fork_plan_kernel(const ForkArgs a, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ int warp_sum[32];
     const int tid = threadIdx.x;
     int wanted = 0;
@@ -187,6 +193,8 @@ __global__ void __launch_bounds__(PL_NT) fork_plan_kernel(const ForkArgs a, cons
 __global__ void __launch_bounds__(CP_NT)
 copy_pages_kernel(const int* __restrict__ moves, const int* __restrict__ src, const int* __restrict__ dst, char* data, int planes,
                   long long plane_stride, long long page_bytes) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int per_page = (int)((page_bytes + CP_CHUNK - 1) / CP_CHUNK);
     const long long n = (long long)*moves * planes * per_page;
     for (long long i = blockIdx.x; i < n; i += gridDim.x) {
@@ -215,6 +223,8 @@ struct GrowArgs {
 
 // One CTA: pages wanted by each lane, the free pages in order, and who gets which.
 __global__ void __launch_bounds__(PL_NT) grow_kernel(const GrowArgs a, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ int warp_sum[32];
     const int tid = threadIdx.x;
     const long long most = (long long)a.max_pages * a.page_size;
@@ -258,6 +268,8 @@ __global__ void __launch_bounds__(PL_NT) grow_kernel(const GrowArgs a, const Pag
 
 // One CTA: the number of pages in use, the holes below it and the pages to move there.
 __global__ void __launch_bounds__(PL_NT) compact_plan_kernel(const int* ref, int* ref_out, int n_pages, int* used_out, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ int warp_sum[32];
     const int tid = threadIdx.x;
     int n = 0;
@@ -282,6 +294,8 @@ __global__ void __launch_bounds__(PL_NT) compact_plan_kernel(const int* ref, int
 
 __global__ void __launch_bounds__(256)
 compact_table_kernel(const int* table, int* table_out, long long n, int n_pages, const int* used, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int u = *used;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
         const int g = table[i];
@@ -314,6 +328,11 @@ static int check_shape(int lanes, int max_pages, int page_size, int n_pages) {
     if ((long long)max_pages * page_size > (1LL << 30) || n_pages > (1 << 20))
         return set_err(AS_ERR_UNSUPPORTED, "max_pages * page_size must not exceed 2^30, n_pages not 2^20");
     return AS_OK;
+}
+
+static cudaError_t launch_copy(const PageWork& w, void* data, int planes, long long plane_stride, long long page_bytes, int sms, cudaStream_t st) {
+    return launch_after(copy_pages_kernel, 8 * sms, CP_NT, 0, st, (const int*)w.moves, (const int*)w.src, (const int*)w.dst, static_cast<char*>(data), planes, plane_stride,
+                        page_bytes);
 }
 
 static unsigned lanes_grid(int n, int sms) { return (unsigned)(n < 16 * sms ? (n > 0 ? n : 1) : 16 * sms); }
@@ -349,12 +368,10 @@ int as_pages_fork(const int32_t* d_parent, int lanes_in, int lanes_out, int max_
     a.parent = d_parent; a.table = d_table; a.len = d_len; a.ref = d_ref;
     a.table_out = d_table_out; a.len_out = d_len_out; a.ref_out = d_ref_out; a.lane_status = d_lane_status;
     a.lanes_in = lanes_in; a.lanes_out = lanes_out; a.max_pages = max_pages; a.page_size = page_size; a.n_pages = n_pages;
-    fork_count_kernel<<<lanes_grid(lanes_in, di->sms), PG_NT, 0, st>>>(a, w);
-    fork_table_kernel<<<lanes_grid(lanes_in > lanes_out ? lanes_in : lanes_out, di->sms), PG_NT, 0, st>>>(a, w);
-    fork_plan_kernel<<<1, PL_NT, 0, st>>>(a, w);
-    if (d_data && planes > 0)
-        copy_pages_kernel<<<8 * di->sms, CP_NT, 0, st>>>(w.moves, w.src, w.dst, static_cast<char*>(d_data), planes, plane_stride, page_bytes);
-    const cudaError_t e = cudaGetLastError();
+    cudaError_t e = launch_after(fork_count_kernel, lanes_grid(lanes_in, di->sms), PG_NT, 0, st, a, w);
+    if (e == cudaSuccess) e = launch_after(fork_table_kernel, lanes_grid(lanes_in > lanes_out ? lanes_in : lanes_out, di->sms), PG_NT, 0, st, a, w);
+    if (e == cudaSuccess) e = launch_after(fork_plan_kernel, 1, PL_NT, 0, st, a, w);
+    if (e == cudaSuccess && d_data && planes > 0) e = launch_copy(w, d_data, planes, plane_stride, page_bytes, di->sms, st);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "page fork kernel launch");
 }
 
@@ -370,8 +387,7 @@ int as_pages_grow(const int32_t* d_add, int lanes, int max_pages, int page_size,
     GrowArgs a;
     a.add = d_add; a.table = d_table; a.len = d_len; a.ref = d_ref; a.lane_status = d_lane_status;
     a.lanes = lanes; a.max_pages = max_pages; a.page_size = page_size; a.n_pages = n_pages;
-    grow_kernel<<<1, PL_NT, 0, (cudaStream_t)stream>>>(a, carve(d_work, lanes, lanes, n_pages));
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_after(grow_kernel, 1, PL_NT, 0, (cudaStream_t)stream, a, carve(d_work, lanes, lanes, n_pages));
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "page grow kernel launch");
 }
 
@@ -388,13 +404,11 @@ int as_pages_compact(int lanes, int max_pages, int n_pages, const int32_t* d_tab
     if ((rc = device_info(&di)) != AS_OK) return rc;
     cudaStream_t st = (cudaStream_t)stream;
     const PageWork w = carve(d_work, lanes, lanes, n_pages);
-    compact_plan_kernel<<<1, PL_NT, 0, st>>>(d_ref, d_ref_out, n_pages, d_used, w);
+    cudaError_t e = launch_after(compact_plan_kernel, 1, PL_NT, 0, st, d_ref, d_ref_out, n_pages, d_used, w);
     const long long n = (long long)lanes * max_pages, blocks = (n + 255) / 256;
-    if (n > 0)
-        compact_table_kernel<<<(unsigned)(blocks < 16 * di->sms ? blocks : 16 * di->sms), 256, 0, st>>>(d_table, d_table_out, n, n_pages, d_used, w);
-    if (d_data && planes > 0)
-        copy_pages_kernel<<<8 * di->sms, CP_NT, 0, st>>>(w.moves, w.src, w.dst, static_cast<char*>(d_data), planes, plane_stride, page_bytes);
-    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess && n > 0)
+        e = launch_after(compact_table_kernel, (unsigned)(blocks < 16 * di->sms ? blocks : 16 * di->sms), 256, 0, st, d_table, d_table_out, n, n_pages, d_used, w);
+    if (e == cudaSuccess && d_data && planes > 0) e = launch_copy(w, d_data, planes, plane_stride, page_bytes, di->sms, st);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "page compact kernel launch");
 }
 
