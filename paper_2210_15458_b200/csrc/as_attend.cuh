@@ -12,7 +12,7 @@ namespace asx {
 constexpr int AT_W = 4;                     // warps of a CTA; a unit of work is 2 tiles of 16 tokens for each
 constexpr int AT_NT = 32 * AT_W;
 constexpr int AT_STAGES = 2;                // pairs of tiles that a warp has in flight or in use
-constexpr int AT_MAX_CTAS = 1024;
+constexpr int AT_MAX_RUNS = 2560;           // CTAs, or warps where each has a run of its own
 constexpr float AT_LAZY = 8.f;              // the running maximum may lag by 8 (weights stay below 2^8, well within f16)
 
 struct AttendArgs {
@@ -29,8 +29,8 @@ struct AttendArgs {
 // One pass over the cache.  An item is a set of query rows that read the same tokens of one head: the
 // rows of `group` lanes (1, or all N lanes of a group for their shared beginning) x T tokens x the
 // query heads of a key head, cut into row tiles of tile_rows.  Items are ordered by entry (lane or
-// group, row tile), then head; their units (2^unit_shift tokens each) are dealt out to the CTAs in equal
-// contiguous runs.  (The host holds the number of units below 2^31.)
+// group, row tile), then head; their units (2^unit_shift tokens each) are dealt out in equal
+// contiguous runs, one for each CTA (or warp).  (The host holds the number of units below 2^31.)
 struct PassArgs {
     int n;                                  // lanes, or groups
     int group;                              // lanes of an item
@@ -39,10 +39,10 @@ struct PassArgs {
     const int* begin;                       // [lanes / N] usable shared lengths, or null (0)
     int rows, tile_rows, row_tiles, unit_shift;
     Divisor by_row_tiles, by_tile_rows, by_N;
-    int *first_cta, *last_cta;              // [items] the CTAs that have an item's first and last units, written by them
-    float* part_item;                       // states of items that one CTA saw whole; null: it writes the output itself
-    float* part_cta;                        // [2 * ctas] states of the others: a CTA's first and last item
-    int ctas;
+    int *first_run, *last_run;              // [items] the runs that have an item's first and last units, written by them
+    float* part_item;                       // states of items that one run saw whole; null: it writes the output itself
+    float* part_run;                        // [2 * runs] states of the others: a run's first and last item
+    int runs;
     long long wait_cycles;
 };
 
@@ -108,17 +108,18 @@ struct Cursor {
     }
 };
 
-// The CTA's run: how many units it has, and where it starts; called by all NT threads.  0: it has none.
+// The run of the thread's CTA (WORKERS = 1) or warp (one of WORKERS): how many units it has, and where it starts; called
+// by all NT threads.  0: it has none.
 struct RunSmem {
     int warp_sum[32];
-    int start[3];
+    int start[4][3];
 };
 __device__ __noinline__ int entry_units(const AttendArgs& a, const PassArgs& p, int entry) {
     int lo, hi;
     token_range(a, p, entry, p.by_row_tiles.div(entry), lo, hi);
     return units_of(p, lo, hi);
 }
-template <int NT>
+template <int NT, int WORKERS = 1>
 __device__ __forceinline__ int find_run(const AttendArgs& a, const PassArgs& p, RunSmem& sm, Cursor& cu) {
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, n = p.n * p.row_tiles;
     const int per = (n + NT - 1) / NT, j0 = min(tid * per, n), j1 = min(j0 + per, n);
@@ -141,28 +142,35 @@ __device__ __forceinline__ int find_run(const AttendArgs& a, const PassArgs& p, 
         total += v;
     }
     // U = q G + r units in G equal shares, none of them empty
-    const unsigned U = (unsigned)total * a.c.heads, G = min((unsigned)p.ctas, U);
-    if (blockIdx.x >= G) return 0;
+    const unsigned U = (unsigned)total * a.c.heads, G = min((unsigned)p.runs, U);
+    const unsigned first = blockIdx.x * WORKERS;
+    if (first >= G) return 0;
     const unsigned q = U / G, r = U - q * G;
-    const unsigned x0 = q * blockIdx.x + r * blockIdx.x / G, x1 = q * (blockIdx.x + 1) + r * (blockIdx.x + 1) / G;
+    auto start = [&](unsigned k) { return q * k + r * k / G; };
     unsigned at = (unsigned)before * a.c.heads;
     const unsigned end = at + (unsigned)mine * a.c.heads;
-    if (x0 >= at && x0 < end) {
+    if (start(first) < end && start(min(first + WORKERS, G)) > at) {
 #pragma unroll 1
         for (int j = j0; j < j1; ++j) {
             const unsigned nu = entry_units(a, p, j), all = nu * a.c.heads;
-            if (x0 >= at && x0 < at + all) {
-                sm.start[0] = j;
-                sm.start[1] = (int)((x0 - at) / nu);
-                sm.start[2] = (int)((x0 - at) % nu);
+#pragma unroll 1
+            for (int k = 0; k < WORKERS; ++k) {
+                const unsigned x = start(first + k) - at;
+                if (first + k < G && start(first + k) >= at && x < all) {
+                    sm.start[k][0] = j;
+                    sm.start[k][1] = (int)(x / nu);
+                    sm.start[k][2] = (int)(x % nu);
+                }
             }
             at += all;
         }
     }
     __syncthreads();
-    cu.entry = sm.start[0]; cu.head = sm.start[1]; cu.u = sm.start[2];
+    const unsigned k = WORKERS == 1 ? 0 : w;
+    if (first + k >= G) return 0;
+    cu.entry = sm.start[k][0]; cu.head = sm.start[k][1]; cu.u = sm.start[k][2];
     cu.enter(a, p);
-    return (int)(x1 - x0);
+    return (int)(start(first + k + 1) - start(first + k));
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -244,14 +252,15 @@ template <int D> struct AttendSmem {
 // A state as it is kept in scratch: rows x D sums, then m and l of each row.
 template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(int rows) { return rows * (D + 2); }
 
-// Each warp takes every fourth pair of tiles of the CTA's run.  Scores are formed transposed, S^T = K q^T (tokens
+// Each warp takes every fourth pair of tiles of the CTA's run; SOLO: every pair of a run of its own, so that nothing is
+// joined within the CTA (for many items of few tokens).  Scores are formed transposed, S^T = K q^T (tokens
 // x rows, so that 16 x 16 keys go through one instruction whatever the number of rows up to 8), and
 // so is the output, O^T = V^T P^T.  Keys and values become f16 in registers: code x scale is exact
 // there; queries are scaled by a power of two to lie in f16's range (bf16: exact) or split in two f16
 // (32 bits).  Which dimension of a tile goes to which index of the products is free, and chosen so that a
 // thread's keys are 16 neighbouring bytes and its values the 16 dimensions of one block, which share
 // their scale.  Token l of the products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
-template <int DT, int D, int NT>
+template <int DT, int D, int NT, bool SOLO>
 __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
     constexpr bool F32 = DT == AS_F32;
@@ -265,7 +274,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     Cursor cu, ahead;
-    int left = find_run<AT_NT>(a, p, sm.run, cu), to_issue = left;
+    int left = find_run<AT_NT, SOLO ? AT_W : 1>(a, p, sm.run, cu), to_issue = left;
     if (left == 0) return;
     ahead = cu;
 
@@ -275,11 +284,11 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     const int page_mask = (1 << c.page_shift) - 1, tiles_per_page = 1 << (c.page_shift - 4);
     int page = 0;
     auto look = [&]() {                             // page id of the half-warp's tile under `ahead`
-        const int pos = ahead.lo + ((ahead.u * AT_W + w) * 2 + half) * 16;
+        const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
         if (pos < ahead.hi) page = c.table[(size_t)ahead.lane0 * c.max_pages + (pos >> c.page_shift)];
     };
     auto issue = [&](int stage) {
-        const int pos = ahead.lo + ((ahead.u * AT_W + w) * 2 + half) * 16;
+        const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
         if (pos < ahead.hi) {
             if (page < 0 || page >= c.n_pages) {
                 if (hl == 0) {
@@ -372,7 +381,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
         __syncwarp();
         if (to_issue > 0) issue(stage ^ 1);
         cp_commit();
-        const int pos = cu.lo + (cu.u * AT_W + w) * 32;
+        const int pos = cu.lo + (SOLO ? cu.u : cu.u * AT_W + w) * 32;
         if (pos < cu.hi) {
             const uint32_t st = ring0 + stage * 2 * Ti::BYTES;
             const bool two = pos + 16 < cu.hi;              // (the second tile may lie behind the last token: nothing was copied)
@@ -531,20 +540,60 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
         __syncwarp();
         stage ^= 1;
 
-        // ---- the end of an item, or of the run: the four warps' states become one ----
+        // ---- the end of an item, or of the run (the four warps' states become one) ----
         const bool item_ends = cu.u + 1 == cu.nu;
         if (item_ends || left == 1) {
-            const int head = cu.head;
+            const int head = cu.head, mine = SOLO ? blockIdx.x * AT_W + w : blockIdx.x;
             const bool whole = item_ends && seg_u0 == 0;
             const size_t item = (size_t)cu.entry * c.heads + cu.head;
-            if (tid == 0) {
-                if (seg_u0 == 0) p.first_cta[item] = blockIdx.x;
-                if (item_ends) p.last_cta[item] = blockIdx.x;
+            if ((SOLO ? lane : tid) == 0) {
+                if (seg_u0 == 0) p.first_run[item] = mine;
+                if (item_ends) p.last_run[item] = mine;
             }
             float* part = nullptr;
-            if (!whole) part = p.part_cta + (size_t)(2 * blockIdx.x + (seg_u0 == 0)) * state_floats<D>(8 * NT);
+            if (!whole) part = p.part_run + (size_t)(2 * mine + (seg_u0 == 0)) * state_floats<D>(8 * NT);
             else if (p.part_item) part = p.part_item + item * state_floats<D>(8 * NT);
             const float vg = c.v_scale ? c.v_scale[head] : 1.f;
+            if constexpr (SOLO) {
+                // a thread has D / 8 neighbouring dimensions of the rows 2 cc and 2 cc + 1
+                constexpr int PER = D / 8;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float L = l[n][h];
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, d);
+                        const int rw = n * 8 + 2 * cc + h, row = cu.row0 + rw;
+                        if (part) {
+                            float* at = part + rw * D + r * PER;
+#pragma unroll
+                            for (int i = 0; i < KS; i += 2) *reinterpret_cast<float4*>(at + 2 * i) = make_float4(o[n][i][h], o[n][i][2 + h], o[n][i + 1][h], o[n][i + 1][2 + h]);
+                            if (r == 0) { part[8 * NT * D + rw] = m[n][h]; part[8 * NT * (D + 1) + rw] = L; }
+                        } else if (row < p.rows) {
+                            const float inv = L > 0.f ? vg / L : 0.f;
+                            const size_t orow = out_row(a, cu.lane0, head, row);
+                            E* at = static_cast<E*>(a.out) + orow * D + r * PER;
+                            if constexpr (F32) {
+#pragma unroll
+                                for (int i = 0; i < KS; i += 2)
+                                    *reinterpret_cast<float4*>(at + 2 * i) = make_float4(o[n][i][h] * inv, o[n][i][2 + h] * inv, o[n][i + 1][h] * inv, o[n][i + 1][2 + h] * inv);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < KS; i += 4) {
+                                    uint32_t x[4];
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const __nv_bfloat162 b2 = __floats2bfloat162_rn(o[n][i + e][h] * inv, o[n][i + e][2 + h] * inv);
+                                        x[e] = *reinterpret_cast<const uint32_t*>(&b2);
+                                    }
+                                    *reinterpret_cast<uint4*>(at + 2 * i) = make_uint4(x[0], x[1], x[2], x[3]);
+                                }
+                            }
+                            if (a.lse && r == 0) a.lse[orow] = L > 0.f ? 0.693147180559945f * (m[n][h] + log2f(L)) : -INFINITY;
+                        }
+                    }
+            } else {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -593,20 +642,21 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 }
                 __syncthreads();
             }
+            }
             fresh = true;
         }
         cu.step(a, p);
     }
 }
 
-// Joins the states of row rw of an item into (M, L, acc): dimensions d0 .. d0 + PER - 1.  The item was shared by CTAs
+// Joins the states of row rw of an item into (M, L, acc): dimensions d0 .. d0 + PER - 1.  The item was shared by runs
 // c0 .. c1: the first kept its state in its second slot (that item was its last), the others in their first; one
-// that a CTA saw whole has a state of its own.
+// that a run saw whole has a state of its own.
 template <int D, int PER>
 __device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int c0, int c1, int rw, int d0, float& M, float& L, float (&acc)[PER]) {
 #pragma unroll 1
     for (int k = c0; k <= c1; ++k) {
-        const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_cta + (size_t)(2 * k + (k == c0)) * state_floats<D>(p.tile_rows);
+        const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_run + (size_t)(2 * k + (k == c0)) * state_floats<D>(p.tile_rows);
         const float m2 = s[p.tile_rows * D + rw], l2 = s[p.tile_rows * (D + 1) + rw];
         float x[PER];
 #pragma unroll
@@ -626,7 +676,7 @@ __device__ __forceinline__ void join_shared(const AttendArgs& a, const PassArgs&
     if (pre.begin[gr] == 0) return;
     const int prow = (lane - gr * pre.N) * rows + row, pt = pre.by_tile_rows.div(prow);
     const size_t item = ((size_t)gr * pre.row_tiles + pt) * a.c.heads + head;
-    join_states<D>(pre, item, pre.first_cta[item], pre.last_cta[item], prow - pt * pre.tile_rows, d0, M, L, acc);
+    join_states<D>(pre, item, pre.first_run[item], pre.last_run[item], prow - pt * pre.tile_rows, d0, M, L, acc);
 }
 
 // One CTA per item of the lanes' own pass and 32 of its rows, a warp to a row: joins the states of rows that were split
@@ -644,7 +694,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     for (unsigned i = blockIdx.x; i < items; i += gridDim.x) {
         const int entry = c.by_heads.div(i), head = (int)i - entry * c.heads, ln = own.by_row_tiles.div(entry);
         const bool none = entry_units(a, own, entry) == 0;
-        const int c0 = none ? 0 : own.first_cta[i], c1 = none ? -1 : own.last_cta[i];
+        const int c0 = none ? 0 : own.first_run[i], c1 = none ? -1 : own.last_run[i];
         if (!none && c0 == c1 && !own.part_item) continue;                  // the pass has written the output itself
         const int row0 = (entry - ln * own.row_tiles) * own.tile_rows;
         const int end = min(min(own.tile_rows, own.rows - row0), (int)(blockIdx.y + 1) * JOIN_ROWS);

@@ -305,11 +305,11 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             const bool whole = cu.u == 0 && tiles == cu.nu;
             const size_t at_item = (size_t)cu.entry * c.heads + cu.head;
             if (tid == TC_NT - 1) {
-                if (cu.u == 0) p.first_cta[at_item] = blockIdx.x;
-                if (cu.u + tiles == cu.nu) p.last_cta[at_item] = blockIdx.x;
+                if (cu.u == 0) p.first_run[at_item] = blockIdx.x;
+                if (cu.u + tiles == cu.nu) p.last_run[at_item] = blockIdx.x;
             }
             float* part = nullptr;
-            if (!whole) part = p.part_cta + (size_t)(2 * blockIdx.x + (cu.u == 0)) * state_floats<D>(p.tile_rows);
+            if (!whole) part = p.part_run + (size_t)(2 * blockIdx.x + (cu.u == 0)) * state_floats<D>(p.tile_rows);
             else if (p.part_item) part = p.part_item + at_item * state_floats<D>(p.tile_rows);
             // DUAL: a thread writes its row; else the two groups' states of a row join, and each group writes half of it
             float M = m, L = l, f0 = 1.f, f1 = 0.f;

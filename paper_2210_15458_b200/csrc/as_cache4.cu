@@ -119,10 +119,10 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
         p.by_N.set(N);
         p.unit_shift = 7;               // TC_KV = 32 * AT_W tokens
         const size_t items = (size_t)n * heads * p.row_tiles;
-        p.first_cta = reinterpret_cast<int*>(take(sizeof(int) * items));
-        p.last_cta = reinterpret_cast<int*>(take(sizeof(int) * items));
+        p.first_run = reinterpret_cast<int*>(take(sizeof(int) * items));
+        p.last_run = reinterpret_cast<int*>(take(sizeof(int) * items));
         const size_t state = sizeof(float) * (size_t)p.tile_rows * (D + 2);
-        p.part_cta = reinterpret_cast<float*>(take(2 * (size_t)(tc ? TC_MAX_CTAS : AT_MAX_CTAS) * state));
+        p.part_run = reinterpret_cast<float*>(take(2 * (size_t)(tc ? TC_MAX_CTAS : AT_MAX_RUNS) * state));
         if (N > 1) p.part_item = reinterpret_cast<float*>(take(items * state));
     };
     pass(pl.own, pl.own_kernel, lanes, 1, false);
@@ -131,12 +131,12 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
     return pl;
 }
 
-template <int DT, int D, int NT>
-static cudaError_t launch_mma(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
+template <int DT, int D, int NT, bool SOLO>
+static cudaError_t launch_mma_runs(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
     static int per_sm[64] = {0};
     int dev = 0;
     cudaGetDevice(&dev);
-    auto kern = attend_mma_kernel<DT, D, NT>;
+    auto kern = attend_mma_kernel<DT, D, NT, SOLO>;
     if (per_sm[dev] == 0) {
         int n = 0;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(AttendSmem<D>));
@@ -144,8 +144,18 @@ static cudaError_t launch_mma(const AttendArgs& a, PassArgs& p, int sms, cudaStr
         if (e != cudaSuccess) return e;
         per_sm[dev] = n > 0 ? n : 1;
     }
-    p.ctas = per_sm[dev] * sms < AT_MAX_CTAS ? per_sm[dev] * sms : AT_MAX_CTAS;
-    return launch_after(kern, p.ctas, AT_NT, sizeof(AttendSmem<D>), st, a, p);
+    const int most = SOLO ? AT_MAX_RUNS / AT_W : AT_MAX_RUNS, ctas = per_sm[dev] * sms < most ? per_sm[dev] * sms : most;
+    p.runs = SOLO ? ctas * AT_W : ctas;
+    p.unit_shift = SOLO ? 5 : 7;                    // 32 tokens for a warp, 32 * AT_W for a CTA
+    return launch_after(kern, ctas, AT_NT, sizeof(AttendSmem<D>), st, a, p);
+}
+template <int DT, int D, int NT>
+static cudaError_t launch_mma(const AttendArgs& a, PassArgs& p, int sms, cudaStream_t st) {
+    // A run for each warp where the items are many, or behind shared beginnings, where they are short; else a run for each
+    // CTA, whose four warps share an item's tokens.  1024 items of up to 300 / 1000 / 8192 tokens: 26.5 / 41.9 / 179.7 us by
+    // warps, 28.0 / 46.5 / 179.6 us by CTAs; few items leave most warps without a run of their own.
+    const long long items = (long long)p.n * p.row_tiles * a.c.heads;
+    return (p.begin && !p.prefix) || items >= 512 ? launch_mma_runs<DT, D, NT, true>(a, p, sms, st) : launch_mma_runs<DT, D, NT, false>(a, p, sms, st);
 }
 
 template <int D, bool DUAL>
@@ -159,9 +169,9 @@ static cudaError_t launch_tc(const AttendArgs& a, PassArgs& p, int sms, cudaStre
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    p.ctas = sms < TC_MAX_CTAS ? sms : TC_MAX_CTAS;
+    p.runs = sms < TC_MAX_CTAS ? sms : TC_MAX_CTAS;
     p.wait_cycles = wait_cycles_now();
-    return launch_after(kern, p.ctas, TC_NT, tc_smem_bytes<D, DUAL>(), st, a, p);
+    return launch_after(kern, p.runs, TC_NT, tc_smem_bytes<D, DUAL>(), st, a, p);
 }
 
 template <int DT, int D>
