@@ -259,7 +259,9 @@ template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(
 // there; queries are scaled by a power of two to lie in f16's range (bf16: exact) or split in two f16
 // (32 bits).  Which dimension of a tile goes to which index of the products is free, and chosen so that a
 // thread's keys are 16 neighbouring bytes and its values the 16 dimensions of one block, which share
-// their scale.  Token l of the products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
+// their scale.  The tensor cores cut sums off instead of rounding them: with 32-bit queries (one row tile) chains of products
+// are kept to two and joined by additions (12 x 30001 tokens: 3.0e-6 off otherwise, from the bias alone).  Token l of the
+// products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
 template <int DT, int D, int NT, bool SOLO>
 __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
@@ -412,8 +414,10 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][n][e] = 0.f;
+                float rest[4] = {0.f, 0.f, 0.f, 0.f};       // (32-bit queries: the sum over their second halves)
 #pragma unroll
                 for (int j = 0; j < KS; j += 2) {           // a word of each token is two steps of 16 dimensions
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};   // (32-bit queries: two steps' sum)
                     uint32_t f[2][4];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) codes_f16x2(kw[i][j / 2], f[i]);
@@ -425,9 +429,17 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            mma_f16(s[b][n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[0][n][j + h][0], qf[0][n][j + h][1]);
-                            if (F32) mma_f16(s[b][n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[PARTS - 1][n][j + h][0], qf[PARTS - 1][n][j + h][1]);
+                            mma_f16(F32 ? part : s[b][n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[0][n][j + h][0], qf[0][n][j + h][1]);
+                            if (F32) mma_f16(rest, f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[PARTS - 1][n][j + h][0], qf[PARTS - 1][n][j + h][1]);
                         }
+                    if (F32) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[b][0][e] += part[e];
+                    }
+                }
+                if (F32) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][0][e] += rest[e];
                 }
             }
             // ---- weights ----
@@ -530,8 +542,15 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                         const uint32_t f0 = mul_f16(f[0][i], vs[0]), f1 = mul_f16(f[1][i], vs[0]), f2 = mul_f16(f[2][i], vs[1]), f3 = mul_f16(f[3][i], vs[1]);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[b][0][n][0], pf[b][0][n][1]);
-                            if (F32) mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[b][PARTS - 1][n][0], pf[b][PARTS - 1][n][1]);
+                            if constexpr (F32) {
+                                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_f16(part, f0, f1, f2, f3, pf[b][PARTS - 1][n][0], pf[b][PARTS - 1][n][1]);
+                                mma_f16(part, f0, f1, f2, f3, pf[b][0][n][0], pf[b][0][n][1]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[n][4 * i4 + i][e] += part[e];
+                            } else {
+                                mma_f16(o[n][4 * i4 + i], f0, f1, f2, f3, pf[b][0][n][0], pf[b][0][n][1]);
+                            }
                         }
                     }
                 }
