@@ -378,7 +378,7 @@ int as_reward_mean(const int32_t *d_seq, const int32_t *d_len, int S, int N, int
 /*
  * Logit edits: penalties for repeated tokens, a bias and a grammar mask, applied to every lane's
  * row in this order, in binary32, rounded once to the row's type:
- *   seen tokens (anywhere in the lane's history):  x = x > 0 ? x / repetition : x * repetition
+ *   seen tokens (anywhere in the lane's history):  x = x > 0 ? x * (1 / repetition) : x * repetition
  *   x = x - (frequency * n + presence * [n > 0])   n = how often the token occurs in the output,
  *                                                  that is at history positions >= d_prompt_len
  *   x = x + d_bias[row, j]
@@ -486,7 +486,10 @@ int as_cache4_load(const as_cache4 *cache, void *d_k, void *d_v, int dtype, int 
  *              [0, max_pages * page_size] (the lane is then empty) or a page id outside [0, n_pages)
  *              (page 0 is read in its place)
  *   d_work     as_cache4_attend_work_bytes(...) bytes of device scratch, 256-byte aligned
- * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (head_dim, page_size), AS_ERR_CUDA.
+ * A row sees tokens by scores in 32 bits; with bf16 queries the weights are rounded to 11 bits (binary16, relative to the
+ * row's largest within a factor of 2^8), sums and outputs are kept in 32 bits until the end.  AS_TUNE_WAIT_KCYCLES bounds
+ * the waits of the kernel for many rows; a lane_status of AS_ERR_TIMEOUT reports one that ran out.
+ * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (head_dim, page_size, more than 2^31 rows or units of work), AS_ERR_CUDA.
  */
 size_t as_cache4_attend_work_bytes(const as_cache4 *cache, int dtype, int lanes, int T, int q_heads, int N);
 int as_cache4_attend(const as_cache4 *cache, const void *d_q, long long q_ld, int dtype, int lanes, int T,

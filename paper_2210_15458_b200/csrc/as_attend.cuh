@@ -673,6 +673,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
 // that a run saw whole has a state of its own.
 template <int D, int PER>
 __device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int c0, int c1, int rw, int d0, float& M, float& L, float (&acc)[PER]) {
+    if (c0 < 0 || c1 >= p.runs) return;                 // (a pass whose waits ran out may not have noted its runs)
 #pragma unroll 1
     for (int k = c0; k <= c1; ++k) {
         const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_run + (size_t)(2 * k + (k == c0)) * state_floats<D>(p.tile_rows);

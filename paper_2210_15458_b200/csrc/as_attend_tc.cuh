@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             tc_commit(bar(sm.fin));
             const long long start = clock64();
 #pragma unroll 1
-            while (!tc_try(bar(sm.fin), 0) && clock64() - start < limit) {}
+            while (!tc_try(bar(sm.fin), 0) && clock64() - start < 2000000000LL) {}     // (whatever the bound on the other waits)
         }
     }
     tc_fence_before();

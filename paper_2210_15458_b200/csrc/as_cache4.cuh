@@ -64,14 +64,7 @@ __device__ __forceinline__ uint32_t to_codes(float lo, float hi) {
     asm("{\n\t.reg .b8 b;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n\tcvt.u32.u8 %0, b;\n\t}" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-// a byte of two codes -> two f16 (the low half of the byte in the low half of the result)
-__device__ __forceinline__ uint32_t codes_f16x2(uint32_t byte) {
-    uint32_t d;
-    asm("{\n\t.reg .b8 b;\n\tcvt.u8.u32 b, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(d) : "r"(byte));
-    return d;
-}
-
-// the four bytes of a word at once (the conversion picks its byte itself: no shifts)
+// the eight codes of a word -> four pairs of f16 (the conversion picks its byte itself: no shifts)
 __device__ __forceinline__ void codes_f16x2(uint32_t word, uint32_t (&d)[4]) {
     asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
         "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}" : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "r"(word));

@@ -328,3 +328,21 @@ def test_unaligned_queries_keys_and_values(B):
     assert torch.equal(pages, other)
     pages, table, k, v = filled(B, lens, H, D, P, 3, None, None)
     assert torch.equal(B.as_cache4_attend(pages, x, table, i32(lens), 0.1), B.as_cache4_attend(pages, x.contiguous(), table, i32(lens), 0.1))
+
+
+def test_a_wait_that_runs_out_reports_timeout_and_the_next_call_is_fine(B):
+    """The kernel for many rows with a bound of a thousand cycles on its waits: it returns, says so, and nothing lingers."""
+    lens, T = [700, 900], 300
+    pages, table, k, v = filled(B, lens, 2, 128, 64, 11, None, None)
+    q = torch.randn(2, T, 8, 128).cuda().bfloat16()
+    good = B.as_cache4_attend(pages, q, table, i32(lens), 0.09)
+    status = i32([9, 9])
+    try:
+        B.as_tune(B.TUNE_WAIT_KCYCLES, 1)
+        B.as_cache4_attend(pages, q, table, i32(lens), 0.09, lane_status=status)
+        torch.cuda.synchronize()
+    finally:
+        B.as_tune(B.TUNE_WAIT_KCYCLES, 0)
+    assert status.tolist() == [B.ERR_TIMEOUT, B.ERR_TIMEOUT]
+    again = B.as_cache4_attend(pages, q, table, i32(lens), 0.09, lane_status=status)
+    assert torch.equal(again, good) and status.tolist() == [0, 0]
