@@ -171,18 +171,23 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+_DTYPE_CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.int16: BF16, torch.uint16: BF16}
+_I32 = torch.int32
+
+
 def _logits_dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
-        return BF16
+    d = _DTYPE_CODE.get(t.dtype)
+    if d is not None:
+        return d
     raise TypeError("logits must be float32 or bfloat16 (or 16-bit integer bit patterns)")
 
 
 def _logits_layout(t: torch.Tensor):
-    if t.dim() != 2 or t.stride(1) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or stride[1] != 1:
         raise ValueError("logits / table must be 2-D with unit stride along the vocabulary")
-    return t.shape[0], t.shape[1], (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]))
+    lanes, width = shape
+    return lanes, width, (stride[0] if lanes > 1 else max(stride[0], width))
 
 
 def as_version() -> int:
@@ -441,7 +446,7 @@ def _int32(t: Optional[torch.Tensor], name: str, numel: Optional[int] = None):
     """Device pointer of a contiguous int32 tensor (None stays None)."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+    if t.dtype is not _I32 or not t.is_contiguous() or (numel is not None and t.numel() != numel):
         raise ValueError("%s must be a contiguous int32 tensor%s" % (name, "" if numel is None else " of %d entries" % numel))
     return t.data_ptr()
 
@@ -470,14 +475,16 @@ def as_logits_edit(logits: torch.Tensor, seq: Optional[torch.Tensor] = None, len
         e.d_seq, e.seq_ld = _int32(seq, "seq"), seq.shape[1]
         e.d_len, e.d_prompt_len = _int32(length, "length", lanes), _int32(prompt_length, "prompt_length", lanes)
     if bias is not None:
-        if bias.dtype != torch.float32 or bias.stride(-1) != 1 or bias.shape[-1] < V or (bias.dim() == 2 and bias.shape[0] not in (1, lanes)):
+        shape, stride = bias.shape, bias.stride()
+        rows = shape[0] if len(shape) == 2 else 1
+        if bias.dtype is not torch.float32 or stride[-1] != 1 or shape[-1] < V or len(shape) > 2 or rows not in (1, lanes):
             raise ValueError("bias must be float32, [V] or [lanes, V], with unit stride along the vocabulary")
-        e.d_bias, e.bias_ld = bias.data_ptr(), (bias.stride(0) if bias.dim() == 2 and bias.shape[0] > 1 else 0)
+        e.d_bias, e.bias_ld = bias.data_ptr(), (stride[0] if rows > 1 else 0)
     if mask is not None:
-        if mask.dtype != torch.int32 or mask.dim() != 2 or mask.stride(1) != 1 or mask.shape[1] < (V + 31) // 32:
+        shape, stride = mask.shape, mask.stride()
+        if mask.dtype is not _I32 or len(shape) != 2 or stride[1] != 1 or shape[1] < (V + 31) // 32:
             raise ValueError("mask must be int32 [rows, ceil(V / 32)] with unit stride along a row")
-        e.d_mask, e.mask_rows = mask.data_ptr(), mask.shape[0]
-        e.mask_ld = mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
+        e.d_mask, e.mask_rows, e.mask_ld = mask.data_ptr(), shape[0], (stride[0] if shape[0] > 1 else shape[1])
         e.d_mask_row = _int32(mask_row, "mask_row", lanes)
     _check(lib().as_logits_edit(logits.data_ptr(), _logits_dtype(logits), lanes, V, ld, ctypes.byref(e), out.data_ptr(),
                                 out_ld, _int32(lane_status, "lane_status", lanes), _stream(stream)))
@@ -497,20 +504,22 @@ def cache4_pages(n_pages: int, heads: int, head_dim: int, page_size: int, planes
 
 
 def _cache4(pages: torch.Tensor, k_scale, v_scale) -> as_cache4:
-    if pages.dtype != torch.uint8 or pages.dim() != 4 or not pages.is_contiguous() or pages.shape[3] % 18:
+    shape = pages.shape
+    if pages.dtype is not torch.uint8 or len(shape) != 4 or not pages.is_contiguous() or shape[3] % 18:
         raise ValueError("pages must be a contiguous uint8 tensor [n_pages, heads, page_size / 16, 18 * head_dim]")
-    n, heads, tiles, width = pages.shape
+    n, heads, tiles, width = shape
     for s in (k_scale, v_scale):
-        if s is not None and (s.dtype != torch.float32 or s.numel() != heads or not s.is_contiguous()):
+        if s is not None and (s.dtype is not torch.float32 or s.numel() != heads or not s.is_contiguous()):
             raise ValueError("k_scale and v_scale must be contiguous float32 with an entry for each head")
     return as_cache4(pages.data_ptr(), n, heads, width // 18, tiles * 16, _ptr(k_scale), _ptr(v_scale))
 
 
 def _tokens(t: torch.Tensor, D: int, name: str):
     """(lanes, T, heads, elements from token to token) of a [lanes, T, heads, D] tensor whose heads lie side by side."""
-    if t.dim() != 4 or t.shape[3] != D:
+    shape = t.shape
+    if len(shape) != 4 or shape[3] != D:
         raise ValueError("%s must be [lanes, T, heads, %d]" % (name, D))
-    lanes, T, heads, _ = t.shape
+    lanes, T, heads, _ = shape
     sl, st, sh, sd = t.stride()
     ld = st if T > 1 else sl if lanes > 1 else heads * D
     if sd != 1 or (heads > 1 and sh != D) or (lanes > 1 and T > 1 and sl != T * st):
@@ -519,9 +528,10 @@ def _tokens(t: torch.Tensor, D: int, name: str):
 
 
 def _table(table: torch.Tensor, length: torch.Tensor, lanes: int):
-    if table.dim() != 2 or table.shape[0] != lanes:
+    shape = table.shape
+    if len(shape) != 2 or shape[0] != lanes:
         raise ValueError("table must be [lanes, max_pages]")
-    return _int32(table, "table"), table.shape[1], _int32(length, "length", lanes)
+    return _int32(table, "table"), shape[1], _int32(length, "length", lanes)
 
 
 def as_cache4_append(pages: torch.Tensor, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor,
