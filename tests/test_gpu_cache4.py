@@ -346,3 +346,37 @@ def test_a_wait_that_runs_out_reports_timeout_and_the_next_call_is_fine(B):
     assert status.tolist() == [B.ERR_TIMEOUT, B.ERR_TIMEOUT]
     again = B.as_cache4_attend(pages, q, table, i32(lens), 0.09, lane_status=status)
     assert torch.equal(again, good) and status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,T,Hq,H,D,P,shared,tails", [(2, 3, 4, 2, 64, 16, [64, 0], [6, 9, 3, 4]), (4, 40, 4, 1, 128, 32, [96], [40, 41, 60, 45]),
+                                                       (2, 20, 2, 1, 64, 64, [64], [6, 30]), (3, 70, 4, 1, 64, 16, [160], [1, 70, 200]), (1, 5, 4, 2, 128, 16, [32], [7])])
+def test_several_tokens_behind_a_shared_beginning(B, dtype, N, T, Hq, H, D, P, shared, tails):
+    """Chunks of T tokens for lanes that share a beginning; some of their rows end within it."""
+    lens = [shared[i // N] + t for i, t in enumerate(tails)]
+    gen = torch.Generator().manual_seed(T)
+    pages, table, k, v = filled(B, lens, H, D, P, 12, None, None, shared, N)
+    q = (torch.randn(len(lens), T, Hq, D, generator=gen) * 1.5).to(DT[dtype]).cuda()
+    lse = torch.empty(len(lens), T, Hq, device="cuda")
+    out = B.as_cache4_attend(pages, q, table, i32(lens), 0.11, N=N, shared=i32(shared), lse=lse)
+    want, wlse, size = attention(q.cpu(), k, v, lens, 0.11)
+    tol, ltol = bounds(dtype, size, max(float(x.abs().max()) for x in v), want)
+    assert ((out.double().cpu() - want).abs() <= tol).all()
+    empty = torch.isinf(wlse)
+    got = lse.double().cpu()
+    assert torch.equal(got[empty], wlse[empty]) and (out.cpu()[empty] == 0).all()
+    assert ((got - wlse)[~empty].abs() <= ltol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_lanes_of_many_lengths(B, dtype):
+    """Enough items for a warp each, lengths of zero among them."""
+    gen = torch.Generator().manual_seed(2)
+    lens = torch.randint(0, 150, (700,), generator=gen).tolist()
+    lens[0] = lens[350] = lens[699] = 0
+    pages, table, k, v = filled(B, lens, 1, 64, 16, 13, None, None)
+    q = torch.randn(700, 1, 2, 64, generator=gen).to(DT[dtype]).cuda()
+    out = B.as_cache4_attend(pages, q, table, i32(lens), 0.125)
+    want, _, size = attention(q.cpu(), k, v, lens, 0.125)
+    tol, _ = bounds(dtype, size, max(float(x.abs().max()) for x in v if x.numel()), want)
+    assert ((out.double().cpu() - want).abs() <= tol).all()
