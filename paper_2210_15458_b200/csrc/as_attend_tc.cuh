@@ -147,7 +147,7 @@ __device__ __forceinline__ void tc_read_row(const uint16_t* from, bool there, bo
 }
 
 struct TcSmem {
-    unsigned long long k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], q_full[2], q_empty[2], o_full, o_empty, ml_full, fin;
+    unsigned long long k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2][2], p_full[2][2], pv_done[2], q_full[2], q_empty[2], o_full, o_empty, ml_full, fin;
     uint32_t tmem;
     int failed;
     RunSmem run;
@@ -162,13 +162,15 @@ template <int D, bool DUAL> constexpr size_t tc_smem_bytes() { return 1024 + (si
 // O += P V with P taken from TMEM; two groups of 128 softmax threads, a thread to a row, turn S into P in
 // place.  DUAL: each group has a row tile and takes every tile of tokens; else the groups take the
 // tiles of tokens in turn, each with its own m, l and O, joined at the end, and the next item's queries have
-// a buffer of their own.  Either way step i belongs to
-// group i % 2, so that one group's products run while the other's weights are formed.
+// a buffer of their own.  DUAL takes a tile in two pieces of 64 tokens, each with columns of its own: while
+// the weights of one are formed, the products of the other run (2 x 2048 tokens over up to 8192: 498 -> 468 us).
+// The other form waits for the filling, and pieces cost it more than they give (8 x 32 codes behind shared tokens: 89.2 -> 90.1 us).
 template <int D, bool DUAL>
 __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
     constexpr int FILL = TC_FIRST / 32, SOFT = FILL + 2 * TC_FILL / 32;     // first warps of the groups
     constexpr int MAT = TC_KV * D * 2, BLK = TC_KV * 128, CHUNKS = D / 8, KSTEPS = D / 16;
+    constexpr int PIECES = DUAL ? 2 : 1, PIECE = TC_KV / PIECES;            // of a tile's tokens
     extern __shared__ char raw[];
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(raw) + 1023) & ~1023u;
     const uint32_t q_s = base, k_s = q_s + 2 * MAT, v_s = k_s + 2 * MAT, raw_s = v_s + 2 * MAT;
@@ -182,7 +184,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
         for (int i = 0; i < 2; ++i) {
             tc_bar_init(bar(sm.k_full[i]), TC_FILL / 32); tc_bar_init(bar(sm.v_full[i]), TC_FILL / 32);
             tc_bar_init(bar(sm.k_empty[i]), 1); tc_bar_init(bar(sm.v_empty[i]), 1);
-            tc_bar_init(bar(sm.s_full[i]), 1); tc_bar_init(bar(sm.p_full[i]), 4);
+            for (int h = 0; h < 2; ++h) { tc_bar_init(bar(sm.s_full[i][h]), 1); tc_bar_init(bar(sm.p_full[i][h]), 4); }
+            tc_bar_init(bar(sm.pv_done[i]), 1);
             tc_bar_init(bar(sm.q_full[i]), (DUAL ? 2 : 1) * TC_FILL / 32); tc_bar_init(bar(sm.q_empty[i]), 1 + TC_SOFT / 32);
         }
         tc_bar_init(bar(sm.o_full), 1); tc_bar_init(bar(sm.o_empty), TC_SOFT / 32);
@@ -233,17 +236,21 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             bool first = true;
 #pragma unroll 1
             for (int j = DUAL ? 0 : s; j < tiles && ok; j += DUAL ? 1 : 2, ++steps) {
-                ok = wait_warp(sm.s_full[s], steps & 1);
+#pragma unroll 1
+              for (int hf = 0; hf < PIECES; ++hf) {
+                ok = wait_warp(sm.s_full[s][hf], steps & 1);
                 if (!ok) break;
                 tc_fence_after();
-                const int left = lim - (cu.lo + (cu.u + j) * TC_KV);        // visible tokens of the tile
-                const bool cut = __any_sync(0xFFFFFFFFu, left < TC_KV);
+                const uint32_t sh = st + PIECE * hf;
+                const int left = lim - (cu.lo + (cu.u + j) * TC_KV + PIECE * hf);   // visible tokens of the piece
+                const bool cut = __any_sync(0xFFFFFFFFu, left < PIECE);
+                bool settled = false;
                 // One pass over the row, 32 columns at a time.  The running maximum hardly ever rises after the first tiles;
                 // where it does, what was written with the old one is scaled.
 #pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
+                for (int ch = 0; ch < PIECE / 32; ++ch) {
                     uint32_t v[32];
-                    tc_ld32(st + 32 * ch, v);
+                    tc_ld32(sh + 32 * ch, v);
                     tc_wait_ld();
                     if (cut) {
                         const int have = left - 32 * ch;
@@ -266,8 +273,14 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                             m = mu = top;
                             l *= f;
                         }
-                        if (!first) tc_scale_sums(ot, D / 16, f);
-                        if (ch > 0) tc_scale_weights(st, ch, f);
+                        if (!first) {
+                            // (the products of the piece before may still be adding to the sums)
+                            if (PIECES > 1 && !settled) ok = wait_warp(sm.pv_done[s], (2 * steps + hf - 1) & 1);
+                            if (!ok) break;
+                            settled = true;
+                            tc_scale_sums(ot, D / 16, f);
+                        }
+                        if (ch > 0) tc_scale_weights(sh, ch, f);
                     }
                     const uint64_t kk = pair(k2, k2), mm = pair(-mu, -mu);
                     uint64_t sum[2] = {0, 0};
@@ -281,13 +294,16 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     }
                     const float2 total = unpair(add2(sum[0], sum[1]));
                     l += total.x + total.y;
-                    tc_st16(st + 16 * ch, pk);
+                    tc_st16(sh + 16 * ch, pk);
                 }
+                if (!ok) break;
                 first = false;
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc_bar_arrive(bar(sm.p_full[s]));
+                if (lane == 0) tc_bar_arrive(bar(sm.p_full[s][hf]));
+              }
+              if (!ok) break;
             }
             if (!ok) break;
             // ---- the end of an item or of the run ----
@@ -534,49 +550,61 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             // One thread walks the steps.  (Chosen by elect.sync, not by its number: the compiler then keeps operands in uniform
             // registers, where each product otherwise costs a dozen instructions that wait their turn behind the other
             // groups'.  TMEM, allocated whole, starts at 0.)
-            constexpr uint32_t ID_S = tc_idesc(128, TC_KV, false), ID_O = tc_idesc(128, D, true);
+            constexpr uint32_t ID_S = tc_idesc(128, PIECE, false), ID_O = tc_idesc(128, D, true);
+            constexpr int HALF = (PIECE * 128) >> 4, QS = DUAL ? 4 : 1, AHEAD = DUAL ? 1 : 2;   // QS: pieces (group, half) of a tile
             const uint64_t q_d = tc_desc(q_s, 0), k_d = tc_desc(k_s, 0), v_d = tc_desc(v_s, BLK);
-            uint32_t n0 = 0, p_seen0 = 0, p_seen1 = 0;              // tiles before this item; weights taken, by group
+            uint32_t n0 = 0, seen[2] = {0, 0};                      // tiles before this item; tiles of weights taken, by group
 #pragma unroll 1
             for (int item = 0; x < run && ok; ++item) {
-                const int tiles = min(cu.nu - cu.u, run - x), steps = DUAL ? 2 * tiles : tiles;
+                const int tiles = min(cu.nu - cu.u, run - x);
                 ok = tc_wait(bar(sm.q_full[q_buf(item)]), q_use(item) & 1, limit, failed);
-                if (!ok) break;
-#pragma unroll 1
-                for (int i = 0; i <= steps; ++i) {
-                    if (i < steps) {
-                        const int j = DUAL ? i >> 1 : i, s = i & 1;
-                        const uint32_t n = n0 + j, b = n & 1;
-                        if (!DUAL || s == 0) ok = tc_wait(bar(sm.k_full[b]), (n >> 1) & 1, limit, failed);
-                        if (!ok) break;
+                // scores of piece z of tile j, into the columns that the piece has
+                auto scores = [&](int j, int z) {
+                    const int s = DUAL ? z & 1 : j & 1, hf = DUAL ? z >> 1 : 0;
+                    const uint32_t n = n0 + j, b = n & 1;
+                    if (z == 0) {
+                        ok = tc_wait(bar(sm.k_full[b]), (n >> 1) & 1, limit, failed);
+                        if (!ok) return;
                         tc_fence_after();
-                        const uint64_t qa = q_d + (DUAL ? s : q_buf(item)) * (MAT >> 4), ka = k_d + b * (MAT >> 4);
-#pragma unroll
-                        for (int k = 0; k < KSTEPS; ++k) {
-                            const uint32_t at = (k / 4) * (BLK >> 4) + (k % 4) * 2;
-                            tc_mma_ss(s_t + 128 * s, qa + at, ka + at, ID_S, k > 0);
-                        }
-                        tc_commit(bar(sm.s_full[s]));
-                        if (!DUAL || s == 1) tc_commit(bar(sm.k_empty[b]));
-                        if (i + 1 == steps) tc_commit(bar(sm.q_empty[q_buf(item)]));
                     }
-                    if (i > 0) {
-                        const int i2 = i - 1, j = DUAL ? i2 >> 1 : i2, s = i2 & 1;
-                        const uint32_t n = n0 + j, b = n & 1;
-                        if (i2 == 0 && item > 0) ok = tc_wait(bar(sm.o_empty), (item - 1) & 1, limit, failed);
-                        if (ok && (!DUAL || s == 0)) ok = tc_wait(bar(sm.v_full[b]), (n >> 1) & 1, limit, failed);
-                        if (ok) ok = tc_wait(bar(sm.p_full[s]), (s ? p_seen1 : p_seen0) & 1, limit, failed);
-                        if (!ok) break;
-                        if (s) ++p_seen1;
-                        else ++p_seen0;
-                        tc_fence_after();
-                        const uint64_t va = v_d + b * (MAT >> 4);
-                        const bool add = DUAL ? j > 0 : j > 1;
+                    const uint64_t qa = q_d + (DUAL ? s : q_buf(item)) * (MAT >> 4), ka = k_d + b * (MAT >> 4) + hf * HALF;
 #pragma unroll
-                        for (int k = 0; k < TC_KV / 16; ++k)
-                            tc_mma_ts(o_t + 128 * s, s_t + 128 * s + 8 * k, va + k * (2048 >> 4), ID_O, k > 0 || add);
-                        if (!DUAL || s == 1) tc_commit(bar(sm.v_empty[b]));
-                        if (i == steps) tc_commit(bar(sm.o_full));
+                    for (int k = 0; k < KSTEPS; ++k) {
+                        const uint32_t at = (k / 4) * (BLK >> 4) + (k % 4) * 2;
+                        tc_mma_ss(s_t + 128 * s + PIECE * hf, qa + at, ka + at, ID_S, k > 0);
+                    }
+                    tc_commit(bar(sm.s_full[s][hf]));
+                    if (z == QS - 1) {
+                        tc_commit(bar(sm.k_empty[b]));
+                        if (j + 1 == tiles) tc_commit(bar(sm.q_empty[q_buf(item)]));
+                    }
+                };
+#pragma unroll 1
+                for (int z = 0; z < QS * AHEAD && ok; ++z)
+                    if (z / QS < tiles) scores(z / QS, z % QS);
+#pragma unroll 1
+                for (int j = 0; j < tiles && ok; ++j) {
+                    const uint32_t n = n0 + j, b = n & 1;
+                    if (j == 0 && item > 0) ok = tc_wait(bar(sm.o_empty), (item - 1) & 1, limit, failed);
+                    if (ok) ok = tc_wait(bar(sm.v_full[b]), (n >> 1) & 1, limit, failed);
+#pragma unroll 1
+                    for (int z = 0; z < QS && ok; ++z) {
+                        const int s = DUAL ? z & 1 : j & 1, hf = DUAL ? z >> 1 : 0;
+                        ok = tc_wait(bar(sm.p_full[s][hf]), (s ? seen[1] : seen[0]) & 1, limit, failed);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t va = v_d + b * (MAT >> 4) + hf * HALF;
+                        const bool add = j >= AHEAD || hf > 0;
+#pragma unroll
+                        for (int k = 0; k < PIECE / 16; ++k)
+                            tc_mma_ts(o_t + 128 * s, s_t + 128 * s + PIECE * hf + 8 * k, va + k * (2048 >> 4), ID_O, k > 0 || add);
+                        if constexpr (PIECES > 1) tc_commit(bar(sm.pv_done[s]));
+                        if (z == QS - 1) {
+                            tc_commit(bar(sm.v_empty[b]));
+                            if (j + 1 == tiles) tc_commit(bar(sm.o_full));
+                        }
+                        if (hf == PIECES - 1) { if (s) ++seen[1]; else ++seen[0]; }
+                        if (j + AHEAD < tiles) scores(j + AHEAD, z);
                     }
                 }
                 if (!ok) break;
