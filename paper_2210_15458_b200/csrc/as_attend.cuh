@@ -262,6 +262,9 @@ template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(
 // their scale.  The tensor cores cut sums off instead of rounding them: with 32-bit queries (one row tile) chains of products
 // are kept to two and joined by additions (12 x 30001 tokens: 3.0e-6 off otherwise, from the bias alone).  Token l of the
 // products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
+// Bound by issue slots: 364 instructions for a tile of 16 tokens at head dimension 128, conversions and products mostly
+// (62 % of the slots, ALU pipe 56 %, DRAM 49 %).  128 lanes of up to 8192 tokens, 32 heads on 8: 180 us (4.5 TB/s); in 32
+// bits, 12 lanes of up to 30001: 97 us (3.0 TB/s).
 template <int DT, int D, int NT, bool SOLO>
 __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
@@ -670,11 +673,11 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
 
 // Joins the states of row rw of an item into (M, L, acc): dimensions d0 .. d0 + PER - 1.  The item was shared by runs
 // c0 .. c1: the first kept its state in its second slot (that item was its last), the others in their first; one
-// that a run saw whole has a state of its own.
+// that a run saw whole has a state of its own.  Two states are read at a time (12 x 30001 tokens in 32 bits 98.2 -> 97.1 us).
 template <int D, int PER>
 __device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int c0, int c1, int rw, int d0, float& M, float& L, float (&acc)[PER]) {
     if (c0 < 0 || c1 >= p.runs) return;                 // (a pass whose waits ran out may not have noted its runs)
-#pragma unroll 1
+#pragma unroll 2
     for (int k = c0; k <= c1; ++k) {
         const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_run + (size_t)(2 * k + (k == c0)) * state_floats<D>(p.tile_rows);
         const float m2 = s[p.tile_rows * D + rw], l2 = s[p.tile_rows * (D + 1) + rw];
@@ -700,7 +703,8 @@ __device__ __forceinline__ void join_shared(const AttendArgs& a, const PassArgs&
 }
 
 // One CTA per item of the lanes' own pass and 32 of its rows, a warp to a row: joins the states of rows that were split
-// over CTAs or passes, in a fixed order, and writes rows that saw nothing.
+// over CTAs or passes, in a fixed order, and writes rows that saw nothing.  Latency: 7 us for 1024 items of 4 rows.  8 or 16 rows
+// a CTA cost the chunk of 2 x 2048 tokens more CTAs that leave at once than they save (465 -> 471 and 467 us).
 constexpr int JOIN_ROWS = 32;
 template <int DT, int D>
 __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs own, const __grid_constant__ PassArgs pre) {

@@ -163,7 +163,8 @@ template <int D, bool DUAL> constexpr size_t tc_smem_bytes() { return 1024 + (si
 // place.  DUAL: each group has a row tile and takes every tile of tokens; else the groups take the
 // tiles of tokens in turn, each with its own m, l and O, joined at the end, and the next item's queries have
 // a buffer of their own.  DUAL takes a tile in two pieces of 64 tokens, each with columns of its own: while
-// the weights of one are formed, the products of the other run (2 x 2048 tokens over up to 8192: 498 -> 468 us).
+// the weights of one are formed, the products of the other run (2 x 2048 tokens over up to 8192: 498 -> 465 us,
+// 875 TFLOP/s; nothing is busy for more than half of it, waiting is spread over softmax, filling and products).
 // The other form waits for the filling, and pieces cost it more than they give (8 x 32 codes behind shared tokens: 89.2 -> 90.1 us).
 template <int D, bool DUAL>
 __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {

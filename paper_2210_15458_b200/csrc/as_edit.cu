@@ -83,6 +83,8 @@ __device__ __forceinline__ float penalise(float x, uint32_t n, const EditArgs& a
 // their way (those that the mask leaves anything of) while the CTA counts the lane's history within the chunk in
 // shared memory: a bit per seen token, a count per token.  Bound by HBM: each element is read and written once; the
 // history is read once per chunk, from L2 (a lane's 4096 tokens are an eighth of what its chunks of 8192 move).
+// 1024 x 128256 in 32 bits: 249 us (1.06 GB; 206 us without bias and mask, 157 without a history: 6.7 TB/s); 256 x 50257 bf16: 20.5 us,
+// 12.6 without a history, whose counting is latency; 8 x 32000 bf16: 5.6 us on the device.
 template <int DT, int VPT>
 __global__ void __launch_bounds__(ED_NT) edit_kernel(const __grid_constant__ EditArgs a) {
     using El = Elem<DT>;
@@ -270,7 +272,8 @@ extern "C" int as_logits_edit(const void* d_logits, int dtype, int lanes, int V,
     a.same_grid = ((in ^ out) & 15) == 0 && ((ld - out_ld) * es) % 16 == 0;
     a.seq_vec = ((reinterpret_cast<uintptr_t>(e->d_seq) | (uintptr_t)(e->seq_ld * 4)) & 15) == 0;
     a.bias_vec = ((reinterpret_cast<uintptr_t>(e->d_bias) | (uintptr_t)(e->bias_ld * 4)) & 15) == 0;
-    // Chunks of 8192 tokens, or of 2048 where those would not fill the SMs twice
+    // Chunks of 8192 tokens, or of 2048 where those would not fill the SMs twice (50257 bf16, large / small chunks, us: 256 lanes
+    // 22.4 / 27.0, 128 lanes 16.9 / 17.4; from 64 lanes down the host's call hides the difference)
     const cudaStream_t st = (cudaStream_t)stream;
     const bool large = (long long)lanes * ((V + 8191) / 8192) >= 2 * di->sms;
     if (in == out && !a.seq && !a.bias && !a.mask && !d_lane_status) return AS_OK;

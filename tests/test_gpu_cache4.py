@@ -380,3 +380,25 @@ def test_many_lanes_of_many_lengths(B, dtype):
     want, _, size = attention(q.cpu(), k, v, lens, 0.125)
     tol, _ = bounds(dtype, size, max(float(x.abs().max()) for x in v if x.numel()), want)
     assert ((out.double().cpu() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_long_prompts_bit_for_bit(B, dtype, D):
+    """Many tokens a lane in one call: what the definition says, and what the same tokens give in pieces."""
+    lens, T, H, P = [1999, 700, 31, 0, 703], 700, 3, 64
+    gen = torch.Generator().manual_seed(D)
+    k, v = ((torch.randn(len(lens), T, H, D, generator=gen) * torch.exp(2 * torch.randn(len(lens), T, H, 1, generator=gen))).to(DT[dtype]).cuda() for _ in range(2))
+    gk, gv = 0.1 + torch.rand(H, generator=gen), 0.1 + torch.rand(H, generator=gen)
+    pages, table = pool(B, lens, H, D, P)
+    B.as_cache4_append(pages, k, v, table, i32(lens), gk.cuda(), gv.cuda())
+    gotk, gotv = B.as_cache4_load(pages, table, i32(lens), T, gk.cuda(), gv.cuda(), dtype=torch.float32)
+    for got, x, g in ((gotk, k, gk), (gotv, v, gv)):
+        want = np.stack([quantise(x[:, :, h].float().cpu().numpy(), g[h])[0] for h in range(H)], axis=2)
+        for i, n in enumerate(lens):
+            want[i, :max(0, T - n)] = 0
+        assert np.array_equal(got.cpu().numpy(), want)
+    again, _ = pool(B, lens, H, D, P)
+    for t in range(0, T, 100):
+        B.as_cache4_append(again, k[:, t:t + 100].contiguous(), v[:, t:t + 100].contiguous(), table, i32([max(0, n - T + 100 + t) for n in lens]), gk.cuda(), gv.cuda())
+    assert torch.equal(again, pages)
