@@ -8,6 +8,7 @@ library is missing or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -160,11 +161,33 @@ def _check(rc: int) -> None:
         raise AsError(rc, lib().as_last_error().decode())
 
 
+def _current_stream() -> int:
+    # the current device's current stream, without building a Stream object around it (0.3 us instead of 4.8)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
 def _stream(stream) -> int:
     if stream is None:
-        # the current device's current stream, without building a Stream object around it (0.3 us instead of 4.8)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return _current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+_NO_SWITCH = contextlib.nullcontext()
+
+
+def _owner(stream, device):
+    """A context in which tensors are allocated from the memory of the stream that the call launches on.  Scratch is dropped on
+    return: its block may only go to later work of the stream whose kernels still use it, and may only come from earlier work
+    of that stream.  (`stream` as the calls take it: None, an object with a cuda_stream, or a raw handle.)"""
+    if stream is None:
+        return _NO_SWITCH
+    raw = _stream(stream)
+    if raw == _current_stream():
+        return _NO_SWITCH
+    if isinstance(stream, torch.cuda.Stream):
+        return torch.cuda.stream(stream)
+    # (0 and 1 are both the default stream)
+    return torch.cuda.stream(torch.cuda.default_stream(device) if raw in (0, 1) else torch.cuda.ExternalStream(raw, device))
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -442,6 +465,10 @@ def as_reward_mean(seq: torch.Tensor, length: torch.Tensor, N: int, r: torch.Ten
     return lane_reward, mean
 
 
+# The calls below allocate what is not passed (outputs, scratch) from the memory of the stream they launch on, as if they stood
+# under torch.cuda.stream(stream): an output that other streams use as well is the caller's to record there.
+
+
 def _int32(t: Optional[torch.Tensor], name: str, numel: Optional[int] = None):
     """Device pointer of a contiguous int32 tensor (None stays None)."""
     if t is None:
@@ -463,7 +490,8 @@ def as_logits_edit(logits: torch.Tensor, seq: Optional[torch.Tensor] = None, len
     V = width if V is None else V
     out_ld = V
     if out is None:
-        out = logits.new_empty((lanes, V))
+        with _owner(stream, logits.device):
+            out = logits.new_empty((lanes, V))
     elif out.dtype != logits.dtype or out.dim() != 2 or out.shape[0] != lanes or out.shape[1] < V:
         raise ValueError("out must have the logits' dtype and a row of at least V for each lane")
     else:
@@ -554,8 +582,9 @@ def as_cache4_load(pages: torch.Tensor, table: torch.Tensor, length: torch.Tenso
     """(k, v) [lanes, T, heads, D]: what is stored for the last T tokens of each lane (zeros where there is none)."""
     c = _cache4(pages, k_scale, v_scale)
     lanes = length.numel()
-    k = pages.new_empty((lanes, T, c.heads, c.head_dim), dtype=dtype)
-    v = torch.empty_like(k)
+    with _owner(stream, pages.device):
+        k = pages.new_empty((lanes, T, c.heads, c.head_dim), dtype=dtype)
+        v = torch.empty_like(k)
     tp, max_pages, lp = _table(table, length, lanes)
     _check(lib().as_cache4_load(ctypes.byref(c), k.data_ptr(), v.data_ptr(), _logits_dtype(k), lanes, T, tp, max_pages, lp,
                                 _int32(lane_status, "lane_status", lanes), _stream(stream)))
@@ -575,18 +604,18 @@ def as_cache4_attend(pages: torch.Tensor, q: torch.Tensor, table: torch.Tensor, 
     shared [lanes / N] int32: how many leading tokens the N lanes of a group have in the same pages."""
     c = _cache4(pages, k_scale, v_scale)
     lanes, T, heads, q_ld = _tokens(q, c.head_dim, "q")
-    if out is None:
-        out = q.new_empty((lanes, T, heads, c.head_dim))
-    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+    if out is not None and (out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous()):
         raise ValueError("out must be contiguous, with the shape and dtype of q")
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() != lanes * T * heads or not lse.is_contiguous()):
         raise ValueError("lse must be contiguous float32 [lanes, T, q_heads]")
     L = lib()
     dt = _logits_dtype(q)
     need = L.as_cache4_attend_work_bytes(ctypes.byref(c), dt, lanes, T, heads, N)
-    if work is None:
-        work = length.new_empty((need + 3) // 4)
     tp, max_pages, lp = _table(table, length, lanes)
+    if out is None or work is None:
+        with _owner(stream, q.device):
+            out = q.new_empty((lanes, T, heads, c.head_dim)) if out is None else out
+            work = length.new_empty((need + 3) // 4) if work is None else work
     _check(L.as_cache4_attend(ctypes.byref(c), q.data_ptr(), q_ld, dt, lanes, T, heads, tp, max_pages, lp, scale, N,
                               _int32(shared, "shared", lanes // N if N > 0 else None), out.data_ptr(), _ptr(lse),
                               _int32(lane_status, "lane_status", lanes), work.data_ptr(),
@@ -609,6 +638,7 @@ def _pool(pool: Optional[torch.Tensor], n_pages: int):
 
 
 def _pages_work(work: Optional[torch.Tensor], lanes_in: int, lanes_out: int, n_pages: int, like: torch.Tensor):
+    """(scratch, its bytes); allocated under _owner."""
     if work is None:
         work = like.new_empty((lib().as_pages_work_bytes(lanes_in, lanes_out, n_pages) + 3) // 4)
     return work, work.numel() * work.element_size()
@@ -622,14 +652,15 @@ def as_pages_fork(parent: torch.Tensor, table: torch.Tensor, length: torch.Tenso
     cache whose partly filled last pages are copied.  ref_out may be ref; the other outputs are new tensors."""
     lanes, max_pages = table.shape
     n = parent.numel()
-    if table_out is None:
-        table_out = table.new_empty((n, max_pages))
-    if length_out is None:
-        length_out = table.new_empty(n)
-    if ref_out is None:
-        ref_out = torch.empty_like(ref)
     data, planes, stride, page_bytes = _pool(pool, ref.numel())
-    work, nbytes = _pages_work(work, lanes, n, ref.numel(), ref)
+    with _owner(stream, ref.device):
+        if table_out is None:
+            table_out = table.new_empty((n, max_pages))
+        if length_out is None:
+            length_out = table.new_empty(n)
+        if ref_out is None:
+            ref_out = torch.empty_like(ref)
+        work, nbytes = _pages_work(work, lanes, n, ref.numel(), ref)
     _check(lib().as_pages_fork(_int32(parent, "parent"), lanes, n, max_pages, page_size, ref.numel(), _int32(table, "table"),
                                _int32(length, "length", lanes), _int32(ref, "ref"),
                                _int32(table_out, "table_out", n * max_pages), _int32(length_out, "length_out", n),
@@ -642,7 +673,8 @@ def as_pages_grow(add: torch.Tensor, table: torch.Tensor, length: torch.Tensor, 
                   lane_status: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None, stream=None) -> None:
     """Give every lane the pages for add[lane] more tokens; table, length and ref are updated in place."""
     lanes, max_pages = table.shape
-    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), ref)
+    with _owner(stream, ref.device):
+        work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), ref)
     _check(lib().as_pages_grow(_int32(add, "add", lanes), lanes, max_pages, page_size, ref.numel(), _int32(table, "table"),
                                _int32(length, "length", lanes), _int32(ref, "ref"),
                                _int32(lane_status, "lane_status", lanes), work.data_ptr(), nbytes, _stream(stream)))
@@ -656,10 +688,11 @@ def as_pages_compact(table: torch.Tensor, ref: torch.Tensor, pool: Optional[torc
     lanes, max_pages = table.shape
     table_out = table if table_out is None else table_out
     ref_out = ref if ref_out is None else ref_out
-    if used is None:
-        used = table.new_empty(())
     data, planes, stride, page_bytes = _pool(pool, ref.numel())
-    work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), ref)
+    with _owner(stream, ref.device):
+        if used is None:
+            used = table.new_empty(())
+        work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), ref)
     _check(lib().as_pages_compact(lanes, max_pages, ref.numel(), _int32(table, "table"), _int32(ref, "ref"),
                                   _int32(table_out, "table_out", table.numel()), _int32(ref_out, "ref_out", ref.numel()),
                                   _int32(used, "used", 1), data, planes, stride, page_bytes, work.data_ptr(), nbytes,
