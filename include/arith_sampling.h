@@ -473,6 +473,7 @@ int as_cache4_load(const as_cache4 *cache, void *d_k, void *d_v, int dtype, int 
  *   out = sum_t softmax_t(scale * q . k_t) v_t    over positions t < d_len[lane] - T + 1 + i,
  * k, v those of head h / (q_heads / heads).  T = 1 is the decode step, T > 1 a chunk of a prompt whose
  * tokens have been appended before.  A row that sees nothing gives zeros (and -inf in d_lse).
+ * A row whose query holds a NaN, or that has a score of +inf, is NaN (and in d_lse); other rows are not touched by it.
  *   d_q        token i of a lane at d_q + (lane * T + i) * q_ld, [q_heads, head_dim] there
  *   q_heads    a multiple of heads;  scale finite
  *   N, d_shared  lanes g*N .. g*N+N-1 form group g (lanes is a multiple of N; the lanes of one prompt).

@@ -250,6 +250,8 @@ template <int D> struct AttendSmem {
 };
 
 // A state as it is kept in scratch: rows x D sums, then m and l of each row.
+// l = 0: the row saw nothing (zeros, lse -inf).  A NaN in the row's query or scores, or a score of +inf, makes l NaN whatever m
+// is, and 1 / l carries it into the output and lse.
 template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(int rows) { return rows * (D + 2); }
 
 // Each warp takes every fourth pair of tiles of the CTA's run; SOLO: every pair of a run of its own, so that nothing is
@@ -593,7 +595,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                             for (int i = 0; i < KS; i += 2) *reinterpret_cast<float4*>(at + 2 * i) = make_float4(o[n][i][h], o[n][i][2 + h], o[n][i + 1][h], o[n][i + 1][2 + h]);
                             if (r == 0) { part[8 * NT * D + rw] = m[n][h]; part[8 * NT * (D + 1) + rw] = L; }
                         } else if (row < p.rows) {
-                            const float inv = L > 0.f ? vg / L : 0.f;
+                            const float inv = L == 0.f ? 0.f : vg / L;
                             const size_t orow = out_row(a, cu.lane0, head, row);
                             E* at = static_cast<E*>(a.out) + orow * D + r * PER;
                             if constexpr (F32) {
@@ -612,7 +614,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                                     *reinterpret_cast<uint4*>(at + 2 * i) = make_uint4(x[0], x[1], x[2], x[3]);
                                 }
                             }
-                            if (a.lse && r == 0) a.lse[orow] = L > 0.f ? 0.693147180559945f * (m[n][h] + log2f(L)) : -INFINITY;
+                            if (a.lse && r == 0) a.lse[orow] = L == 0.f ? -INFINITY : 0.693147180559945f * (m[n][h] + log2f(L));
                         }
                     }
             } else {
@@ -652,7 +654,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     for (int e = 0; e < PER; e += 4) *reinterpret_cast<float4*>(at + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
                     if (d0 == 0) { part[8 * NT * D + n * 8 + rw] = M; part[8 * NT * (D + 1) + n * 8 + rw] = L; }
                 } else if (row < p.rows) {
-                    const float inv = L > 0.f ? vg / L : 0.f;
+                    const float inv = L == 0.f ? 0.f : vg / L;
                     const size_t orow = out_row(a, cu.lane0, head, row);
                     E* at = static_cast<E*>(a.out) + orow * D + d0;
 #pragma unroll
@@ -660,7 +662,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                         if constexpr (F32) *reinterpret_cast<float2*>(at + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
                         else *reinterpret_cast<__nv_bfloat162*>(at + e) = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
                     }
-                    if (a.lse && d0 == 0) a.lse[orow] = L > 0.f ? 0.693147180559945f * (M + log2f(L)) : -INFINITY;
+                    if (a.lse && d0 == 0) a.lse[orow] = L == 0.f ? -INFINITY : 0.693147180559945f * (M + log2f(L));
                 }
                 __syncthreads();
             }
@@ -730,12 +732,12 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
             for (int e = 0; e < PER; ++e) acc[e] = 0.f;
             if (pre.begin) join_shared<D>(a, pre, ln, row, own.rows, head, lane * PER, M, L, acc);
             join_states<D>(own, i, c0, c1, rw, lane * PER, M, L, acc);
-            const float inv = L > 0.f ? (c.v_scale ? c.v_scale[head] : 1.f) / L : 0.f;
+            const float inv = L == 0.f ? 0.f : (c.v_scale ? c.v_scale[head] : 1.f) / L;
             const size_t orow = out_row(a, ln, head, row);
             typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + orow * D + lane * PER;
 #pragma unroll
             for (int e = 0; e < PER; ++e) out[e] = acc[e] * inv;
-            if (a.lse && lane == 0) a.lse[orow] = L > 0.f ? 0.693147180559945f * (M + log2f(L)) : -INFINITY;
+            if (a.lse && lane == 0) a.lse[orow] = L == 0.f ? -INFINITY : 0.693147180559945f * (M + log2f(L));
         }
     }
 }

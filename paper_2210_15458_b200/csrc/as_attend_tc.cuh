@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             }
             const int tr = (DUAL ? 128 * s : 0) + r;
             const size_t orow = row < p.rows ? out_row(a, cu.lane0, cu.head, row) : 0;
-            const float inv = L > 0.f ? vg / L : 0.f;
+            const float inv = L == 0.f ? 0.f : vg / L;
 #pragma unroll 1
             for (int ch = 0; ch < (DUAL ? D / 32 : D / 64); ++ch) {
                 const int col = (DUAL ? 0 : s * (D / 2)) + 32 * ch;
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     part[(size_t)p.tile_rows * D + tr] = M;
                     part[(size_t)p.tile_rows * (D + 1) + tr] = L;
                 } else if (row < p.rows && a.lse) {
-                    a.lse[orow] = L > 0.f ? 0.693147180559945f * (M + log2f(L)) : -INFINITY;
+                    a.lse[orow] = L == 0.f ? -INFINITY : 0.693147180559945f * (M + log2f(L));
                 }
             }
             tc_fence_before();

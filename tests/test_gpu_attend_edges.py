@@ -1,0 +1,97 @@
+"""Attention over the 4-bit cache where its inputs are at their edges, in every kernel: rows of few and of many queries, with and
+without a shared beginning."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+# query rows on the same tokens: a tile of 8 rows, of 16, of 128 and of 256 (in 32 bits all are cut into tiles of 8)
+ROWS = [1, 7, 12, 64, 300]
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2210_15458_b200 import binding
+    return binding
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def cache(B, lanes, n, D, P=64, seed=0, k=None, v=None):
+    """Lanes of n tokens, one head, that hold the same pages: (pages, table, lengths, stored k, v [n, D] as float64)."""
+    g = torch.Generator().manual_seed(seed)
+    k = torch.randn(n, D, generator=g) * 1.5 if k is None else k
+    v = torch.randn(n, D, generator=g) if v is None else v
+    M = -(-n // P)
+    pages = B.cache4_pages(M, 1, D, P)
+    row = torch.randperm(M, generator=g).to(torch.int32).view(1, M).cuda()
+    B.as_cache4_append(pages, k.view(1, n, 1, D).cuda(), v.view(1, n, 1, D).cuda(), row, i32([n]))
+    ks, vs = B.as_cache4_load(pages, row, i32([n]), n, dtype=torch.float32)
+    return pages, row.expand(lanes, M).contiguous(), i32([n] * lanes), ks[0, :, 0].double().cpu(), vs[0, :, 0].double().cpu()
+
+
+def poisoned(q, rows, how):
+    bad = q.clone()
+    for j in rows:
+        flat = bad.view(-1, q.shape[-1])[j]
+        if how == "nan":
+            flat[5] = float("nan")
+        elif how == "all_nan":
+            flat[:] = float("nan")
+        else:
+            flat[3], flat[40] = float("inf"), float("-inf")
+    return bad
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("how", ["nan", "all_nan", "inf"])
+@pytest.mark.parametrize("rows", ROWS)
+def test_a_query_that_is_not_finite_makes_its_own_row_nan(B, dtype, rows, how):
+    D, n = 64, 700
+    pages, table, length, k, v = cache(B, 1, n, D)
+    g = torch.Generator().manual_seed(rows)
+    q = torch.randn(1, 1, rows, D, generator=g).to(DT[dtype]).cuda()
+    hit = sorted({0, rows // 2, rows - 1}) if rows > 2 else [0]
+    lse, blse = (torch.empty(1, 1, rows, device="cuda") for _ in range(2))
+    clean = B.as_cache4_attend(pages, q, table, length, 0.125, lse=lse)
+    got = B.as_cache4_attend(pages, poisoned(q, hit, how), table, length, 0.125, lse=blse)
+    rest = [r for r in range(rows) if r not in hit]
+    assert torch.isnan(got[0, 0, hit]).all() and torch.isnan(blse[0, 0, hit]).all()
+    assert torch.equal(got[0, 0, rest], clean[0, 0, rest]) and torch.equal(blse[0, 0, rest], lse[0, 0, rest])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,g", [(2, 1), (3, 4), (16, 4), (40, 8)])
+def test_the_same_behind_a_shared_beginning(B, dtype, N, g):
+    D, n, P = 128, 700, 64
+    pages, table, length, k, v = cache(B, N, n, D, P)
+    gen = torch.Generator().manual_seed(N)
+    q = torch.randn(N, 1, g, D, generator=gen).to(DT[dtype]).cuda()
+    bad = poisoned(q, [1, N * g - 1], "all_nan")
+    lse = torch.empty(N, 1, g, device="cuda")
+    for shared in (i32([640]), i32([64]), None):
+        clean = B.as_cache4_attend(pages, q, table, length, 0.1, N=N, shared=shared)
+        got = B.as_cache4_attend(pages, bad, table, length, 0.1, N=N, shared=shared, lse=lse)
+        hit = torch.zeros(N * g, dtype=torch.bool)
+        hit[[1, N * g - 1]] = True
+        assert torch.isnan(got.view(N * g, D)[hit.cuda()]).all() and torch.equal(torch.isnan(lse.view(-1)).cpu(), hit)
+        assert torch.equal(got.view(N * g, D)[~hit.cuda()], clean.view(N * g, D)[~hit.cuda()])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 90, 300])
+def test_rows_that_see_nothing_stay_zero_beside_rows_that_are_nan(B, dtype, T):
+    """More query tokens than the lane has: the first ones are padding, whatever their queries hold."""
+    D, n = 64, 2
+    pages, table, length, k, v = cache(B, 1, n, D, 16)
+    q = torch.full((1, T, 2, D), float("nan")).to(DT[dtype]).cuda()
+    q[:, -1] = 1.0
+    lse = torch.empty(1, T, 2, device="cuda")
+    out = B.as_cache4_attend(pages, q, table, length, 0.125, lse=lse)
+    assert (out[0, :T - n] == 0).all() and (lse[0, :T - n] == -math.inf).all()
+    assert torch.isnan(out[0, T - n:-1]).all() and torch.isfinite(out[0, -1]).all()
