@@ -30,7 +30,7 @@ struct AttendArgs {
 // rows of `group` lanes (1, or all N lanes of a group for their shared beginning) x T tokens x the
 // query heads of a key head, cut into row tiles of tile_rows.  Items are ordered by entry (lane or
 // group, row tile), then head; their units (2^unit_shift tokens each) are dealt out in equal
-// contiguous runs, one for each CTA (or warp).  (The host holds the number of units below 2^31.)
+// contiguous runs, one for each CTA (or warp).  (The host holds the number of units below 2^31, at either size.)
 struct PassArgs {
     int n;                                  // lanes, or groups
     int group;                              // lanes of an item

@@ -2,6 +2,7 @@
 #include "as_attend.cuh"
 #include "as_attend_tc.cuh"
 #include "as_cache4.cuh"
+#include "as_units.h"
 
 #include <cmath>
 
@@ -160,8 +161,8 @@ static cudaError_t launch_mma(const AttendArgs& a, PassArgs& p, int sms, cudaStr
     // A run for each warp where the items are many, or behind shared beginnings, where they are short; else a run for each
     // CTA, whose four warps share an item's tokens.  1024 items of up to 300 / 1000 / 8192 tokens: 26.5 / 41.9 / 179.7 us by
     // warps, 28.0 / 46.5 / 179.6 us by CTAs; few items leave most warps without a run of their own.
-    const long long items = (long long)p.n * p.row_tiles * a.c.heads;
-    return (p.begin && !p.prefix) || items >= 512 ? launch_mma_runs<DT, D, NT, true>(a, p, sms, st) : launch_mma_runs<DT, D, NT, false>(a, p, sms, st);
+    const bool warps = runs_by_warps((long long)p.n * p.row_tiles, a.c.heads, (long long)a.c.max_pages << a.c.page_shift, p.begin && !p.prefix);
+    return warps ? launch_mma_runs<DT, D, NT, true>(a, p, sms, st) : launch_mma_runs<DT, D, NT, false>(a, p, sms, st);
 }
 
 template <int D, bool DUAL>
@@ -290,8 +291,8 @@ int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, in
     if (!std::isfinite(scale)) return set_err(AS_ERR_INVALID_ARG, "scale must be finite");
     if (N < 1 || lanes % N) return set_err(AS_ERR_INVALID_ARG, "N = %d must be >= 1 and divide lanes = %d", N, lanes);
     // units of 128 tokens over all lanes, heads and tiles of 8 rows, and rows, are counted in 31 bits
-    const long long tiles = ((long long)T * (q_heads / cache->heads) + 7) / 8, units = ((long long)max_pages * cache->page_size + 127) / 128;
-    if ((long long)lanes * T * q_heads > 0x7FFFFFFFLL || (double)lanes * cache->heads * tiles * units > 2147483647.0)
+    const long long tiles = ((long long)T * (q_heads / cache->heads) + 7) / 8;
+    if ((long long)lanes * T * q_heads > 0x7FFFFFFFLL || !units_fit(lanes * tiles, cache->heads, (long long)max_pages * cache->page_size, 7))
         return set_err(AS_ERR_UNSUPPORTED, "lanes, T, q_heads and max_pages * page_size make more than 2^31 rows or units of work");
     if (lanes == 0) return AS_OK;
     if (!d_q || !d_out) return set_err(AS_ERR_INVALID_ARG, "d_q or d_out is NULL");

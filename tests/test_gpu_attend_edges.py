@@ -95,3 +95,21 @@ def test_rows_that_see_nothing_stay_zero_beside_rows_that_are_nan(B, dtype, T):
     out = B.as_cache4_attend(pages, q, table, length, 0.125, lse=lse)
     assert (out[0, :T - n] == 0).all() and (lse[0, :T - n] == -math.inf).all()
     assert torch.isnan(out[0, T - n:-1]).all() and torch.isfinite(out[0, -1]).all()
+
+
+def test_a_page_table_so_wide_that_units_for_warps_could_not_be_counted(B):
+    """512 items of lanes whose tables have room for 2^29 tokens: a run for each CTA, the same rows as with a table that is cut."""
+    lanes, H, T, Hq, D, P, n = 8, 8, 8, 64, 64, 128, 300
+    g = torch.Generator().manual_seed(5)
+    M = (1 << 22) - 1
+    wide = torch.full((lanes, M), -1, dtype=torch.int32, device="cuda")
+    wide[:, :3] = torch.randperm(3 * lanes, generator=g).to(torch.int32).view(lanes, 3).cuda()
+    pages = B.cache4_pages(3 * lanes, H, D, P)
+    k, v = (torch.randn(lanes, n, H, D, generator=g).cuda() for _ in range(2))
+    length = i32([n - i for i in range(lanes)])
+    B.as_cache4_append(pages, k, v, wide, length)
+    q = torch.randn(lanes, T, Hq, D, generator=g).cuda()
+    near = B.as_cache4_attend(pages, q, wide[:, :3].contiguous(), length, 0.125)
+    # two results, each off by at most what sums and weights of 24 bits are (scores here are below 100)
+    tol = 2 * (2 * (2.0 ** -21 * 100 + 2.0 ** -20) + 2.0 ** -22) * float(v.abs().max()) * 1.2
+    assert ((B.as_cache4_attend(pages, q, wide, length, 0.125) - near).abs() <= tol).all()
