@@ -487,8 +487,8 @@ int as_cache4_load(const as_cache4 *cache, void *d_k, void *d_v, int dtype, int 
  *              [0, max_pages * page_size] (the lane is then empty) or a page id outside [0, n_pages)
  *              (page 0 is read in its place)
  *   d_work     as_cache4_attend_work_bytes(...) bytes of device scratch, 256-byte aligned
- * A row sees tokens by scores in 32 bits; with bf16 queries the weights are rounded to 11 bits (binary16, relative to the
- * row's largest within a factor of 2^8), sums and outputs are kept in 32 bits until the end.  AS_TUNE_WAIT_KCYCLES bounds
+ * Scores, sums and outputs are kept in 32 bits until the end.  For the product with the values a weight is rounded to 11 bits with
+ * bf16 queries, to 22 with 32-bit ones, or to 2^-32 (32-bit queries: 2^-37) of the row's largest weight where that is more.  AS_TUNE_WAIT_KCYCLES bounds
  * the waits of the kernel for many rows; a lane_status of AS_ERR_TIMEOUT reports one that ran out.
  * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (head_dim, page_size, more than 2^31 rows or units of work), AS_ERR_CUDA.
  */

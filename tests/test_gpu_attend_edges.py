@@ -113,3 +113,41 @@ def test_a_page_table_so_wide_that_units_for_warps_could_not_be_counted(B):
     # two results, each off by at most what sums and weights of 24 bits are (scores here are below 100)
     tol = 2 * (2 * (2.0 ** -21 * 100 + 2.0 ** -20) + 2.0 ** -22) * float(v.abs().max()) * 1.2
     assert ((B.as_cache4_attend(pages, q, wide, length, 0.125) - near).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("peak", [0, 15000, 29999])
+@pytest.mark.parametrize("down", [25.5, 30.0])
+@pytest.mark.parametrize("many", [False, True])
+def test_one_peak_and_a_long_tail(B, dtype, rows, peak, down, many):
+    """One token stands above 29999 others, each of which has 2^-down of its weight; only the others have a value.  Their part
+    of the result is theirs together, however small each is: n 2^-25.5 is 6.3e-4 of all weight.
+
+    Relative error of that part: scores as in the other tests (e, in numerator and sum), sums in 32 bits of n / 8 weights
+    (2^-24 each) and of n / 16 products (2^-23 each, cut off by the tensor cores), and the output's rounding (2^-22; bf16: 2^-8, and 2^-11 of a weight);
+    absolute: a weight is held to 2^-25 in units in which the largest is at least 2^7 (32 bits: 2^12).
+    Many lanes: an item's tokens are then seen by one run, or few, in place of all of them."""
+    D, n = 64, 30000
+    k, v = torch.zeros(n, D), torch.ones(n, D)
+    k[peak], v[peak] = 1.0, 0.0
+    g, N = (rows, 1) if rows < 300 else (30, 10)
+    pages, table, length, ks, vs = cache(B, N, n, D, 64, 1, k, v)
+    size = down * math.log(2.0)
+    scale = size / float(ks[peak].sum())
+    q = torch.ones(N, 1, g, D).to(DT[dtype]).cuda()
+    w = 2.0 ** -down * (n - 1)
+    v1 = float(vs[(peak + 1) % n, 0])
+    want, wlse = w * v1 / (1 + w), size + math.log1p(w)
+    e = 2.0 ** -21 * size + 2.0 ** -20
+    rel = 2 * e + n / 8 * 2.0 ** -24 + n / 16 * 2.0 ** -23 + (2.0 ** -8 + 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22)
+    tol = want * rel + n * v1 * 2.0 ** (-37 if dtype == "f32" else -32)
+    if many:
+        copies = (600 if rows < 64 else 200) // N
+        table, length, q = table.repeat(copies, 1), length.repeat(copies), q.repeat(copies, 1, 1, 1)
+    lanes = q.shape[0]
+    lse = torch.empty(lanes, 1, g, device="cuda")
+    for shared in (None,) if N == 1 else (None, i32([n // 64 * 64] * (lanes // N)), i32([n // 128 * 64] * (lanes // N))):
+        out = B.as_cache4_attend(pages, q, table, length, scale, N=N, shared=shared, lse=lse)
+        assert float((out.double() - want).abs().max()) <= tol
+        assert float((lse.double() - wlse).abs().max()) <= 2 * e + n / 8 * 2.0 ** -24 + 2.0 ** -20
