@@ -276,7 +276,10 @@ int as_cache4_load(const as_cache4* cache, void* d_k, void* d_v, int dtype, int 
 }
 
 size_t as_cache4_attend_work_bytes(const as_cache4* cache, int dtype, int lanes, int T, int q_heads, int N) {
-    if (!cache || cache->heads < 1 || lanes < 0 || T < 1 || q_heads < cache->heads || N < 1) return 0;
+    // (a shape that the call refuses may not even be planned: its rows may pass 32 bits)
+    if (!cache || cache->heads < 1 || (cache->head_dim != 64 && cache->head_dim != 128) || (dtype != AS_F32 && dtype != AS_BF16)) return 0;
+    if (lanes < 1 || T < 1 || q_heads < 1 || q_heads % cache->heads || N < 1 || lanes % N) return 0;
+    if ((long long)lanes * T > (1LL << 30) || (long long)lanes * T * q_heads > 0x7FFFFFFFLL) return 0;
     return plan_attend(dtype, lanes, T, cache->heads, q_heads, cache->head_dim, N, nullptr).bytes;
 }
 

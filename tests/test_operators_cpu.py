@@ -1,7 +1,10 @@
 """Refusals of the logit edit, cache and page calls: every host-detectable error comes back before the device is touched."""
 import ctypes
+import os
 
 import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -145,3 +148,26 @@ def test_binding_checks_layouts(B):
         B.as_cache4_attend(pages, k, table[0], length, 1.0)
     with pytest.raises(ValueError):
         B.as_pages_fork(torch.zeros(2, dtype=torch.int32), table, length, torch.zeros(4, dtype=torch.int32), 16, pool=torch.zeros(2, 5, 4))
+
+
+def test_scratch_sizes_of_shapes_that_are_refused():
+    """Sizes whose products leave 32 bits end neither the process nor in a size: 0, as for every shape that the call refuses."""
+    import subprocess
+    import sys
+    code = """
+import ctypes
+from paper_2210_15458_b200 import binding as B
+L = B.lib()
+c = lambda **k: ctypes.byref(B.as_cache4(**dict(dict(d_pages=256, n_pages=4, heads=1, head_dim=64, page_size=16), **k)))
+f = L.as_cache4_attend_work_bytes
+for args in ((1, 65536, 65536, 1), (1, 1 << 30, 4, 1), (1, 1 << 16, 1 << 15, 1), (65536, 65536, 1, 65536), (0, 65536, 1, 65536), (1 << 16, 1 << 15, 1, 1), (3, 1, 1, 2),
+             (2, 1, 1, 0), (2, 0, 1, 1), (-1, 1, 1, 1), (2, 1, 0, 1), (2147483647, 1, 2, 2147483647), (0, 1, 1, 1)):
+    for dtype in (0, 1):
+        assert f(c(), dtype, *args) == 0, args
+assert f(c(heads=2), 1, 2, 1, 3, 1) == 0 and f(c(head_dim=96), 1, 2, 1, 2, 1) == 0 and f(c(heads=0), 1, 2, 1, 2, 1) == 0 and f(c(), 7, 2, 1, 2, 1) == 0
+assert f(None, 1, 2, 1, 2, 1) == 0
+assert f(c(), 1, 2, 1, 2, 1) % 256 == 0 and f(c(), 1, 2, 1, 2, 2) > f(c(), 1, 2, 1, 2, 1) > 0
+print("fine")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT)
+    assert r.returncode == 0 and r.stdout.strip() == "fine", (r.returncode, r.stderr[-500:])
