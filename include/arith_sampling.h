@@ -475,7 +475,7 @@ int as_cache4_load(const as_cache4 *cache, void *d_k, void *d_v, int dtype, int 
  * tokens have been appended before.  A row that sees nothing gives zeros (and -inf in d_lse).
  * A row whose query holds a NaN, or that has a score of +inf, is NaN (and in d_lse); other rows are not touched by it.
  *   d_q        token i of a lane at d_q + (lane * T + i) * q_ld, [q_heads, head_dim] there
- *   q_heads    a multiple of heads;  scale finite
+ *   q_heads    a multiple of heads;  scale finite in binary32
  *   N, d_shared  lanes g*N .. g*N+N-1 form group g (lanes is a multiple of N; the lanes of one prompt).
  *              d_shared NULL, or [lanes / N] i32 device: the first d_shared[g] positions of the
  *              group's lanes lie in the same pages (a multiple of page_size, <= every d_len of the

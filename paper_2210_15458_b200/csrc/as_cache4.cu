@@ -291,7 +291,7 @@ int as_cache4_attend(const as_cache4* cache, const void* d_q, long long q_ld, in
     if ((rc = check_lanes(dtype, lanes, T, d_table, max_pages, d_len, cache->page_size)) != AS_OK) return rc;
     if (q_heads < 1 || q_heads % cache->heads) return set_err(AS_ERR_INVALID_ARG, "q_heads = %d must be a multiple of heads = %d", q_heads, cache->heads);
     if (q_ld < (long long)q_heads * cache->head_dim) return set_err(AS_ERR_INVALID_ARG, "q_ld = %lld is smaller than q_heads * head_dim", q_ld);
-    if (!std::isfinite(scale)) return set_err(AS_ERR_INVALID_ARG, "scale must be finite");
+    if (!std::isfinite((float)scale)) return set_err(AS_ERR_INVALID_ARG, "scale = %g must be finite in binary32", scale);
     if (N < 1 || lanes % N) return set_err(AS_ERR_INVALID_ARG, "N = %d must be >= 1 and divide lanes = %d", N, lanes);
     // units of 128 tokens over all lanes, heads and tiles of 8 rows, and rows, are counted in 31 bits
     const long long tiles = ((long long)T * (q_heads / cache->heads) + 7) / 8;

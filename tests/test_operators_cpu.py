@@ -171,3 +171,10 @@ print("fine")
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT)
     assert r.returncode == 0 and r.stdout.strip() == "fine", (r.returncode, r.stderr[-500:])
+
+
+def test_a_scale_that_is_infinite_in_32_bits_is_refused(B):
+    c = _cache(B)
+    for scale in (1e39, -1e300, 3.5e38):
+        assert _attend(B, c, scale=scale) == B.ERR_INVALID_ARG, scale
+        assert b"scale" in B.lib().as_last_error(), scale
