@@ -525,7 +525,8 @@ int as_cache4_attend(const as_cache4 *cache, const void *d_q, long long q_ld, in
  * pass max_pages or has a bad length or a negative d_add: AS_ERR_INVALID_ARG, unchanged.
  *
  * as_pages_compact: with U pages in use, every page in use at U or above moves into a free page
- * below U (the lowest into the lowest), so that the pool's end is free.
+ * below U (the lowest into the lowest), so that the pool's end is free.  Table entries that name a page in use follow it;
+ * any other entry (-1, or a page that no lane holds by d_ref) stays as it is.
  *   d_table_out may be d_table, d_ref_out may be d_ref;  d_used  [1] i32 device, written: U
  *
  *   d_work     as_pages_work_bytes(lanes_in, lanes_out, n_pages) bytes of device scratch, 256-byte aligned

@@ -278,6 +278,7 @@ __global__ void __launch_bounds__(PL_NT) compact_plan_kernel(const int* ref, int
     for (int i = tid; i < n_pages; i += PL_NT) {
         const int r = ref[i];
         n += r > 0;
+        w.free_page[i] = i;                             // (a page that does not move, or that nobody holds)
         if (ref_out != ref) ref_out[i] = r;
     }
     int used;

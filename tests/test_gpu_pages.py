@@ -187,3 +187,13 @@ def test_other_stream(B):
     s.synchronize()
     assert t.tolist() == [[0, 1], [2, -1], [0, 3], [4, 5]] and n.tolist() == [6, 3, 6, 6] and r.tolist() == [2, 1, 1, 1, 1, 1]
     assert torch.equal(pool[:, 3], pool[:, 1]) and torch.equal(pool[:, 4], pool[:, 2])
+
+
+def test_compact_leaves_entries_of_pages_that_nobody_holds(B):
+    """Rows that a finished lane left behind name free pages: below the pages in use, or behind them.  They stay."""
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    table, ref = i32([[7, 2, -1], [5, 9, 3], [8, 1, 100]]), i32([0, 1, 1, 0, 0, 0, 0, 1, 0, 0])      # 5, 9, 3 and 8 are free
+    work = torch.full((B.as_pages_work_bytes(3, 3, 10) // 4,), 0x77777777, dtype=torch.int32, device="cuda")
+    used = B.as_pages_compact(table, ref, work=work)
+    assert int(used) == 3 and ref.tolist() == [1, 1, 1] + [0] * 7
+    assert table.tolist() == [[0, 2, -1], [5, 9, 3], [8, 1, 100]]
