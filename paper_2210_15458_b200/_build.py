@@ -9,7 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libarith_sampling.so")
-# the same sources with every shared-memory index checked (-DAS_BOUNDS_CHECK): for the tests
+# the same sources with computed indices checked (-DAS_BOUNDS_CHECK, as_bounds.cuh): for the tests
 LIB_CHECKED = os.path.join(_HERE, "libarith_sampling_check.so")
 SOURCES = ["as_api.cu", "as_edit.cu", "as_cache4.cu", "as_pages.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

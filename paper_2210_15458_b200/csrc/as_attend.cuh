@@ -53,14 +53,14 @@ struct PassArgs {
 };
 
 __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad = nullptr) {
-    const int len = c.len[lane];
+    const int len = c.len[ASX_AT(lane, c.lanes, 121)];
     const bool b = len < 0 || len > ((long long)c.max_pages << c.page_shift);
     if (bad) *bad = b;
     return b ? 0 : len;
 }
 // the tokens [lo, hi) that the rows of an entry read; behind a tile's last row nothing is seen
 __device__ __forceinline__ void token_range(const AttendArgs& a, const PassArgs& p, int entry, int b, int& lo, int& hi) {
-    const int s = p.begin ? p.begin[p.prefix ? b : p.by_N.div(b)] : 0;
+    const int s = p.begin ? p.begin[ASX_AT(p.prefix ? b : p.by_N.div(b), a.c.lanes / p.N, 122)] : 0;
     lo = p.prefix ? 0 : s;
     hi = p.prefix ? s : lane_len(a.c, b);
     if (!p.prefix && a.c.T > 1) {
@@ -76,7 +76,7 @@ __device__ __forceinline__ int row_limit(const AttendArgs& a, int lane0, int row
 }
 __device__ __forceinline__ size_t out_row(const AttendArgs& a, int lane0, int head, int row) {
     const int tok = a.by_g.div(row), g = (int)a.by_g.d;
-    return ((size_t)lane0 * a.c.T + tok) * a.q_heads + head * g + row - tok * g;
+    return ASX_AT(((size_t)lane0 * a.c.T + tok) * a.q_heads + head * g + row - tok * g, (long long)a.c.lanes * a.c.T * a.q_heads, 123);
 }
 
 // The first entry from `entry` on that has tokens: (entry, lo, hi, lane or group).  A call: it is rare, and inlined it
@@ -163,6 +163,7 @@ __device__ __forceinline__ int find_run(const AttendArgs& a, const PassArgs& p, 
             for (int k = 0; k < WORKERS; ++k) {
                 const unsigned x = start(first + k) - at;
                 if (first + k < G && start(first + k) >= at && x < all) {
+                    (void)ASX_AT(k, 4, 124);
                     sm.start[k][0] = j;
                     sm.start[k][1] = (int)(x / nu);
                     sm.start[k][2] = (int)(x % nu);
@@ -245,7 +246,7 @@ template <> __device__ __forceinline__ unsigned char lds<unsigned char>(uint32_t
 template <int DT, int D>
 __device__ __forceinline__ const typename Io<DT>::type* query_row(const AttendArgs& a, int lane0, int head, int row) {
     const int tok = a.by_g.div(row), g = (int)a.by_g.d;
-    return static_cast<const typename Io<DT>::type*>(a.q) + ((long long)lane0 * a.c.T + tok) * a.q_ld + (head * g + row - tok * g) * D;
+    return static_cast<const typename Io<DT>::type*>(a.q) + ASX_AT((long long)lane0 * a.c.T + tok, (long long)a.c.lanes * a.c.T, 125) * a.q_ld + ASX_AT(head * g + row - tok * g, a.q_heads, 126) * D;
 }
 
 template <int D> struct AttendSmem {
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     int page = 0;
     auto look = [&]() {                             // page id of the half-warp's tile under `ahead`
         const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
-        if (pos < ahead.hi) page = c.table[(size_t)ahead.lane0 * c.max_pages + (pos >> c.page_shift)];
+        if (pos < ahead.hi) page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 127) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 128)];
     };
     auto issue = [&](int stage) {
         const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
@@ -310,11 +311,12 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 }
                 page = 0;
             }
-            const char* src = c.pages + (((size_t)page * c.heads + ahead.head) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES + hl * 16;
-            const uint32_t dst = ring0 + (stage * 2 + half) * Ti::BYTES + hl * 16;
+            const char* src = c.pages + (((size_t)page * c.heads + ASX_AT(ahead.head, c.heads, 129)) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES + hl * 16;
+            const uint32_t dst = ring0 + ASX_AT((stage * 2 + half) * Ti::BYTES, (2 * AT_STAGES - 1) * Ti::BYTES + 1, 130) + hl * 16;
 #pragma unroll
             for (int i = 0; i < (Ti::BYTES / 16 + 15) / 16; ++i)
-                if (i * 16 + 16 <= Ti::BYTES / 16 || i * 16 + hl < Ti::BYTES / 16) cp_async16(dst + i * 256, src + i * 256);
+                if (i * 16 + 16 <= Ti::BYTES / 16 || i * 16 + hl < Ti::BYTES / 16)
+                    cp_async16(dst + ASX_AT(i * 256 + hl * 16, Ti::BYTES - 15, 131) - hl * 16, src + i * 256);
         }
         if (--to_issue > 0) {
             ahead.step(a, p);
@@ -396,7 +398,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
         cp_commit();
         const int pos = cu.lo + (SOLO ? cu.u : cu.u * AT_W + w) * 32;
         if (pos < cu.hi) {
-            const uint32_t st = ring0 + stage * 2 * Ti::BYTES;
+            const uint32_t st = ring0 + ASX_AT(stage, AT_STAGES, 132) * 2 * Ti::BYTES;
             const bool two = pos + 16 < cu.hi;              // (the second tile may lie behind the last token: nothing was copied)
             // ---- S^T = K q^T ----
             const int t0 = 4 * (r >> 1) + (r & 1);      // the thread's tokens of a tile: t0 and t0 + 2
@@ -409,15 +411,15 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 for (int i = 0; i < 2; ++i) {
                     const int t = t0 + 2 * i;
                     if (D == 128) {
-                        const uint4 v = lds<uint4>(sb + Ti::K + t * (D / 2) + cc * 16);
+                        const uint4 v = lds<uint4>(sb + Ti::K + ASX_AT(t * (D / 2) + cc * 16, 8 * D - 15, 133));
                         kw[i][0] = v.x; kw[i][1] = v.y; kw[i][D / 32 - 2] = v.z; kw[i][D / 32 - 1] = v.w;
-                        const uint32_t s2 = e4m3_f16x2(lds<unsigned short>(sb + Ti::KS + t * Ti::NB + 2 * cc));
+                        const uint32_t s2 = e4m3_f16x2(lds<unsigned short>(sb + Ti::KS + ASX_AT(t * Ti::NB + 2 * cc, D - 1, 134)));
                         ks[i][0] = __byte_perm(s2, s2, 0x1010);
                         ks[i][D / 64 - 1] = __byte_perm(s2, s2, 0x3232);
                     } else {
-                        const uint2 v = lds<uint2>(sb + Ti::K + t * (D / 2) + cc * 8);
+                        const uint2 v = lds<uint2>(sb + Ti::K + ASX_AT(t * (D / 2) + cc * 8, 8 * D - 7, 135));
                         kw[i][0] = v.x; kw[i][1] = v.y;
-                        const uint32_t s2 = e4m3_f16x2(lds<unsigned char>(sb + Ti::KS + t * Ti::NB + cc));
+                        const uint32_t s2 = e4m3_f16x2(lds<unsigned char>(sb + Ti::KS + ASX_AT(t * Ti::NB + cc, D, 136)));
                         ks[i][0] = __byte_perm(s2, s2, 0x1010);
                     }
                 }
@@ -513,7 +515,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 if (b == 1 && !two) break;
                 const uint32_t sb = st + b * Ti::BYTES;
                 uint32_t vw[4][D / 64];             // tokens 4 cc .. 4 cc + 3, the thread's D / 8 dimensions
-                const uint32_t vb = sb + Ti::V + (D == 128 ? r : r >> 1) * 128 + cc * 32;
+                const uint32_t vb = sb + Ti::V + ASX_AT((D == 128 ? r : r >> 1) * 128 + cc * 32, 8 * D - 31, 137);
                 const bool odd = r & 1;
                 {
                     // (odd r reads its two halves in the other order: no two threads of a phase meet in a bank)
@@ -528,7 +530,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                         vw[2][0] = odd ? v1.y : v1.x; vw[3][0] = odd ? v1.w : v1.z;
                     }
                 }
-                uint32_t vs4 = lds<uint32_t>(sb + Ti::VS + (D == 128 ? r : r >> 1) * 16 + cc * 4);
+                uint32_t vs4 = lds<uint32_t>(sb + Ti::VS + ASX_AT((D == 128 ? r : r >> 1) * 16 + cc * 4, D - 3, 138));
                 if (pos + 32 > cu.hi) {             // tokens behind the last one: whatever the page holds there counts as zero
                     const int have = cu.hi - pos - 16 * b - 4 * cc;
                     vs4 &= have >= 4 ? 0xFFFFFFFFu : have <= 0 ? 0u : (1u << (8 * have)) - 1;
@@ -575,13 +577,13 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
         if (item_ends || left == 1) {
             const int head = cu.head, mine = SOLO ? blockIdx.x * AT_W + w : blockIdx.x;
             const bool whole = item_ends && seg_u0 == 0;
-            const size_t item = (size_t)cu.entry * c.heads + cu.head;
+            const size_t item = ASX_AT((size_t)cu.entry * c.heads + cu.head, (long long)p.n * p.row_tiles * c.heads, 139);
             if ((SOLO ? lane : tid) == 0) {
                 if (seg_u0 == 0) p.first_run[item] = mine;
                 if (item_ends) p.last_run[item] = mine;
             }
             float* part = nullptr;
-            if (!whole) part = p.part_run + (size_t)(2 * mine + (seg_u0 == 0)) * state_floats<D>(8 * NT);
+            if (!whole) part = p.part_run + (size_t)ASX_AT(2 * mine + (seg_u0 == 0), 2 * p.runs, 140) * state_floats<D>(8 * NT);
             else if (p.part_item) part = p.part_item + item * state_floats<D>(8 * NT);
             const float vg = c.v_scale ? c.v_scale[head] : 1.f;
             if constexpr (SOLO) {
@@ -596,7 +598,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                         for (int d = 4; d < 32; d <<= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, d);
                         const int rw = n * 8 + 2 * cc + h, row = cu.row0 + rw;
                         if (part) {
-                            float* at = part + rw * D + r * PER;
+                            float* at = part + ASX_AT(rw * D + r * PER, 8 * NT * D - PER + 1, 141);
 #pragma unroll
                             for (int i = 0; i < KS; i += 2) *reinterpret_cast<float4*>(at + 2 * i) = make_float4(o[n][i][h], o[n][i][2 + h], o[n][i + 1][h], o[n][i + 1][2 + h]);
                             if (r == 0) { part[8 * NT * D + rw] = m[n][h]; part[8 * NT * (D + 1) + rw] = L; }
@@ -634,7 +636,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     if (r == 0) { sm.join_m[w][2 * cc + h] = m[n][h]; sm.join_l[w][2 * cc + h] = sum; }
 #pragma unroll
                     for (int i = 0; i < KS; ++i)
-                        *reinterpret_cast<float2*>(&sm.join[w][2 * cc + h][r * (D / 8 + 2) + 2 * i]) = make_float2(o[n][i][h], o[n][i][2 + h]);
+                        *reinterpret_cast<float2*>(&sm.join[w][2 * cc + h][ASX_AT(r * (D / 8 + 2) + 2 * i, D + 19, 142)]) = make_float2(o[n][i][h], o[n][i][2 + h]);
                 }
                 __syncthreads();
                 constexpr int PER = D / 16;         // dimensions of a thread; 16 threads a row
@@ -651,11 +653,11 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 for (int e = 0; e < PER; ++e) {
                     acc[e] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < AT_W; ++i) acc[e] += f[i] * sm.join[i][rw][(d0 / (D / 8)) * (D / 8 + 2) + d0 % (D / 8) + e];
+                    for (int i = 0; i < AT_W; ++i) acc[e] += f[i] * sm.join[i][ASX_AT(rw, 8, 143)][ASX_AT((d0 / (D / 8)) * (D / 8 + 2) + d0 % (D / 8) + e, D + 20, 144)];
                 }
                 const int row = cu.row0 + n * 8 + rw;
                 if (part) {
-                    float* at = part + (n * 8 + rw) * D + d0;
+                    float* at = part + ASX_AT((n * 8 + rw) * D + d0, 8 * NT * D - PER + 1, 145);
 #pragma unroll
                     for (int e = 0; e < PER; e += 4) *reinterpret_cast<float4*>(at + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
                     if (d0 == 0) { part[8 * NT * D + n * 8 + rw] = M; part[8 * NT * (D + 1) + n * 8 + rw] = L; }
@@ -687,11 +689,11 @@ __device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int 
     if (c0 < 0 || c1 >= p.runs) return;                 // (a pass whose waits ran out may not have noted its runs)
 #pragma unroll 2
     for (int k = c0; k <= c1; ++k) {
-        const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_run + (size_t)(2 * k + (k == c0)) * state_floats<D>(p.tile_rows);
+        const float* s = c0 == c1 ? p.part_item + item * state_floats<D>(p.tile_rows) : p.part_run + (size_t)ASX_AT(2 * k + (k == c0), 2 * p.runs, 146) * state_floats<D>(p.tile_rows);
         const float m2 = s[p.tile_rows * D + rw], l2 = s[p.tile_rows * (D + 1) + rw];
         float x[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) x[e] = s[rw * D + d0 + e];
+        for (int e = 0; e < PER; ++e) x[e] = s[ASX_AT(rw * D + d0 + e, p.tile_rows * D, 147)];
         const float top = fmaxf(M, m2);
         const float f = M == -INFINITY ? 0.f : ex2(M - top), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - top);
         L = L * f + l2 * f2;
@@ -706,7 +708,7 @@ __device__ __forceinline__ void join_shared(const AttendArgs& a, const PassArgs&
     const int gr = pre.by_N.div(lane);
     if (pre.begin[gr] == 0) return;
     const int prow = (lane - gr * pre.N) * rows + row, pt = pre.by_tile_rows.div(prow);
-    const size_t item = ((size_t)gr * pre.row_tiles + pt) * a.c.heads + head;
+    const size_t item = ASX_AT(((size_t)gr * pre.row_tiles + pt) * a.c.heads + head, (long long)pre.n * pre.row_tiles * a.c.heads, 148);
     join_states<D>(pre, item, pre.first_run[item], pre.last_run[item], prow - pt * pre.tile_rows, d0, M, L, acc);
 }
 

@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             const float vg = c.v_scale ? c.v_scale[cu.head] : 1.f;
             ok = wait_warp(sm.q_full[q_buf(item)], q_use(item) & 1);
             if (!ok) break;
-            float k2 = sm.up[item & 1][(DUAL ? 128 * s : 0) + r] * fabsf(a.scale) * (c.k_scale ? c.k_scale[cu.head] : 1.f) * 1.44269504088896f;
+            float k2 = sm.up[item & 1][ASX_AT((DUAL ? 128 * s : 0) + r, 256, 151)] * fabsf(a.scale) * (c.k_scale ? c.k_scale[cu.head] : 1.f) * 1.44269504088896f;
             k2 = fmaxf(k2, 1e-37f);         // (a scale of 0: -inf x k2 stays -inf)
             __syncwarp();
             if (lane == 0) tc_bar_arrive(bar(sm.q_empty[q_buf(item)]));          // (so that no group falls two items behind the filling)
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
 #pragma unroll 1
                 for (int ch = 0; ch < PIECE / 32; ++ch) {
                     uint32_t v[32];
-                    tc_ld32(sh + 32 * ch, v);
+                    tc_ld32(sh + ASX_AT(128 * s + PIECE * hf + 32 * ch, 225, 152) - (128 * s + PIECE * hf), v);
                     tc_wait_ld();
                     if (cut) {
                         const int have = left - 32 * ch;
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     }
                     const float2 total = unpair(add2(sum[0], sum[1]));
                     l += total.x + total.y;
-                    tc_st16(sh + 16 * ch, pk);
+                    tc_st16(sh + ASX_AT(16 * ch, PIECE / 2 - 15, 157), pk);
                 }
                 if (!ok) break;
                 first = false;
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             if (!ok) break;
             // ---- the end of an item or of the run ----
             if (!DUAL) {
-                sm.ml[item & 1][s][0][r] = m;
+                sm.ml[item & 1][ASX_AT(s, 2, 158)][0][r] = m;
                 sm.ml[item & 1][s][1][r] = l;
                 __syncwarp();
                 if (lane == 0) tc_bar_arrive(bar(sm.ml_full));
@@ -321,13 +321,13 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             if (!ok) break;
             tc_fence_after();
             const bool whole = cu.u == 0 && tiles == cu.nu;
-            const size_t at_item = (size_t)cu.entry * c.heads + cu.head;
+            const size_t at_item = ASX_AT((size_t)cu.entry * c.heads + cu.head, (long long)p.n * p.row_tiles * c.heads, 153);
             if (tid == TC_NT - 1) {
                 if (cu.u == 0) p.first_run[at_item] = blockIdx.x;
                 if (cu.u + tiles == cu.nu) p.last_run[at_item] = blockIdx.x;
             }
             float* part = nullptr;
-            if (!whole) part = p.part_run + (size_t)(2 * blockIdx.x + (cu.u == 0)) * state_floats<D>(p.tile_rows);
+            if (!whole) part = p.part_run + (size_t)ASX_AT(2 * blockIdx.x + (cu.u == 0), 2 * TC_MAX_CTAS, 154) * state_floats<D>(p.tile_rows);
             else if (p.part_item) part = p.part_item + at_item * state_floats<D>(p.tile_rows);
             // DUAL: a thread writes its row; else the two groups' states of a row join, and each group writes half of it
             float M = m, L = l, f0 = 1.f, f1 = 0.f;
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             const float inv = L == 0.f ? 0.f : vg / L;
 #pragma unroll 1
             for (int ch = 0; ch < (DUAL ? D / 32 : D / 64); ++ch) {
-                const int col = (DUAL ? 0 : s * (D / 2)) + 32 * ch;
+                const int col = ASX_AT((DUAL ? 0 : s * (D / 2)) + 32 * ch, D - 31, 155);
                 uint32_t v[32], u[32];
                 tc_ld32((DUAL ? ot : o_t + mine) + col, v);
                 if (!DUAL) tc_ld32(o_t + 128 + mine + col, u);
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     else if (m == -INFINITY) y[e] = 0.f;
                 }
                 if (part) {
-                    float* at = part + (size_t)tr * D + col;
+                    float* at = part + (size_t)ASX_AT(tr, p.tile_rows, 156) * D + col;
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(at + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
                 } else if (row < p.rows) {
@@ -436,8 +436,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                 if (looked < run) {
                     const int pos = ahead.lo + ahead.u * TC_KV + r;
                     if (pos < ahead.hi) {
-                        page = c.table[(size_t)ahead.lane0 * c.max_pages + (pos >> c.page_shift)];
-                        next_base = c.pages + ((size_t)ahead.head * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
+                        page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 159) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 160)];
+                        next_base = c.pages + ((size_t)ASX_AT(ahead.head, c.heads, 161) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
                         next_lane = ahead.lane0;
                         next_real = true;
                     }
@@ -472,8 +472,9 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     {
                         constexpr int h = keys ? 0 : 1;             // (the values' group takes the second row tile)
                         const int row = cu.row0 + 128 * h + r;
-                        const uint16_t* from = reinterpret_cast<const uint16_t*>(query_row<AS_BF16, D>(a, cu.lane0, cu.head, row));
-                        const bool there = row < p.rows, wide = (reinterpret_cast<uintptr_t>(from) & 15) == 0;
+                        const bool there = row < p.rows;
+                        const uint16_t* from = there ? reinterpret_cast<const uint16_t*>(query_row<AS_BF16, D>(a, cu.lane0, cu.head, row)) : nullptr;
+                        const bool wide = (reinterpret_cast<uintptr_t>(from) & 15) == 0;
                         uint32_t top = 0;                               // largest magnitude's bits
                         // (twice over the row, 4 pieces of 8 elements at a time: code that runs once an item is fetched anew each
                         // time, so that a short loop is faster than straight code)
@@ -489,7 +490,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         int ex = (int)(top >> 7) - 127;
                         ex = ex > 126 ? 126 : ex < -126 ? -126 : ex;
                         const float down = __uint_as_float((uint32_t)(127 - ex) << 23 | (a.scale < 0.f ? 0x80000000u : 0u));
-                        sm.up[item & 1][128 * h + r] = __uint_as_float((uint32_t)(127 + ex) << 23);
+                        sm.up[item & 1][ASX_AT(128 * h + r, 256, 162)] = __uint_as_float((uint32_t)(127 + ex) << 23);
                         const uint32_t to_q = q_s + (DUAL ? h : q_buf(item)) * MAT;
                         auto both = [&](uint32_t z) { return pack_f16(__uint_as_float(z << 16) * down, __uint_as_float(z & 0xFFFF0000u) * down); };
 #pragma unroll 1
@@ -498,7 +499,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                             tc_read_row(from + 8 * i, there, wide, q);
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                put(to_q + (i / 8) * BLK + tc_at(r, (i & 4) + e), make_uint4(both(q[e].x), both(q[e].y), both(q[e].z), both(q[e].w)));
+                                put(q_s + ASX_AT(to_q - q_s + (i / 8) * BLK + tc_at(r, (i & 4) + e), 2 * MAT - 15, 163), make_uint4(both(q[e].x), both(q[e].y), both(q[e].z), both(q[e].w)));
                         }
                     }
                     filled(bar(sm.q_full[q_buf(item)]));
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     if (!ok) break;
                     // piece i of a token's codes lies TC_KV * 16 bytes behind piece i - 1: threads side by side, 16 bytes each
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) put(own + i * (TC_KV * 16), code[i]);
+                    for (int i = 0; i < D / 32; ++i) put(raw_s + ASX_AT(own - raw_s + i * (TC_KV * 16), TC_KV * D - 15, 164), code[i]);
                     if constexpr (!keys) {
                         scale.x = byte[0] | byte[1] << 8 | byte[2] << 16 | byte[3] << 24;
                         if constexpr (D == 128) scale.y = byte[KSTEPS - 4] | byte[KSTEPS - 3] << 8 | byte[KSTEPS - 2] << 16 | byte[KSTEPS - 1] << 24;
@@ -528,10 +529,10 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                     load();
 #pragma unroll 1
                     for (int i = 0; i < D / 32; ++i) {
-                        const uint4 q = lds<uint4>(own + i * (TC_KV * 16));
+                        const uint4 q = lds<uint4>(raw_s + ASX_AT(own - raw_s + i * (TC_KV * 16), TC_KV * D - 15, 165));
                         const uint32_t two = e4m3_f16x2(((D == 128 && i >= 2 ? sc_hi : sc_lo) >> (16 * (i & 1))) & 0xFFFFu);
                         const uint32_t sa = __byte_perm(two, two, 0x1010), sb = __byte_perm(two, two, 0x3232);
-                        const uint32_t at = to + b * MAT + (i >> 1) * BLK;
+                        const uint32_t at = (keys ? k_s : v_s) + ASX_AT(to - (keys ? k_s : v_s) + b * MAT + (i >> 1) * BLK, 2 * MAT - 127, 166);
                         const int cx = (4 * (i & 1)) ^ (r & 7);
                         put(at + ((cx ^ 0) << 4), widen(q.x, sa));
                         put(at + ((cx ^ 1) << 4), widen(q.y, sa));

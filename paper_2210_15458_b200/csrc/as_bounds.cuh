@@ -1,5 +1,7 @@
 // Checked builds (-DAS_BOUNDS_CHECK): every index into a ring stage, a hit or candidate list, a
-// rank array, a histogram, a chunk array, the mass table or a row buffer goes through ASX_AT.  An
+// rank array, a histogram, a chunk array, the mass table or a row buffer goes through ASX_AT; of the cache,
+// attention and page kernels the places in tiles, tables, rings, shared matrices, TMEM columns, joins, states
+// in scratch, query and output rows, page lists and page numbers that were computed.  An
 // index outside [0, n) is recorded (the count of failures and the first one's site, index and
 // bound) and replaced by 0, so that the access stays in bounds: nothing traps, and the host reads
 // the record after the launch.  In ordinary builds ASX_AT(i, n, site) is just i.

@@ -15,10 +15,10 @@ namespace asx {
 template <int D> struct Tile4 {
     static constexpr int NB = D / 16;               // blocks of 16 dimensions, one scale each
     static constexpr int K = 0, V = 8 * D, KS = 16 * D, VS = 17 * D, BYTES = 18 * D;
-    __device__ static int k_code(int t, int b) { return K + t * (D / 2) + b * 8; }
-    __device__ static int v_code(int t, int b) { return V + b * 128 + t * 8; }
-    __device__ static int k_scale(int t, int b) { return KS + t * NB + b; }
-    __device__ static int v_scale(int t, int b) { return VS + b * 16 + t; }
+    __device__ static int k_code(int t, int b) { return K + ASX_AT(t * (D / 2) + b * 8, 8 * D - 7, 101); }
+    __device__ static int v_code(int t, int b) { return V + ASX_AT(b * 128 + t * 8, 8 * D - 7, 102); }
+    __device__ static int k_scale(int t, int b) { return KS + ASX_AT(t * NB + b, D, 103); }
+    __device__ static int v_scale(int t, int b) { return VS + ASX_AT(b * 16 + t, D, 104); }
 };
 
 // n / d for n < 2^31 by a multiplication (Granlund and Montgomery's round-up method)
@@ -197,14 +197,14 @@ __device__ __forceinline__ void tiles_of(const CacheArgs& c, const Block& at, ch
     for (int u = 0; u < U; ++u) {
         const int tok = at.tok + 16 * u, p = p0 + 16 * u;
         real[u] = len_ok && tok >= 0 && tok < c.T && p >= 0;
-        page[u] = real[u] ? c.table[(size_t)at.lane * c.max_pages + (p >> c.page_shift)] : 0;
+        page[u] = real[u] ? c.table[(size_t)ASX_AT(at.lane, c.lanes, 105) * c.max_pages + ASX_AT(p >> c.page_shift, c.max_pages, 106)] : 0;
     }
     bool bad = !len_ok;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const bool in = page[u] >= 0 && page[u] < c.n_pages;
         bad |= !in;
-        tile[u] = real[u] && in ? c.pages + (((size_t)page[u] * c.heads + at.head) * (mask + 1 >> 4) + (((p0 + 16 * u) & mask) >> 4)) * Tile4<D>::BYTES : nullptr;
+        tile[u] = real[u] && in ? c.pages + (((size_t)page[u] * c.heads + ASX_AT(at.head, c.heads, 107)) * (mask + 1 >> 4) + (((p0 + 16 * u) & mask) >> 4)) * Tile4<D>::BYTES : nullptr;
     }
     if (bad) flag_lane(c.lane_status, at.lane, AS_ERR_INVALID_ARG);
 }
@@ -222,7 +222,7 @@ append_kernel(const __grid_constant__ CacheArgs c, const typename Io<DT>::type* 
         char* tile[U];
         typename Io<DT>::raw16 raw[U];
         const long long ld = at.is_v ? v_ld : k_ld;
-        const typename Io<DT>::type* src = (at.is_v ? v : k) + ((long long)at.lane * c.T + at.tok) * ld + at.head * D + at.b * 16;
+        const typename Io<DT>::type* src = (at.is_v ? v : k) + ((long long)ASX_AT(at.lane, c.lanes, 108) * c.T + at.tok) * ld + ASX_AT(at.head, c.heads, 109) * D + ASX_AT(at.b, D / 16, 110) * 16;
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (at.tok + 16 * u >= 0 && at.tok + 16 * u < c.T) raw[u] = Io<DT>::load16(src + 16 * u * ld, VEC);
@@ -301,7 +301,7 @@ load_kernel(const __grid_constant__ CacheArgs c, typename Io<DT>::type* __restri
                     x[8 * i + 2 * e + 1] = f.y * s * g;
                 }
             }
-            Io<DT>::write16((at.is_v ? v : k) + ((size_t)at.lane * c.T + tok) * c.heads * D + at.head * D + at.b * 16, x);
+            Io<DT>::write16((at.is_v ? v : k) + ((size_t)ASX_AT(at.lane, c.lanes, 111) * c.T + tok) * c.heads * D + ASX_AT(at.head, c.heads, 112) * D + ASX_AT(at.b, D / 16, 113) * 16, x);
         }
     };
     if constexpr (TILES) each_block_by_tiles<D>(c, read);

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(PG_NT) fork_table_kernel(const ForkArgs a, con
                 for (int m = tid; m < pages_of(len, a.page_size); m += PG_NT) {
                     // a part page stays with one child, if there is any
                     const int change = (m + 1) * (long long)a.page_size > len ? min(c, 1) - 1 : c - 1;
-                    if (change) atomicAdd(&a.ref_out[row[m]], change);
+                    if (change) atomicAdd(&a.ref_out[ASX_AT(row[ASX_AT(m, a.max_pages, 201)], a.n_pages, 202)], change);
                 }
         }
         if (j < a.lanes_out) {
@@ -126,8 +126,8 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sum, int& total) {
 }
 
 // The first `want` pages i in [lo, hi) with (ref[i] > 0) == used, in order, into list; returns how many there are
-// (at most want).
-__device__ int collect(const int* ref, int lo, int hi, bool used, int want, int* list, int* warp_sum) {
+// (at most want).  list has room for n_pages.
+__device__ int collect(const int* ref, int lo, int hi, bool used, int want, int* list, int n_pages, int* warp_sum) {
     constexpr int PER = 16;
     int got = 0;
     for (int base = lo; base < hi && got < want; base += PL_NT * PER) {
@@ -135,11 +135,11 @@ __device__ int collect(const int* ref, int lo, int hi, bool used, int want, int*
         unsigned bits = 0;
 #pragma unroll
         for (int e = 0; e < PER; ++e)
-            if (at + e < hi && (ref[at + e] > 0) == used) bits |= 1u << e;
+            if (at + e < hi && (ref[ASX_AT(at + e, n_pages, 203)] > 0) == used) bits |= 1u << e;
         int total;
         int r = got + block_scan(__popc(bits), warp_sum, total) - __popc(bits);
         for (; bits; bits &= bits - 1, ++r)
-            if (r < want) list[r] = at + __ffs(bits) - 1;
+            if (r < want) list[ASX_AT(r, n_pages, 204)] = at + __ffs(bits) - 1;
         got += total;
     }
     __syncthreads();
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(PL_NT) fork_plan_kernel(const ForkArgs a, cons
         if (i < a.lanes_out) w.off[i] = need ? r : -1;
         wanted += total;
     }
-    const int got = collect(a.ref_out, 0, a.n_pages, false, wanted, w.free_page, warp_sum);
+    const int got = collect(a.ref_out, 0, a.n_pages, false, wanted, w.free_page, a.n_pages, warp_sum);
     for (int i = tid; i < a.lanes_out; i += PL_NT) {
         const int p = a.parent[i], r = w.off[i];
         const bool known = p >= 0 && p < a.lanes_in;
@@ -175,11 +175,11 @@ __global__ void __launch_bounds__(PL_NT) fork_plan_kernel(const ForkArgs a, cons
         int len = max(eff, 0);
         int status = (p < -1 || p >= a.lanes_in || eff < 0) ? AS_ERR_INVALID_ARG : AS_OK;
         if (r >= 0 && r < got) {
-            const int m = len / a.page_size, g = w.free_page[r];
-            w.src[r] = a.table[(size_t)p * a.max_pages + m];
-            w.dst[r] = g;
+            const int at = ASX_AT(r, a.n_pages, 205), m = ASX_AT(len / a.page_size, a.max_pages, 206), g = w.free_page[at];
+            w.src[at] = a.table[(size_t)p * a.max_pages + m];
+            w.dst[at] = g;
             a.table_out[(size_t)i * a.max_pages + m] = g;
-            a.ref_out[g] = 1;
+            a.ref_out[ASX_AT(g, a.n_pages, 207)] = 1;
         } else if (r >= 0) {
             len -= len % a.page_size;
             status = AS_ERR_NO_PAGES;
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(PL_NT) fork_plan_kernel(const ForkArgs a, cons
 // Copies pages src[r] to dst[r], r < *moves, of every plane.  Bound by HBM: 8 planes of about 256 pages of 72 KB in 27 to 47 us.
 __global__ void __launch_bounds__(CP_NT)
 copy_pages_kernel(const int* __restrict__ moves, const int* __restrict__ src, const int* __restrict__ dst, char* data, int planes,
-                  long long plane_stride, long long page_bytes) {
+                  long long plane_stride, long long page_bytes, int n_pages) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int per_page = (int)((page_bytes + CP_CHUNK - 1) / CP_CHUNK);
@@ -203,8 +203,8 @@ copy_pages_kernel(const int* __restrict__ moves, const int* __restrict__ src, co
         const long long rest = i / per_page;
         const int plane = (int)(rest % planes), r = (int)(rest / planes);
         char* at = data + plane * plane_stride;
-        const uint4* from = reinterpret_cast<const uint4*>(at + src[r] * page_bytes);
-        uint4* to = reinterpret_cast<uint4*>(at + dst[r] * page_bytes);
+        const uint4* from = reinterpret_cast<const uint4*>(at + ASX_AT(src[ASX_AT(r, n_pages, 208)], n_pages, 209) * page_bytes);
+        uint4* to = reinterpret_cast<uint4*>(at + ASX_AT(dst[r], n_pages, 210) * page_bytes);
         const long long vecs = page_bytes / 16, v0 = (long long)c * (CP_CHUNK / 16) + threadIdx.x;
         uint4 q[4];
 #pragma unroll
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(PL_NT) grow_kernel(const GrowArgs a, const Pag
         if (i < a.lanes) w.off[i] = r;
         wanted = min(wanted + total, a.n_pages + 1);
     }
-    const int got = collect(a.ref, 0, a.n_pages, false, min(wanted, a.n_pages), w.free_page, warp_sum);
+    const int got = collect(a.ref, 0, a.n_pages, false, min(wanted, a.n_pages), w.free_page, a.n_pages, warp_sum);
     for (int i = tid; i < a.lanes; i += PL_NT) {
         const int len = a.len[i], add = a.add[i];
         int status = AS_OK;
@@ -256,9 +256,9 @@ __global__ void __launch_bounds__(PL_NT) grow_kernel(const GrowArgs a, const Pag
                 status = AS_ERR_NO_PAGES;
             } else {
                 for (int m = 0; m < need; ++m) {
-                    const int g = w.free_page[r + m];
-                    a.table[(size_t)i * a.max_pages + have + m] = g;
-                    a.ref[g] = 1;
+                    const int g = w.free_page[ASX_AT(r + m, a.n_pages, 211)];
+                    a.table[(size_t)i * a.max_pages + ASX_AT(have + m, a.max_pages, 212)] = g;
+                    a.ref[ASX_AT(g, a.n_pages, 213)] = 1;
                 }
                 a.len[i] = len + add;
             }
@@ -283,11 +283,11 @@ __global__ void __launch_bounds__(PL_NT) compact_plan_kernel(const int* ref, int
     }
     int used;
     block_scan(n, warp_sum, used);
-    const int holes = collect(ref, 0, used, false, n_pages, w.dst, warp_sum);
-    const int late = collect(ref, used, n_pages, true, n_pages, w.src, warp_sum);
+    const int holes = collect(ref, 0, used, false, n_pages, w.dst, n_pages, warp_sum);
+    const int late = collect(ref, used, n_pages, true, n_pages, w.src, n_pages, warp_sum);
     const int moves = min(holes, late);                 // (they are equal)
     for (int r = tid; r < moves; r += PL_NT) {
-        const int s = w.src[r], d = w.dst[r];
+        const int s = ASX_AT(w.src[r], n_pages, 214), d = ASX_AT(w.dst[r], n_pages, 215);
         w.free_page[s] = d;                             // where page s went
         ref_out[d] = ref[s];
         ref_out[s] = 0;
@@ -302,7 +302,7 @@ compact_table_kernel(const int* table, int* table_out, long long n, int n_pages,
     const int u = *used;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
         const int g = table[i];
-        table_out[i] = g >= u && g < n_pages ? w.free_page[g] : g;
+        table_out[i] = g >= u && g < n_pages ? w.free_page[ASX_AT(g, n_pages, 216)] : g;
     }
 }
 
@@ -333,9 +333,9 @@ static int check_shape(int lanes, int max_pages, int page_size, int n_pages) {
     return AS_OK;
 }
 
-static cudaError_t launch_copy(const PageWork& w, void* data, int planes, long long plane_stride, long long page_bytes, int sms, cudaStream_t st) {
+static cudaError_t launch_copy(const PageWork& w, void* data, int planes, long long plane_stride, long long page_bytes, int n_pages, int sms, cudaStream_t st) {
     return launch_after(copy_pages_kernel, 8 * sms, CP_NT, 0, st, (const int*)w.moves, (const int*)w.src, (const int*)w.dst, static_cast<char*>(data), planes, plane_stride,
-                        page_bytes);
+                        page_bytes, n_pages);
 }
 
 static unsigned lanes_grid(int n, int sms) { return (unsigned)(n < 16 * sms ? (n > 0 ? n : 1) : 16 * sms); }
@@ -374,7 +374,7 @@ int as_pages_fork(const int32_t* d_parent, int lanes_in, int lanes_out, int max_
     cudaError_t e = launch_after(fork_count_kernel, lanes_grid(lanes_in, di->sms), PG_NT, 0, st, a, w);
     if (e == cudaSuccess) e = launch_after(fork_table_kernel, lanes_grid(lanes_in > lanes_out ? lanes_in : lanes_out, di->sms), PG_NT, 0, st, a, w);
     if (e == cudaSuccess) e = launch_after(fork_plan_kernel, 1, PL_NT, 0, st, a, w);
-    if (e == cudaSuccess && d_data && planes > 0) e = launch_copy(w, d_data, planes, plane_stride, page_bytes, di->sms, st);
+    if (e == cudaSuccess && d_data && planes > 0) e = launch_copy(w, d_data, planes, plane_stride, page_bytes, n_pages, di->sms, st);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "page fork kernel launch");
 }
 
@@ -411,7 +411,7 @@ int as_pages_compact(int lanes, int max_pages, int n_pages, const int32_t* d_tab
     const long long n = (long long)lanes * max_pages, blocks = (n + 255) / 256;
     if (e == cudaSuccess && n > 0)
         e = launch_after(compact_table_kernel, (unsigned)(blocks < 16 * di->sms ? blocks : 16 * di->sms), 256, 0, st, d_table, d_table_out, n, n_pages, d_used, w);
-    if (e == cudaSuccess && d_data && planes > 0) e = launch_copy(w, d_data, planes, plane_stride, page_bytes, di->sms, st);
+    if (e == cudaSuccess && d_data && planes > 0) e = launch_copy(w, d_data, planes, plane_stride, page_bytes, n_pages, di->sms, st);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "page compact kernel launch");
 }
 

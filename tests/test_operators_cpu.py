@@ -173,6 +173,18 @@ print("fine")
     assert r.returncode == 0 and r.stdout.strip() == "fine", (r.returncode, r.stderr[-500:])
 
 
+def test_every_unit_that_keeps_a_record_of_indices_checks_some():
+    """A translation unit with a reader of out-of-range indices has indices that are checked, in its own file or its headers."""
+    import re
+    from paper_2210_15458_b200 import _build
+    for name in _build.SOURCES:
+        files = [f for f in _build._depends(os.path.join(_build.CSRC, name)) if not f.endswith("as_bounds.cuh")]
+        text = "".join(open(f).read() for f in files)
+        assert "ASX_BOUNDS_READER(" in text
+        sites = re.findall(r"ASX_AT\(", text)
+        assert len(sites) >= 3, (name, len(sites))
+
+
 def test_a_scale_that_is_infinite_in_32_bits_is_refused(B):
     c = _cache(B)
     for scale in (1e39, -1e300, 3.5e38):
