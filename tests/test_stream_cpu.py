@@ -77,3 +77,16 @@ def test_scratch_and_outputs_belong_to_the_stream_of_the_launch(B, name):
         with Allocations(current) as a:
             call(stream=same)
         assert a.seen == [None] * n
+
+
+def test_the_current_stream_by_public_names_alone(monkeypatch):
+    """A torch without the two unlisted look-ups: the public one gives the same handle."""
+    import importlib
+    from paper_2210_15458_b200 import binding
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    monkeypatch.delattr(torch._C, "_cuda_getDevice")
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: type("S", (), {"cuda_stream": 4242})())
+    spec = importlib.util.spec_from_file_location("paper_2210_15458_b200.binding_again", binding.__file__)
+    again = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(again)
+    assert again._stream(None) == 4242 and again._current_stream() == 4242
