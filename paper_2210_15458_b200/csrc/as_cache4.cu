@@ -56,28 +56,17 @@ static unsigned grid_of(long long threads, int nt) {
     return (unsigned)(n < (1 << 14) ? n : (1 << 14));       // (the kernels loop)
 }
 
-// Blocks by tiles where a lane has many tokens, else by rows: a tile that the call's tokens only touch, and a set of tiles
-// that is not full, leave threads without work.  Store and load, by tiles / by rows, us: 512 lanes x 16 tokens 52.9 / 33.6,
-// 128 x 64 40.6 / 32.4, 64 x 256 56.9 / 55.0, 16 x 1024 53.5 / 53.8, 8 x 4096 92.5 / 94.3.
-static bool by_tiles(const CacheArgs& a) { return a.T >= 512 && (long long)a.lanes * ((a.T + 15) / 16 + 1) * a.heads < (1LL << 31); }
-static unsigned block_grid(const CacheArgs& a, int D, bool tiles) {
-    const long long tokens = tiles ? (long long)a.lanes * (((a.T + 15) / 16 + C4_U) / C4_U) * 16 : (long long)a.lanes * a.T;
-    return grid_of(tokens * 2 * a.heads * (D / 16), C4_NT);
-}
+static unsigned block_grid(const CacheArgs& a, int D) { return grid_of((long long)a.lanes * a.T * 2 * a.heads * (D / 16), C4_NT); }
 template <int DT, int D>
 static void launch_append(const CacheArgs& a, const void* k, long long k_ld, const void* v, long long v_ld, bool vec, cudaStream_t st) {
     using E = typename Io<DT>::type;
-    const bool tiles = by_tiles(a);
-    auto kern = tiles ? (vec ? append_kernel<DT, D, true, true> : append_kernel<DT, D, true, false>)
-                      : (vec ? append_kernel<DT, D, false, true> : append_kernel<DT, D, false, false>);
-    kern<<<block_grid(a, D, tiles), C4_NT, 0, st>>>(a, static_cast<const E*>(k), k_ld, static_cast<const E*>(v), v_ld);
+    auto kern = vec ? append_kernel<DT, D, true> : append_kernel<DT, D, false>;
+    kern<<<block_grid(a, D), C4_NT, 0, st>>>(a, static_cast<const E*>(k), k_ld, static_cast<const E*>(v), v_ld);
 }
 template <int DT, int D>
 static void launch_load(const CacheArgs& a, void* k, void* v, cudaStream_t st) {
     using E = typename Io<DT>::type;
-    const bool tiles = by_tiles(a);
-    auto kern = tiles ? load_kernel<DT, D, true> : load_kernel<DT, D, false>;
-    kern<<<block_grid(a, D, tiles), C4_NT, 0, st>>>(a, static_cast<E*>(k), static_cast<E*>(v));
+    load_kernel<DT, D><<<block_grid(a, D), C4_NT, 0, st>>>(a, static_cast<E*>(k), static_cast<E*>(v));
 }
 
 // ---------------------------------------------------------------------------

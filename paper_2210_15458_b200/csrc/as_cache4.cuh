@@ -7,8 +7,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <type_traits>
-
 namespace asx {
 
 // A tile: 16 tokens of one head (see as_cache4 in the header).
@@ -126,20 +124,20 @@ __device__ __forceinline__ void flag_lane(int* lane_status, int lane, int code) 
     if (lane_status) atomicMin(&lane_status[lane], code);
 }
 
-// Storing and reading back work on blocks: 16 dimensions of one token, which are 8 bytes of codes and a scale.  A thread
-// has U of them at a time, 16 tokens apart, so that their loads are in flight together.
+// Storing and reading back work on blocks: 16 dimensions of one token, which are 8 bytes of codes and a scale.
 struct Block {
-    int lane, len, tok, head, b;                    // tok: the first token within the call (one outside 0 .. T - 1 is none)
+    int lane, len, tok, head, b;                    // tok: the token within the call
     bool is_v;
 };
-constexpr int C4_U = 4;
-
 constexpr int C4_NT = 256;
 
-// Few tokens a lane: blocks side by side in the caller's tensors run along the threads.  Tokens are rows
-// (at most 2^30), a row has 2 x heads x D / 16 blocks.
+// A thread to a block, blocks side by side in the caller's tensors side by side along the threads.  Tokens are rows (at most
+// 2^30), a row has 2 x heads x D / 16 blocks.  (A group of threads to a tile of 16 positions, four of them at a time, moves whole
+// sectors of the cache, but leaves threads without work where a call's tokens only touch a tile: 8 + 8 heads x 128, bf16, store +
+// load, by tiles / by rows, us: 512 lanes x 16 tokens 52.8 / 34.3, 64 x 256 57.5 / 52.5, 16 x 1024 53.6 / 50.4, 8 x 4096 95.5 / 93.5; in 32
+// bits 8 x 4096 149.5 / 136.6.)
 template <int D, class F>
-__device__ __forceinline__ void each_block_by_rows(const CacheArgs& c, F&& f) {
+__device__ __forceinline__ void each_block(const CacheArgs& c, F&& f) {
     constexpr int NB = D / 16;
     const unsigned per_row = 2 * c.heads * NB, rows = (unsigned)c.lanes * c.T;
     const unsigned step = gridDim.x * C4_NT, first = blockIdx.x * C4_NT + threadIdx.x;
@@ -156,156 +154,96 @@ __device__ __forceinline__ void each_block_by_rows(const CacheArgs& c, F&& f) {
         k.lane = c.by_T.div(row);
         k.tok = row - k.lane * c.T;
         k.len = c.len[k.lane];
-        f(k, std::integral_constant<int, 1>{});
+        f(k);
     }
 }
 
-// Many tokens a lane: a group of 2 x D threads takes a tile of 16 positions of one head, keys in the order of their
-// codes (blocks of a token side by side), values in the order of theirs (tokens of a block side by side): every 32-byte
-// sector of the caller's tensors and of the cache is moved once and whole.
-template <int D, class F>
-__device__ __forceinline__ void each_block_by_tiles(const CacheArgs& c, F&& f) {
-    constexpr int NB = D / 16, GROUP = 32 * NB;
-    const int groups = ((c.T + 15) / 16 + 1 + C4_U - 1) / C4_U;     // sets of U tiles that T positions can touch
-    const unsigned r = threadIdx.x % GROUP;
-    const unsigned n = (unsigned)c.lanes * groups * c.heads, step = gridDim.x * (C4_NT / GROUP);
-#pragma unroll 1
-    for (unsigned i = blockIdx.x * (C4_NT / GROUP) + threadIdx.x / GROUP; i < n; i += step) {
-        Block k;
-        const unsigned j = c.by_heads.div(i), lane = j / groups;
-        k.head = i - j * c.heads;
-        k.lane = lane;
-        k.is_v = r >= 16 * NB;
-        const unsigned q = r % (16 * NB);
-        const int t = k.is_v ? q % 16 : q / NB;
-        k.b = k.is_v ? q / 16 : q % NB;
-        k.len = c.len[lane];
-        const int start = k.len - c.T, tile0 = start >> 4;          // (the first position may lie below 0)
-        k.tok = (tile0 + (int)(j - lane * groups) * C4_U) * 16 + t - start;
-        f(k, std::integral_constant<int, C4_U>{});
-    }
-}
-
-// The tiles of a thread's U tokens: null for one that is outside the call, in front of the first position or in no page.
-template <int D, int U>
-__device__ __forceinline__ void tiles_of(const CacheArgs& c, const Block& at, char* (&tile)[U]) {
-    const int p0 = at.len - c.T + at.tok, mask = (1 << c.page_shift) - 1;
+// The tile of a token: null for one in front of the first position or in no page.
+template <int D>
+__device__ __forceinline__ char* tile_of(const CacheArgs& c, const Block& at) {
+    const int p = at.len - c.T + at.tok, mask = (1 << c.page_shift) - 1;
     const bool len_ok = at.len >= 0 && at.len <= ((long long)c.max_pages << c.page_shift);
-    int page[U];
-    bool real[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int tok = at.tok + 16 * u, p = p0 + 16 * u;
-        real[u] = len_ok && tok >= 0 && tok < c.T && p >= 0;
-        page[u] = real[u] ? c.table[(size_t)ASX_AT(at.lane, c.lanes, 105) * c.max_pages + ASX_AT(p >> c.page_shift, c.max_pages, 106)] : 0;
-    }
-    bool bad = !len_ok;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const bool in = page[u] >= 0 && page[u] < c.n_pages;
-        bad |= !in;
-        tile[u] = real[u] && in ? c.pages + (((size_t)page[u] * c.heads + ASX_AT(at.head, c.heads, 107)) * (mask + 1 >> 4) + (((p0 + 16 * u) & mask) >> 4)) * Tile4<D>::BYTES : nullptr;
-    }
-    if (bad) flag_lane(c.lane_status, at.lane, AS_ERR_INVALID_ARG);
+    const bool real = len_ok && p >= 0;
+    const int page = real ? c.table[(size_t)ASX_AT(at.lane, c.lanes, 105) * c.max_pages + ASX_AT(p >> c.page_shift, c.max_pages, 106)] : 0;
+    const bool in = page >= 0 && page < c.n_pages;
+    if (!len_ok || !in) flag_lane(c.lane_status, at.lane, AS_ERR_INVALID_ARG);
+    return real && in ? c.pages + (((size_t)page * c.heads + ASX_AT(at.head, c.heads, 107)) * (mask + 1 >> 4) + ((p & mask) >> 4)) * Tile4<D>::BYTES : nullptr;
 }
 
-// Store: a thread takes 16 neighbouring dimensions of a token (one scale), by tiles four tokens at a time so that their loads
-// are in flight together: code = nearest e2m1 of x / (head scale x scale), scale = e4m3 of the largest |x| / 6.  Bound
-// by loads in flight: 8 x 4096 tokens of 8 + 8 heads x 128 in 50 us (168 MB: 3.4 TB/s), one token each of 256 lanes in 4.5 us.
-template <int DT, int D, bool TILES, bool VEC>
+// Store: a thread takes 16 neighbouring dimensions of a token (one scale): code = nearest e2m1 of x / (head scale x scale), scale
+// = e4m3 of the largest |x| / 6.  Bound by loads in flight: 8 x 4096 tokens of 8 + 8 heads x 128 in 52 us (168 MB: 3.2 TB/s),
+// one token each of 256 lanes in 4.5 us.
+template <int DT, int D, bool VEC>
 __global__ void __launch_bounds__(C4_NT)
 append_kernel(const __grid_constant__ CacheArgs c, const typename Io<DT>::type* __restrict__ k, long long k_ld,
               const typename Io<DT>::type* __restrict__ v, long long v_ld) {
     using Ti = Tile4<D>;
-    auto store = [&](const Block& at, auto many) {
-        constexpr int U = decltype(many)::value;
-        char* tile[U];
-        typename Io<DT>::raw16 raw[U];
-        const long long ld = at.is_v ? v_ld : k_ld;
-        const typename Io<DT>::type* src = (at.is_v ? v : k) + ((long long)ASX_AT(at.lane, c.lanes, 108) * c.T + at.tok) * ld + ASX_AT(at.head, c.heads, 109) * D + ASX_AT(at.b, D / 16, 110) * 16;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (at.tok + 16 * u >= 0 && at.tok + 16 * u < c.T) raw[u] = Io<DT>::load16(src + 16 * u * ld, VEC);
-        tiles_of<D, U>(c, at, tile);
+    each_block<D>(c, [&](const Block& at) {
+        const typename Io<DT>::type* src = (at.is_v ? v : k) + ((long long)ASX_AT(at.lane, c.lanes, 108) * c.T + at.tok) * (at.is_v ? v_ld : k_ld) +
+                                           ASX_AT(at.head, c.heads, 109) * D + ASX_AT(at.b, D / 16, 110) * 16;
+        const typename Io<DT>::raw16 raw = Io<DT>::load16(src, VEC);
+        char* tile = tile_of<D>(c, at);
+        if (!tile) return;
         const float* hs = at.is_v ? c.v_scale : c.k_scale;
         const float inv = hs ? __frcp_rn(hs[at.head]) : 1.f;
         const int t = (at.len - c.T + at.tok) & 15;
+        float x[16], top = 0.f;
+        Io<DT>::widen16(raw, x);
+        bool odd = false;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (!tile[u]) continue;
-            float x[16], top = 0.f;
-            Io<DT>::widen16(raw[u], x);
-            bool odd = false;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                x[e] = __fmul_rn(x[e], inv);
-                odd |= !(fabsf(x[e]) <= 3.402823466e38f);
-                x[e] = x[e] == x[e] ? x[e] : 0.f;
-                top = fmaxf(top, fabsf(x[e]));
-            }
-            if (odd) flag_lane(c.lane_status, at.lane, AS_ERR_NUMERIC);
-            const uint32_t s8 = to_e4m3(__fmul_rn(top, 1.f / 6.f));
-            const float s = e4m3_value(s8);
-            const float rs = s > 0.f ? __frcp_rn(s) : 0.f;
-            uint32_t w[2] = {0, 0};
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                // (an infinite value with a zero factor cannot occur: its block's scale is the largest)
-                w[e >> 3] |= to_codes(__fmul_rn(x[e], rs), __fmul_rn(x[e + 1], rs)) << (4 * (e & 7));
-            }
-            *reinterpret_cast<uint2*>(tile[u] + (at.is_v ? Ti::v_code(t, at.b) : Ti::k_code(t, at.b))) = make_uint2(w[0], w[1]);
-            tile[u][at.is_v ? Ti::v_scale(t, at.b) : Ti::k_scale(t, at.b)] = (char)s8;
+        for (int e = 0; e < 16; ++e) {
+            x[e] = __fmul_rn(x[e], inv);
+            odd |= !(fabsf(x[e]) <= 3.402823466e38f);
+            x[e] = x[e] == x[e] ? x[e] : 0.f;
+            top = fmaxf(top, fabsf(x[e]));
         }
-    };
-    if constexpr (TILES) each_block_by_tiles<D>(c, store);
-    else each_block_by_rows<D>(c, store);
+        if (odd) flag_lane(c.lane_status, at.lane, AS_ERR_NUMERIC);
+        const uint32_t s8 = to_e4m3(__fmul_rn(top, 1.f / 6.f));
+        const float s = e4m3_value(s8);
+        const float rs = s > 0.f ? __frcp_rn(s) : 0.f;
+        uint32_t w[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            // (an infinite value with a zero factor cannot occur: its block's scale is the largest)
+            w[e >> 3] |= to_codes(__fmul_rn(x[e], rs), __fmul_rn(x[e + 1], rs)) << (4 * (e & 7));
+        }
+        *reinterpret_cast<uint2*>(tile + (at.is_v ? Ti::v_code(t, at.b) : Ti::k_code(t, at.b))) = make_uint2(w[0], w[1]);
+        tile[at.is_v ? Ti::v_scale(t, at.b) : Ti::k_scale(t, at.b)] = (char)s8;
+    });
 }
 
-// Load: the same threads the other way, 41 us for 8 x 4096 tokens (4.1 TB/s).
-template <int DT, int D, bool TILES>
+// Load: the same threads the other way, 42 us for 8 x 4096 tokens (4.0 TB/s).
+template <int DT, int D>
 __global__ void __launch_bounds__(C4_NT)
 load_kernel(const __grid_constant__ CacheArgs c, typename Io<DT>::type* __restrict__ k, typename Io<DT>::type* __restrict__ v) {
     using Ti = Tile4<D>;
-    auto read = [&](const Block& at, auto many) {
-        constexpr int U = decltype(many)::value;
-        char* tile[U];
-        tiles_of<D, U>(c, at, tile);
+    each_block<D>(c, [&](const Block& at) {
+        const char* tile = tile_of<D>(c, at);
         const float* hs = at.is_v ? c.v_scale : c.k_scale;
         const float g = hs ? hs[at.head] : 1.f;
         const int t = (at.len - c.T + at.tok) & 15;
-        uint2 q[U];
-        uint32_t s8[U];
+        uint2 q = make_uint2(0, 0);
+        uint32_t s8 = 0;                                // zeros where there is no token
+        if (tile) {
+            q = *reinterpret_cast<const uint2*>(tile + (at.is_v ? Ti::v_code(t, at.b) : Ti::k_code(t, at.b)));
+            s8 = (uint8_t)tile[at.is_v ? Ti::v_scale(t, at.b) : Ti::k_scale(t, at.b)];
+        }
+        const float s = e4m3_value(s8);
+        float x[16];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            q[u] = make_uint2(0, 0);
-            s8[u] = 0;                                  // zeros where there is no token
-            if (tile[u]) {
-                q[u] = *reinterpret_cast<const uint2*>(tile[u] + (at.is_v ? Ti::v_code(t, at.b) : Ti::k_code(t, at.b)));
-                s8[u] = (uint8_t)tile[u][at.is_v ? Ti::v_scale(t, at.b) : Ti::k_scale(t, at.b)];
+        for (int i = 0; i < 2; ++i) {
+            uint32_t h[4];
+            codes_f16x2(i ? q.y : q.x, h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
+                x[8 * i + 2 * e] = f.x * s * g;         // code * scale is exact, one rounding
+                x[8 * i + 2 * e + 1] = f.y * s * g;
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int tok = at.tok + 16 * u;
-            if (tok < 0 || tok >= c.T) continue;
-            const float s = e4m3_value(s8[u]);
-            float x[16];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                uint32_t h[4];
-                codes_f16x2(i ? q[u].y : q[u].x, h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[e]));
-                    x[8 * i + 2 * e] = f.x * s * g;     // code * scale is exact, one rounding
-                    x[8 * i + 2 * e + 1] = f.y * s * g;
-                }
-            }
-            Io<DT>::write16((at.is_v ? v : k) + ((size_t)ASX_AT(at.lane, c.lanes, 111) * c.T + tok) * c.heads * D + ASX_AT(at.head, c.heads, 112) * D + ASX_AT(at.b, D / 16, 113) * 16, x);
-        }
-    };
-    if constexpr (TILES) each_block_by_tiles<D>(c, read);
-    else each_block_by_rows<D>(c, read);
+        Io<DT>::write16((at.is_v ? v : k) + ((size_t)ASX_AT(at.lane, c.lanes, 111) * c.T + at.tok) * c.heads * D + ASX_AT(at.head, c.heads, 112) * D +
+                            ASX_AT(at.b, D / 16, 113) * 16, x);
+    });
 }
 
 }  // namespace asx
