@@ -29,7 +29,6 @@ struct Divisor {
         mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
     }
     __device__ __forceinline__ int div(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
-    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
 };
 
 struct CacheArgs {
