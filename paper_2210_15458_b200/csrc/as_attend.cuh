@@ -13,13 +13,18 @@ constexpr int AT_W = 4;                     // warps of a CTA; a unit of work is
 constexpr int AT_NT = 32 * AT_W;
 constexpr int AT_STAGES = 2;                // pairs of tiles that a warp has in flight or in use
 constexpr int AT_MAX_RUNS = 2560;           // CTAs, or warps where each has a run of its own
-// Weights are 2^(s - m).  They become f16 for the products with the values, so a weight is off by up to 2^-25 however small it
-// is, while its place in the sum is exact: m is set AT_TOP below a row's largest score, so that the largest weight is at least 2^AT_TOP
-// and the loss at most 2^(-25 - AT_TOP) of it for each token, and is set anew when a weight would pass 2^AT_MOST (f16 ends at 2^16).  The
-// distance is how far m may lag, which saves scalings of the sums: a lag of 8 / 4 / 0 takes 462 / 500 / 733 us for a chunk of 2 x 2048
-// tokens, 87 / 92 / 110 us behind shared beginnings; in 32 bits one of 8 / 3 / 0 takes 313 / 313 / 319 us for 2 x 300 tokens over 4096.
-constexpr float AT_MOST = 15.f;
+// Weights are 2^(s - m).  They become f16 for the products with the values, off by up to 2^-25 however small they are, while
+// their place in the sum is exact: so they are formed large, the largest of a row at least 2^AT_TOP, and never above 2^15 (f16 ends at
+// 2^16).  What a token loses is then at most 2^(-25 - AT_TOP) of the largest weight.  m is set anew when a score passes it by
+// 15 - AT_TOP; that lag saves scalings of the sums: a lag of 8 / 4 / 0 takes 462 / 500 / 733 us for a chunk of 2 x 2048 tokens, 87 /
+// 92 / 110 us behind shared beginnings; in 32 bits one of 8 / 3 / 0 takes 313 / 313 / 319 us for 2 x 300 tokens over 4096.
+// bf16: m itself stands AT_TOP below the largest score.  32 bits: s - m would lose digits there (12 x 30001 tokens: 3.8e-7 in place
+// of 3.1e-7 off the 64-bit result), so the weights are multiplied after the exponential and the outputs by the inverse.
 template <int DT> constexpr float AT_TOP = DT == AS_F32 ? 12.f : 7.f;
+template <int DT> constexpr float AT_BELOW = DT == AS_F32 ? 0.f : AT_TOP<DT>;                   // m below the largest score
+template <int DT> constexpr float AT_RISE = 15.f - AT_TOP<DT> + AT_BELOW<DT>;                   // a score this far above m sets it anew
+template <int DT> constexpr float AT_UP = DT == AS_F32 ? 4096.f : 1.f;                          // on weights
+template <int DT> constexpr float AT_DOWN = 1.f / AT_UP<DT>;                                    // on outputs
 
 struct AttendArgs {
     CacheArgs c;
@@ -470,7 +475,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                         if (cut && pos + 16 * (e >> 1) + t0 + 2 * (e & 1) >= lim[n][h]) x = -INFINITY;
                         top = fmaxf(top, x);
                     }
-                    rise |= top > m[n][h] + AT_MOST;
+                    rise |= top > m[n][h] + AT_RISE<DT>;
                 }
             if (__any_sync(0xFFFFFFFFu, rise)) {
 #pragma unroll
@@ -480,7 +485,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                         float top = fmaxf(fmaxf(s[0][n][h], s[0][n][2 + h]), fmaxf(s[1][n][h], s[1][n][2 + h]));
 #pragma unroll
                         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-                        top = fmaxf(top - AT_TOP<DT>, m[n][h]);
+                        top = fmaxf(top - AT_BELOW<DT>, m[n][h]);
                         const float f = top == -INFINITY ? 1.f : ex2(m[n][h] - top);
                         m[n][h] = top;
                         mu[n][h] = top == -INFINITY ? 0.f : top;
@@ -501,11 +506,12 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     l[n][1] += pr[1] + pr[3];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const uint32_t hi = pack_f16(pr[2 * i], pr[2 * i + 1]);
+                        const float w0 = pr[2 * i] * AT_UP<DT>, w1 = pr[2 * i + 1] * AT_UP<DT>;
+                        const uint32_t hi = pack_f16(w0, w1);
                         pf[b][0][n][i] = transpose8x8(hi);
                         if (F32) {
                             const float2 h2 = unpack_f16(hi);
-                            pf[b][PARTS - 1][n][i] = transpose8x8(pack_f16(pr[2 * i] - h2.x, pr[2 * i + 1] - h2.y));
+                            pf[b][PARTS - 1][n][i] = transpose8x8(pack_f16(w0 - h2.x, w1 - h2.y));
                         }
                     }
                 }
@@ -603,7 +609,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                             for (int i = 0; i < KS; i += 2) *reinterpret_cast<float4*>(at + 2 * i) = make_float4(o[n][i][h], o[n][i][2 + h], o[n][i + 1][h], o[n][i + 1][2 + h]);
                             if (r == 0) { part[8 * NT * D + rw] = m[n][h]; part[8 * NT * (D + 1) + rw] = L; }
                         } else if (row < p.rows) {
-                            const float inv = L == 0.f ? 0.f : vg / L;
+                            const float inv = L == 0.f ? 0.f : vg / L * AT_DOWN<DT>;
                             const size_t orow = out_row(a, cu.lane0, head, row);
                             E* at = static_cast<E*>(a.out) + orow * D + r * PER;
                             if constexpr (F32) {
@@ -662,7 +668,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     for (int e = 0; e < PER; e += 4) *reinterpret_cast<float4*>(at + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
                     if (d0 == 0) { part[8 * NT * D + n * 8 + rw] = M; part[8 * NT * (D + 1) + n * 8 + rw] = L; }
                 } else if (row < p.rows) {
-                    const float inv = L == 0.f ? 0.f : vg / L;
+                    const float inv = L == 0.f ? 0.f : vg / L * AT_DOWN<DT>;
                     const size_t orow = out_row(a, cu.lane0, head, row);
                     E* at = static_cast<E*>(a.out) + orow * D + d0;
 #pragma unroll
@@ -740,7 +746,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
             for (int e = 0; e < PER; ++e) acc[e] = 0.f;
             if (pre.begin) join_shared<D>(a, pre, ln, row, own.rows, head, lane * PER, M, L, acc);
             join_states<D>(own, i, c0, c1, rw, lane * PER, M, L, acc);
-            const float inv = L == 0.f ? 0.f : (c.v_scale ? c.v_scale[head] : 1.f) / L;
+            const float inv = L == 0.f ? 0.f : (c.v_scale ? c.v_scale[head] : 1.f) / L * AT_DOWN<DT>;
             const size_t orow = out_row(a, ln, head, row);
             typename Io<DT>::type* out = static_cast<typename Io<DT>::type*>(a.out) + orow * D + lane * PER;
 #pragma unroll

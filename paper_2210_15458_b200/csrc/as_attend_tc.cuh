@@ -266,11 +266,11 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         for (int e = 2; e < 8; e += 2) tops[i] = fmaxf(fmaxf(tops[i], __uint_as_float(v[8 * i + e])), __uint_as_float(v[8 * i + e + 1]));
                     }
                     const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * k2;
-                    const bool rise = top > m + AT_MOST;
+                    const bool rise = top > m + AT_RISE<AS_BF16>;
                     if (__any_sync(0xFFFFFFFFu, rise)) {
                         float f = 1.f;
                         if (rise) {
-                            mu = top - AT_TOP<AS_BF16>;
+                            mu = top - AT_BELOW<AS_BF16>;
                             f = ex2(m - mu);
                             m = mu;
                             l *= f;
