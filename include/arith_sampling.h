@@ -379,6 +379,7 @@ int as_reward_mean(const int32_t *d_seq, const int32_t *d_len, int S, int N, int
  * Logit edits: penalties for repeated tokens, a bias and a grammar mask, applied to every lane's
  * row in this order, in binary32, rounded once to the row's type:
  *   seen tokens (anywhere in the lane's history):  x = x > 0 ? x * (1 / repetition) : x * repetition
+ *                                                  (1 / repetition in binary32: infinite below 2^-128)
  *   x = x - (frequency * n + presence * [n > 0])   n = how often the token occurs in the output,
  *                                                  that is at history positions >= d_prompt_len
  *   x = x + d_bias[row, j]
@@ -438,7 +439,8 @@ int as_logits_edit(const void *d_logits, int dtype, int lanes, int V, long long 
  *              are divided by before they are stored, so that they lie in the scales' range
  * The value stored for x is code * scale * head scale; with y = x / head scale, scale is max|y| of
  * the block over 6, rounded to e4m3 (at most 448), and code is y / scale rounded to nearest (half way:
- * to the even code), at most 6.  code * scale is exact in bf16 and in binary16.
+ * to the even code), at most 6; each division is a product with the binary32 reciprocal.  code * scale is
+ * exact in bf16 and in binary16.
  */
 typedef struct as_cache4 {
     void *d_pages;
@@ -489,7 +491,9 @@ int as_cache4_load(const as_cache4 *cache, void *d_k, void *d_v, int dtype, int 
  *   d_work     as_cache4_attend_work_bytes(...) bytes of device scratch, 256-byte aligned
  * Scores, sums and outputs are kept in 32 bits until the end.  For the product with the values a weight is rounded to 11 bits with
  * bf16 queries, to 22 with 32-bit ones, or to 2^-32 (32-bit queries: 2^-37) of the row's largest weight where that is more.  AS_TUNE_WAIT_KCYCLES bounds
- * the waits of the kernel for many rows; a lane_status of AS_ERR_TIMEOUT reports one that ran out.
+ * the waits of the kernel for many rows; a lane_status of AS_ERR_TIMEOUT reports one that ran out: rows of the call may
+ * then not have been written.  Bad lengths and pages and time-outs are reported through d_lane_status alone, as in as_step: a
+ * caller who passes NULL does not learn of them.
  * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (head_dim, page_size, more than 2^31 rows or units of work), AS_ERR_CUDA.
  */
 size_t as_cache4_attend_work_bytes(const as_cache4 *cache, int dtype, int lanes, int T, int q_heads, int N);

@@ -18,6 +18,8 @@ constexpr int AT_MAX_RUNS = 2560;           // CTAs, or warps where each has a r
 // 2^16).  What a token loses is then at most 2^(-25 - AT_TOP) of the largest weight.  m is set anew when a score passes it by
 // 15 - AT_TOP; that lag saves scalings of the sums: a lag of 8 / 4 / 0 takes 462 / 500 / 733 us for a chunk of 2 x 2048 tokens, 87 /
 // 92 / 110 us behind shared beginnings; in 32 bits one of 8 / 3 / 0 takes 313 / 313 / 319 us for 2 x 300 tokens over 4096.
+// Eleven bits are enough for bf16 outputs: the 64-bit result is missed by 1.67e-3 instead of 1.66e-3, nearly all of it the output's
+// own 8 bits.  In 32 bits a weight goes in as two f16.
 // bf16: m itself stands AT_TOP below the largest score.  32 bits: s - m would lose digits there (12 x 30001 tokens: 3.8e-7 in place
 // of 3.1e-7 off the 64-bit result), so the weights are multiplied after the exponential and the outputs by the inverse.
 template <int DT> constexpr float AT_TOP = DT == AS_F32 ? 12.f : 7.f;
@@ -270,15 +272,16 @@ template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(
 // joined within the CTA (for many items of few tokens).  Scores are formed transposed, S^T = K q^T (tokens
 // x rows, so that 16 x 16 keys go through one instruction whatever the number of rows up to 8), and
 // so is the output, O^T = V^T P^T.  Keys and values become f16 in registers: code x scale is exact
-// there; queries are scaled by a power of two to lie in f16's range (bf16: exact) or split in two f16
-// (32 bits).  Which dimension of a tile goes to which index of the products is free, and chosen so that a
+// there; queries are scaled by a power of two to lie in f16's range (bf16: exact down to 2^-17 of the row's largest, below that
+// within 2^-25 of it) or split in two f16 (32 bits).  Which dimension of a tile goes to which index of the products is free, and chosen so that a
 // thread's keys are 16 neighbouring bytes and its values the 16 dimensions of one block, which share
 // their scale.  The tensor cores cut sums off instead of rounding them: with 32-bit queries (one row tile) chains of products
-// are kept to two and joined by additions (12 x 30001 tokens: 3.0e-6 off otherwise, from the bias alone).  Token l of the
+// are kept to two and joined by additions (12 x 30001 tokens: 3.0e-6 off otherwise, from the bias alone; a bf16 output is rounded by a
+// thousand times that, and its chains stay long).  Token l of the
 // products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
 // Bound by issue slots: 364 instructions for a tile of 16 tokens at head dimension 128, conversions and products mostly
-// (62 % of the slots, ALU pipe 56 %, DRAM 49 %).  128 lanes of up to 8192 tokens, 32 heads on 8: 180 us (4.5 TB/s); in 32
-// bits, 12 lanes of up to 30001: 97 us (3.0 TB/s).
+// (60 % of the slots, ALU pipe 54 %, DRAM 52 %: no unit is full, 3.5 warps a scheduler do not hide every wait).  128 lanes of up to 8192 tokens, 32 heads on 8: 178 to 194 us (4.2 to 4.6 TB/s); in 32
+// bits, 12 lanes of up to 30001: 95 us (3.1 TB/s).
 template <int DT, int D, int NT, bool SOLO>
 __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;

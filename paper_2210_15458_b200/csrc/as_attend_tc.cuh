@@ -163,8 +163,8 @@ template <int D, bool DUAL> constexpr size_t tc_smem_bytes() { return 1024 + (si
 // place.  DUAL: each group has a row tile and takes every tile of tokens; else the groups take the
 // tiles of tokens in turn, each with its own m, l and O, joined at the end, and the next item's queries have
 // a buffer of their own.  DUAL takes a tile in two pieces of 64 tokens, each with columns of its own: while
-// the weights of one are formed, the products of the other run (2 x 2048 tokens over up to 8192: 498 -> 465 us,
-// 875 TFLOP/s; nothing is busy for more than half of it, waiting is spread over softmax, filling and products).
+// the weights of one are formed, the products of the other run (2 x 2048 tokens over up to 8192: 498 -> 465 us;
+// 460 to 480 us in all runs, 848 to 885 TFLOP/s; nothing is busy for more than half of it, waiting is spread over softmax, filling and products).
 // The other form waits for the filling, and pieces cost it more than they give (8 x 32 codes behind shared tokens: 89.2 -> 90.1 us).
 template <int D, bool DUAL>
 __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
@@ -550,9 +550,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
     } else {
         // ------------------------------------------------ issuing ------------------------------------------------
         if (w == 0 && tc_elect()) {
-            // One thread walks the steps.  (Chosen by elect.sync, not by its number: the compiler then keeps operands in uniform
-            // registers, where each product otherwise costs a dozen instructions that wait their turn behind the other
-            // groups'.  TMEM, allocated whole, starts at 0.)
+            // One thread walks the steps.  (Chosen by elect.sync, not by its number: 8 products then take 512 cycles in place of
+            // 920 beside the other groups' warps.  TMEM, allocated whole, starts at 0.)
             constexpr uint32_t ID_S = tc_idesc(128, PIECE, false), ID_O = tc_idesc(128, D, true);
             constexpr int HALF = (PIECE * 128) >> 4, QS = DUAL ? 4 : 1, AHEAD = DUAL ? 1 : 2;   // QS: pieces (group, half) of a tile
             const uint64_t q_d = tc_desc(q_s, 0), k_d = tc_desc(k_s, 0), v_d = tc_desc(v_s, BLK);

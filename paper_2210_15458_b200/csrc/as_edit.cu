@@ -81,10 +81,11 @@ __device__ __forceinline__ float penalise(float x, uint32_t n, const EditArgs& a
 // One CTA edits one chunk of one row, VPT vectors of 16 bytes a thread; the vectors of the row's own 16-byte grid
 // decide where a chunk starts, so that any row start is served by 16-byte accesses.  The thread's vectors are on
 // their way (those that the mask leaves anything of) while the CTA counts the lane's history within the chunk in
-// shared memory: a bit per seen token, a count per token.  Bound by HBM: each element is read and written once; the
+// shared memory: a bit per seen token, a count per token.  Bound by HBM where histories are short: each element is read and written once; the
 // history is read once per chunk, from L2 (a lane's 4096 tokens are an eighth of what its chunks of 8192 move).
-// 1024 x 128256 in 32 bits: 249 us (1.06 GB; 206 us without bias and mask, 157 without a history: 6.7 TB/s); 256 x 50257 bf16: 20.5 us,
-// 12.6 without a history, whose counting is latency; 8 x 32000 bf16: 5.6 us on the device.
+// 1024 x 128256 in 32 bits: 249 us (1.06 GB; 206 us without bias and mask, 157 without a history: 6.7 TB/s); 256 x 50257 bf16: 20.6 us,
+// 12.6 without a history (each of a row's chunks reads and filters all of it: issue slots 65 % busy, DRAM 10 %); 8 x 32000 bf16: 5.6 us
+// on the device.
 template <int DT, int VPT>
 __global__ void __launch_bounds__(ED_NT) edit_kernel(const __grid_constant__ EditArgs a) {
     using El = Elem<DT>;
