@@ -151,3 +151,24 @@ def test_one_peak_and_a_long_tail(B, dtype, rows, peak, down, many):
         out = B.as_cache4_attend(pages, q, table, length, scale, N=N, shared=shared, lse=lse)
         assert float((out.double() - want).abs().max()) <= tol
         assert float((lse.double() - wlse).abs().max()) <= 2 * e + n / 8 * 2.0 ** -24 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("fill", [0x7F, 0xFF])
+def test_what_lies_behind_the_last_token_does_not_count(B, dtype, D, rows, fill):
+    """Pages that end inside a tile, the rest of them filled with bytes whose scales are NaN: the same bits as with zeros."""
+    P, lens = 128, [1, 15, 17, 33, 129, 250, 511]
+    g = torch.Generator().manual_seed(D)
+    k, v = (torch.randn(len(lens), 511, 2, D, generator=g).cuda() for _ in range(2))
+    table = torch.randperm(4 * len(lens), generator=g).to(torch.int32).view(len(lens), 4).cuda()
+    q = torch.randn(len(lens), 1, 2 * rows, D, generator=g).to(DT[dtype]).cuda()
+    got = []
+    for byte in (0, fill):
+        pages = B.cache4_pages(4 * len(lens), 2, D, P)
+        pages.fill_(byte)
+        B.as_cache4_append(pages, k, v, table, i32(lens))
+        lse = torch.empty(len(lens), 1, 2 * rows, device="cuda")
+        got.append((B.as_cache4_attend(pages, q, table, i32(lens), 0.125, lse=lse), lse))
+    assert torch.isfinite(got[0][0]).all() and torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
