@@ -607,7 +607,8 @@ def as_cache4_attend(pages: torch.Tensor, q: torch.Tensor, table: torch.Tensor, 
                      lse: Optional[torch.Tensor] = None, lane_status: Optional[torch.Tensor] = None,
                      work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of q [lanes, T, q_heads, D], the last T tokens of each lane, over the lane's cached tokens (causal).
-    shared [lanes / N] int32: how many leading tokens the N lanes of a group have in the same pages."""
+    shared [lanes / N] int32: how many leading tokens the N lanes of a group have in the same pages.  Bad lengths and pages
+    and waits that ran out are reported in lane_status alone."""
     c = _cache4(pages, k_scale, v_scale)
     lanes, T, heads, q_ld = _tokens(q, c.head_dim, "q")
     if out is not None and (out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous()):
