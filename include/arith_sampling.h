@@ -175,6 +175,35 @@ int as_step_lattice(const void *d_logits, int dtype, int lanes, int V, long long
                     const as_step_diag *diag, void *stream);
 
 /*
+ * A step over drafted tokens: a smaller model has drawn up to K tokens for each lane, one after the other, and the model has been
+ * run over all of them at once; the call takes those that the model agrees to.  With p_i the model's distribution at the place of
+ * drafted token x_i and q_i the draft's (both under temperature, top-k and nucleus as in as_step), x_i is accepted if
+ *   u_i q_i(x_i) < p_i(x_i)
+ * as long as all before it were.  At the first refused one the lane takes a token from max(p_i - q_i, 0) over its sum (from p_i
+ * should that be 0 everywhere), after n accepted ones one from p_n; it is the one whose interval holds the lane's code, which is
+ * rescaled into it as in as_step.  With u uniform and independent of the code, tokens are distributed as those of as_step, one by one.
+ *   d_target     [lanes, K + 1] rows of V logits, target_ld >= V elements apart: row i is the model's prediction of token i
+ *   d_draft      [lanes, K] rows, draft_ld >= V apart, or NULL: drafts that were not drawn but looked up (q_i(x_i) = 1)
+ *   K            >= 0;  d_drafted  [lanes, K] i32;  d_u  [lanes, K] f64 in [0, 1)
+ *   d_n          NULL (K for every lane) or [lanes] i32: drafted tokens of the lane, 0 .. K; rows behind row n are not looked at
+ *   d_codes      [lanes] f64, as for as_step
+ *   d_tokens     [lanes, K + 1] i32, written: the accepted tokens, the one taken, -1 behind it
+ *   d_accepted   [lanes] i32, written: how many were accepted
+ *   d_codes_out  [lanes] f64, written; may be d_codes
+ *   d_lane_status  NULL or [lanes]: AS_OK; AS_ERR_INVALID_ARG for a d_n or a drafted token out of range; AS_ERR_NUMERIC for a code or u out of
+ *                range or a row that as_step could not use.  Rows, tokens and u behind the first refusal do not count.  Such a lane gets -1 throughout,
+ *                accepts 0 tokens and keeps its code
+ *   d_work       as_step_verify_work_bytes(...) bytes of device scratch, 256-byte aligned
+ * Decisions are those of 64-bit arithmetic.  Errors: as as_step.
+ */
+size_t as_step_verify_work_bytes(int dtype, int lanes, int K, int V);
+int as_step_verify(const void *d_target, long long target_ld, const void *d_draft, long long draft_ld, int dtype,
+                   int lanes, int K, int V, const int32_t *d_drafted, const int32_t *d_n, const double *d_u,
+                   const double *d_codes, double temp, int top_k, double top_p, int32_t *d_tokens,
+                   int32_t *d_accepted, double *d_codes_out, int32_t *d_lane_status, void *d_work,
+                   size_t work_bytes, void *stream);
+
+/*
  * Same step with HOST buffers: copies logits and codes to the device, runs
  * as_step, copies tokens and codes back, and returns after the results are in
  * the host buffers (it synchronises `stream`).  Pinned host memory makes the
@@ -503,6 +532,67 @@ int as_cache4_attend(const as_cache4 *cache, const void *d_q, long long q_ld, in
                      int32_t *d_lane_status, void *d_work, size_t work_bytes, void *stream);
 
 /*
+ * as_cache4_attend with a sliding window: a query token at position p looks at positions p - window + 1 .. p and at the first
+ * `sinks` of its lane.  Everything else as as_cache4_attend, its scratch included (as_cache4_attend_work_bytes): chunks, shared
+ * beginnings, rows that see nothing.  Pages that lie wholly between the sinks and the first query token's window are not
+ * looked up: a lane may have given them up (as_pages_trim).
+ *   window  >= 1;  sinks  >= 0
+ * Errors: as as_cache4_attend, plus AS_ERR_INVALID_ARG for window < 1 or sinks < 0.
+ */
+int as_cache4_attend_window(const as_cache4 *cache, const void *d_q, long long q_ld, int dtype, int lanes, int T,
+                            int q_heads, const int32_t *d_table, int max_pages, const int32_t *d_len,
+                            double scale, int N, const int32_t *d_shared, int window, int sinks, void *d_out,
+                            float *d_lse, int32_t *d_lane_status, void *d_work, size_t work_bytes, void *stream);
+
+/*
+ * What the cached tokens are worth, and giving up those that are worth least.  d_weight [lanes, heads, weight_ld] f32: entry t of
+ * a lane and key / value head is the weight that the token at position t has got so far.
+ *
+ * as_cache4_weigh: for the T query tokens of a lane (laid out as for as_cache4_attend) and position t,
+ *   w_t = sum over the T tokens and the q_heads / heads query heads of a key head of exp(scale * q . k_t - lse)
+ * over the rows that look at t, causal as in as_cache4_attend, with its d_lse.  Weights of the call's own tokens (t >= d_len - T) become w_t;
+ * those of earlier ones grow by it (add = 1) or become it too (add = 0).  Passing the last few tokens of a prompt with add = 0
+ * weighs the prompt by what they look at.
+ *   d_lse      [lanes, T, q_heads] f32 device.  A row whose entry is -inf adds nothing.  A NaN, in it or in the row's query,
+ *              reaches the tokens that the row looks at
+ *   window, sinks  as for as_cache4_attend_window; window = 0: none
+ *   d_first    NULL (0) or [lanes] i32 device: positions in front of it are left alone (a beginning that is kept anyway)
+ *   d_lane_status  NULL or [lanes]: AS_OK, or AS_ERR_INVALID_ARG for a d_len outside [0, max_pages * page_size] or above weight_ld,
+ *              a d_first outside [0, d_len] (the lane's weights are then left as they were) or a page id outside [0, n_pages) (page 0
+ *              is read in its place)
+ *   d_work     as_cache4_weigh_work_bytes(...) bytes of device scratch, 256-byte aligned
+ * Scores, weights and sums are in 32 bits; results do not depend on scheduling.
+ * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED, AS_ERR_CUDA as for as_cache4_attend.
+ */
+size_t as_cache4_weigh_work_bytes(const as_cache4 *cache, int dtype, int lanes, int T, int q_heads);
+int as_cache4_weigh(const as_cache4 *cache, const void *d_q, long long q_ld, int dtype, int lanes, int T,
+                    int q_heads, const float *d_lse, const int32_t *d_table, int max_pages, const int32_t *d_len,
+                    double scale, int window, int sinks, int add, const int32_t *d_first, float *d_weight,
+                    long long weight_ld, int32_t *d_lane_status, void *d_work, size_t work_bytes, void *stream);
+
+/*
+ * as_cache4_evict: every lane longer than d_keep gives up tokens until d_keep are left, in each key / value head on its own: the
+ * first d_first and the last `recent` tokens stay, of those in between the ones of most weight (equal weights: the lower position;
+ * a NaN is less than any number).  Kept tokens lie at positions 0 .. d_keep - 1 afterwards: one that was at a position below
+ * d_keep - recent stays where it is; one from behind goes to the place of one that was given up, the lowest to the lowest; the
+ * recent ones follow in their order.  d_weight_out holds the weights of the same places, 0 from d_keep up to the old length and
+ * what d_weight has behind it.  Pages behind d_keep are left as they were, and so are d_table and d_len: as_pages_trim cuts the
+ * lanes to d_keep once the layers that share them have been through.
+ *   d_keep     [lanes] i32 device, >= d_first + recent for a lane that is cut;  recent >= 0
+ *   d_first    NULL (0) or [lanes] i32 device
+ *   d_weight_out  [lanes, heads, weight_ld]; may be d_weight, otherwise the two must not overlap
+ *   d_ref      NULL, or [n_pages] i32 device (see below): a lane that would write into a page that other lanes hold too is refused
+ *   d_lane_status  NULL or [lanes]: AS_OK, or AS_ERR_INVALID_ARG (a d_len outside [0, max_pages * page_size] or above weight_ld, a negative
+ *              d_keep or d_first, d_first + recent > d_keep, a page id outside [0, n_pages), a page held by others): the lane then keeps
+ *              tokens and weights as they are
+ * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED, AS_ERR_CUDA.
+ */
+int as_cache4_evict(const as_cache4 *cache, const float *d_weight, long long weight_ld, int lanes,
+                    const int32_t *d_table, int max_pages, const int32_t *d_len, const int32_t *d_keep,
+                    const int32_t *d_first, int recent, const int32_t *d_ref, float *d_weight_out,
+                    int32_t *d_lane_status, void *stream);
+
+/*
  * The pages of a cache: a page table [lanes, max_pages] i32 (-1 behind a lane's last page), lengths
  * [lanes] i32, and for every page the number of lanes that hold it, d_ref [n_pages] i32 (0 = free).
  * A lane's partly filled last page is held by that lane alone; full pages may be held by many.  Free
@@ -533,8 +623,18 @@ int as_cache4_attend(const as_cache4 *cache, const void *d_q, long long q_ld, in
  * any other entry (-1, or a page that no lane holds by d_ref) stays as it is.
  *   d_table_out may be d_table, d_ref_out may be d_ref;  d_used  [1] i32 device, written: U
  *
+ * as_pages_trim: lane i is cut to d_keep[i] tokens (a lane that is not longer keeps its length) and gives up the pages behind
+ * them; of what is left it gives up the pages that lie wholly within positions d_gone[i][0] .. d_gone[i][1] - 1, say those that a
+ * sliding window has left behind.  Table entries of pages given up become -1.  A lane that has given up pages in its middle can
+ * grow and be trimmed, to 0 tokens as well, but as_pages_fork reads it as out of range.
+ *   d_keep     NULL (no lane is cut) or [lanes] i32;  d_gone  NULL or [lanes, 2] i32
+ *   d_table_out, d_len_out, d_ref_out  may be d_table, d_len and d_ref
+ *   d_lane_status  NULL or [lanes]: AS_OK, or AS_ERR_INVALID_ARG: a length or a page within it out of range (-1, given up before,
+ *              is in range), a negative d_keep, or a new last page that is partly filled and held by other lanes too (by d_ref as it was):
+ *              the lane is left as it is
+ *
  *   d_work     as_pages_work_bytes(lanes_in, lanes_out, n_pages) bytes of device scratch, 256-byte aligned
- *              (lanes_in = lanes_out = lanes for the last two calls)
+ *              (lanes_in = lanes_out = lanes for the last three calls)
  * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED (n_pages > 2^20, max_pages * page_size > 2^30), AS_ERR_CUDA.
  */
 size_t as_pages_work_bytes(int lanes_in, int lanes_out, int n_pages);
@@ -550,6 +650,10 @@ int as_pages_compact(int lanes, int max_pages, int n_pages, const int32_t *d_tab
                      int32_t *d_table_out, int32_t *d_ref_out, int32_t *d_used, void *d_data, int planes,
                      long long plane_stride, long long page_bytes, void *d_work, size_t work_bytes,
                      void *stream);
+int as_pages_trim(const int32_t *d_keep, const int32_t *d_gone, int lanes, int max_pages, int page_size,
+                  int n_pages, const int32_t *d_table, const int32_t *d_len, const int32_t *d_ref,
+                  int32_t *d_table_out, int32_t *d_len_out, int32_t *d_ref_out, int32_t *d_lane_status,
+                  void *d_work, size_t work_bytes, void *stream);
 
 /*
  * Launch-shape overrides for measurement sweeps and tests (0 restores the built-in

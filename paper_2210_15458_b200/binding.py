@@ -41,10 +41,11 @@ TUNE_DEBUG_NO_COPY = 8
 TUNE_RADIX_NUCLEUS = 9
 
 EXPORTS = ["as_lattice_codes", "as_lattice_codes_variant", "as_step", "as_step_typical", "as_step_lattice", "as_step_host", "as_step_host_work_bytes", "as_step_host_static",
-           "as_decode_bigram",
+           "as_step_verify_work_bytes", "as_step_verify", "as_decode_bigram",
            "as_decode_bigram_codes", "as_xp_lattice_state", "as_decode_bigram_xp", "as_encode_bigram", "as_ngram_diversity", "as_reward_mean", "as_logits_edit",
            "as_cache4_bytes", "as_cache4_append", "as_cache4_load", "as_cache4_attend_work_bytes", "as_cache4_attend",
-           "as_pages_work_bytes", "as_pages_fork", "as_pages_grow", "as_pages_compact", "as_tune",
+           "as_cache4_attend_window", "as_cache4_weigh_work_bytes", "as_cache4_weigh", "as_cache4_evict",
+           "as_pages_work_bytes", "as_pages_fork", "as_pages_grow", "as_pages_trim", "as_pages_compact", "as_tune",
            "as_last_error", "as_version"]
 
 
@@ -139,17 +140,25 @@ def lib():
         L.as_cache4_load.argtypes = [PC, P, P, I, I, I, P, I, P, P, P]
         L.as_cache4_attend_work_bytes.argtypes = [PC, I, I, I, I, I]
         L.as_cache4_attend.argtypes = [PC, P, LL, I, I, I, I, P, I, P, D, I, P, P, P, P, P, Z, P]
+        L.as_cache4_attend_window.argtypes = [PC, P, LL, I, I, I, I, P, I, P, D, I, P, I, I, P, P, P, P, Z, P]
+        L.as_cache4_weigh_work_bytes.argtypes = [PC, I, I, I, I]
+        L.as_cache4_weigh.argtypes = [PC, P, LL, I, I, I, I, P, P, I, P, D, I, I, I, P, P, LL, P, P, Z, P]
+        L.as_cache4_evict.argtypes = [PC, P, LL, I, P, I, P, P, P, I, P, P, P, P]
+        L.as_step_verify_work_bytes.argtypes = [I, I, I, I]
+        L.as_step_verify.argtypes = [P, LL, P, LL, I, I, I, I, P, P, P, P, D, I, D, P, P, P, P, P, Z, P]
         L.as_pages_work_bytes.argtypes = [I, I, I]
         L.as_pages_fork.argtypes = [P, I, I, I, I, I, P, P, P, P, P, P, P, I, LL, LL, P, P, Z, P]
         L.as_pages_grow.argtypes = [P, I, I, I, I, P, P, P, P, P, Z, P]
         L.as_pages_compact.argtypes = [I, I, I, P, P, P, P, P, P, I, LL, LL, P, Z, P]
-        for n in ("as_cache4_bytes", "as_cache4_attend_work_bytes", "as_pages_work_bytes"):
+        L.as_pages_trim.argtypes = [P, P, I, I, I, I, P, P, P, P, P, P, P, P, Z, P]
+        for n in ("as_cache4_bytes", "as_cache4_attend_work_bytes", "as_cache4_weigh_work_bytes", "as_step_verify_work_bytes", "as_pages_work_bytes"):
             getattr(L, n).restype = Z
         L.as_tune.argtypes = [I, I]
         L.as_last_error.restype = ctypes.c_char_p
         for n in ("as_lattice_codes", "as_step", "as_step_host", "as_decode_bigram",
                   "as_decode_bigram_codes", "as_xp_lattice_state", "as_decode_bigram_xp", "as_encode_bigram", "as_ngram_diversity", "as_reward_mean",
                   "as_logits_edit", "as_cache4_append", "as_cache4_load", "as_cache4_attend", "as_pages_fork", "as_pages_grow",
+                  "as_cache4_attend_window", "as_cache4_weigh", "as_cache4_evict", "as_step_verify", "as_pages_trim",
                   "as_pages_compact", "as_tune", "as_version"):
             getattr(L, n).restype = I
         _lib = L
@@ -525,6 +534,60 @@ def as_logits_edit(logits: torch.Tensor, seq: Optional[torch.Tensor] = None, len
     return out
 
 
+def _rows(t: torch.Tensor, lanes: int, n: int, name: str):
+    """(V, elements from row to row) of logits [lanes, n, V] whose rows lie at one distance."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != lanes or shape[1] != n or stride[2] != 1 or (lanes > 1 and n > 1 and stride[0] != n * stride[1]):
+        raise ValueError("%s must be [%d, %d, V] with unit stride along the vocabulary and rows at one distance" % (name, lanes, n))
+    return shape[2], stride[1] if n > 1 else stride[0] if lanes > 1 else shape[2]
+
+
+def as_step_verify_work_bytes(dtype: int, lanes: int, K: int, V: int) -> int:
+    return lib().as_step_verify_work_bytes(dtype, lanes, K, V)
+
+
+def as_step_verify(target: torch.Tensor, draft: Optional[torch.Tensor], drafted: torch.Tensor, u: torch.Tensor, codes: torch.Tensor,
+                   temp: float = 1.0, top_k: int = 0, top_p: float = 1.0, n_drafts: Optional[torch.Tensor] = None,
+                   tokens: Optional[torch.Tensor] = None, accepted: Optional[torch.Tensor] = None,
+                   codes_out: Optional[torch.Tensor] = None, lane_status: Optional[torch.Tensor] = None, V: Optional[int] = None,
+                   work: Optional[torch.Tensor] = None, stream=None):
+    """(tokens [lanes, K + 1], accepted [lanes], codes'): the drafted tokens [lanes, K] int32 that logits target [lanes, K + 1, V]
+    agree to, given the draft's [lanes, K, V] (None: looked up, not drawn) and uniform u [lanes, K] float64, then one token
+    taken by the lane's code, then -1.  n_drafts [lanes] int32: how many drafted tokens a lane has."""
+    if drafted.dim() != 2:
+        raise ValueError("drafted must be [lanes, K]")
+    lanes, K = drafted.shape
+    width, target_ld = _rows(target, lanes, K + 1, "target")
+    V = width if V is None else V
+    draft_ld = V
+    if draft is not None and K > 0:
+        draft_width, draft_ld = _rows(draft, lanes, K, "draft")
+        if draft.dtype != target.dtype or draft_width < V:
+            raise ValueError("draft must have the dtype and vocabulary of target")
+    if width < V:
+        raise ValueError("target must have V logits a row")
+    for t, n, name in ((u, lanes * K, "u"), (codes, lanes, "codes"), (codes_out, lanes, "codes_out")):
+        if t is not None and (t.dtype != torch.float64 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("%s must be contiguous float64 of %d entries" % (name, n))
+    L = lib()
+    dt = _logits_dtype(target)
+    with _owner(stream, target.device):
+        if tokens is None:
+            tokens = drafted.new_empty((lanes, K + 1))
+        if accepted is None:
+            accepted = drafted.new_empty(lanes)
+        if codes_out is None:
+            codes_out = torch.empty_like(codes)
+        if work is None:
+            work = drafted.new_empty((L.as_step_verify_work_bytes(dt, lanes, K, V) + 3) // 4)
+    _check(L.as_step_verify(target.data_ptr(), target_ld, None if draft is None else draft.data_ptr(), draft_ld, dt, lanes, K, V,
+                            _int32(drafted, "drafted"), _int32(n_drafts, "n_drafts", lanes), u.data_ptr(), codes.data_ptr(), temp,
+                            top_k, top_p, _int32(tokens, "tokens", lanes * (K + 1)), _int32(accepted, "accepted", lanes),
+                            codes_out.data_ptr(), _int32(lane_status, "lane_status", lanes), work.data_ptr(),
+                            work.numel() * work.element_size(), _stream(stream)))
+    return tokens, accepted, codes_out
+
+
 def as_cache4_bytes(n_pages: int, heads: int, head_dim: int, page_size: int) -> int:
     return lib().as_cache4_bytes(n_pages, heads, head_dim, page_size)
 
@@ -605,10 +668,13 @@ def as_cache4_attend(pages: torch.Tensor, q: torch.Tensor, table: torch.Tensor, 
                      k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, N: int = 1,
                      shared: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                      lse: Optional[torch.Tensor] = None, lane_status: Optional[torch.Tensor] = None,
-                     work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                     work: Optional[torch.Tensor] = None, stream=None, window: Optional[int] = None, sinks: int = 0) -> torch.Tensor:
     """Attention of q [lanes, T, q_heads, D], the last T tokens of each lane, over the lane's cached tokens (causal).
     shared [lanes / N] int32: how many leading tokens the N lanes of a group have in the same pages.  Bad lengths and pages
-    and waits that ran out are reported in lane_status alone."""
+    and waits that ran out are reported in lane_status alone.  With window the call goes to as_cache4_attend_window: each token
+    looks at the last `window` positions up to its own and at the first `sinks`."""
+    if window is None and sinks:
+        raise ValueError("sinks come with a window")
     c = _cache4(pages, k_scale, v_scale)
     lanes, T, heads, q_ld = _tokens(q, c.head_dim, "q")
     if out is not None and (out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous()):
@@ -623,11 +689,75 @@ def as_cache4_attend(pages: torch.Tensor, q: torch.Tensor, table: torch.Tensor, 
         with _owner(stream, q.device):
             out = q.new_empty((lanes, T, heads, c.head_dim)) if out is None else out
             work = length.new_empty((need + 3) // 4) if work is None else work
-    _check(L.as_cache4_attend(ctypes.byref(c), q.data_ptr(), q_ld, dt, lanes, T, heads, tp, max_pages, lp, scale, N,
-                              _int32(shared, "shared", lanes // N if N > 0 else None), out.data_ptr(), _ptr(lse),
-                              _int32(lane_status, "lane_status", lanes), work.data_ptr(),
-                              work.numel() * work.element_size(), _stream(stream)))
+    sp, st = _int32(shared, "shared", lanes // N if N > 0 else None), _int32(lane_status, "lane_status", lanes)
+    nbytes = work.numel() * work.element_size()
+    if window is None:
+        _check(L.as_cache4_attend(ctypes.byref(c), q.data_ptr(), q_ld, dt, lanes, T, heads, tp, max_pages, lp, scale, N, sp,
+                                  out.data_ptr(), _ptr(lse), st, work.data_ptr(), nbytes, _stream(stream)))
+    else:
+        _check(L.as_cache4_attend_window(ctypes.byref(c), q.data_ptr(), q_ld, dt, lanes, T, heads, tp, max_pages, lp, scale, N, sp,
+                                         window, sinks, out.data_ptr(), _ptr(lse), st, work.data_ptr(), nbytes, _stream(stream)))
     return out
+
+
+def _weights(t: torch.Tensor, lanes: int, heads: int, name: str):
+    """(pointer, entries from head to head) of weights [lanes, heads, n] float32, contiguous."""
+    shape = t.shape
+    if t.dtype is not torch.float32 or len(shape) != 3 or shape[0] != lanes or shape[1] != heads or not t.is_contiguous():
+        raise ValueError("%s must be contiguous float32 [lanes, heads, positions]" % name)
+    return t.data_ptr(), shape[2]
+
+
+def as_cache4_weigh_work_bytes(pages: torch.Tensor, dtype: int, lanes: int, T: int, q_heads: int) -> int:
+    return lib().as_cache4_weigh_work_bytes(ctypes.byref(_cache4(pages, None, None)), dtype, lanes, T, q_heads)
+
+
+def as_cache4_weigh(pages: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, table: torch.Tensor, length: torch.Tensor, scale: float,
+                    weight: torch.Tensor, k_scale: Optional[torch.Tensor] = None, window: Optional[int] = None, sinks: int = 0,
+                    add: bool = True, first: Optional[torch.Tensor] = None, lane_status: Optional[torch.Tensor] = None,
+                    work: Optional[torch.Tensor] = None, stream=None) -> None:
+    """weight [lanes, heads, positions] float32, in place: what q [lanes, T, q_heads, D], the last T tokens of each lane, give to the
+    lane's cached tokens, with the lse [lanes, T, q_heads] of as_cache4_attend.  add: on top of what earlier tokens have; else it
+    takes its place.  first [lanes] int32: positions in front of it are left alone."""
+    c = _cache4(pages, k_scale, None)
+    lanes, T, heads, q_ld = _tokens(q, c.head_dim, "q")
+    if lse.dtype != torch.float32 or lse.numel() != lanes * T * heads or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous float32 [lanes, T, q_heads]")
+    if window is None and sinks:
+        raise ValueError("sinks come with a window")
+    if window is not None and window < 1:
+        raise ValueError("window must be >= 1")
+    L = lib()
+    dt = _logits_dtype(q)
+    tp, max_pages, lp = _table(table, length, lanes)
+    wp, weight_ld = _weights(weight, lanes, c.heads, "weight")
+    if work is None:
+        with _owner(stream, q.device):
+            work = length.new_empty((L.as_cache4_weigh_work_bytes(ctypes.byref(c), dt, lanes, T, heads) + 3) // 4)
+    _check(L.as_cache4_weigh(ctypes.byref(c), q.data_ptr(), q_ld, dt, lanes, T, heads, lse.data_ptr(), tp, max_pages, lp, scale,
+                             0 if window is None else window, sinks, 1 if add else 0, _int32(first, "first", lanes), wp, weight_ld,
+                             _int32(lane_status, "lane_status", lanes), work.data_ptr(), work.numel() * work.element_size(),
+                             _stream(stream)))
+
+
+def as_cache4_evict(pages: torch.Tensor, weight: torch.Tensor, table: torch.Tensor, length: torch.Tensor, keep: torch.Tensor,
+                    recent: int = 0, first: Optional[torch.Tensor] = None, ref: Optional[torch.Tensor] = None,
+                    weight_out: Optional[torch.Tensor] = None, lane_status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Leave keep[lane] tokens of each longer lane, per key head: the first `first[lane]`, the last `recent`, and those of most
+    weight.  They lie at the lane's first keep[lane] positions afterwards; returns their weights (in place without weight_out).
+    table and length stay: as_pages_trim cuts the lanes."""
+    c = _cache4(pages, None, None)
+    lanes = length.numel()
+    weight_out = weight if weight_out is None else weight_out
+    wp, weight_ld = _weights(weight, lanes, c.heads, "weight")
+    op, out_ld = _weights(weight_out, lanes, c.heads, "weight_out")
+    if out_ld != weight_ld:
+        raise ValueError("weight_out must have the shape of weight")
+    tp, max_pages, lp = _table(table, length, lanes)
+    _check(lib().as_cache4_evict(ctypes.byref(c), wp, weight_ld, lanes, tp, max_pages, lp, _int32(keep, "keep", lanes),
+                                 _int32(first, "first", lanes), recent, _int32(ref, "ref", c.n_pages), op,
+                                 _int32(lane_status, "lane_status", lanes), _stream(stream)))
+    return weight_out
 
 
 def as_pages_work_bytes(lanes_in: int, lanes_out: int, n_pages: int) -> int:
@@ -685,6 +815,26 @@ def as_pages_grow(add: torch.Tensor, table: torch.Tensor, length: torch.Tensor, 
     _check(lib().as_pages_grow(_int32(add, "add", lanes), lanes, max_pages, page_size, ref.numel(), _int32(table, "table"),
                                _int32(length, "length", lanes), _int32(ref, "ref"),
                                _int32(lane_status, "lane_status", lanes), work.data_ptr(), nbytes, _stream(stream)))
+
+
+def as_pages_trim(keep: Optional[torch.Tensor], table: torch.Tensor, length: torch.Tensor, ref: torch.Tensor, page_size: int,
+                  gone: Optional[torch.Tensor] = None, table_out: Optional[torch.Tensor] = None,
+                  length_out: Optional[torch.Tensor] = None, ref_out: Optional[torch.Tensor] = None,
+                  lane_status: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None, stream=None):
+    """Cut each lane to keep[lane] tokens (None: none is cut); gone [lanes, 2] int32: positions whose pages it gives up as well.
+    Returns (table, length, ref), updated in place where no output is given."""
+    lanes, max_pages = table.shape
+    table_out = table if table_out is None else table_out
+    length_out = length if length_out is None else length_out
+    ref_out = ref if ref_out is None else ref_out
+    with _owner(stream, ref.device):
+        work, nbytes = _pages_work(work, lanes, lanes, ref.numel(), ref)
+    _check(lib().as_pages_trim(_int32(keep, "keep", lanes), _int32(gone, "gone", 2 * lanes), lanes, max_pages, page_size, ref.numel(),
+                               _int32(table, "table"), _int32(length, "length", lanes), _int32(ref, "ref"),
+                               _int32(table_out, "table_out", table.numel()), _int32(length_out, "length_out", lanes),
+                               _int32(ref_out, "ref_out", ref.numel()), _int32(lane_status, "lane_status", lanes), work.data_ptr(),
+                               nbytes, _stream(stream)))
+    return table_out, length_out, ref_out
 
 
 def as_pages_compact(table: torch.Tensor, ref: torch.Tensor, pool: Optional[torch.Tensor] = None,

@@ -487,7 +487,7 @@ __global__ void decode_wrapup_kernel(const int* __restrict__ seq, int lanes, int
 // ---------------------------------------------------------------------------
 // argument checks
 // ---------------------------------------------------------------------------
-static int check_scalars(int dtype, int V, long long ld, double temp, double top_p) {
+int check_scalars(int dtype, int V, long long ld, double temp, double top_p) {
     if (dtype != AS_F32 && dtype != AS_BF16) return set_err(AS_ERR_INVALID_ARG, "unknown dtype %d", dtype);
     if (V < 1) return set_err(AS_ERR_INVALID_ARG, "V = %d must be >= 1", V);
     if (V > AS_MAX_V) return set_err(AS_ERR_UNSUPPORTED, "V = %d exceeds AS_MAX_V = %d", V, AS_MAX_V);
@@ -497,7 +497,7 @@ static int check_scalars(int dtype, int V, long long ld, double temp, double top
     return AS_OK;
 }
 
-static int check_data(const void* data, int dtype) {
+int check_data(const void* data, int dtype) {
     if (!data) return set_err(AS_ERR_INVALID_ARG, "logits/table pointer is NULL");
     const uintptr_t a = reinterpret_cast<uintptr_t>(data);
     if (a % (dtype == AS_F32 ? 4 : 2)) return set_err(AS_ERR_INVALID_ARG, "logits/table pointer is not element-aligned");
@@ -541,7 +541,7 @@ int as_debug_counts(unsigned long long* h_out) {
 // checked builds only: the record of out-of-range indices (failures, first site, its index, its
 // bound) since the last reset
 int as_debug_bounds(int* h_out4, int reset) {
-    int (*const unit[])(int*, int) = {bounds_step, bounds_edit, bounds_cache4, bounds_pages};
+    int (*const unit[])(int*, int) = {bounds_step, bounds_edit, bounds_cache4, bounds_pages, bounds_window, bounds_weigh, bounds_evict, bounds_verify};
     int got[4] = {0, 0, 0, 0};
     for (auto f : unit) {           // the failures of all units, the first one's place
         int one[4] = {0, 0, 0, 0};

@@ -57,6 +57,8 @@ struct PassArgs {
     float* part_run;                        // [2 * runs] states of the others: a run's first and last item
     int runs;
     long long wait_cycles;
+    int window, sinks;                      // (of kernels built with WIN alone)
+    const int* shortest;                    // [lanes / N] length of a group's shortest lane
 };
 
 __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad = nullptr) {
@@ -65,14 +67,37 @@ __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad 
     if (bad) *bad = b;
     return b ? 0 : len;
 }
+// With a window, a row that may see positions below `limit` sees [limit - window, limit) and the first `sinks`.  What no row of an
+// entry sees lies between those two parts and is stepped over, whole tiles of 16 tokens at a time: tokens are counted without
+// the `skip` positions from `at` on (both multiples of 16), and a place in a page is looked up at real().  Pages that lie wholly in between
+// are not even looked up.  [sinks, low): counted places that no row sees.
+template <bool WIN> struct Hole {
+    __device__ __forceinline__ int real(int pos) const { return pos; }
+};
+template <> struct Hole<true> {
+    int at, skip, low;
+    __device__ __forceinline__ int real(int pos) const { return pos >= at ? pos + skip : pos; }
+};
+
 // the tokens [lo, hi) that the rows of an entry read; behind a tile's last row nothing is seen
-__device__ __forceinline__ void token_range(const AttendArgs& a, const PassArgs& p, int entry, int b, int& lo, int& hi) {
+template <bool WIN>
+__device__ __forceinline__ void token_range(const AttendArgs& a, const PassArgs& p, int entry, int b, int& lo, int& hi, Hole<WIN>& hole) {
     const int s = p.begin ? p.begin[ASX_AT(p.prefix ? b : p.by_N.div(b), a.c.lanes / p.N, 122)] : 0;
     lo = p.prefix ? 0 : s;
     hi = p.prefix ? s : lane_len(a.c, b);
     if (!p.prefix && a.c.T > 1) {
         const int last = min(p.rows, (entry - b * p.row_tiles + 1) * p.tile_rows) - 1;
         hi = max(lo, hi - a.c.T + 1 + a.by_g.div(last));
+    }
+    if constexpr (WIN) {
+        // (the lanes of a group differ in length: the shortest one's window reaches furthest back)
+        const int first = p.prefix ? p.shortest[ASX_AT(b, a.c.lanes / p.N, 171)] - a.c.T + 1
+                                   : lane_len(a.c, b) - a.c.T + 1 + a.by_g.div((entry - b * p.row_tiles) * p.tile_rows);
+        const int low = max(0, first - p.window);
+        hole.at = max(lo, (p.sinks + 15) & ~15);
+        hole.skip = max(0, min(low & ~15, hi) - hole.at);       // (hi is cut by `low` only where it ends a page)
+        hole.low = low - hole.skip;
+        hi -= hole.skip;
     }
 }
 __device__ __forceinline__ int units_of(const PassArgs& p, int lo, int hi) { return (hi - lo + (1 << p.unit_shift) - 1) >> p.unit_shift; }
@@ -88,23 +113,31 @@ __device__ __forceinline__ size_t out_row(const AttendArgs& a, int lane0, int he
 
 // The first entry from `entry` on that has tokens: (entry, lo, hi, lane or group).  A call: it is rare, and inlined it
 // would swell every loop that moves on through the units beyond the instruction caches.
+template <bool WIN>
 __device__ __noinline__ int4 find_entry(const AttendArgs& a, const PassArgs& p, int entry) {
     int b = 0, lo = 0, hi = 0;
+    Hole<WIN> hole;
 #pragma unroll 1
     for (; entry < p.n * p.row_tiles; ++entry) {
         b = p.by_row_tiles.div(entry);
-        token_range(a, p, entry, b, lo, hi);
+        token_range(a, p, entry, b, lo, hi, hole);
         if (hi > lo) break;
     }
     return make_int4(entry, lo, hi, b);
 }
 
 // Where a CTA stands in its run of units.
+template <bool WIN>
 struct Cursor {
     int entry, head, u, nu, lo, hi, lane0, row0;    // row0: the tile's first row
+    Hole<WIN> hole;
     __device__ __forceinline__ void enter(const AttendArgs& a, const PassArgs& p) {
-        const int4 e = find_entry(a, p, entry);
+        const int4 e = find_entry<WIN>(a, p, entry);
         entry = e.x; lo = e.y; hi = e.z;
+        if constexpr (WIN) {
+            int l, h;
+            if (entry < p.n * p.row_tiles) token_range<true>(a, p, entry, e.w, l, h, hole);
+        }
         nu = units_of(p, lo, hi);
         lane0 = p.prefix ? e.w * p.N : e.w;
         row0 = (entry - e.w * p.row_tiles) * p.tile_rows;
@@ -127,18 +160,20 @@ struct RunSmem {
     int warp_sum[32];
     int start[4][3];
 };
+template <bool WIN>
 __device__ __noinline__ int entry_units(const AttendArgs& a, const PassArgs& p, int entry) {
     int lo, hi;
-    token_range(a, p, entry, p.by_row_tiles.div(entry), lo, hi);
+    Hole<WIN> hole;
+    token_range(a, p, entry, p.by_row_tiles.div(entry), lo, hi, hole);
     return units_of(p, lo, hi);
 }
-template <int NT, int WORKERS = 1>
-__device__ __forceinline__ int find_run(const AttendArgs& a, const PassArgs& p, RunSmem& sm, Cursor& cu) {
+template <int NT, int WORKERS, bool WIN>
+__device__ __forceinline__ int find_run(const AttendArgs& a, const PassArgs& p, RunSmem& sm, Cursor<WIN>& cu) {
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, n = p.n * p.row_tiles;
     const int per = (n + NT - 1) / NT, j0 = min(tid * per, n), j1 = min(j0 + per, n);
     int mine = 0;
 #pragma unroll 1
-    for (int j = j0; j < j1; ++j) mine += entry_units(a, p, j);
+    for (int j = j0; j < j1; ++j) mine += entry_units<WIN>(a, p, j);
     int incl = mine;
 #pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
@@ -165,7 +200,7 @@ __device__ __forceinline__ int find_run(const AttendArgs& a, const PassArgs& p, 
     if (start(first) < end && start(min(first + WORKERS, G)) > at) {
 #pragma unroll 1
         for (int j = j0; j < j1; ++j) {
-            const unsigned nu = entry_units(a, p, j), all = nu * a.c.heads;
+            const unsigned nu = entry_units<WIN>(a, p, j), all = nu * a.c.heads;
 #pragma unroll 1
             for (int k = 0; k < WORKERS; ++k) {
                 const unsigned x = start(first + k) - at;
@@ -256,6 +291,97 @@ __device__ __forceinline__ const typename Io<DT>::type* query_row(const AttendAr
     return static_cast<const typename Io<DT>::type*>(a.q) + ASX_AT((long long)lane0 * a.c.T + tok, (long long)a.c.lanes * a.c.T, 125) * a.q_ld + ASX_AT(head * g + row - tok * g, a.q_heads, 126) * D;
 }
 
+// A thread's quarter of a query row (null: no row) as f16 operands, to(part, step of 16 dimensions, half); the return value is the
+// power of two that they have been divided by.
+template <int DT, int D, class To>
+__device__ __forceinline__ float row_queries(const typename Io<DT>::type* src, To&& to) {
+    constexpr bool F32 = DT == AS_F32;
+    float top = 0.f, xq[D / 4];
+#pragma unroll
+    for (int e = 0; e < D / 4; ++e) xq[e] = 0.f;
+    if (src) {
+        const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
+#pragma unroll
+        for (int e = 0; e < D / 4; e += 16) Io<DT>::read16(src + e, vec, *reinterpret_cast<float(*)[16]>(&xq[e]));
+    }
+#pragma unroll
+    for (int e = 0; e < D / 4; ++e) top = fmaxf(top, fabsf(xq[e]));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+    // the row's largest magnitude is brought into [1, 2)
+    int ex = (int)(__float_as_uint(top) >> 23) - 127;
+    ex = ex > 126 ? 126 : ex < -126 ? -126 : ex;
+    const float down = __uint_as_float((uint32_t)(127 - ex) << 23), up = __uint_as_float((uint32_t)(127 + ex) << 23);
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float f0 = xq[4 * j + 2 * h] * down, f1 = xq[4 * j + 2 * h + 1] * down;
+            const uint32_t hi2 = pack_f16(f0, f1);
+            to(0, j, h) = hi2;
+            if (F32) {
+                const float2 hi = unpack_f16(hi2);
+                to(1, j, h) = pack_f16(f0 - hi.x, f1 - hi.y);
+            }
+        }
+    return up;
+}
+
+// S^T = K q^T of a tile of 16 tokens: its key codes at kb and key scales at ksb in shared memory; the thread's tokens are t0 and t0 + 2.
+template <int DT, int D, int NT, class Q>
+__device__ __forceinline__ void tile_scores(uint32_t kb, uint32_t ksb, int t0, int cc, Q&& qf, float (&s)[NT][4]) {
+    using Ti = Tile4<D>;
+    constexpr bool F32 = DT == AS_F32;
+    uint32_t kw[2][D / 32], ks[2][D / 64];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = t0 + 2 * i;
+        if (D == 128) {
+            const uint4 v = lds<uint4>(kb + ASX_AT(t * (D / 2) + cc * 16, 8 * D - 15, 133));
+            kw[i][0] = v.x; kw[i][1] = v.y; kw[i][D / 32 - 2] = v.z; kw[i][D / 32 - 1] = v.w;
+            const uint32_t s2 = e4m3_f16x2(lds<unsigned short>(ksb + ASX_AT(t * Ti::NB + 2 * cc, D - 1, 134)));
+            ks[i][0] = __byte_perm(s2, s2, 0x1010);
+            ks[i][D / 64 - 1] = __byte_perm(s2, s2, 0x3232);
+        } else {
+            const uint2 v = lds<uint2>(kb + ASX_AT(t * (D / 2) + cc * 8, 8 * D - 7, 135));
+            kw[i][0] = v.x; kw[i][1] = v.y;
+            const uint32_t s2 = e4m3_f16x2(lds<unsigned char>(ksb + ASX_AT(t * Ti::NB + cc, D, 136)));
+            ks[i][0] = __byte_perm(s2, s2, 0x1010);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+    float rest[4] = {0.f, 0.f, 0.f, 0.f};       // (32-bit queries: the sum over their second halves)
+#pragma unroll
+    for (int j = 0; j < D / 16; j += 2) {           // a word of each token is two steps of 16 dimensions
+        float part[4] = {0.f, 0.f, 0.f, 0.f};   // (32-bit queries: two steps' sum)
+        uint32_t f[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) codes_f16x2(kw[i][j / 2], f[i]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[i][e] = mul_f16(f[i][e], ks[i][j / 4]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                mma_f16(F32 ? part : s[n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf(0, n, j + h, 0), qf(0, n, j + h, 1));
+                if (F32) mma_f16(rest, f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf(1, n, j + h, 0), qf(1, n, j + h, 1));
+            }
+        if (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[0][e] += part[e];
+        }
+    }
+    if (F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[0][e] += rest[e];
+    }
+}
+
 template <int D> struct AttendSmem {
     char ring[AT_W][AT_STAGES][2 * Tile4<D>::BYTES];
     float join[AT_W][8][D + 20];            // the warps' sums (the pitch spreads rows over the banks)
@@ -282,7 +408,7 @@ template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(
 // Bound by issue slots: 364 instructions for a tile of 16 tokens at head dimension 128, conversions and products mostly
 // (60 % of the slots, ALU pipe 54 %, DRAM 52 %: no unit is full, 3.5 warps a scheduler do not hide every wait).  128 lanes of up to 8192 tokens, 32 heads on 8: 178 to 194 us (4.2 to 4.6 TB/s); in 32
 // bits, 12 lanes of up to 30001: 95 us (3.1 TB/s).
-template <int DT, int D, int NT, bool SOLO>
+template <int DT, int D, int NT, bool SOLO, bool WIN>
 __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
     constexpr bool F32 = DT == AS_F32;
@@ -295,8 +421,8 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    Cursor cu, ahead;
-    int left = find_run<AT_NT, SOLO ? AT_W : 1>(a, p, sm.run, cu), to_issue = left;
+    Cursor<WIN> cu, ahead;
+    int left = find_run<AT_NT, SOLO ? AT_W : 1, WIN>(a, p, sm.run, cu), to_issue = left;
     if (left == 0) return;
     ahead = cu;
 
@@ -307,7 +433,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     int page = 0;
     auto look = [&]() {                             // page id of the half-warp's tile under `ahead`
         const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
-        if (pos < ahead.hi) page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 127) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 128)];
+        if (pos < ahead.hi) page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 127) * c.max_pages + ASX_AT(ahead.hole.real(pos) >> c.page_shift, c.max_pages, 128)];
     };
     auto issue = [&](int stage) {
         const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
@@ -319,7 +445,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 }
                 page = 0;
             }
-            const char* src = c.pages + (((size_t)page * c.heads + ASX_AT(ahead.head, c.heads, 129)) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES + hl * 16;
+            const char* src = c.pages + (((size_t)page * c.heads + ASX_AT(ahead.head, c.heads, 129)) * tiles_per_page + ((ahead.hole.real(pos) & page_mask) >> 4)) * Ti::BYTES + hl * 16;
             const uint32_t dst = ring0 + ASX_AT((stage * 2 + half) * Ti::BYTES, (2 * AT_STAGES - 1) * Ti::BYTES + 1, 130) + hl * 16;
 #pragma unroll
             for (int i = 0; i < (Ti::BYTES / 16 + 15) / 16; ++i)
@@ -343,6 +469,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     uint32_t qf[PARTS][NT][KS][2];
     float o[NT][KS][4], m[NT][2], mu[NT][2], l[NT][2], k2[NT][2];
     int lim[NT][2], lim_min = 0;
+    int low[WIN ? NT : 1][2], low_max = 0;          // windows' first places
     int seg_u0 = 0, stage = 0;
     bool fresh = true;
 #pragma unroll 1
@@ -354,42 +481,23 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
             const float kg = c.k_scale ? c.k_scale[head] : 1.f;
             const float to_log2 = a.scale * kg * 1.44269504088896f;
             lim_min = 0x7FFFFFFF;
+            low_max = 0;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int row = row0 + n * 8 + r;
-                float top = 0.f, xq[D / 4];
-#pragma unroll
-                for (int e = 0; e < D / 4; ++e) xq[e] = 0.f;
-                if (row < p.rows) {
-                    const E* src = query_row<DT, D>(a, lane0, head, row) + cc * (D / 4);
-                    const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
-#pragma unroll
-                    for (int e = 0; e < D / 4; e += 16) Io<DT>::read16(src + e, vec, *reinterpret_cast<float(*)[16]>(&xq[e]));
-                }
-#pragma unroll
-                for (int e = 0; e < D / 4; ++e) top = fmaxf(top, fabsf(xq[e]));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                // the row's largest magnitude is brought into [1, 2)
-                int ex = (int)(__float_as_uint(top) >> 23) - 127;
-                ex = ex > 126 ? 126 : ex < -126 ? -126 : ex;
-                const float down = __uint_as_float((uint32_t)(127 - ex) << 23), up = __uint_as_float((uint32_t)(127 + ex) << 23);
-#pragma unroll
-                for (int j = 0; j < KS; ++j)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float f0 = xq[4 * j + 2 * h] * down, f1 = xq[4 * j + 2 * h + 1] * down;
-                        qf[0][n][j][h] = pack_f16(f0, f1);
-                        if (F32) {
-                            const float2 hi = unpack_f16(qf[0][n][j][h]);
-                            qf[PARTS - 1][n][j][h] = pack_f16(f0 - hi.x, f1 - hi.y);
-                        }
-                    }
+                const float up = row_queries<DT, D>(row < p.rows ? query_row<DT, D>(a, lane0, head, row) + cc * (D / 4) : nullptr, [&](int part, int j, int h) -> uint32_t& { return qf[part][n][j][h]; });
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int rw = row0 + n * 8 + 2 * cc + h;
                     k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
-                    lim[n][h] = rw < p.rows ? min(row_limit(a, lane0, rw), cu.hi) : 0;
+                    if constexpr (WIN) {
+                        const int rl = rw < p.rows ? row_limit(a, lane0, rw) : 0;
+                        lim[n][h] = rw < p.rows ? min(rl - cu.hole.skip, cu.hi) : 0;
+                        low[n][h] = max(rl - p.window, 0) - cu.hole.skip;
+                        if (rw < p.rows) low_max = max(low_max, low[n][h]);
+                    } else {
+                        lim[n][h] = rw < p.rows ? min(row_limit(a, lane0, rw), cu.hi) : 0;
+                    }
                     if (rw < p.rows) lim_min = min(lim_min, lim[n][h]);
                     m[n][h] = -INFINITY; mu[n][h] = 0.f; l[n][h] = 0.f;
                 }
@@ -399,6 +507,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
             }
             lim_min = __reduce_min_sync(0xFFFFFFFFu, lim_min);
+            if constexpr (WIN) low_max = __reduce_max_sync(0xFFFFFFFFu, low_max);
         }
         cp_wait<0>();
         __syncwarp();
@@ -414,58 +523,11 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const uint32_t sb = st + b * Ti::BYTES;
-                uint32_t kw[2][D / 32], ks[2][D / 64];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int t = t0 + 2 * i;
-                    if (D == 128) {
-                        const uint4 v = lds<uint4>(sb + Ti::K + ASX_AT(t * (D / 2) + cc * 16, 8 * D - 15, 133));
-                        kw[i][0] = v.x; kw[i][1] = v.y; kw[i][D / 32 - 2] = v.z; kw[i][D / 32 - 1] = v.w;
-                        const uint32_t s2 = e4m3_f16x2(lds<unsigned short>(sb + Ti::KS + ASX_AT(t * Ti::NB + 2 * cc, D - 1, 134)));
-                        ks[i][0] = __byte_perm(s2, s2, 0x1010);
-                        ks[i][D / 64 - 1] = __byte_perm(s2, s2, 0x3232);
-                    } else {
-                        const uint2 v = lds<uint2>(sb + Ti::K + ASX_AT(t * (D / 2) + cc * 8, 8 * D - 7, 135));
-                        kw[i][0] = v.x; kw[i][1] = v.y;
-                        const uint32_t s2 = e4m3_f16x2(lds<unsigned char>(sb + Ti::KS + ASX_AT(t * Ti::NB + cc, D, 136)));
-                        ks[i][0] = __byte_perm(s2, s2, 0x1010);
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b][n][e] = 0.f;
-                float rest[4] = {0.f, 0.f, 0.f, 0.f};       // (32-bit queries: the sum over their second halves)
-#pragma unroll
-                for (int j = 0; j < KS; j += 2) {           // a word of each token is two steps of 16 dimensions
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};   // (32-bit queries: two steps' sum)
-                    uint32_t f[2][4];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) codes_f16x2(kw[i][j / 2], f[i]);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) f[i][e] = mul_f16(f[i][e], ks[i][j / 4]);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            mma_f16(F32 ? part : s[b][n], f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[0][n][j + h][0], qf[0][n][j + h][1]);
-                            if (F32) mma_f16(rest, f[0][2 * h], f[1][2 * h], f[0][2 * h + 1], f[1][2 * h + 1], qf[PARTS - 1][n][j + h][0], qf[PARTS - 1][n][j + h][1]);
-                        }
-                    if (F32) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) s[b][0][e] += part[e];
-                    }
-                }
-                if (F32) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b][0][e] += rest[e];
-                }
+                tile_scores<DT, D, NT>(sb + Ti::K, sb + Ti::KS, t0, cc, [&](int part, int n, int j, int h) { return qf[part < PARTS ? part : 0][n][j][h]; }, s[b]);
             }
             // ---- weights ----
             bool rise = false;
-            const bool cut = pos + 32 > lim_min;
+            const bool cut = pos + 32 > lim_min || (WIN && pos < low_max && pos + 32 > p.sinks);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -475,7 +537,8 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                     for (int e = 0; e < 4; ++e) {           // tokens t0, t0 + 2 of the first tile, then of the second
                         float& x = s[e >> 1][n][2 * (e & 1) + h];
                         x *= k2[n][h];
-                        if (cut && pos + 16 * (e >> 1) + t0 + 2 * (e & 1) >= lim[n][h]) x = -INFINITY;
+                        const int at = pos + 16 * (e >> 1) + t0 + 2 * (e & 1);
+                        if (cut && (at >= lim[n][h] || (WIN && at < low[WIN ? n : 0][h] && at >= p.sinks))) x = -INFINITY;
                         top = fmaxf(top, x);
                     }
                     rise |= top > m[n][h] + AT_RISE<DT>;
@@ -543,6 +606,14 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
                 if (pos + 32 > cu.hi) {             // tokens behind the last one: whatever the page holds there counts as zero
                     const int have = cu.hi - pos - 16 * b - 4 * cc;
                     vs4 &= have >= 4 ? 0xFFFFFFFFu : have <= 0 ? 0u : (1u << (8 * have)) - 1;
+                }
+                if constexpr (WIN) {
+                    if (pos < cu.hole.low && pos + 32 > p.sinks) {          // nor do those that no row's window reaches
+                        const int at = pos + 16 * b + 4 * cc;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (at + e >= p.sinks && at + e < cu.hole.low) vs4 &= ~(0xFFu << (8 * e));
+                    }
                 }
                 const uint32_t vs[2] = {e4m3_f16x2(vs4 & 0xFFFFu), e4m3_f16x2(vs4 >> 16)};
 #pragma unroll
@@ -712,12 +783,13 @@ __device__ __forceinline__ void join_states(const PassArgs& p, size_t item, int 
     }
 }
 // the same for what the pass over shared beginnings has left for a row of a lane
-template <int D, int PER>
+template <int D, bool WIN, int PER>
 __device__ __forceinline__ void join_shared(const AttendArgs& a, const PassArgs& pre, int lane, int row, int rows, int head, int d0, float& M, float& L, float (&acc)[PER]) {
     const int gr = pre.by_N.div(lane);
     if (pre.begin[gr] == 0) return;
     const int prow = (lane - gr * pre.N) * rows + row, pt = pre.by_tile_rows.div(prow);
     const size_t item = ASX_AT(((size_t)gr * pre.row_tiles + pt) * a.c.heads + head, (long long)pre.n * pre.row_tiles * a.c.heads, 148);
+    if (WIN && entry_units<WIN>(a, pre, gr * pre.row_tiles + pt) == 0) return;      // (the windows have left the beginning behind)
     join_states<D>(pre, item, pre.first_run[item], pre.last_run[item], prow - pt * pre.tile_rows, d0, M, L, acc);
 }
 
@@ -725,7 +797,7 @@ __device__ __forceinline__ void join_shared(const AttendArgs& a, const PassArgs&
 // over CTAs or passes, in a fixed order, and writes rows that saw nothing.  Latency: 7 us for 1024 items of 4 rows.  8 or 16 rows
 // a CTA cost the chunk of 2 x 2048 tokens more CTAs that leave at once than they save (465 -> 471 and 467 us).
 constexpr int JOIN_ROWS = 32;
-template <int DT, int D>
+template <int DT, int D, bool WIN>
 __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs own, const __grid_constant__ PassArgs pre) {
     constexpr int PER = D / 32;
     const CacheArgs& c = a.c;
@@ -736,7 +808,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
 #pragma unroll 1
     for (unsigned i = blockIdx.x; i < items; i += gridDim.x) {
         const int entry = c.by_heads.div(i), head = (int)i - entry * c.heads, ln = own.by_row_tiles.div(entry);
-        const bool none = entry_units(a, own, entry) == 0;
+        const bool none = entry_units<WIN>(a, own, entry) == 0;
         const int c0 = none ? 0 : own.first_run[i], c1 = none ? -1 : own.last_run[i];
         if (!none && c0 == c1 && !own.part_item) continue;                  // the pass has written the output itself
         const int row0 = (entry - ln * own.row_tiles) * own.tile_rows;
@@ -747,7 +819,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
             float M = -INFINITY, L = 0.f, acc[PER];
 #pragma unroll
             for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-            if (pre.begin) join_shared<D>(a, pre, ln, row, own.rows, head, lane * PER, M, L, acc);
+            if (pre.begin) join_shared<D, WIN>(a, pre, ln, row, own.rows, head, lane * PER, M, L, acc);
             join_states<D>(own, i, c0, c1, rw, lane * PER, M, L, acc);
             const float inv = L == 0.f ? 0.f : (c.v_scale ? c.v_scale[head] : 1.f) / L * AT_DOWN<DT>;
             const size_t orow = out_row(a, ln, head, row);
@@ -759,18 +831,27 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     }
 }
 
-// One CTA per group: the shared beginning that can be used (0 where the caller's does not fit).
-__global__ void __launch_bounds__(128) attend_shared_kernel(const CacheArgs c, int N, const int* shared, int* begin) {
+// One CTA per group: the shared beginning that can be used (0 where the caller's does not fit), and, if `shortest` is not null, the
+// length of the group's shortest lane.
+static __global__ void __launch_bounds__(128) attend_shared_kernel(const CacheArgs c, int N, const int* shared, int* begin, int* shortest) {
     const int gr = blockIdx.x, s = shared[gr];
+    __shared__ int least;
+    if (threadIdx.x == 0) least = 0x7FFFFFFF;
+    __syncthreads();
     bool ok = s > 0 && (s & ((1 << c.page_shift) - 1)) == 0;
-    for (int j = threadIdx.x; j < N; j += 128) ok &= s <= lane_len(c, gr * N + j);
-    ok = __syncthreads_and(ok);
-    if (threadIdx.x == 0) begin[gr] = ok ? s : 0;
+    int len = 0x7FFFFFFF;
+    for (int j = threadIdx.x; j < N; j += 128) len = min(len, lane_len(c, gr * N + j));
+    atomicMin(&least, len);
+    ok = __syncthreads_and(ok && s <= len);
+    if (threadIdx.x == 0) {
+        begin[gr] = ok ? s : 0;
+        if (shortest) shortest[gr] = least;
+    }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // Lanes whose length is out of range.
-__global__ void __launch_bounds__(256) attend_status_kernel(const CacheArgs c) {
+static __global__ void __launch_bounds__(256) attend_status_kernel(const CacheArgs c) {
     for (int j = blockIdx.x * 256 + threadIdx.x; j < c.lanes; j += gridDim.x * 256) {
         bool bad;
         lane_len(c, j, &bad);

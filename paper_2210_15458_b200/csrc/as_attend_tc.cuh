@@ -31,7 +31,7 @@ __device__ __forceinline__ bool tc_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok;
 }
-__device__ __noinline__ bool tc_wait_long(uint32_t bar, uint32_t parity, long long limit, volatile int* failed) {
+static __device__ __noinline__ bool tc_wait_long(uint32_t bar, uint32_t parity, long long limit, volatile int* failed) {
     const long long start = clock64();
 #pragma unroll 1
     while (!tc_try(bar, parity)) {
@@ -87,7 +87,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return d;
 }
 // columns at .. at + 16 n of the warp's lanes, each thread's times f: 32-bit sums, or pairs of f16 weights
-__device__ __noinline__ void tc_scale_sums(uint32_t at, int n, float f) {
+static __device__ __noinline__ void tc_scale_sums(uint32_t at, int n, float f) {
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
         uint32_t o[16];
@@ -98,7 +98,7 @@ __device__ __noinline__ void tc_scale_sums(uint32_t at, int n, float f) {
         tc_st16(at + 16 * i, o);
     }
 }
-__device__ __noinline__ void tc_scale_weights(uint32_t at, int n, float f) {
+static __device__ __noinline__ void tc_scale_weights(uint32_t at, int n, float f) {
     tc_wait_st();
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
@@ -166,7 +166,7 @@ template <int D, bool DUAL> constexpr size_t tc_smem_bytes() { return 1024 + (si
 // the weights of one are formed, the products of the other run (2 x 2048 tokens over up to 8192: 498 -> 465 us;
 // 460 to 480 us in all runs, 848 to 885 TFLOP/s; nothing is busy for more than half of it, waiting is spread over softmax, filling and products).
 // The other form waits for the filling, and pieces cost it more than they give (8 x 32 codes behind shared tokens: 89.2 -> 90.1 us).
-template <int D, bool DUAL>
+template <int D, bool DUAL, bool WIN>
 __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;
     constexpr int FILL = TC_FIRST / 32, SOFT = FILL + 2 * TC_FILL / 32;     // first warps of the groups
@@ -194,8 +194,8 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
         sm.failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    Cursor cu;
-    const int run = find_run<TC_NT>(a, p, sm.run, cu);      // units of the CTA
+    Cursor<WIN> cu;
+    const int run = find_run<TC_NT, 1, WIN>(a, p, sm.run, cu);      // units of the CTA
     if (run == 0) return;
     if (w == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"((uint32_t)__cvta_generic_to_shared(&sm.tmem)) : "memory");
@@ -225,7 +225,14 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
         for (int item = 0; x < run && ok; ++item) {
             const int tiles = min(cu.nu - cu.u, run - x);
             const int row = cu.row0 + (DUAL ? 128 * s : 0) + r;
-            const int lim = row < p.rows ? min(row_limit(a, cu.lane0, row), cu.hi) : 0;
+            int lim, low = 0;                                       // (low: of the row's window)
+            if constexpr (WIN) {
+                const int rl = row < p.rows ? row_limit(a, cu.lane0, row) : 0;
+                lim = row < p.rows ? min(rl - cu.hole.skip, cu.hi) : 0;
+                low = max(rl - p.window, 0) - cu.hole.skip;
+            } else {
+                lim = row < p.rows ? min(row_limit(a, cu.lane0, row), cu.hi) : 0;
+            }
             const float vg = c.v_scale ? c.v_scale[cu.head] : 1.f;
             ok = wait_warp(sm.q_full[q_buf(item)], q_use(item) & 1);
             if (!ok) break;
@@ -245,6 +252,15 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                 const uint32_t sh = st + PIECE * hf;
                 const int left = lim - (cu.lo + (cu.u + j) * TC_KV + PIECE * hf);   // visible tokens of the piece
                 const bool cut = __any_sync(0xFFFFFFFFu, left < PIECE);
+                // places [hide, show) of the piece lie in front of the row's window and behind the sinks
+                int hide = 0, show = 0;
+                bool front = false;
+                if constexpr (WIN) {
+                    const int at = lim - left;
+                    hide = p.sinks - at;
+                    show = low - at;
+                    front = __any_sync(0xFFFFFFFFu, hide < PIECE && show > 0);
+                }
                 bool settled = false;
                 // One pass over the row, 32 columns at a time.  The running maximum hardly ever rises after the first tiles;
                 // where it does, what was written with the old one is scaled.
@@ -257,6 +273,11 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         const int have = left - 32 * ch;
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = e < have ? v[e] : 0xFF800000u;
+                    }
+                    if (WIN && front) {
+                        const int from = hide - 32 * ch, to = show - 32 * ch;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = e >= from && e < to ? 0xFF800000u : v[e];
                     }
                     float tops[4];
 #pragma unroll
@@ -397,7 +418,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
             const int page_mask = (1 << c.page_shift) - 1, tiles_per_page = 1 << (c.page_shift - 4);
             // Each thread takes its token's codes into registers a tile before they are widened, and the page's id a tile
             // before that.  They are widened from the thread's own place in shared memory, by a loop.
-            Cursor ahead = cu;
+            Cursor<WIN> ahead = cu;
             int looked = 0;
             int page = 0, next_lane = 0;
             uint4 code[D / 32];
@@ -434,8 +455,13 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                 real = next_real;
                 next_real = false;
                 if (looked < run) {
-                    const int pos = ahead.lo + ahead.u * TC_KV + r;
-                    if (pos < ahead.hi) {
+                    int pos = ahead.lo + ahead.u * TC_KV + r;
+                    bool seen = pos < ahead.hi;
+                    if constexpr (WIN) {
+                        seen = seen && !(pos >= p.sinks && pos < ahead.hole.low);
+                        pos = ahead.hole.real(pos);
+                    }
+                    if (seen) {
                         page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 159) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 160)];
                         next_base = c.pages + ((size_t)ASX_AT(ahead.head, c.heads, 161) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
                         next_lane = ahead.lane0;
@@ -463,7 +489,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
 #pragma unroll 1
             for (int item = 0; x < run && ok; ++item) {
                 const int tiles = min(cu.nu - cu.u, run - x);
-                Cursor next = cu;
+                Cursor<WIN> next = cu;
                 if (x + tiles < run) next.next_item(a, p);
                 if constexpr (keys || DUAL) {
                     // ---- the item's queries, scaled by a power of two into f16's range; a negative scale goes in here ----

@@ -15,6 +15,9 @@ struct DeviceInfo {
 };
 int device_info(const DeviceInfo** out);            // the current device's, looked up once
 
+int check_scalars(int dtype, int V, long long ld, double temp, double top_p);   // what the step calls check of their logits
+int check_data(const void* data, int dtype);
+
 long long wait_cycles_now();                        // bound on every on-device wait, in clock cycles (AS_TUNE_WAIT_KCYCLES)
 
 constexpr size_t SMEM_OPTIN_MAX = 232448;           // 227 KB per CTA on sm_100
@@ -42,6 +45,10 @@ inline cudaError_t launch_after(K kern, dim3 grid, unsigned block, size_t smem, 
 int bounds_edit(int* h_out4, int reset);
 int bounds_cache4(int* h_out4, int reset);
 int bounds_pages(int* h_out4, int reset);
+int bounds_window(int* h_out4, int reset);
+int bounds_weigh(int* h_out4, int reset);
+int bounds_evict(int* h_out4, int reset);
+int bounds_verify(int* h_out4, int reset);
 #endif
 
 }  // namespace asx

@@ -1,4 +1,4 @@
-// Pages of a cache: forking with copy of part pages, growing, compacting.
+// Pages of a cache: forking with copy of part pages, growing, trimming, compacting.
 #include "../../include/arith_sampling.h"
 #include "as_bounds.cuh"
 #include "as_host.h"
@@ -267,6 +267,64 @@ __global__ void __launch_bounds__(PL_NT) grow_kernel(const GrowArgs a, const Pag
     }
 }
 
+struct TrimArgs {
+    const int *keep, *gone, *table, *len, *ref;
+    int *table_out, *len_out, *ref_out, *lane_status;
+    int lanes, max_pages, page_size, n_pages;
+};
+
+// CTA j: lane j's new length (-1: it is left as it is), judged by the reference counts as they were; its share of the copy of those.
+__global__ void __launch_bounds__(PG_NT) trim_check_kernel(const TrimArgs a, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x;
+    if (a.ref_out != a.ref)
+        for (int i = blockIdx.x * PG_NT + tid; i < a.n_pages; i += gridDim.x * PG_NT) a.ref_out[i] = a.ref[i];
+    for (int j = blockIdx.x; j < a.lanes; j += gridDim.x) {
+        const int len = a.len[j], keep = a.keep ? a.keep[j] : len;
+        bool bad = len < 0 || len > (long long)a.max_pages * a.page_size || keep < 0;
+        const int left = min(len, keep);
+        if (!bad) {
+            const int* row = a.table + (size_t)j * a.max_pages;
+            for (int m = tid; m < pages_of(len, a.page_size); m += PG_NT) {
+                const int g = row[ASX_AT(m, a.max_pages, 217)];
+                bad |= g < -1 || g >= a.n_pages;
+                // the page that ends up as the lane's partly filled last one
+                if (!bad && left < len && left % a.page_size != 0 && m == left / a.page_size && g >= 0) bad = a.ref[g] > 1;
+            }
+        }
+        bad = __syncthreads_or(bad);
+        if (tid == 0) w.eff[j] = bad ? -1 : left;
+    }
+}
+
+// CTA j: row j of the new table, its length, and the reference counts of the pages it gives up.
+__global__ void __launch_bounds__(PG_NT) trim_table_kernel(const TrimArgs a, const PageWork w) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x;
+    for (int j = blockIdx.x; j < a.lanes; j += gridDim.x) {
+        const int left = w.eff[j], len = a.len[j];
+        const int held = left < 0 ? 0 : pages_of(len, a.page_size);
+        const int lo = a.gone ? a.gone[2 * j] : 0, hi = a.gone ? min(a.gone[2 * j + 1], left) : 0;
+        for (int m = tid; m < a.max_pages; m += PG_NT) {
+            const size_t at = (size_t)j * a.max_pages + m;
+            int g = a.table[at];
+            const long long from = (long long)m * a.page_size;
+            if (left >= 0 && (from >= left || (from >= lo && from + a.page_size <= hi))) {
+                if (m < held && g >= 0) atomicSub(&a.ref_out[ASX_AT(g, a.n_pages, 218)], 1);
+                g = -1;
+            }
+            a.table_out[at] = g;
+        }
+        __syncthreads();                    // (every thread has read len)
+        if (tid == 0) {
+            a.len_out[j] = left < 0 ? len : left;
+            if (a.lane_status) a.lane_status[j] = left < 0 ? AS_ERR_INVALID_ARG : AS_OK;
+        }
+    }
+}
+
 // One CTA: the number of pages in use, the holes below it and the pages to move there.  Two ordered scans over the reference
 // counts, latency (7 us for 1024 pages).
 __global__ void __launch_bounds__(PL_NT) compact_plan_kernel(const int* ref, int* ref_out, int n_pages, int* used_out, const PageWork w) {
@@ -413,6 +471,27 @@ int as_pages_compact(int lanes, int max_pages, int n_pages, const int32_t* d_tab
         e = launch_after(compact_table_kernel, (unsigned)(blocks < 16 * di->sms ? blocks : 16 * di->sms), 256, 0, st, d_table, d_table_out, n, n_pages, d_used, w);
     if (e == cudaSuccess && d_data && planes > 0) e = launch_copy(w, d_data, planes, plane_stride, page_bytes, n_pages, di->sms, st);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "page compact kernel launch");
+}
+
+int as_pages_trim(const int32_t* d_keep, const int32_t* d_gone, int lanes, int max_pages, int page_size, int n_pages, const int32_t* d_table,
+                  const int32_t* d_len, const int32_t* d_ref, int32_t* d_table_out, int32_t* d_len_out, int32_t* d_ref_out,
+                  int32_t* d_lane_status, void* d_work, size_t work_bytes, void* stream) {
+    int rc = check_shape(lanes, max_pages, page_size, n_pages);
+    if (rc != AS_OK) return rc;
+    if (!d_ref || !d_ref_out || (lanes > 0 && (!d_table || !d_len || !d_table_out || !d_len_out)))
+        return set_err(AS_ERR_INVALID_ARG, "a table, length or reference array is NULL");
+    if ((rc = check_work(d_work, work_bytes, lanes, lanes, n_pages)) != AS_OK) return rc;
+    const DeviceInfo* di;
+    if ((rc = device_info(&di)) != AS_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    const PageWork w = carve(d_work, lanes, lanes, n_pages);
+    TrimArgs a;
+    a.keep = d_keep; a.gone = d_gone; a.table = d_table; a.len = d_len; a.ref = d_ref;
+    a.table_out = d_table_out; a.len_out = d_len_out; a.ref_out = d_ref_out; a.lane_status = d_lane_status;
+    a.lanes = lanes; a.max_pages = max_pages; a.page_size = page_size; a.n_pages = n_pages;
+    cudaError_t e = launch_after(trim_check_kernel, lanes_grid(lanes, di->sms), PG_NT, 0, st, a, w);
+    if (e == cudaSuccess) e = launch_after(trim_table_kernel, lanes_grid(lanes, di->sms), PG_NT, 0, st, a, w);
+    return e == cudaSuccess ? AS_OK : cuda_fail(e, "page trim kernel launch");
 }
 
 }  // extern "C"

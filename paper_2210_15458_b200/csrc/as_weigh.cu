@@ -1,0 +1,108 @@
+// C-ABI entry point of the cached tokens' attention weights.
+#include "as_attend_host.cuh"
+#include "as_weigh.cuh"
+
+namespace asx {
+
+ASX_BOUNDS_READER(bounds_weigh)
+
+struct WeighPlan {
+    int *eff, *from, *begin;
+    size_t bytes;
+};
+
+// Where the scratch lies in d_work (sizes alone if it is null).
+static WeighPlan plan_weigh(int lanes, void* d_work) {
+    WeighPlan pl = {};
+    char* base = static_cast<char*>(d_work);
+    auto take = [&](size_t bytes) {
+        char* q = base ? base + pl.bytes : nullptr;
+        pl.bytes += (bytes + 255) & ~(size_t)255;
+        return q;
+    };
+    for (int** q : {&pl.eff, &pl.from, &pl.begin}) *q = reinterpret_cast<int*>(take(sizeof(int) * (size_t)lanes));
+    return pl;
+}
+
+template <int DT, int D, int NT>
+static cudaError_t launch_weigh_mma(WeighArgs& wa, int sms, cudaStream_t st) {
+    static int per_sm[64] = {0};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    auto kern = weigh_mma_kernel<DT, D, NT>;
+    if (per_sm[dev] == 0) {
+        int n = 0;
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(WeighSmem<D>));
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, WG_NT, sizeof(WeighSmem<D>));
+        if (e != cudaSuccess) return e;
+        per_sm[dev] = n > 0 ? n : 1;
+    }
+    const int ctas = per_sm[dev] * sms;
+    wa.p.runs = ctas * WG_W;
+    wa.p.unit_shift = 5;
+    return launch_after(kern, ctas, WG_NT, sizeof(WeighSmem<D>), st, wa);
+}
+
+template <int DT, int D>
+static int launch_weigh(WeighArgs& wa, int sms, cudaStream_t st) {
+    const cudaError_t e = DT == AS_BF16 && wa.p.rows > 8 ? launch_weigh_mma<DT, D, DT == AS_BF16 ? 2 : 1>(wa, sms, st) : launch_weigh_mma<DT, D, 1>(wa, sms, st);
+    return e == cudaSuccess ? AS_OK : cuda_fail(e, "weigh kernel launch");
+}
+
+}  // namespace asx
+
+using namespace asx;
+
+extern "C" {
+
+size_t as_cache4_weigh_work_bytes(const as_cache4* cache, int dtype, int lanes, int T, int q_heads) {
+    if (!cache || cache->heads < 1 || (cache->head_dim != 64 && cache->head_dim != 128) || (dtype != AS_F32 && dtype != AS_BF16)) return 0;
+    if (lanes < 1 || T < 1 || q_heads < 1 || q_heads % cache->heads) return 0;
+    if ((long long)lanes * T > (1LL << 30) || (long long)lanes * T * q_heads > 0x7FFFFFFFLL) return 0;
+    return plan_weigh(lanes, nullptr).bytes;
+}
+
+int as_cache4_weigh(const as_cache4* cache, const void* d_q, long long q_ld, int dtype, int lanes, int T, int q_heads, const float* d_lse,
+                    const int32_t* d_table, int max_pages, const int32_t* d_len, double scale, int window, int sinks, int add,
+                    const int32_t* d_first, float* d_weight, long long weight_ld, int32_t* d_lane_status, void* d_work, size_t work_bytes,
+                    void* stream) {
+    int rc = check_cache(cache);
+    if (rc != AS_OK) return rc;
+    if ((rc = check_lanes(dtype, lanes, T, d_table, max_pages, d_len, cache->page_size)) != AS_OK) return rc;
+    if ((rc = check_queries(cache, d_q, q_ld, dtype, lanes, T, q_heads, max_pages, scale)) != AS_OK) return rc;
+    if (window < 0 || sinks < 0) return set_err(AS_ERR_INVALID_ARG, "window = %d and sinks = %d must be >= 0", window, sinks);
+    if (weight_ld < 1) return set_err(AS_ERR_INVALID_ARG, "weight_ld = %lld must be >= 1", weight_ld);
+    // (the keys of 32 tokens are a warp's unit of work)
+    if (!units_fit(lanes, cache->heads, (long long)max_pages * cache->page_size, 5)) return set_err(AS_ERR_UNSUPPORTED, "lanes, heads and max_pages * page_size make more than 2^31 units of work");
+    if (lanes == 0) return AS_OK;
+    if (!d_q || !d_lse || !d_weight) return set_err(AS_ERR_INVALID_ARG, "d_q, d_lse or d_weight is NULL");
+    if (reinterpret_cast<uintptr_t>(d_q) % (dtype == AS_F32 ? 4 : 2) || (reinterpret_cast<uintptr_t>(d_lse) | reinterpret_cast<uintptr_t>(d_weight)) % 4)
+        return set_err(AS_ERR_INVALID_ARG, "d_q, d_lse or d_weight is not element-aligned");
+    if ((rc = check_scratch(d_work, work_bytes, as_cache4_weigh_work_bytes(cache, dtype, lanes, T, q_heads))) != AS_OK) return rc;
+    const DeviceInfo* di;
+    if ((rc = device_info(&di)) != AS_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    constexpr int most = 1 << 30;                   // (a lane has at most 2^30 positions)
+    const WeighPlan pl = plan_weigh(lanes, d_work);
+    WeighArgs wa = {};
+    wa.a.c = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
+    const int g = q_heads / cache->heads, win = window == 0 || window > most ? most : window, sk = sinks < most ? sinks : most;
+    cudaError_t e = launch_after(weigh_start_kernel, (unsigned)(lanes < 16 * di->sms ? lanes : 16 * di->sms), 128, 0, st, wa.a.c, (const int*)d_first, pl.eff, pl.from, pl.begin, d_weight,
+                                 weight_ld, win, sk, add != 0);
+    if (e != cudaSuccess) return cuda_fail(e, "weigh start kernel launch");
+    wa.a.c.len = pl.eff;
+    wa.a.q = d_q; wa.a.q_ld = q_ld; wa.a.q_heads = q_heads; wa.a.scale = (float)scale;
+    wa.a.by_g.set(g);
+    wa.a.by_Tg.set(T * g);
+    PassArgs& p = wa.p;
+    p.n = lanes; p.group = 1; p.N = 1; p.begin = pl.begin;
+    p.rows = p.tile_rows = T * g;
+    p.row_tiles = 1;
+    p.by_row_tiles.set(1); p.by_tile_rows.set(p.tile_rows); p.by_N.set(1);
+    p.window = win; p.sinks = sk;
+    wa.lse = d_lse; wa.first = pl.from; wa.weight = d_weight; wa.weight_ld = weight_ld; wa.add = add != 0;
+    if (dtype == AS_F32) return cache->head_dim == 64 ? launch_weigh<AS_F32, 64>(wa, di->sms, st) : launch_weigh<AS_F32, 128>(wa, di->sms, st);
+    return cache->head_dim == 64 ? launch_weigh<AS_BF16, 64>(wa, di->sms, st) : launch_weigh<AS_BF16, 128>(wa, di->sms, st);
+}
+
+}  // extern "C"

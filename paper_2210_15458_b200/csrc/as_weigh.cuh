@@ -1,0 +1,182 @@
+// Attention weights of cached tokens, summed over the rows that look at them.
+//
+// For a token t of a lane and key head: w_t = sum over query rows r of 2^(s_rt - z_r), scores s and the rows' log-sums z in units of
+// log 2.  The log-sums are known, so there is no running maximum, and a token's sum belongs to one warp or thread: nothing is joined.
+#pragma once
+#include "as_attend.cuh"
+
+namespace asx {
+
+struct WeighArgs {
+    AttendArgs a;                           // c.len: lengths that can be used (0 for a lane that is left alone)
+    PassArgs p;                             // one entry a lane; begin[lane]: its first tile that has a token to weigh
+    const float* lse;
+    const int* first;                       // [lanes] first position to weigh
+    float* weight;
+    long long weight_ld;
+    bool add;
+};
+
+// One CTA per lane: the length and beginning that the other kernels use, the lane's status, and 0 for the places that no row looks
+// at (in between the sinks and the first row's window) where sums are not added to older ones.
+static __global__ void __launch_bounds__(128) weigh_start_kernel(const CacheArgs c, const int* first, int* eff, int* from, int* begin, float* weight, long long weight_ld,
+                                                                 int window, int sinks, bool add) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    for (int b = blockIdx.x; b < c.lanes; b += gridDim.x) {
+        bool bad;
+        int len = lane_len(c, b, &bad);
+        const int f = first ? first[b] : 0;
+        bad = bad || len > weight_ld || f < 0 || f > len;
+        if (bad) len = 0;
+        if (threadIdx.x == 0) {
+            eff[b] = len;
+            from[b] = bad ? 0 : f;
+            begin[b] = bad ? 0 : f & ~15;
+            if (c.lane_status) c.lane_status[b] = bad ? AS_ERR_INVALID_ARG : AS_OK;
+        }
+        if (!add && !bad) {
+            const int lo = max(f, sinks), hi = min(len, len - c.T + 1 - window);
+            for (int h = 0; h < c.heads; ++h)
+                for (int t = lo + threadIdx.x; t < hi; t += 128) weight[((size_t)b * c.heads + h) * weight_ld + t] = 0.f;
+        }
+    }
+}
+
+// Adds what a token has got to its weight, or sets it.
+__device__ __forceinline__ void put_weight(const WeighArgs& wa, int lane, int head, int pos, int from, int len, float x) {
+    if (pos < from || pos >= len) return;
+    float* at = wa.weight + ((size_t)ASX_AT(lane, wa.a.c.lanes, 301) * wa.a.c.heads + ASX_AT(head, wa.a.c.heads, 302)) * wa.weight_ld + ASX_AT(pos, wa.weight_ld, 303);
+    *at = wa.add && pos < len - wa.a.c.T ? *at + x : x;
+}
+
+constexpr int WG_W = 4, WG_NT = 32 * WG_W;  // warps of a CTA; a unit of work is 2 tiles of 16 tokens for one of them
+constexpr int WG_STAGES = 3;                // pairs of tiles (their keys) that a warp has in flight or in use
+
+template <int D> struct WeighSmem {
+    char ring[WG_W][WG_STAGES][2 * 9 * D];  // of each tile: key codes, key scales
+    RunSmem run;
+};
+
+// A warp has a run of its own.  Scores are formed as in attention, S^T = K q^T (tokens x rows); rows beyond 8 NT are taken 8 NT at a
+// time on the same keys.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant__ WeighArgs wa) {
+    using Ti = Tile4<D>;
+    constexpr int PARTS = DT == AS_F32 ? 2 : 1;
+    extern __shared__ __align__(16) char wg_smem[];
+    WeighSmem<D>& sm = *reinterpret_cast<WeighSmem<D>*>(wg_smem);
+    const AttendArgs& a = wa.a;
+    const PassArgs& p = wa.p;
+    const CacheArgs& c = a.c;
+    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31, r = lane >> 2, cc = lane & 3;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    Cursor<true> cu, ahead;
+    int left = find_run<WG_NT, WG_W, true>(a, p, sm.run, cu), to_issue = left;
+    if (left == 0) return;
+    ahead = cu;
+
+    // ---- copies: half a warp brings in the keys of one of its two tiles; the page id is fetched a unit before ----
+    const int half = lane >> 4, hl = lane & 15;
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(&sm.ring[w][0][0]);
+    const int page_mask = (1 << c.page_shift) - 1, tiles_per_page = 1 << (c.page_shift - 4);
+    int page = 0;
+    auto look = [&]() {
+        const int pos = ahead.lo + (ahead.u * 2 + half) * 16;
+        if (pos < ahead.hi) page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 304) * c.max_pages + ASX_AT(ahead.hole.real(pos) >> c.page_shift, c.max_pages, 305)];
+    };
+    auto issue = [&](int stage) {
+        if (to_issue > 0) {
+            const int pos = ahead.lo + (ahead.u * 2 + half) * 16;
+            if (pos < ahead.hi) {
+                if (page < 0 || page >= c.n_pages) {
+                    if (hl == 0) flag_lane(c.lane_status, ahead.lane0, AS_ERR_INVALID_ARG);
+                    page = 0;
+                }
+                const char* src = c.pages + (((size_t)page * c.heads + ASX_AT(ahead.head, c.heads, 306)) * tiles_per_page + ((ahead.hole.real(pos) & page_mask) >> 4)) * Ti::BYTES + hl * 16;
+                const uint32_t dst = ring0 + ASX_AT((stage * 2 + half) * 9 * D, (2 * WG_STAGES - 1) * 9 * D + 1, 307) + hl * 16;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) cp_async16(dst + i * 256, src + Ti::K + i * 256);
+                if (hl < D / 16) cp_async16(dst + 8 * D, src + Ti::KS);
+            }
+            if (--to_issue > 0) {
+                ahead.step(a, p);
+                look();
+            }
+        }
+        cp_commit();
+    };
+    look();
+#pragma unroll
+    for (int i = 0; i < WG_STAGES - 1; ++i) issue(i);
+
+    uint32_t qf[PARTS][NT][D / 16][2];
+    float k2[NT][2], z[NT][2];
+    int lim[NT][2], low[NT][2];
+    const int row_tiles = (p.rows + 8 * NT - 1) / (8 * NT);
+    const int t0 = 4 * (r >> 1) + (r & 1);          // the thread's tokens of a tile: t0 and t0 + 2
+    int stage = 0;
+    bool fresh = true;
+#pragma unroll 1
+    for (; left > 0; --left) {
+        cp_wait<WG_STAGES - 2>();
+        __syncwarp();
+        issue(stage == 0 ? WG_STAGES - 1 : stage - 1);
+        const int pos = cu.lo + cu.u * 32;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};        // tokens t0, t0 + 2 of the first tile, then of the second
+#pragma unroll 1
+        for (int rt = 0; rt < row_tiles; ++rt) {
+            if (fresh || row_tiles > 1) {           // ---- these rows' queries ----
+                fresh = false;
+                const float to_log2 = a.scale * (c.k_scale ? c.k_scale[cu.head] : 1.f) * 1.44269504088896f;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int row = (rt * NT + n) * 8 + r;
+                    const float up = row_queries<DT, D>(row < p.rows ? query_row<DT, D>(a, cu.lane0, cu.head, row) + cc * (D / 4) : nullptr,
+                                                        [&](int part, int j, int h) -> uint32_t& { return qf[part][n][j][h]; });
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int rw = (rt * NT + n) * 8 + 2 * cc + h;
+                        k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
+                        const float lse = rw < p.rows ? wa.lse[out_row(a, cu.lane0, cu.head, rw)] : -INFINITY;
+                        const int rl = lse == -INFINITY ? 0 : row_limit(a, cu.lane0, rw);
+                        z[n][h] = lse * 1.44269504088896f;
+                        lim[n][h] = lse == -INFINITY ? -1 : min(rl - cu.hole.skip, cu.hi);
+                        low[n][h] = max(rl - p.window, 0) - cu.hole.skip;
+                    }
+                }
+            }
+            const uint32_t st = ring0 + ASX_AT(stage, WG_STAGES, 308) * 2 * 9 * D;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                float s[NT][4];
+                tile_scores<DT, D, NT>(st + b * 9 * D, st + b * 9 * D + 8 * D, t0, cc, [&](int part, int n, int j, int h) { return qf[part < PARTS ? part : 0][n][j][h]; }, s);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {   // (token t0 + 2 (e / 2), row e mod 2)
+                        const int at = pos + 16 * b + t0 + 2 * (e >> 1);
+                        const float x = ex2(s[n][e] * k2[n][e & 1] - z[n][e & 1]);
+                        const bool seen = at < lim[n][e & 1] && (at >= low[n][e & 1] || at < p.sinks);
+                        sum[2 * b + (e >> 1)] += seen ? x : 0.f;
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sum[i] += __shfl_xor_sync(0xFFFFFFFFu, sum[i], 1);
+            sum[i] += __shfl_xor_sync(0xFFFFFFFFu, sum[i], 2);
+        }
+        const float mine = cc == 0 ? sum[0] : cc == 1 ? sum[1] : cc == 2 ? sum[2] : sum[3];
+        const int at = pos + 16 * (cc >> 1) + t0 + 2 * (cc & 1);
+        if (at < cu.hi) put_weight(wa, cu.lane0, cu.head, cu.hole.real(at), wa.first[cu.lane0], c.len[cu.lane0], mine);
+        __syncwarp();
+        if (++stage == WG_STAGES) stage = 0;
+        if (cu.u + 1 == cu.nu) fresh = true;
+        cu.step(a, p);
+    }
+    cp_wait<0>();
+}
+
+}  // namespace asx
