@@ -1,18 +1,26 @@
 // C-ABI entry point of the cached tokens' attention weights.
 #include "as_attend_host.cuh"
 #include "as_weigh.cuh"
+#include "as_weigh_tc.cuh"
 
 namespace asx {
 
 ASX_BOUNDS_READER(bounds_weigh)
 
+// bf16 rows beyond 16 go to the tensor cores' 128-row tiles; up to 16 fit the instructions on registers.  32-bit ones stay there
+// whatever their number: an f16 operand holds half of one.
+static bool many_rows(int dtype, int rows) { return dtype == AS_BF16 && rows > 16; }
+
 struct WeighPlan {
-    int *eff, *from, *begin;
+    int *eff, *from, *begin, *steps;
+    char* tiles;
+    float* part;
+    int4* info;
     size_t bytes;
 };
 
 // Where the scratch lies in d_work (sizes alone if it is null).
-static WeighPlan plan_weigh(int lanes, void* d_work) {
+static WeighPlan plan_weigh(int dtype, int lanes, int T, int heads, int q_heads, int D, void* d_work) {
     WeighPlan pl = {};
     char* base = static_cast<char*>(d_work);
     auto take = [&](size_t bytes) {
@@ -21,6 +29,13 @@ static WeighPlan plan_weigh(int lanes, void* d_work) {
         return q;
     };
     for (int** q : {&pl.eff, &pl.from, &pl.begin}) *q = reinterpret_cast<int*>(take(sizeof(int) * (size_t)lanes));
+    const int rows = T * (q_heads / heads);
+    if (many_rows(dtype, rows)) {
+        pl.steps = reinterpret_cast<int*>(take(sizeof(int) * (size_t)lanes));
+        pl.part = reinterpret_cast<float*>(take(sizeof(float) * 2 * WT_MAX_RUNS * TC_KV));
+        pl.info = reinterpret_cast<int4*>(take(sizeof(int4) * WT_MAX_RUNS));
+        pl.tiles = take((size_t)lanes * heads * ((rows + WT_ROWS - 1) / WT_ROWS) * (D == 128 ? WT_TILE<128> : WT_TILE<64>));
+    }
     return pl;
 }
 
@@ -43,9 +58,37 @@ static cudaError_t launch_weigh_mma(WeighArgs& wa, int sms, cudaStream_t st) {
     return launch_after(kern, ctas, WG_NT, sizeof(WeighSmem<D>), st, wa);
 }
 
+template <int D>
+static cudaError_t launch_weigh_tc(const WeighArgs& wa, const WeighPlan& pl, int sms, cudaStream_t st) {
+    static bool attr_set[64] = {false};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (!attr_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(weigh_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)weigh_tc_smem<D>());
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    WeighTcArgs t;
+    t.w = wa;
+    t.w.p.wait_cycles = wait_cycles_now();
+    t.tiles = pl.tiles; t.steps = pl.steps; t.part = pl.part; t.info = pl.info;
+    t.row_tiles = (wa.p.rows + WT_ROWS - 1) / WT_ROWS;
+    t.runs = sms < WT_MAX_RUNS ? sms : WT_MAX_RUNS;
+    const int lanes = wa.a.c.lanes;
+    const long long items = (long long)lanes * wa.a.c.heads * t.row_tiles;
+    cudaError_t e = launch_after(weigh_steps_kernel, (unsigned)(lanes < 16 * sms ? lanes : 16 * sms), 128, 0, st, t, pl.steps);
+    if (e == cudaSuccess) e = launch_after(weigh_rows_kernel<D>, (unsigned)(items < 64 * sms ? items : 64 * sms), 256, 0, st, t);
+    if (e == cudaSuccess) e = launch_after(weigh_tc_kernel<D>, t.runs, WT_NT, weigh_tc_smem<D>(), st, t);
+    if (e == cudaSuccess) e = launch_after(weigh_join_kernel, t.runs, TC_KV, 0, st, t);
+    return e;
+}
+
 template <int DT, int D>
-static int launch_weigh(WeighArgs& wa, int sms, cudaStream_t st) {
-    const cudaError_t e = DT == AS_BF16 && wa.p.rows > 8 ? launch_weigh_mma<DT, D, DT == AS_BF16 ? 2 : 1>(wa, sms, st) : launch_weigh_mma<DT, D, 1>(wa, sms, st);
+static int launch_weigh(WeighArgs& wa, const WeighPlan& pl, int sms, cudaStream_t st) {
+    cudaError_t e;
+    if (many_rows(DT, wa.p.rows)) e = launch_weigh_tc<D>(wa, pl, sms, st);
+    else if (DT == AS_BF16 && wa.p.rows > 8) e = launch_weigh_mma<DT, D, DT == AS_BF16 ? 2 : 1>(wa, sms, st);
+    else e = launch_weigh_mma<DT, D, 1>(wa, sms, st);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "weigh kernel launch");
 }
 
@@ -59,7 +102,7 @@ size_t as_cache4_weigh_work_bytes(const as_cache4* cache, int dtype, int lanes, 
     if (!cache || cache->heads < 1 || (cache->head_dim != 64 && cache->head_dim != 128) || (dtype != AS_F32 && dtype != AS_BF16)) return 0;
     if (lanes < 1 || T < 1 || q_heads < 1 || q_heads % cache->heads) return 0;
     if ((long long)lanes * T > (1LL << 30) || (long long)lanes * T * q_heads > 0x7FFFFFFFLL) return 0;
-    return plan_weigh(lanes, nullptr).bytes;
+    return plan_weigh(dtype, lanes, T, cache->heads, q_heads, cache->head_dim, nullptr).bytes;
 }
 
 int as_cache4_weigh(const as_cache4* cache, const void* d_q, long long q_ld, int dtype, int lanes, int T, int q_heads, const float* d_lse,
@@ -83,7 +126,7 @@ int as_cache4_weigh(const as_cache4* cache, const void* d_q, long long q_ld, int
     if ((rc = device_info(&di)) != AS_OK) return rc;
     cudaStream_t st = (cudaStream_t)stream;
     constexpr int most = 1 << 30;                   // (a lane has at most 2^30 positions)
-    const WeighPlan pl = plan_weigh(lanes, d_work);
+    const WeighPlan pl = plan_weigh(dtype, lanes, T, cache->heads, q_heads, cache->head_dim, d_work);
     WeighArgs wa = {};
     wa.a.c = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
     const int g = q_heads / cache->heads, win = window == 0 || window > most ? most : window, sk = sinks < most ? sinks : most;
@@ -101,8 +144,8 @@ int as_cache4_weigh(const as_cache4* cache, const void* d_q, long long q_ld, int
     p.by_row_tiles.set(1); p.by_tile_rows.set(p.tile_rows); p.by_N.set(1);
     p.window = win; p.sinks = sk;
     wa.lse = d_lse; wa.first = pl.from; wa.weight = d_weight; wa.weight_ld = weight_ld; wa.add = add != 0;
-    if (dtype == AS_F32) return cache->head_dim == 64 ? launch_weigh<AS_F32, 64>(wa, di->sms, st) : launch_weigh<AS_F32, 128>(wa, di->sms, st);
-    return cache->head_dim == 64 ? launch_weigh<AS_BF16, 64>(wa, di->sms, st) : launch_weigh<AS_BF16, 128>(wa, di->sms, st);
+    if (dtype == AS_F32) return cache->head_dim == 64 ? launch_weigh<AS_F32, 64>(wa, pl, di->sms, st) : launch_weigh<AS_F32, 128>(wa, pl, di->sms, st);
+    return cache->head_dim == 64 ? launch_weigh<AS_BF16, 64>(wa, pl, di->sms, st) : launch_weigh<AS_BF16, 128>(wa, pl, di->sms, st);
 }
 
 }  // extern "C"
