@@ -281,8 +281,616 @@ __global__ void __launch_bounds__(VF_NT) verify_finish_kernel(const __grid_const
     }
 }
 
+// ---------------------------------------------------------------------------
+// Without a cut: a cluster of CTAs to a lane (one CTA where the lanes are many), from the first row to the last token.
+//
+// A decision needs u q(x) < p(x), that is the rows' sums, and those only as exactly as it takes: rows are read once, in 32 bits, with a
+// running maximum, and where the two sides are then within VN_NEAR of each other the pair is read again in 64 bits.  Rows behind
+// the first refusal are not read.  The last row pair is read once in 64 bits: with w near Zp / Zq from the sums in 32, every token but
+// those within VN_NEAR of e_p = w e_q is known to have p > q or not, and
+//   sum of max(p - q, 0) over a chunk = A / Zp - B / Zq,   A, B the masses of its tokens with p > q;
+// the few others are listed and added once Zp and Zq are known.
+// ---------------------------------------------------------------------------
+constexpr int VN_NT = 256, VN_NW = VN_NT / 32;
+constexpr int VN_CHUNKS = 128;              // of a CTA
+constexpr int VN_LIST = 256;
+constexpr int VN_BATCH = 8;                 // places whose rows are read before the decisions are taken
+constexpr int VN_MAX_CTAS = 8;
+// Of a sum in 32 bits: terms are off by 2^-22 (the exponential) and 2^-23 of their exponent, at most 90 before they vanish; 32 of
+// them are added up before 64 bits take over (2^-19): 2^-16 in all, and two sums to a ratio.
+constexpr double VN_NEAR = 1.0 / 16384;
+
+struct RowSum { double s; float m; int bad; };
+struct PairSum { double zp, zq; int listed, pad; };
+
+struct VerifySmem {
+    RowSum warp[2 * VN_BATCH][VN_NW];
+    RowSum mine[2 * VN_BATCH];              // of the CTA's part of each row
+    RowSum row[2 * VN_BATCH];
+    PairSum part, warp_pair[VN_NW];
+    double a[VN_CHUNKS + 1], b[VN_CHUNKS + 1];
+    double sub[VN_NW];                      // (of the chosen chunk)
+    double list_p[VN_LIST], list_q[VN_LIST];
+    int list_j[VN_LIST], order[VN_LIST];
+    int listed;
+    double exp_tbl[64];
+    double rest;                            // mass of max(p - q, 0) in the CTA's chunks
+    int at, status, chunk, force_last;
+};
+
+__device__ __forceinline__ void cluster_sync(int ctas) {
+    if (ctas == 1) {
+        __syncthreads();
+    } else {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+}
+// an object of another CTA of the cluster at the place that it has in this one
+template <class V>
+__device__ __forceinline__ V peer(const V& mine, int rank, int ctas) {
+    if (ctas == 1) return mine;
+    V got;
+    uint32_t at, *to = reinterpret_cast<uint32_t*>(&got);
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(&mine)), "r"(rank));
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(V) / 4; ++i) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(to[i]) : "r"(at + 4 * i));
+    return got;
+}
+
+// A row as 16-byte granules from the boundary at or below its start: element e of granule g is token g E + e - off.
+template <int DT>
+struct Granules {
+    static constexpr int E = Traits<DT>::E;
+    const char* from;
+    int off, n;
+    __device__ __forceinline__ Granules(const char* row, int V) {
+        const int low = (int)(reinterpret_cast<uintptr_t>(row) & 15);
+        from = row - low;
+        off = low / Traits<DT>::BYTES;
+        n = (off + V + E - 1) / E;
+    }
+    __device__ __forceinline__ uint4 load(int g) const { return __ldg(reinterpret_cast<const uint4*>(from) + g); }
+    // the same with -inf outside the row
+    __device__ __forceinline__ void masked(int g, int V, uint4& q) const {
+        if (g > 0 && (g + 1) * E - off <= V) return;
+        uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int j = g * E + e - off;
+            if (j >= 0 && j < V) continue;
+            if constexpr (DT == DT_F32) w[e] = 0xFF800000u;
+            else w[e / 2] = (w[e / 2] & (e & 1 ? 0x0000FFFFu : 0xFFFF0000u)) | (e & 1 ? 0xFF800000u : 0x0000FF80u);
+        }
+    }
+};
+
+__device__ __forceinline__ uint64_t two(float lo, float hi) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ float2 both(uint64_t x) {
+    float2 d;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(x));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+__device__ __forceinline__ RowSum join_sums(const RowSum& a, const RowSum& b, float c) {
+    RowSum r;
+    r.bad = a.bad | b.bad;
+    r.m = fmaxf(a.m, b.m);
+    r.s = (a.m == -INFINITY ? 0.0 : a.s * (double)ex2_approx((a.m - r.m) * c)) + (b.m == -INFINITY ? 0.0 : b.s * (double)ex2_approx((b.m - r.m) * c));
+    return r;
+}
+
+// The CTA's part (granules rank, rank + ctas, ... of 4 VN_NT each) of a row's maximum and sum; a warp's goes to out[warp].
+template <int DT>
+__device__ __forceinline__ void row_sum(const char* row, int V, float c, int rank, int ctas, RowSum* out) {
+    constexpr int E = Traits<DT>::E, U = 4;
+    using P = Pass<DT>;
+    const Granules<DT> g(row, V);
+    typename P::Acc acc = P::init();
+    float m = -INFINITY;
+    double s = 0.0;
+    const uint64_t cc = two(c, c);
+#pragma unroll 1
+    for (int g0 = rank * U * VN_NT + threadIdx.x; g0 < g.n; g0 += ctas * U * VN_NT) {
+        uint4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = g0 + u * VN_NT;
+            q[u] = at < g.n ? g.load(at) : DT == DT_F32 ? make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (g0 + u * VN_NT < g.n) g.masked(g0 + u * VN_NT, V, q[u]);
+        typename P::Acc now = P::reduce(q[0]);
+#pragma unroll
+        for (int u = 1; u < U; ++u) P::fold(now, q[u]);
+        P::merge(acc, now);
+        const float top = P::part_max(now);
+        if (top > m) {
+            s *= (double)ex2_approx((m - top) * c);     // (0 before the first)
+            m = top;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        const uint64_t mm = two(-ref, -ref);
+        uint64_t sum[2] = {0, 0};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[E];
+            P::floats(q[u], x);
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                // (the difference first: its rounding is that of a small number)
+                const float2 y = both(mul_two(add_two(two(x[e], x[e + 1]), mm), cc));
+                sum[e / 2 & 1] = add_two(sum[e / 2 & 1], two(ex2_approx(y.x), ex2_approx(y.y)));
+            }
+        }
+        const float2 t = both(add_two(sum[0], sum[1]));
+        s += (double)(t.x + t.y);
+    }
+    uint32_t k0, k1;
+    P::keys(acc, k0, k1);
+    RowSum r;
+    r.bad = max(k0, k1) >= Traits<DT>::KEY_PINF || min(k0, k1) < Traits<DT>::KEY_NINF;      // +inf or a NaN
+    r.m = m;
+    r.s = s;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        RowSum other;
+        other.s = __shfl_xor_sync(FULL, r.s, o);
+        other.m = __shfl_xor_sync(FULL, r.m, o);
+        other.bad = __shfl_xor_sync(FULL, r.bad, o);
+        r = join_sums(r, other, c);
+    }
+    if ((threadIdx.x & 31) == 0) out[threadIdx.x >> 5] = r;
+}
+
+// e of a logit of a row with maximum m; c64 = 64 log2(e) / temp
+__device__ __forceinline__ double mass64(float x, double c64, double m, const double* tbl) { return exp2_64th(((double)x - m) * c64, tbl); }
+
+// The last row pair of a lane (q.from null: p alone).
+template <int DT>
+struct LastPair {
+    static constexpr int E = Traits<DT>::E;
+    Granules<DT> p;
+    const char* q;                          // the draft's row
+    bool q_vec;                             // both rows lie alike on the granules
+    double mp, mq, c64;
+    int V, drop, R, per, c0, c1;            // R: sub-rows of 32 granules of a chunk; the CTA's chunks [c0, c1)
+    const double* tbl;
+    __device__ __forceinline__ LastPair(const VerifyArgs& a, const char* prow, const char* qrow, float mp_, float mq_, int drop_, double c64_, int rank, int ctas, const double* tbl_)
+        : p(prow, a.V), q(qrow), mp(mp_), mq(mq_), c64(c64_), V(a.V), drop(drop_), tbl(tbl_) {
+        q_vec = qrow && Granules<DT>(qrow, a.V).off == p.off;
+        const int rows = (p.n + 31) / 32;
+        R = (rows + ctas * (VN_CHUNKS / 2) - 1) / (ctas * (VN_CHUNKS / 2));
+        const int chunks = (rows + R - 1) / R;
+        per = (chunks + ctas - 1) / ctas;
+        c0 = min(rank * per, chunks);
+        c1 = min(c0 + per, chunks);
+    }
+    // masses of granule g's tokens (0 outside the row)
+    __device__ __forceinline__ void masses(int g, double (&ep)[E], double (&eq)[E]) const {
+        if (g >= p.n) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) ep[e] = eq[e] = 0.0;
+            return;
+        }
+        float x[E];
+        uint4 v = p.load(g);
+        p.masked(g, V, v);
+        Pass<DT>::floats(v, x);
+        float y[E];
+        if (q) {
+            if (q_vec) {
+                const Granules<DT> qg(q, V);
+                v = qg.load(g);
+                qg.masked(g, V, v);
+                Pass<DT>::floats(v, y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int j = g * E + e - p.off;
+                    y[e] = j >= 0 && j < V ? Pass<DT>::load_f(q, j) : -INFINITY;
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            ep[e] = g * E + e - p.off == drop ? 0.0 : mass64(x[e], c64, mp, tbl);
+            eq[e] = q ? mass64(y[e], c64, mq, tbl) : 0.0;
+        }
+    }
+};
+
+// Once over the CTA's chunks of the pair: their masses of tokens with p > q, the rows' sums, the list.  near = 0: w is exact.
+template <int DT>
+__device__ __forceinline__ void pair_pass(VerifySmem& sm, const LastPair<DT>& l, double w, double near) {
+    constexpr int E = Traits<DT>::E;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) sm.listed = 0;
+    __syncthreads();
+    double zp = 0.0, zq = 0.0;
+#pragma unroll 1
+    for (int ci = l.c0 + warp; ci < l.c1; ci += VN_NW) {
+        double A = 0.0, Bq = 0.0, cp = 0.0, cq = 0.0;
+#pragma unroll 1
+        for (int r = 0; r < l.R; ++r) {
+            const int g = (ci * l.R + r) * 32 + lane;
+            double ep[E], eq[E];
+            l.masses(g, ep, eq);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                cp += ep[e];
+                cq += eq[e];
+                const double d = fma(-w, eq[e], ep[e]);
+                if (near > 0.0 && fabs(d) <= near * ep[e] && ep[e] > 0.0 && eq[e] > 0.0) {
+                    const int at = atomicAdd(&sm.listed, 1);
+                    if (at < VN_LIST) { sm.list_p[at] = ep[e]; sm.list_q[at] = eq[e]; sm.list_j[at] = g * E + e; }
+                } else if (d > 0.0) {
+                    A += ep[e];
+                    Bq += eq[e];
+                }
+            }
+        }
+        A = warp_sum_d(A);
+        Bq = warp_sum_d(Bq);
+        zp += cp;
+        zq += cq;
+        if (lane == 0) { sm.a[ASX_AT(ci - l.c0, VN_CHUNKS, 343)] = A; sm.b[ci - l.c0] = Bq; }
+    }
+    zp = warp_sum_d(zp);
+    zq = warp_sum_d(zq);
+    if (lane == 0) { sm.warp_pair[warp].zp = zp; sm.warp_pair[warp].zq = zq; }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        PairSum t = {0.0, 0.0, sm.listed, 0};
+        for (int i = 0; i < VN_NW; ++i) { t.zp += sm.warp_pair[i].zp; t.zq += sm.warp_pair[i].zq; }
+        sm.part = t;
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_constant__ VerifyArgs a, int ctas, int batch) {
+    constexpr int E = Traits<DT>::E;
+    extern __shared__ __align__(16) char vn_smem[];
+    VerifySmem& sm = *reinterpret_cast<VerifySmem*>(vn_smem);
+    const int tid = threadIdx.x, lane32 = tid & 31, warp = tid >> 5;
+    const int rank = ctas == 1 ? 0 : (int)(blockIdx.x % ctas);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    fill_exp_table(sm.exp_tbl, tid);
+    __syncthreads();
+    const double c64 = 64.0 * 1.4426950408889634 * a.inv_tau;
+    const float c = (float)fmin(1.4426950408889634 * a.inv_tau, 3e38);
+#pragma unroll 1
+    for (int lane = blockIdx.x / ctas; lane < a.lanes; lane += gridDim.x / ctas) {
+        const int n = drafts_of(a, lane);
+        const double c_in = a.codes[lane];
+        int at = max(n, 0), status = n < 0 ? AS_ERR_INVALID_ARG : !(c_in >= 0.0 && c_in <= 1.0) ? AS_ERR_NUMERIC : AS_OK;
+        bool refused = false, exact = false;
+        RowSum rp = {1.0, 0.f, 0}, rq = {1.0, 0.f, 0};
+        // (a bad code ends the lane whatever its rows hold; but rows' errors and drafted tokens' come first where both are there)
+        int i0 = 0;
+        bool done = n < 0;
+#pragma unroll 1
+        while (!done) {
+            const int count = min(batch, n + 1 - i0);
+#pragma unroll 1
+            for (int b = 0; b < count; ++b) {
+                row_sum<DT>(target_row(a, lane, i0 + b), a.V, c, rank, ctas, sm.warp[2 * b]);
+                if (a.draft && i0 + b < n) row_sum<DT>(draft_row(a, lane, i0 + b), a.V, c, rank, ctas, sm.warp[2 * b + 1]);
+            }
+            __syncthreads();
+            if (tid < 2 * count && (tid % 2 == 0 || (a.draft && i0 + tid / 2 < n))) {
+                RowSum r = sm.warp[tid][0];
+                for (int i = 1; i < VN_NW; ++i) r = join_sums(r, sm.warp[tid][i], c);
+                sm.mine[tid] = r;
+            }
+            cluster_sync(ctas);
+            if (warp == 0) {
+                // a thread to a place
+                int what = 0;
+                RowSum p = {1.0, 0.f, 0}, q = {1.0, 0.f, 0};
+                const int i = i0 + lane32;
+                if (lane32 < count) {
+                    p = peer(sm.mine[2 * lane32], 0, ctas);
+                    for (int k = 1; k < ctas; ++k) p = join_sums(p, peer(sm.mine[2 * lane32], k, ctas), c);
+                    if (a.draft && i < n) {
+                        q = peer(sm.mine[2 * lane32 + 1], 0, ctas);
+                        for (int k = 1; k < ctas; ++k) q = join_sums(q, peer(sm.mine[2 * lane32 + 1], k, ctas), c);
+                    }
+                    sm.row[2 * lane32] = p;
+                    sm.row[2 * lane32 + 1] = q;
+                    // 0 accepted, 1 refused, 2 too near, 3 the last place; else an error
+                    const bool p_bad = p.bad || p.m == -INFINITY, q_bad = q.bad || q.m == -INFINITY;
+                    if (i == n) {
+                        what = p_bad ? AS_ERR_NUMERIC : 3;
+                    } else {
+                        const int x = a.drafted[(size_t)lane * a.K + i];
+                        const double u = a.u[(size_t)lane * a.K + i];
+                        if (x < 0 || x >= a.V) {
+                            what = AS_ERR_INVALID_ARG;
+                        } else if (!(u >= 0.0 && u < 1.0) || p_bad || q_bad) {
+                            what = AS_ERR_NUMERIC;
+                        } else {
+                            const double px = mass64(Pass<DT>::load_f(target_row(a, lane, i), x), c64, p.m, sm.exp_tbl) / p.s;
+                            const double qx = u * (a.draft ? mass64(Pass<DT>::load_f(draft_row(a, lane, i), x), c64, q.m, sm.exp_tbl) / q.s : 1.0);
+                            // (a side that is 0 is so whatever the sums)
+                            what = px > 0.0 && qx > 0.0 && fabs(qx - px) <= VN_NEAR * fmax(qx, px) ? 2 : qx < px ? 0 : 1;
+                        }
+                    }
+                }
+                const unsigned stop = __ballot_sync(FULL, what != 0);
+                const int l = stop ? __ffs(stop) - 1 : 0;
+                what = stop ? __shfl_sync(FULL, what, l) : 0;
+                if (lane32 == 0) { sm.at = l; sm.status = what; }
+            }
+            __syncthreads();
+            const int what = sm.status, l = sm.at;
+            rp = sm.row[2 * l];
+            rq = sm.row[2 * l + 1];
+            if (what == 0) {
+                i0 += count;
+            } else if (what == 2) {         // once more in 64 bits
+                const int i = i0 + l;
+                const LastPair<DT> pair(a, target_row(a, lane, i), a.draft ? draft_row(a, lane, i) : nullptr, rp.m, rq.m, -1, c64, rank, ctas, sm.exp_tbl);
+                cluster_sync(ctas);         // (the other CTAs have read this one's sums)
+                pair_pass<DT>(sm, pair, 0.0, 0.0);
+                cluster_sync(ctas);
+                double zp = 0.0, zq = 0.0;
+                for (int k = 0; k < ctas; ++k) {
+                    const PairSum t = peer(sm.part, k, ctas);
+                    zp += t.zp;
+                    zq += t.zq;
+                }
+                const int x = a.drafted[(size_t)lane * a.K + i];
+                const double px = mass64(Pass<DT>::load_f(target_row(a, lane, i), x), c64, pair.mp, sm.exp_tbl) / zp;
+                const double qx = a.draft ? mass64(Pass<DT>::load_f(draft_row(a, lane, i), x), c64, pair.mq, sm.exp_tbl) / zq : 1.0;
+                if (a.u[(size_t)lane * a.K + i] * qx < px) {
+                    i0 = i + 1;
+                } else {
+                    at = i;
+                    refused = done = exact = true;
+                    rp.s = zp;
+                    rq.s = zq;
+                }
+            } else {
+                at = i0 + l;
+                refused = what == 1;
+                if (what < 0) status = status == AS_ERR_INVALID_ARG ? status : what;
+                done = true;
+            }
+            cluster_sync(ctas);             // (sums that others read are written anew)
+        }
+
+        int token = -1;
+        double code = c_in;
+        if (status == AS_OK) {
+            const bool pairs = refused && a.draft;
+            const int drop = refused && !a.draft ? a.drafted[(size_t)lane * a.K + at] : -1;
+            LastPair<DT> l(a, target_row(a, lane, at), pairs ? draft_row(a, lane, at) : nullptr, rp.m, rq.m, drop, c64, rank, ctas, sm.exp_tbl);
+            double w = pairs ? rp.s / rq.s : 0.0, near = pairs && !exact ? VN_NEAR : 0.0, ratio = 0.0, total = 0.0;
+            // Once; again with the exact w if the list ran over; once more with p alone where nothing is left of p - q.
+#pragma unroll 1
+            for (int turn = 0; turn < 3; ++turn) {
+                pair_pass<DT>(sm, l, w, near);
+                cluster_sync(ctas);
+                double zp = 0.0, zq = 0.0;
+                int most = 0;
+                for (int k = 0; k < ctas; ++k) {
+                    const PairSum t = peer(sm.part, k, ctas);
+                    zp += t.zp;
+                    zq += t.zq;
+                    most = max(most, t.listed);
+                }
+                ratio = l.q ? zp / zq : 0.0;
+                if (most > VN_LIST) {
+                    cluster_sync(ctas);
+                    w = ratio;
+                    near = 0.0;
+                    continue;
+                }
+                // ---- chunks' masses of max(p - q, 0) in units of 1 / Zp; listed tokens in the order of their indices ----
+                const int chunks = l.c1 - l.c0, listed = near > 0.0 ? sm.listed : 0;
+                for (int i = tid; i < chunks; i += VN_NT) sm.a[i] = sm.a[i] > 0.0 ? fmax(fma(-ratio, sm.b[i], sm.a[i]), 0.0) : 0.0;
+                for (int i = tid; i < listed; i += VN_NT) {
+                    int before = 0;
+                    for (int k = 0; k < listed; ++k) before += sm.list_j[k] < sm.list_j[i];
+                    sm.order[ASX_AT(before, VN_LIST, 344)] = i;
+                }
+                __syncthreads();
+                const int width = 32 * l.R * E;
+                for (int i = tid; i < listed; i += VN_NT) {
+                    const int mine = sm.list_j[sm.order[i]] / width;
+                    if (i > 0 && sm.list_j[sm.order[i - 1]] / width == mine) continue;
+                    double more = 0.0;
+                    for (int k = i; k < listed && sm.list_j[sm.order[k]] / width == mine; ++k)
+                        more += fmax(fma(-ratio, sm.list_q[sm.order[k]], sm.list_p[sm.order[k]]), 0.0);
+                    sm.a[ASX_AT(mine - l.c0, VN_CHUNKS, 345)] += more;
+                }
+                __syncthreads();
+                if (warp == 0) {            // exclusive sums in place of b
+                    double run = 0.0;
+                    for (int i = 0; i < chunks; i += 32) {
+                        const double v = i + lane32 < chunks ? sm.a[i + lane32] : 0.0;
+                        const double incl = warp_incl_scan_d(v, lane32);
+                        double before = __shfl_up_sync(FULL, incl, 1);
+                        if (lane32 == 0) before = 0.0;
+                        if (i + lane32 < chunks) sm.b[i + lane32] = run + before;
+                        run += __shfl_sync(FULL, incl, 31);
+                    }
+                    if (lane32 == 0) sm.rest = run;
+                }
+                cluster_sync(ctas);
+                total = 0.0;
+                for (int k = 0; k < ctas; ++k) total += peer(sm.rest, k, ctas);
+                if (total > 0.0) break;
+                cluster_sync(ctas);
+                l.q = nullptr;              // p and q are alike in 64 bits
+                l.drop = -1;
+                w = near = 0.0;
+            }
+            const double t = (c_in == 1.0 ? ASX_ONE_BELOW : c_in) * total;
+            // ---- the CTA, the chunk, the sub-row and the token whose interval holds t ----
+            int owner = -1, last = -1;
+            double base = 0.0, own_base = 0.0, last_base = 0.0;
+            for (int k = 0; k < ctas; ++k) {
+                const double r = peer(sm.rest, k, ctas);
+                if (r > 0.0) {
+                    if (owner < 0 && t < base + r) { owner = k; own_base = base; }
+                    last = k;
+                    last_base = base;
+                }
+                base += r;
+            }
+            const bool top = owner < 0;     // rounding at the top end: the last token
+            if (top) { owner = last; own_base = last_base; }
+            if (owner == rank) {
+                const int chunks = l.c1 - l.c0;
+                if (warp == 0) {
+                    int pick = -1, end = -1;
+                    for (int i = 0; i < chunks && pick < 0; i += 32) {
+                        const bool has = i + lane32 < chunks && sm.a[i + lane32] > 0.0;
+                        const unsigned bal = __ballot_sync(FULL, has), hit = __ballot_sync(FULL, has && !top && t < own_base + (sm.b[has ? i + lane32 : 0] + sm.a[has ? i + lane32 : 0]));
+                        if (bal) end = i + 31 - __clz(bal);
+                        if (hit) pick = i + __ffs(hit) - 1;
+                    }
+                    if (lane32 == 0) { sm.chunk = pick < 0 ? end : pick; sm.force_last = top || pick < 0; }
+                }
+                __syncthreads();
+                const int ci = sm.chunk + l.c0;
+                const bool force = sm.force_last;
+                const double start = own_base + sm.b[ASX_AT(sm.chunk, VN_CHUNKS, 346)];
+                auto rest = [&](int r, double (&ev)[E]) {
+                    double eq[E];
+                    l.masses((ci * l.R + r) * 32 + lane32, ev, eq);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) ev[e] = fmax(fma(-ratio, eq[e], ev[e]), 0.0);
+                };
+                // sub-rows' sums, VN_NW at a time
+                double run = start;
+                int sub = -1, sub_end = -1;
+                double sub_start = 0.0, end_start = 0.0;
+                for (int r0 = 0; r0 < l.R && sub < 0; r0 += VN_NW) {
+                    double local = 0.0;
+                    if (r0 + warp < l.R) {
+                        double ev[E];
+                        rest(r0 + warp, ev);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) local += ev[e];
+                    }
+                    local = warp_sum_d(local);
+                    if (lane32 == 0) sm.sub[warp] = local;
+                    __syncthreads();
+                    for (int i = 0; i < VN_NW && r0 + i < l.R; ++i) {
+                        const double v = sm.sub[i];
+                        if (v > 0.0) {
+                            if (sub < 0 && !force && t < run + v) { sub = r0 + i; sub_start = run; }
+                            sub_end = r0 + i;
+                            end_start = run;
+                        }
+                        run += v;
+                    }
+                    __syncthreads();
+                }
+                const bool force_sub = sub < 0;
+                if (force_sub) { sub = sub_end; sub_start = end_start; }
+                if (warp == 0) {
+                    double ev[E], local = 0.0;
+                    rest(sub, ev);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) local += ev[e];
+                    const double incl = warp_incl_scan_d(local, lane32);
+                    double S = __shfl_up_sync(FULL, incl, 1);
+                    S = sub_start + (lane32 == 0 ? 0.0 : S);
+                    const int j0 = ((ci * l.R + sub) * 32 + lane32) * E - l.p.off;
+                    int mine = -1, mine_last = -1;
+                    double mine_S = 0.0, mine_e = 1.0, last_S = 0.0, last_e = 1.0;
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (ev[e] > 0.0) {
+                            if (mine < 0 && t < S + ev[e]) { mine = j0 + e; mine_S = S; mine_e = ev[e]; }
+                            mine_last = j0 + e; last_S = S; last_e = ev[e];
+                            S += ev[e];
+                        }
+                    const unsigned has = __ballot_sync(FULL, local > 0.0), hit = __ballot_sync(FULL, !force_sub && local > 0.0 && t < sub_start + incl);
+                    const int who = hit ? __ffs(hit) - 1 : 31 - __clz(has);
+                    if (!hit || mine < 0) { mine = mine_last; mine_S = last_S; mine_e = last_e; }
+                    token = __shfl_sync(FULL, mine, who);
+                    mine_S = __shfl_sync(FULL, mine_S, who);
+                    mine_e = __shfl_sync(FULL, mine_e, who);
+                    code = (t - mine_S) / mine_e;
+                    if (!(code >= 0.0)) code = 0.0;
+                    if (code > ASX_ONE_BELOW) code = ASX_ONE_BELOW;
+                }
+            }
+            if (owner == rank && tid == 0) {
+                a.tokens[(size_t)lane * (a.K + 1) + at] = token;
+                a.codes_out[lane] = code;
+            }
+        }
+        if (rank == 0) {
+            const bool good = status == AS_OK;
+            int* out = a.tokens + (size_t)lane * (a.K + 1);
+            for (int i = tid; i <= a.K; i += VN_NT)
+                if (!good || i != at) out[i] = good && i < at ? a.drafted[(size_t)lane * a.K + i] : -1;
+            if (tid == 0) {
+                a.accepted[lane] = good ? at : 0;
+                if (!good) a.codes_out[lane] = c_in;
+                if (a.lane_status) a.lane_status[lane] = status;
+            }
+        }
+        cluster_sync(ctas);
+    }
+}
+
+template <int DT>
+static cudaError_t launch_verify_lanes(const VerifyArgs& a, int sms, cudaStream_t st) {
+    static bool attr_set[64] = {false};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    auto kern = verify_lane_kernel<DT>;
+    if (!attr_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(VerifySmem));
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    // CTAs to a lane: as many as find room side by side, two or three on an SM
+    int ctas = 1;
+    while (ctas < VN_MAX_CTAS && 2LL * ctas * a.lanes <= 2LL * sms) ctas *= 2;
+    // many lanes read no row that may not be needed; few read several places' rows between two meetings
+    const int batch = ctas == 1 ? 1 : VN_BATCH;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.lanes < 64 * sms ? a.lanes : 64 * sms) * ctas));
+    cfg.blockDim = dim3(VN_NT);
+    cfg.dynamicSmemBytes = sizeof(VerifySmem);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {(unsigned)ctas, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, a, ctas, batch);
+}
+
 template <int DT>
 static cudaError_t launch_verify(const VerifyArgs& a, int sms, cudaStream_t st) {
+    if ((a.top_k <= 0 || a.top_k >= a.V) && !(a.top_p > 0.0 && a.top_p < 1.0)) return launch_verify_lanes<DT>(a, sms, st);
     const unsigned rows = (unsigned)((long long)a.lanes * (a.draft ? 2 * a.K + 1 : a.K + 1));
     cudaError_t e = launch_after(verify_rows_kernel<DT>, rows, VF_NT, 0, st, a);
     if (e != cudaSuccess) return e;
@@ -328,7 +936,8 @@ int as_step_verify(const void* d_target, long long target_ld, const void* d_draf
     a.target_ld = target_ld * es; a.draft_ld = draft_ld * es;
     a.lanes = lanes; a.K = K; a.V = V;
     a.drafted = d_drafted; a.n = d_n; a.u = d_u; a.codes = d_codes;
-    a.inv_tau = 1.0 / temp; a.top_p = top_p; a.top_k = top_k;
+    a.inv_tau = temp < 1e-300 ? 1e300 : 1.0 / temp;         // (finite: it is multiplied by differences of 0)
+    a.top_p = top_p; a.top_k = top_k;
     a.tokens = d_tokens; a.accepted = d_accepted; a.codes_out = d_codes_out; a.lane_status = d_lane_status;
     a.cuts = static_cast<RowCut*>(d_work);
     const cudaError_t e = dtype == AS_F32 ? launch_verify<AS_F32>(a, di->sms, (cudaStream_t)stream) : launch_verify<AS_BF16>(a, di->sms, (cudaStream_t)stream);
