@@ -296,13 +296,19 @@ constexpr int VN_CHUNKS = 128;              // of a CTA
 constexpr int VN_LIST = 256;
 constexpr int VN_BATCH = 8;                 // places whose rows are read before the decisions are taken
 constexpr int VN_MAX_CTAS = 8;
-// Of a sum in 32 bits: terms are off by 2^-22 (the exponential) and 2^-23 of their exponent, at most 90 before they vanish; 32 of
-// them are added up before 64 bits take over (2^-19): 2^-16 in all, and two sums to a ratio.
-constexpr double VN_NEAR = 1.0 / 16384;
+constexpr int VN_U = 4, VN_STAGES = 3;      // granules of a thread at a time, steps that it has in flight or in use
+// Of a sum in 32 bits: terms are off by 2^-22 (the exponential) and 2^-23 of their exponent, at most 130 before they vanish; 32 of
+// them are added up before 64 bits take over (2^-19): 2^-15.5 in all, and two sums to a ratio.  Maxima beyond VN_FAR in units of
+// log 2 (nothing that a model says) are left to 64 bits altogether.
+constexpr double VN_NEAR = 1.0 / 8192;
+constexpr int VN_NEAR_BITS = 13;
+constexpr float VN_FAR = 1e6f;
 
 struct RowSum { double s; float m; int bad; };
 struct PairSum { double zp, zq; int listed, pad; };
 
+constexpr int VN_RING = VN_STAGES * VN_U * VN_NT * 16;
+constexpr int VN_SMEM = VN_RING + 16384;
 struct VerifySmem {
     RowSum warp[2 * VN_BATCH][VN_NW];
     RowSum mine[2 * VN_BATCH];              // of the CTA's part of each row
@@ -313,10 +319,12 @@ struct VerifySmem {
     double list_p[VN_LIST], list_q[VN_LIST];
     int list_j[VN_LIST], order[VN_LIST];
     int listed;
-    double exp_tbl[64];
+    double exp_tbl[256];                    // 2^(j / 256)
     double rest;                            // mass of max(p - q, 0) in the CTA's chunks
     int at, status, chunk, force_last;
 };
+
+static_assert(sizeof(VerifySmem) <= VN_SMEM - VN_RING, "shared memory of verify_lane_kernel");
 
 __device__ __forceinline__ void cluster_sync(int ctas) {
     if (ctas == 1) {
@@ -351,17 +359,19 @@ struct Granules {
         n = (off + V + E - 1) / E;
     }
     __device__ __forceinline__ uint4 load(int g) const { return __ldg(reinterpret_cast<const uint4*>(from) + g); }
-    // the same with -inf outside the row
+    // the same with -inf outside the row: only a row's first and last granules need it
     __device__ __forceinline__ void masked(int g, int V, uint4& q) const {
-        if (g > 0 && (g + 1) * E - off <= V) return;
+        if (g == 0 || (g + 1) * E - off > V) q = cut(q, g * E - off, V);
+    }
+    static __device__ __noinline__ uint4 cut(uint4 q, int j0, int V) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&q);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int j = g * E + e - off;
-            if (j >= 0 && j < V) continue;
+            if (j0 + e >= 0 && j0 + e < V) continue;
             if constexpr (DT == DT_F32) w[e] = 0xFF800000u;
             else w[e / 2] = (w[e / 2] & (e & 1 ? 0x0000FFFFu : 0xFFFF0000u)) | (e & 1 ? 0xFF800000u : 0x0000FF80u);
         }
+        return q;
     }
 };
 
@@ -380,9 +390,9 @@ __device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b) {
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
 
@@ -394,59 +404,81 @@ __device__ __forceinline__ RowSum join_sums(const RowSum& a, const RowSum& b, fl
     return r;
 }
 
-// The CTA's part (granules rank, rank + ctas, ... of 4 VN_NT each) of a row's maximum and sum; a warp's goes to out[warp].
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The CTA's part of a row's maximum and sum, steps rank, rank + ctas, ... of VN_U VN_NT granules each; a warp's goes to out[warp].  A thread brings its
+// granules into places of its own in shared memory, VN_STAGES - 1 steps ahead, so that nothing is waited for but its own copies.
 template <int DT>
-__device__ __forceinline__ void row_sum(const char* row, int V, float c, int rank, int ctas, RowSum* out) {
-    constexpr int E = Traits<DT>::E, U = 4;
+__device__ __forceinline__ void row_sum(const char* row, int V, float c, int rank, int ctas, uint32_t ring, RowSum* out) {
+    constexpr int E = Traits<DT>::E;
     using P = Pass<DT>;
     const Granules<DT> g(row, V);
+    const int step = ctas * VN_U * VN_NT, first = rank * VN_U * VN_NT + threadIdx.x;
+    auto issue = [&](int g0, int stage) {
+#pragma unroll
+        for (int u = 0; u < VN_U; ++u)
+            if (g0 + u * VN_NT < g.n) copy16(ring + (ASX_AT(stage, VN_STAGES, 347) * VN_U + u) * (VN_NT * 16), g.from + (size_t)(g0 + u * VN_NT) * 16);
+        copies_close();
+    };
+#pragma unroll
+    for (int i = 0; i < VN_STAGES - 1; ++i) issue(first + i * step, i);
     typename P::Acc acc = P::init();
-    float m = -INFINITY;
+    float m = -INFINITY, ref = 0.f;         // terms are 2^(x c - ref), ref = m c rounded
     double s = 0.0;
     const uint64_t cc = two(c, c);
+    int stage = 0;
 #pragma unroll 1
-    for (int g0 = rank * U * VN_NT + threadIdx.x; g0 < g.n; g0 += ctas * U * VN_NT) {
-        uint4 q[U];
+    for (int g0 = first; g0 < g.n; g0 += step) {
+        copies_wait<VN_STAGES - 2>();
+        issue(g0 + (VN_STAGES - 1) * step, stage == 0 ? VN_STAGES - 1 : stage - 1);
+        uint4 q[VN_U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < VN_U; ++u) {
             const int at = g0 + u * VN_NT;
-            q[u] = at < g.n ? g.load(at) : DT == DT_F32 ? make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+            q[u] = DT == DT_F32 ? make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+            if (at < g.n) {
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(q[u].x), "=r"(q[u].y), "=r"(q[u].z), "=r"(q[u].w)
+                             : "r"(ring + (ASX_AT(stage, VN_STAGES, 348) * VN_U + u) * (VN_NT * 16)));
+                g.masked(at, V, q[u]);
+            }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (g0 + u * VN_NT < g.n) g.masked(g0 + u * VN_NT, V, q[u]);
+        if (++stage == VN_STAGES) stage = 0;
         typename P::Acc now = P::reduce(q[0]);
 #pragma unroll
-        for (int u = 1; u < U; ++u) P::fold(now, q[u]);
+        for (int u = 1; u < VN_U; ++u) P::fold(now, q[u]);
         P::merge(acc, now);
         const float top = P::part_max(now);
         if (top > m) {
-            s *= (double)ex2_approx((m - top) * c);     // (0 before the first)
+            const float to = top * c;
+            s *= (double)ex2_approx(m == -INFINITY ? -INFINITY : ref - to);
             m = top;
+            ref = to;
         }
-        const float ref = m == -INFINITY ? 0.f : m;
         const uint64_t mm = two(-ref, -ref);
         uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < VN_U; ++u) {
             float x[E];
             P::floats(q[u], x);
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
-                // (the difference first: its rounding is that of a small number)
-                const float2 y = both(mul_two(add_two(two(x[e], x[e + 1]), mm), cc));
+                const float2 y = both(fma_two(two(x[e], x[e + 1]), cc, mm));
                 sum[e / 2 & 1] = add_two(sum[e / 2 & 1], two(ex2_approx(y.x), ex2_approx(y.y)));
             }
         }
         const float2 t = both(add_two(sum[0], sum[1]));
         s += (double)(t.x + t.y);
     }
+    copies_wait<0>();
     uint32_t k0, k1;
     P::keys(acc, k0, k1);
     RowSum r;
     r.bad = max(k0, k1) >= Traits<DT>::KEY_PINF || min(k0, k1) < Traits<DT>::KEY_NINF;      // +inf or a NaN
     r.m = m;
-    r.s = s;
+    // (what the rounding of ref has put on every term comes off; the product of two floats is exact in a double)
+    r.s = m == -INFINITY ? 0.0 : s * (double)ex2_approx((float)((double)ref - (double)m * (double)c));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         RowSum other;
@@ -458,8 +490,46 @@ __device__ __forceinline__ void row_sum(const char* row, int V, float c, int ran
     if ((threadIdx.x & 31) == 0) out[threadIdx.x >> 5] = r;
 }
 
-// e of a logit of a row with maximum m; c64 = 64 log2(e) / temp
-__device__ __forceinline__ double mass64(float x, double c64, double m, const double* tbl) { return exp2_64th(((double)x - m) * c64, tbl); }
+// Masses in 64 bits: 2^(t / 256), t = (x - m) 256 log2(e) / temp, = 2^n 2^(j / 256) exp(f ln2 / 256), |f| <= 1/2, the last factor by a polynomial of
+// degree 4 (truncation 4e-17).  Logits far below m are raised to where their mass is 2^-1000: what is below VN_NONE counts as none, masked
+// tokens among it, and 2^20 of them do not come up to it.  t is one fused multiply-add: the rounding of m's product is the same for all of
+// a row.  Maxima beyond VN_FAR are taken off the logits first (which is exact: differences that matter are multiples of a
+// float's spacing there).
+constexpr double VN_NONE = 0x1p-950;
+struct MassRow {
+    float sub, low;
+    double mc;
+    __device__ __forceinline__ MassRow(float m, double c256) {
+        const bool far = fabs((double)m * c256) > 256.0 * VN_FAR;
+        sub = far ? m : 0.f;
+        const double top = far ? 0.0 : m;
+        mc = top * c256;
+        low = fmaxf((float)(top - 256000.0 / c256), -3.4e38f);      // (above -inf, whatever the temperature)
+    }
+};
+__device__ __forceinline__ double mass64(float x, const MassRow& r, double c256, const double* tbl) {
+    x = fmaxf(x - r.sub, r.low);
+    const double MAGIC = 6755399441055744.0;
+    const double t = fma((double)x, c256, -r.mc);
+    double k = t + MAGIC;
+    const int i = __double2loint(k);
+    k -= MAGIC;
+    const double f = t - k;
+    const double L = 0x1.62e42fefa39efp-9;               // ln2 / 256
+    double p = fma(f, L * L * L * L / 24.0, L * L * L / 6.0);
+    p = fma(p, f, L * L / 2.0);
+    p = fma(p, f, L);
+    p = fma(p, f, 1.0);
+    const double v = tbl[i & 255] * p;
+    return __hiloint2double(__double2hiint(v) + ((i >> 8) << 20), __double2loint(v));
+}
+
+// of one token of a row: 0 where it counts as none
+template <int DT>
+__device__ __forceinline__ double token_mass(const char* row, int x, const MassRow& r, double c256, const double* tbl) {
+    const double e = mass64(Pass<DT>::load_f(row, x), r, c256, tbl);
+    return e > VN_NONE ? e : 0.0;
+}
 
 // The last row pair of a lane (q.from null: p alone).
 template <int DT>
@@ -468,11 +538,12 @@ struct LastPair {
     Granules<DT> p;
     const char* q;                          // the draft's row
     bool q_vec;                             // both rows lie alike on the granules
-    double mp, mq, c64;
+    MassRow mp, mq;
+    double c256;
     int V, drop, R, per, c0, c1;            // R: sub-rows of 32 granules of a chunk; the CTA's chunks [c0, c1)
     const double* tbl;
-    __device__ __forceinline__ LastPair(const VerifyArgs& a, const char* prow, const char* qrow, float mp_, float mq_, int drop_, double c64_, int rank, int ctas, const double* tbl_)
-        : p(prow, a.V), q(qrow), mp(mp_), mq(mq_), c64(c64_), V(a.V), drop(drop_), tbl(tbl_) {
+    __device__ __forceinline__ LastPair(const VerifyArgs& a, const char* prow, const char* qrow, float mp_, float mq_, int drop_, double c256_, int rank, int ctas, const double* tbl_)
+        : p(prow, a.V), q(qrow), mp(mp_, c256_), mq(mq_, c256_), c256(c256_), V(a.V), drop(drop_), tbl(tbl_) {
         q_vec = qrow && Granules<DT>(qrow, a.V).off == p.off;
         const int rows = (p.n + 31) / 32;
         R = (rows + ctas * (VN_CHUNKS / 2) - 1) / (ctas * (VN_CHUNKS / 2));
@@ -481,70 +552,86 @@ struct LastPair {
         c0 = min(rank * per, chunks);
         c1 = min(c0 + per, chunks);
     }
-    // masses of granule g's tokens (0 outside the row)
-    __device__ __forceinline__ void masses(int g, double (&ep)[E], double (&eq)[E]) const {
-        if (g >= p.n) {
+    // A granule of the row and the draft's logits of the same tokens, -inf outside the row.
+    struct Raw { uint4 p, q; };
+    __device__ __forceinline__ Raw load(int g) const {
+        Raw v;
+        v.p = v.q = DT == DT_F32 ? make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+        if (g >= p.n) return v;
+        v.p = p.load(g);
+        if (!q) return v;
+        if (q_vec) {
+            v.q = __ldg(reinterpret_cast<const uint4*>(q - p.off * Traits<DT>::BYTES) + g);
+        } else {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v.q);
 #pragma unroll
-            for (int e = 0; e < E; ++e) ep[e] = eq[e] = 0.0;
-            return;
-        }
-        float x[E];
-        uint4 v = p.load(g);
-        p.masked(g, V, v);
-        Pass<DT>::floats(v, x);
-        float y[E];
-        if (q) {
-            if (q_vec) {
-                const Granules<DT> qg(q, V);
-                v = qg.load(g);
-                qg.masked(g, V, v);
-                Pass<DT>::floats(v, y);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int j = g * E + e - p.off;
-                    y[e] = j >= 0 && j < V ? Pass<DT>::load_f(q, j) : -INFINITY;
-                }
+            for (int e = 0; e < E; ++e) {
+                const int j = g * E + e - p.off;
+                if (j < 0 || j >= V) continue;
+                if constexpr (DT == DT_F32) w[e] = reinterpret_cast<const uint32_t*>(q)[j];
+                else w[e / 2] = (w[e / 2] & (e & 1 ? 0x0000FFFFu : 0xFFFF0000u)) | (uint32_t)reinterpret_cast<const uint16_t*>(q)[j] << (e & 1 ? 16 : 0);
             }
         }
+        return v;
+    }
+    // f(e, mass of p, mass of q) for the tokens of a granule; without Q the draft's row is not looked at, and p's dropped token has no mass
+    template <bool Q, class F>
+    __device__ __forceinline__ void each(int g, Raw v, F&& f) const {
+        if (g < p.n) {
+            p.masked(g, V, v.p);
+            if (Q && q_vec) p.masked(g, V, v.q);
+        }
+        float x[E], y[E];
+        Pass<DT>::floats(v.p, x);
+        if constexpr (Q) {
+            Pass<DT>::floats(v.q, y);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            ep[e] = g * E + e - p.off == drop ? 0.0 : mass64(x[e], c64, mp, tbl);
-            eq[e] = q ? mass64(y[e], c64, mq, tbl) : 0.0;
+            for (int e = 0; e < E; ++e) f(e, mass64(x[e], mp, c256, tbl), mass64(y[e], mq, c256, tbl));
+        } else {
+            const int gone = drop < 0 ? -1 : drop + p.off - g * E;
+#pragma unroll
+            for (int e = 0; e < E; ++e) f(e, mass64(e == gone ? -INFINITY : x[e], mp, c256, tbl), 0.0);
         }
     }
 };
 
-// Once over the CTA's chunks of the pair: their masses of tokens with p > q, the rows' sums, the list.  near = 0: w is exact.
-template <int DT>
-__device__ __forceinline__ void pair_pass(VerifySmem& sm, const LastPair<DT>& l, double w, double near) {
+// Once over the CTA's chunks of the pair: their masses of tokens with p > q, the rows' sums, and the list if w is but near Zp / Zq.
+template <int DT, bool Q>
+__device__ __forceinline__ void pair_pass(VerifySmem& sm, const LastPair<DT>& l, double w, bool near) {
     constexpr int E = Traits<DT>::E;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) sm.listed = 0;
     __syncthreads();
+    const unsigned listing = near ? (unsigned)VN_NEAR_BITS << 20 : 0x7FF00000u;
     double zp = 0.0, zq = 0.0;
+    typename LastPair<DT>::Raw next = l.load(((l.c0 + warp) * l.R) * 32 + lane);
 #pragma unroll 1
     for (int ci = l.c0 + warp; ci < l.c1; ci += VN_NW) {
         double A = 0.0, Bq = 0.0, cp = 0.0, cq = 0.0;
 #pragma unroll 1
         for (int r = 0; r < l.R; ++r) {
             const int g = (ci * l.R + r) * 32 + lane;
-            double ep[E], eq[E];
-            l.masses(g, ep, eq);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                cp += ep[e];
-                cq += eq[e];
-                const double d = fma(-w, eq[e], ep[e]);
-                if (near > 0.0 && fabs(d) <= near * ep[e] && ep[e] > 0.0 && eq[e] > 0.0) {
-                    const int at = atomicAdd(&sm.listed, 1);
-                    if (at < VN_LIST) { sm.list_p[at] = ep[e]; sm.list_q[at] = eq[e]; sm.list_j[at] = g * E + e; }
-                } else if (d > 0.0) {
-                    A += ep[e];
-                    Bq += eq[e];
+            const typename LastPair<DT>::Raw now = next;
+            next = l.load(r + 1 < l.R ? g + 32 : ((ci + VN_NW) * l.R) * 32 + lane);
+            l.template each<Q>(g, now, [&](int e, double ep, double eq) {
+                cp += ep;
+                if constexpr (Q) {
+                    cq += eq;
+                    const double d = fma(-w, eq, ep);
+                    const int hd = __double2hiint(d);
+                    double yes = __hiloint2double(hd > 0 ? 0x3FF00000 : 0, 0);     // (a positive d that counts has a high word)
+                    // |d| below 2^-VN_NEAR_BITS of ep, by exponents (2^-VN_NEAR_BITS to 2^(1 - VN_NEAR_BITS))
+                    if ((unsigned)(hd & 0x7FFFFFFF) + listing <= (unsigned)__double2hiint(ep) && ep > VN_NONE) {
+                        const int at = atomicAdd(&sm.listed, 1);
+                        if (at < VN_LIST) { sm.list_p[at] = ep; sm.list_q[at] = eq; sm.list_j[at] = g * E + e; }
+                        yes = 0.0;
+                    }
+                    A = fma(yes, ep, A);
+                    Bq = fma(yes, eq, Bq);
                 }
-            }
+            });
         }
+        if (!Q) A = cp;
         A = warp_sum_d(A);
         Bq = warp_sum_d(Bq);
         zp += cp;
@@ -563,17 +650,19 @@ __device__ __forceinline__ void pair_pass(VerifySmem& sm, const LastPair<DT>& l,
 }
 
 template <int DT>
-__global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_constant__ VerifyArgs a, int ctas, int batch) {
+__global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_constant__ VerifyArgs a, int ctas, int batch) {
     constexpr int E = Traits<DT>::E;
     extern __shared__ __align__(16) char vn_smem[];
-    VerifySmem& sm = *reinterpret_cast<VerifySmem*>(vn_smem);
+    VerifySmem& sm = *reinterpret_cast<VerifySmem*>(vn_smem + VN_RING);
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(vn_smem) + threadIdx.x * 16;
     const int tid = threadIdx.x, lane32 = tid & 31, warp = tid >> 5;
     const int rank = ctas == 1 ? 0 : (int)(blockIdx.x % ctas);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    fill_exp_table(sm.exp_tbl, tid);
+    // 2^(j / 256) = 2^((j / 4) / 64) 2^((j mod 4) / 256)
+    sm.exp_tbl[tid] = ASX_T64[tid >> 2] * (tid & 2 ? 0x1.0163da9fb3335p+0 : 1.0) * (tid & 1 ? 0x1.00b1afa5abcbfp+0 : 1.0);
     __syncthreads();
-    const double c64 = 64.0 * 1.4426950408889634 * a.inv_tau;
+    const double c256 = 256.0 * 1.4426950408889634 * a.inv_tau;
     const float c = (float)fmin(1.4426950408889634 * a.inv_tau, 3e38);
 #pragma unroll 1
     for (int lane = blockIdx.x / ctas; lane < a.lanes; lane += gridDim.x / ctas) {
@@ -590,8 +679,8 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
             const int count = min(batch, n + 1 - i0);
 #pragma unroll 1
             for (int b = 0; b < count; ++b) {
-                row_sum<DT>(target_row(a, lane, i0 + b), a.V, c, rank, ctas, sm.warp[2 * b]);
-                if (a.draft && i0 + b < n) row_sum<DT>(draft_row(a, lane, i0 + b), a.V, c, rank, ctas, sm.warp[2 * b + 1]);
+                row_sum<DT>(target_row(a, lane, i0 + b), a.V, c, rank, ctas, ring, sm.warp[2 * b]);
+                if (a.draft && i0 + b < n) row_sum<DT>(draft_row(a, lane, i0 + b), a.V, c, rank, ctas, ring, sm.warp[2 * b + 1]);
             }
             __syncthreads();
             if (tid < 2 * count && (tid % 2 == 0 || (a.draft && i0 + tid / 2 < n))) {
@@ -626,10 +715,11 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
                         } else if (!(u >= 0.0 && u < 1.0) || p_bad || q_bad) {
                             what = AS_ERR_NUMERIC;
                         } else {
-                            const double px = mass64(Pass<DT>::load_f(target_row(a, lane, i), x), c64, p.m, sm.exp_tbl) / p.s;
-                            const double qx = u * (a.draft ? mass64(Pass<DT>::load_f(draft_row(a, lane, i), x), c64, q.m, sm.exp_tbl) / q.s : 1.0);
+                            const double px = token_mass<DT>(target_row(a, lane, i), x, MassRow(p.m, c256), c256, sm.exp_tbl) / p.s;
+                            const double qx = u * (a.draft ? token_mass<DT>(draft_row(a, lane, i), x, MassRow(q.m, c256), c256, sm.exp_tbl) / q.s : 1.0);
                             // (a side that is 0 is so whatever the sums)
-                            what = px > 0.0 && qx > 0.0 && fabs(qx - px) <= VN_NEAR * fmax(qx, px) ? 2 : qx < px ? 0 : 1;
+                            const bool far = fabsf(p.m) * c > VN_FAR || (a.draft && fabsf(q.m) * c > VN_FAR);
+                            what = px > 0.0 && qx > 0.0 && (far || fabs(qx - px) <= VN_NEAR * fmax(qx, px)) ? 2 : qx < px ? 0 : 1;
                         }
                     }
                 }
@@ -646,9 +736,10 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
                 i0 += count;
             } else if (what == 2) {         // once more in 64 bits
                 const int i = i0 + l;
-                const LastPair<DT> pair(a, target_row(a, lane, i), a.draft ? draft_row(a, lane, i) : nullptr, rp.m, rq.m, -1, c64, rank, ctas, sm.exp_tbl);
+                const LastPair<DT> pair(a, target_row(a, lane, i), a.draft ? draft_row(a, lane, i) : nullptr, rp.m, rq.m, -1, c256, rank, ctas, sm.exp_tbl);
                 cluster_sync(ctas);         // (the other CTAs have read this one's sums)
-                pair_pass<DT>(sm, pair, 0.0, 0.0);
+                if (a.draft) pair_pass<DT, true>(sm, pair, 0.0, false);
+                else pair_pass<DT, false>(sm, pair, 0.0, false);
                 cluster_sync(ctas);
                 double zp = 0.0, zq = 0.0;
                 for (int k = 0; k < ctas; ++k) {
@@ -657,8 +748,8 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
                     zq += t.zq;
                 }
                 const int x = a.drafted[(size_t)lane * a.K + i];
-                const double px = mass64(Pass<DT>::load_f(target_row(a, lane, i), x), c64, pair.mp, sm.exp_tbl) / zp;
-                const double qx = a.draft ? mass64(Pass<DT>::load_f(draft_row(a, lane, i), x), c64, pair.mq, sm.exp_tbl) / zq : 1.0;
+                const double px = token_mass<DT>(target_row(a, lane, i), x, pair.mp, c256, sm.exp_tbl) / zp;
+                const double qx = a.draft ? token_mass<DT>(draft_row(a, lane, i), x, pair.mq, c256, sm.exp_tbl) / zq : 1.0;
                 if (a.u[(size_t)lane * a.K + i] * qx < px) {
                     i0 = i + 1;
                 } else {
@@ -681,12 +772,17 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
         if (status == AS_OK) {
             const bool pairs = refused && a.draft;
             const int drop = refused && !a.draft ? a.drafted[(size_t)lane * a.K + at] : -1;
-            LastPair<DT> l(a, target_row(a, lane, at), pairs ? draft_row(a, lane, at) : nullptr, rp.m, rq.m, drop, c64, rank, ctas, sm.exp_tbl);
-            double w = pairs ? rp.s / rq.s : 0.0, near = pairs && !exact ? VN_NEAR : 0.0, ratio = 0.0, total = 0.0;
+            LastPair<DT> l(a, target_row(a, lane, at), pairs ? draft_row(a, lane, at) : nullptr, rp.m, rq.m, drop, c256, rank, ctas, sm.exp_tbl);
+            bool vague = false;
+            double w = pairs ? rp.s / rq.s : 0.0, ratio = 0.0, total = 0.0;
+            // (w from sums in 32 bits; a row too far out for those has one of 0)
+            bool near = pairs && !exact;
+            if (near && (fabsf(rp.m) * c > VN_FAR || fabsf(rq.m) * c > VN_FAR)) { w = 1.0; near = false; vague = true; }
             // Once; again with the exact w if the list ran over; once more with p alone where nothing is left of p - q.
 #pragma unroll 1
             for (int turn = 0; turn < 3; ++turn) {
-                pair_pass<DT>(sm, l, w, near);
+                if (l.q) pair_pass<DT, true>(sm, l, w, near);
+                else pair_pass<DT, false>(sm, l, w, near);
                 cluster_sync(ctas);
                 double zp = 0.0, zq = 0.0;
                 int most = 0;
@@ -697,15 +793,15 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
                     most = max(most, t.listed);
                 }
                 ratio = l.q ? zp / zq : 0.0;
-                if (most > VN_LIST) {
+                if (most > VN_LIST || vague) {
                     cluster_sync(ctas);
                     w = ratio;
-                    near = 0.0;
+                    near = vague = false;
                     continue;
                 }
                 // ---- chunks' masses of max(p - q, 0) in units of 1 / Zp; listed tokens in the order of their indices ----
-                const int chunks = l.c1 - l.c0, listed = near > 0.0 ? sm.listed : 0;
-                for (int i = tid; i < chunks; i += VN_NT) sm.a[i] = sm.a[i] > 0.0 ? fmax(fma(-ratio, sm.b[i], sm.a[i]), 0.0) : 0.0;
+                const int chunks = l.c1 - l.c0, listed = near ? sm.listed : 0;
+                for (int i = tid; i < chunks; i += VN_NT) sm.a[i] = sm.a[i] > VN_NONE ? fmax(fma(-ratio, sm.b[i], sm.a[i]), 0.0) : 0.0;
                 for (int i = tid; i < listed; i += VN_NT) {
                     int before = 0;
                     for (int k = 0; k < listed; ++k) before += sm.list_j[k] < sm.list_j[i];
@@ -737,11 +833,12 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
                 cluster_sync(ctas);
                 total = 0.0;
                 for (int k = 0; k < ctas; ++k) total += peer(sm.rest, k, ctas);
-                if (total > 0.0) break;
+                if (total > VN_NONE) break;
                 cluster_sync(ctas);
                 l.q = nullptr;              // p and q are alike in 64 bits
                 l.drop = -1;
-                w = near = 0.0;
+                w = 0.0;
+                near = false;
             }
             const double t = (c_in == 1.0 ? ASX_ONE_BELOW : c_in) * total;
             // ---- the CTA, the chunk, the sub-row and the token whose interval holds t ----
@@ -775,10 +872,13 @@ __global__ void __launch_bounds__(VN_NT, 2) verify_lane_kernel(const __grid_cons
                 const bool force = sm.force_last;
                 const double start = own_base + sm.b[ASX_AT(sm.chunk, VN_CHUNKS, 346)];
                 auto rest = [&](int r, double (&ev)[E]) {
-                    double eq[E];
-                    l.masses((ci * l.R + r) * 32 + lane32, ev, eq);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) ev[e] = fmax(fma(-ratio, eq[e], ev[e]), 0.0);
+                    const int g = (ci * l.R + r) * 32 + lane32;
+                    auto take = [&](int e, double ep, double eq) {
+                        const double d = fma(-ratio, eq, ep);
+                        ev[e] = d > VN_NONE ? d : 0.0;
+                    };
+                    if (l.q) l.template each<true>(g, l.load(g), take);
+                    else l.template each<false>(g, l.load(g), take);
                 };
                 // sub-rows' sums, VN_NW at a time
                 double run = start;
@@ -864,7 +964,7 @@ static cudaError_t launch_verify_lanes(const VerifyArgs& a, int sms, cudaStream_
     cudaGetDevice(&dev);
     auto kern = verify_lane_kernel<DT>;
     if (!attr_set[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(VerifySmem));
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, VN_SMEM);
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
@@ -876,7 +976,7 @@ static cudaError_t launch_verify_lanes(const VerifyArgs& a, int sms, cudaStream_
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((a.lanes < 64 * sms ? a.lanes : 64 * sms) * ctas));
     cfg.blockDim = dim3(VN_NT);
-    cfg.dynamicSmemBytes = sizeof(VerifySmem);
+    cfg.dynamicSmemBytes = VN_SMEM;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
