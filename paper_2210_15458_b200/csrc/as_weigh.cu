@@ -39,12 +39,12 @@ static WeighPlan plan_weigh(int dtype, int lanes, int T, int heads, int q_heads,
     return pl;
 }
 
-template <int DT, int D, int NT>
+template <int DT, int D, int NT, bool MANY>
 static cudaError_t launch_weigh_mma(WeighArgs& wa, int sms, cudaStream_t st) {
     static int per_sm[64] = {0};
     int dev = 0;
     cudaGetDevice(&dev);
-    auto kern = weigh_mma_kernel<DT, D, NT>;
+    auto kern = weigh_mma_kernel<DT, D, NT, MANY>;
     if (per_sm[dev] == 0) {
         int n = 0;
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(WeighSmem<D>));
@@ -87,8 +87,9 @@ template <int DT, int D>
 static int launch_weigh(WeighArgs& wa, const WeighPlan& pl, int sms, cudaStream_t st) {
     cudaError_t e;
     if (many_rows(DT, wa.p.rows)) e = launch_weigh_tc<D>(wa, pl, sms, st);
-    else if (DT == AS_BF16 && wa.p.rows > 8) e = launch_weigh_mma<DT, D, DT == AS_BF16 ? 2 : 1>(wa, sms, st);
-    else e = launch_weigh_mma<DT, D, 1>(wa, sms, st);
+    else if (DT == AS_BF16 && wa.p.rows > 8) e = launch_weigh_mma<DT, D, DT == AS_BF16 ? 2 : 1, false>(wa, sms, st);
+    else if (DT == AS_F32 && wa.p.rows > 8) e = launch_weigh_mma<DT, D, 1, DT == AS_F32>(wa, sms, st);
+    else e = launch_weigh_mma<DT, D, 1, false>(wa, sms, st);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "weigh kernel launch");
 }
 

@@ -58,9 +58,9 @@ template <int D> struct WeighSmem {
     RunSmem run;
 };
 
-// A warp has a run of its own.  Scores are formed as in attention, S^T = K q^T (tokens x rows); rows beyond 8 NT are taken 8 NT at a
-// time on the same keys.
-template <int DT, int D, int NT>
+// A warp has a run of its own.  Scores are formed as in attention, S^T = K q^T (tokens x rows); rows beyond 8 NT (MANY) are taken 8 NT
+// at a time on the same keys.
+template <int DT, int D, int NT, bool MANY>
 __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant__ WeighArgs wa) {
     using Ti = Tile4<D>;
     constexpr int PARTS = DT == AS_F32 ? 2 : 1;
@@ -113,10 +113,12 @@ __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant_
 
     uint32_t qf[PARTS][NT][D / 16][2];
     float k2[NT][2], z[NT][2];
-    int lim[NT][2], low[NT][2];
-    const int row_tiles = (p.rows + 8 * NT - 1) / (8 * NT);
+    int lim[NT][2], low[NT][2], lim_min = 0, low_max = 0;
+    const int row_tiles = MANY ? (p.rows + 8 * NT - 1) / (8 * NT) : 1;
     const int t0 = 4 * (r >> 1) + (r & 1);          // the thread's tokens of a tile: t0 and t0 + 2
-    int stage = 0;
+    const int mine = 16 * (cc >> 1) + t0 + 2 * (cc & 1);    // of the unit's tokens the one whose sum it writes
+    int stage = 0, from = 0, len = 0;
+    float* weight = nullptr;
     bool fresh = true;
 #pragma unroll 1
     for (; left > 0; --left) {
@@ -124,12 +126,24 @@ __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant_
         __syncwarp();
         issue(stage == 0 ? WG_STAGES - 1 : stage - 1);
         const int pos = cu.lo + cu.u * 32;
+        if (fresh) {
+            from = wa.first[cu.lane0];
+            len = c.len[cu.lane0];
+            weight = wa.weight + ((size_t)ASX_AT(cu.lane0, c.lanes, 301) * c.heads + ASX_AT(cu.head, c.heads, 302)) * wa.weight_ld;
+        }
+        // the thread's own token: its weight is on its way while the scores are formed
+        const int place = pos + mine, at = cu.hole.real(place);
+        const bool put = place < cu.hi && at >= from && at < len;
+        float old = 0.f;
+        if (put && wa.add && at < len - c.T) old = weight[ASX_AT(at, wa.weight_ld, 303)];
         float sum[4] = {0.f, 0.f, 0.f, 0.f};        // tokens t0, t0 + 2 of the first tile, then of the second
 #pragma unroll 1
         for (int rt = 0; rt < row_tiles; ++rt) {
-            if (fresh || row_tiles > 1) {           // ---- these rows' queries ----
+            if (fresh || MANY) {                    // ---- these rows' queries ----
                 fresh = false;
                 const float to_log2 = a.scale * (c.k_scale ? c.k_scale[cu.head] : 1.f) * 1.44269504088896f;
+                lim_min = 0x7FFFFFFF;
+                low_max = 0;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const int row = (rt * NT + n) * 8 + r;
@@ -138,16 +152,26 @@ __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant_
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int rw = (rt * NT + n) * 8 + 2 * cc + h;
-                        k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
                         const float lse = rw < p.rows ? wa.lse[out_row(a, cu.lane0, cu.head, rw)] : -INFINITY;
                         const int rl = lse == -INFINITY ? 0 : row_limit(a, cu.lane0, rw);
+                        k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
                         z[n][h] = lse * 1.44269504088896f;
                         lim[n][h] = lse == -INFINITY ? -1 : min(rl - cu.hole.skip, cu.hi);
                         low[n][h] = max(rl - p.window, 0) - cu.hole.skip;
+                        if (lse != -INFINITY) {
+                            lim_min = min(lim_min, lim[n][h]);
+                            low_max = max(low_max, low[n][h]);
+                        } else {                    // no row, or one that sees nothing: 2^(score x 0 - inf), unless a row that sees ends the tile
+                            k2[n][h] = 0.f;
+                            z[n][h] = INFINITY;
+                        }
                     }
                 }
+                lim_min = __reduce_min_sync(0xFFFFFFFFu, lim_min);
+                low_max = __reduce_max_sync(0xFFFFFFFFu, low_max);
             }
             const uint32_t st = ring0 + ASX_AT(stage, WG_STAGES, 308) * 2 * 9 * D;
+            const bool cut = pos + 32 > lim_min || (pos < low_max && pos + 32 > p.sinks);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 float s[NT][4];
@@ -156,10 +180,12 @@ __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant_
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {   // (token t0 + 2 (e / 2), row e mod 2)
-                        const int at = pos + 16 * b + t0 + 2 * (e >> 1);
-                        const float x = ex2(s[n][e] * k2[n][e & 1] - z[n][e & 1]);
-                        const bool seen = at < lim[n][e & 1] && (at >= low[n][e & 1] || at < p.sinks);
-                        sum[2 * b + (e >> 1)] += seen ? x : 0.f;
+                        float x = ex2(s[n][e] * k2[n][e & 1] - z[n][e & 1]);
+                        if (cut) {
+                            const int at = pos + 16 * b + t0 + 2 * (e >> 1);
+                            x = at < lim[n][e & 1] && (at >= low[n][e & 1] || at < p.sinks) ? x : 0.f;
+                        }
+                        sum[2 * b + (e >> 1)] += x;
                     }
             }
         }
@@ -168,9 +194,7 @@ __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant_
             sum[i] += __shfl_xor_sync(0xFFFFFFFFu, sum[i], 1);
             sum[i] += __shfl_xor_sync(0xFFFFFFFFu, sum[i], 2);
         }
-        const float mine = cc == 0 ? sum[0] : cc == 1 ? sum[1] : cc == 2 ? sum[2] : sum[3];
-        const int at = pos + 16 * (cc >> 1) + t0 + 2 * (cc & 1);
-        if (at < cu.hi) put_weight(wa, cu.lane0, cu.head, cu.hole.real(at), wa.first[cu.lane0], c.len[cu.lane0], mine);
+        if (put) weight[at] = old + (cc == 0 ? sum[0] : cc == 1 ? sum[1] : cc == 2 ? sum[2] : sum[3]);
         __syncwarp();
         if (++stage == WG_STAGES) stage = 0;
         if (cu.u + 1 == cu.nu) fresh = true;
