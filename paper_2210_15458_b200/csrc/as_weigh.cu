@@ -39,6 +39,44 @@ static WeighPlan plan_weigh(int dtype, int lanes, int T, int heads, int q_heads,
     return pl;
 }
 
+// One CTA per lane: the length and beginning that the other kernels use, the lane's status, 0 for the places that no row looks at (in
+// between the sinks and the first row's window) where sums are not added to older ones, and the lane's steps if the tensor cores are to
+// take them (t.steps not null).
+static __global__ void __launch_bounds__(128) weigh_start_kernel(const __grid_constant__ WeighTcArgs t, const CacheArgs c, const int* first, int* eff, int* from, int* begin, int* steps) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ int sum;
+    const WeighArgs& w = t.w;
+    for (int b = blockIdx.x; b < c.lanes; b += gridDim.x) {
+        bool bad;
+        int len = lane_len(c, b, &bad);
+        const int f = first ? first[b] : 0;
+        bad = bad || len > w.weight_ld || f < 0 || f > len;
+        if (bad) len = 0;
+        if (threadIdx.x == 0) {
+            eff[b] = len;
+            from[b] = bad ? 0 : f;
+            begin[b] = bad ? 0 : f & ~15;
+            if (c.lane_status) c.lane_status[b] = bad ? AS_ERR_INVALID_ARG : AS_OK;
+            sum = 0;
+        }
+        if (!w.add && !bad) {
+            const int lo = max(f, w.p.sinks), hi = min(len, len - c.T + 1 - w.p.window);
+            for (int h = 0; h < c.heads; ++h)
+                for (int k = lo + threadIdx.x; k < hi; k += 128) w.weight[((size_t)b * c.heads + h) * w.weight_ld + k] = 0.f;
+        }
+        if (!steps) continue;
+        __syncthreads();                    // (the lane's length and beginning are read again)
+        const WeighLane l(w, b);
+        int mine = 0;
+        for (int i = threadIdx.x; i < l.tiles(); i += 128) mine += l.row_span(w, i).y;
+        atomicAdd(&sum, mine);
+        __syncthreads();
+        if (threadIdx.x == 0) steps[b] = sum;
+        __syncthreads();
+    }
+}
+
 template <int DT, int D, int NT, bool MANY>
 static cudaError_t launch_weigh_mma(WeighArgs& wa, int sms, cudaStream_t st) {
     static int per_sm[64] = {0};
@@ -76,8 +114,7 @@ static cudaError_t launch_weigh_tc(const WeighArgs& wa, const WeighPlan& pl, int
     t.runs = sms < WT_MAX_RUNS ? sms : WT_MAX_RUNS;
     const int lanes = wa.a.c.lanes;
     const long long items = (long long)lanes * wa.a.c.heads * t.row_tiles;
-    cudaError_t e = launch_after(weigh_steps_kernel, (unsigned)(lanes < 16 * sms ? lanes : 16 * sms), 128, 0, st, t, pl.steps);
-    if (e == cudaSuccess) e = launch_after(weigh_rows_kernel<D>, (unsigned)(items < 64 * sms ? items : 64 * sms), 256, 0, st, t);
+    cudaError_t e = launch_after(weigh_rows_kernel<D>, (unsigned)(items < 64 * sms ? items : 64 * sms), 256, 0, st, t);
     if (e == cudaSuccess) e = launch_after(weigh_tc_kernel<D>, t.runs, WT_NT, weigh_tc_smem<D>(), st, t);
     if (e == cudaSuccess) e = launch_after(weigh_join_kernel, t.runs, TC_KV, 0, st, t);
     return e;
@@ -131,9 +168,6 @@ int as_cache4_weigh(const as_cache4* cache, const void* d_q, long long q_ld, int
     WeighArgs wa = {};
     wa.a.c = cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status);
     const int g = q_heads / cache->heads, win = window == 0 || window > most ? most : window, sk = sinks < most ? sinks : most;
-    cudaError_t e = launch_after(weigh_start_kernel, (unsigned)(lanes < 16 * di->sms ? lanes : 16 * di->sms), 128, 0, st, wa.a.c, (const int*)d_first, pl.eff, pl.from, pl.begin, d_weight,
-                                 weight_ld, win, sk, add != 0);
-    if (e != cudaSuccess) return cuda_fail(e, "weigh start kernel launch");
     wa.a.c.len = pl.eff;
     wa.a.q = d_q; wa.a.q_ld = q_ld; wa.a.q_heads = q_heads; wa.a.scale = (float)scale;
     wa.a.by_g.set(g);
@@ -145,6 +179,11 @@ int as_cache4_weigh(const as_cache4* cache, const void* d_q, long long q_ld, int
     p.by_row_tiles.set(1); p.by_tile_rows.set(p.tile_rows); p.by_N.set(1);
     p.window = win; p.sinks = sk;
     wa.lse = d_lse; wa.first = pl.from; wa.weight = d_weight; wa.weight_ld = weight_ld; wa.add = add != 0;
+    WeighTcArgs t = {};
+    t.w = wa;
+    const cudaError_t e = launch_after(weigh_start_kernel, (unsigned)(lanes < 16 * di->sms ? lanes : 16 * di->sms), 128, 0, st, t,
+                                       cache_args(cache, lanes, T, d_table, max_pages, d_len, d_lane_status), (const int*)d_first, pl.eff, pl.from, pl.begin, pl.steps);
+    if (e != cudaSuccess) return cuda_fail(e, "weigh start kernel launch");
     if (dtype == AS_F32) return cache->head_dim == 64 ? launch_weigh<AS_F32, 64>(wa, pl, di->sms, st) : launch_weigh<AS_F32, 128>(wa, pl, di->sms, st);
     return cache->head_dim == 64 ? launch_weigh<AS_BF16, 64>(wa, pl, di->sms, st) : launch_weigh<AS_BF16, 128>(wa, pl, di->sms, st);
 }

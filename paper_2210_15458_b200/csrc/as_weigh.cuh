@@ -17,32 +17,6 @@ struct WeighArgs {
     bool add;
 };
 
-// One CTA per lane: the length and beginning that the other kernels use, the lane's status, and 0 for the places that no row looks
-// at (in between the sinks and the first row's window) where sums are not added to older ones.
-static __global__ void __launch_bounds__(128) weigh_start_kernel(const CacheArgs c, const int* first, int* eff, int* from, int* begin, float* weight, long long weight_ld,
-                                                                 int window, int sinks, bool add) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    for (int b = blockIdx.x; b < c.lanes; b += gridDim.x) {
-        bool bad;
-        int len = lane_len(c, b, &bad);
-        const int f = first ? first[b] : 0;
-        bad = bad || len > weight_ld || f < 0 || f > len;
-        if (bad) len = 0;
-        if (threadIdx.x == 0) {
-            eff[b] = len;
-            from[b] = bad ? 0 : f;
-            begin[b] = bad ? 0 : f & ~15;
-            if (c.lane_status) c.lane_status[b] = bad ? AS_ERR_INVALID_ARG : AS_OK;
-        }
-        if (!add && !bad) {
-            const int lo = max(f, sinks), hi = min(len, len - c.T + 1 - window);
-            for (int h = 0; h < c.heads; ++h)
-                for (int t = lo + threadIdx.x; t < hi; t += 128) weight[((size_t)b * c.heads + h) * weight_ld + t] = 0.f;
-        }
-    }
-}
-
 // Adds what a token has got to its weight, or sets it.
 __device__ __forceinline__ void put_weight(const WeighArgs& wa, int lane, int head, int pos, int from, int len, float x) {
     if (pos < from || pos >= len) return;

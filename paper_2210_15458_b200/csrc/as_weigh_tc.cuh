@@ -8,13 +8,15 @@ namespace asx {
 
 constexpr int WT_ROWS = 128;                // query rows of a tile
 constexpr int WT_STAGES = 4;                // row tiles in shared memory, and score tiles in TMEM
-// Threads: a warp that issues products, one that brings in query tiles (two are not used), four that fill in keys, eight that sum.
-constexpr int WT_FILL = 4, WT_SUM = 8, WT_NT = 32 * (WT_SUM + 8);
+constexpr int WT_CONSTS = 8;                // row tiles whose factors and log-sums are in shared memory: those are needed until a tile is summed
+// Threads: a warp that issues products, one that brings in query tiles (two are not used), four that fill in keys, groups of four that sum.
+constexpr int WT_FILL = 4, WT_GROUPS = 3, WT_NT = 32 * (4 * WT_GROUPS + 8);
 constexpr int WT_MAX_RUNS = 160;
 
 // A row tile as it lies in scratch and in shared memory: 128 rows of f16, swizzled as tc_at() has it, then for each pair of rows
 // (factor of both, minus log-sum of both): a score s adds 2^(s factor - log-sum).
-template <int D> constexpr int WT_TILE = WT_ROWS * D * 2 + WT_ROWS * 8;
+template <int D> constexpr int WT_MAT = WT_ROWS * D * 2;
+template <int D> constexpr int WT_TILE = WT_MAT<D> + WT_ROWS * 8;
 
 struct WeighTcArgs {
     WeighArgs w;
@@ -52,24 +54,6 @@ struct WeighLane {
     }
 };
 
-// One CTA per lane: its steps.
-static __global__ void __launch_bounds__(128) weigh_steps_kernel(const __grid_constant__ WeighTcArgs t, int* steps) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ int sum;
-    for (int b = blockIdx.x; b < t.w.a.c.lanes; b += gridDim.x) {
-        if (threadIdx.x == 0) sum = 0;
-        __syncthreads();
-        const WeighLane l(t.w, b);
-        int mine = 0;
-        for (int i = threadIdx.x; i < l.tiles(); i += 128) mine += l.row_span(t.w, i).y;
-        atomicAdd(&sum, mine);
-        __syncthreads();
-        if (threadIdx.x == 0) steps[b] = sum;
-        __syncthreads();
-    }
-}
-
 // One CTA per row tile of a lane and key head: rows as f16, scaled by a power of two each, as the products take them.
 template <int D>
 __global__ void __launch_bounds__(256) weigh_rows_kernel(const __grid_constant__ WeighTcArgs t) {
@@ -82,7 +66,7 @@ __global__ void __launch_bounds__(256) weigh_rows_kernel(const __grid_constant__
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         const int rt = item % t.row_tiles, lh = item / t.row_tiles, lane = a.c.by_heads.div(lh), head = lh - lane * a.c.heads;
         char* to = t.tiles + (size_t)item * WT_TILE<D>;
-        float* consts = reinterpret_cast<float*>(to + WT_ROWS * D * 2);
+        float* consts = reinterpret_cast<float*>(to + WT_MAT<D>);
         const float to_log2 = a.scale * (a.c.k_scale ? a.c.k_scale[head] : 1.f) * 1.44269504088896f;
         const int j = threadIdx.x % PER;
 #pragma unroll
@@ -111,7 +95,7 @@ __global__ void __launch_bounds__(256) weigh_rows_kernel(const __grid_constant__
             const float down = __uint_as_float((uint32_t)(127 - ex) << 23);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = pack_f16(__uint_as_float(x[e] << 16) * down, __uint_as_float(x[e] & 0xFFFF0000u) * down);
-            *reinterpret_cast<uint4*>(to + ASX_AT((j / 8) * (WT_ROWS * 128) + tc_at(r, j % 8), WT_ROWS * D * 2 - 15, 361)) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4*>(to + ASX_AT((j / 8) * (WT_ROWS * 128) + tc_at(r, j % 8), WT_MAT<D> - 15, 361)) = make_uint4(x[0], x[1], x[2], x[3]);
             if (j == 0) {
                 consts[(r >> 1) * 4 + (r & 1)] = __uint_as_float((uint32_t)(127 + ex) << 23) * to_log2;
                 consts[(r >> 1) * 4 + 2 + (r & 1)] = -lse * 1.44269504088896f;
@@ -127,36 +111,15 @@ __device__ __forceinline__ void wait16(uint32_t (&r)[16]) {
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
                    "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) : : "memory");
 }
-// 2^x of two numbers without the unit for exponentials, which gives four results a cycle to a quarter of the SM and would bound the sums
-// alone: x = n + f, |f| <= 1/2, a polynomial of degree 5 in f (fitted for the least relative error, 2.3e-7 with the roundings: as near
-// as ex2.approx), times 2^n put together from its bits: 0 for n = -127, infinite for n = 128.  A NaN stays one.
-__device__ __forceinline__ float2 exp2_two(uint64_t x) {
-    const float2 in = unpair(x);
-    float lo, hi;
-    asm("{\n .reg .f32 t;\n max.NaN.f32 t, %1, %2;\n min.NaN.f32 %0, t, %3;\n}" : "=f"(lo) : "f"(in.x), "f"(-127.f), "f"(128.f));
-    asm("{\n .reg .f32 t;\n max.NaN.f32 t, %1, %2;\n min.NaN.f32 %0, t, %3;\n}" : "=f"(hi) : "f"(in.y), "f"(-127.f), "f"(128.f));
-    x = pair(lo, hi);
-    const uint64_t magic = pair(12582912.f, 12582912.f), t = add2(x, magic), f = fma2(add2(t, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x);
-    uint64_t p = fma2(f, pair(0.0013276472f, 0.0013276472f), pair(0.009675541f, 0.009675541f));
-    p = fma2(p, f, pair(0.05550713f, 0.05550713f));
-    p = fma2(p, f, pair(0.2402212f, 0.2402212f));
-    p = fma2(p, f, pair(0.69314694f, 0.69314694f));
-    p = fma2(p, f, pair(1.0000001f, 1.0000001f));
-    const float2 n = unpair(t);
-    uint64_t y;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(p), "l"(pair(__int_as_float((__float_as_int(n.x) << 23) + 0x3F800000), __int_as_float((__float_as_int(n.y) << 23) + 0x3F800000))));
-    return unpair(y);
-}
-
 struct WeighTcSmem {
-    unsigned long long q_full[WT_STAGES], q_empty[WT_STAGES], s_full[WT_STAGES], s_empty[WT_STAGES], k_full[2], k_empty[2], sum_full[2], sum_empty[2], fin;
+    unsigned long long q_full[WT_STAGES], q_empty[WT_STAGES], c_full[WT_CONSTS], c_empty[WT_CONSTS], s_full[WT_STAGES], s_empty[WT_STAGES], k_full[2], k_empty[2], sum_full[2], sum_empty[2], fin;
     uint32_t tmem;
     int failed;
     int start[5];                           // lane, head, token tile, step within it; steps of the run
     int warp_sum[WT_NT / 32];
-    float sum[2][TC_KV];
+    float sum[2][WT_GROUPS - 1][TC_KV];
 };
-template <int D> constexpr size_t weigh_tc_smem() { return 1024 + (size_t)2 * TC_KV * D * 2 + (size_t)WT_STAGES * WT_TILE<D> + (size_t)TC_KV * (D / 2) + sizeof(WeighTcSmem); }
+template <int D> constexpr size_t weigh_tc_smem() { return 1024 + (size_t)2 * TC_KV * D * 2 + (size_t)WT_STAGES * WT_MAT<D> + (size_t)WT_CONSTS * WT_ROWS * 8 + (size_t)TC_KV * (D / 2) + sizeof(WeighTcSmem); }
 
 // Where a run stands: (lane, head, token tile), the row tiles of that and how many of them are behind.
 struct WeighCursor {
@@ -192,7 +155,7 @@ struct WeighCursor {
 };
 
 // A token of a tile of 128 is a thread, S = K Q^T has a row for each token and a column for each query row: a thread adds up
-// 2^(s - z) over the columns that look at its token, row tile after row tile.  Two groups of 128 threads take the row tiles of a
+// 2^(s - z) over the columns that look at its token, row tile after row tile.  Groups of 128 threads take the row tiles of a
 // token tile in turn.  Steps (a token tile with a row tile) are dealt out to the CTAs in equal runs; a token tile that falls to
 // several leaves partial sums that the join kernel adds in the runs' order.
 template <int D>
@@ -201,7 +164,7 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
     constexpr int MAT = TC_KV * D * 2, BLK = TC_KV * 128, KSTEPS = D / 16;
     extern __shared__ char raw[];
     const uint32_t base = ((uint32_t)__cvta_generic_to_shared(raw) + 1023) & ~1023u;
-    const uint32_t k_s = base, q_s = k_s + 2 * MAT, raw_s = q_s + WT_STAGES * WT_TILE<D>;
+    const uint32_t k_s = base, q_s = k_s + 2 * MAT, c_s = q_s + WT_STAGES * WT_MAT<D>, raw_s = c_s + WT_CONSTS * WT_ROWS * 8;
     WeighTcSmem& sm = *reinterpret_cast<WeighTcSmem*>(raw + (raw_s + TC_KV * (D / 2) - (uint32_t)__cvta_generic_to_shared(raw)));
     auto bar = [](const unsigned long long& b) { return (uint32_t)__cvta_generic_to_shared(&b); };
     const WeighArgs& wa = t.w;
@@ -211,12 +174,13 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) {
         for (int i = 0; i < WT_STAGES; ++i) {
-            tc_bar_init(bar(sm.q_full[i]), 1); tc_bar_init(bar(sm.q_empty[i]), 1 + 4);
+            tc_bar_init(bar(sm.q_full[i]), 1); tc_bar_init(bar(sm.q_empty[i]), 1);
             tc_bar_init(bar(sm.s_full[i]), 1); tc_bar_init(bar(sm.s_empty[i]), 4);
         }
+        for (int i = 0; i < WT_CONSTS; ++i) { tc_bar_init(bar(sm.c_full[i]), 1); tc_bar_init(bar(sm.c_empty[i]), 4); }
         for (int i = 0; i < 2; ++i) {
             tc_bar_init(bar(sm.k_full[i]), WT_FILL); tc_bar_init(bar(sm.k_empty[i]), 1);
-            tc_bar_init(bar(sm.sum_full[i]), 4); tc_bar_init(bar(sm.sum_empty[i]), 4);
+            tc_bar_init(bar(sm.sum_full[i]), 4 * (WT_GROUPS - 1)); tc_bar_init(bar(sm.sum_empty[i]), 4);
         }
         tc_bar_init(bar(sm.fin), 1);
         sm.failed = 0;
@@ -305,14 +269,13 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
             const int from = rows_from(wa, cu.l.len, pos), to = place < cu.l.hi ? rows_to(wa, cu.l.len, pos) : 0;
             float sum = 0.f;
 #pragma unroll 1
-            for (int j = (x ^ s) & 1; j < tiles; j += 2) {          // (the groups take a run's steps in turn)
-                const int step = x + j, b = step % WT_STAGES;
-                const uint32_t use = (uint32_t)(step / WT_STAGES) & 1;
-                ok = wait_warp(sm.q_full[b], use) && wait_warp(sm.s_full[b], use);
+            for (int j = (s + WT_GROUPS - x % WT_GROUPS) % WT_GROUPS; j < tiles; j += WT_GROUPS) {          // (the groups take a run's steps in turn)
+                const int step = x + j, b = step % WT_STAGES, cb = step % WT_CONSTS;
+                ok = wait_warp(sm.c_full[cb], (uint32_t)(step / WT_CONSTS) & 1) && wait_warp(sm.s_full[b], (uint32_t)(step / WT_STAGES) & 1);
                 if (!ok) break;
                 tc_fence_after();
                 const int row0 = (cu.first + cu.at + j) * WT_ROWS;
-                const uint32_t consts = q_s + ASX_AT(b, WT_STAGES, 362) * WT_TILE<D> + WT_ROWS * D * 2;
+                const uint32_t consts = c_s + ASX_AT(cb, WT_CONSTS, 362) * (WT_ROWS * 8);
                 const int lo = from - row0, hi = to - row0;
                 const bool cut = __any_sync(0xFFFFFFFFu, lo > 0 || hi < WT_ROWS);
                 uint64_t part[2] = {0, 0};
@@ -323,11 +286,10 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
 #pragma unroll
                     for (int e = 0; e < 16; e += 2) {
                         const uint4 kz = lds<uint4>(at + e * 8);
-                        const uint64_t x = fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), pair(__uint_as_float(kz.x), __uint_as_float(kz.y)),
-                                                pair(__uint_as_float(kz.z), __uint_as_float(kz.w)));
-                        const float2 p = e % 6 == 0 ? exp2_two(x) : make_float2(ex2(unpair(x).x), ex2(unpair(x).y));
-                        y[e] = p.x;
-                        y[e + 1] = p.y;
+                        const float2 x = unpair(fma2(pair(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), pair(__uint_as_float(kz.x), __uint_as_float(kz.y)),
+                                                     pair(__uint_as_float(kz.z), __uint_as_float(kz.w))));
+                        y[e] = ex2(x.x);
+                        y[e + 1] = ex2(x.y);
                     }
                     if (cut) {
 #pragma unroll
@@ -350,7 +312,7 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) { tc_bar_arrive(bar(sm.s_empty[b])); tc_bar_arrive(bar(sm.q_empty[b])); }
+                if (lane == 0) { tc_bar_arrive(bar(sm.s_empty[b])); tc_bar_arrive(bar(sm.c_empty[cb])); }
                 const float2 both = unpair(add2(part[0], part[1]));
                 sum += both.x + both.y;         // (a tile's sum first, then the tiles')
             }
@@ -358,16 +320,17 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
             // ---- the end of a token tile or of the run: the groups' sums become one ----
             const int p = unit & 1;
             const uint32_t again = (uint32_t)(unit >> 1) & 1;
-            if (s == 1) {
+            if (s > 0) {
                 if (unit >= 2) ok = wait_warp(sm.sum_empty[p], again ^ 1);
                 if (!ok) break;
-                sm.sum[p][r] = sum;
+                sm.sum[p][ASX_AT(s - 1, WT_GROUPS - 1, 373)][r] = sum;
                 __syncwarp();
                 if (lane == 0) tc_bar_arrive(bar(sm.sum_full[p]));
             } else {
                 ok = wait_warp(sm.sum_full[p], again);
                 if (!ok) break;
-                sum += sm.sum[p][r];
+#pragma unroll
+                for (int i = 0; i < WT_GROUPS - 1; ++i) sum += sm.sum[p][i][r];
                 __syncwarp();
                 if (lane == 0) tc_bar_arrive(bar(sm.sum_empty[p]));
                 const bool begun = cu.at > 0, ends = cu.at + tiles == cu.n;
@@ -386,21 +349,35 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
         const uint32_t own = raw_s + r * 16;
         uint4 code[D / 32];
         uint2 scale = make_uint2(0, 0);
-        auto load = [&]() {                     // the token's codes and scales, for the cursor's token tile
-            const int place = cu.l.lo + cu.tile * TC_KV + r, pos = cu.l.hole.real(place);
-            const char* src = c.pages;
-            if (place < cu.l.hi) {
-                int page = c.table[(size_t)ASX_AT(cu.lane, c.lanes, 366) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 367)];
-                if (page < 0 || page >= c.n_pages) {
-                    flag_lane(c.lane_status, cu.lane, AS_ERR_INVALID_ARG);
-                    page = 0;
-                }
-                src += (((size_t)page * c.heads + ASX_AT(cu.head, c.heads, 368)) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
+        // the token's codes and scales a token tile before they are widened, its page's id one before that
+        WeighCursor ahead = cu;
+        int looked = 0, page = 0, next_lane = 0;
+        bool real = false;
+        const char* place0 = c.pages;           // the token's place within page 0 of its head
+        auto look = [&]() {
+            real = false;
+            if (looked >= run) return;
+            const int place = ahead.l.lo + ahead.tile * TC_KV + r, pos = ahead.l.hole.real(place);
+            if (place < ahead.l.hi) {
+                page = c.table[(size_t)ASX_AT(ahead.lane, c.lanes, 366) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 367)];
+                place0 = c.pages + ((size_t)ASX_AT(ahead.head, c.heads, 368) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
+                next_lane = ahead.lane;
+                real = true;
             }
+            looked += min(ahead.n - ahead.at, run - looked);
+            if (looked < run) ahead.next(t);
+        };
+        auto load = [&]() {
+            if (real && (page < 0 || page >= c.n_pages)) {
+                flag_lane(c.lane_status, next_lane, AS_ERR_INVALID_ARG);
+                page = 0;
+            }
+            const char* src = real ? place0 + (size_t)page * c.heads * tiles_per_page * Ti::BYTES : c.pages;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) code[i] = __ldg(reinterpret_cast<const uint4*>(src + Ti::k_code(tk, 2 * i)));
             if constexpr (D == 128) scale = __ldg(reinterpret_cast<const uint2*>(src + Ti::k_scale(tk, 0)));
             else scale.x = __ldg(reinterpret_cast<const uint32_t*>(src + Ti::k_scale(tk, 0)));
+            look();
         };
         auto widen = [](uint32_t codes, uint32_t scale2) {
             uint32_t f[4];
@@ -408,6 +385,7 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
             return make_uint4(mul_f16(f[0], scale2), mul_f16(f[1], scale2), mul_f16(f[2], scale2), mul_f16(f[3], scale2));
         };
         auto put = [](uint32_t at, const uint4& v) { asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory"); };
+        look();
         load();
 #pragma unroll 1
         for (int unit = 0; x < run && ok; ++unit) {
@@ -448,21 +426,28 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
                 const char* src = t.tiles + (((size_t)cu.lane * c.heads + cu.head) * t.row_tiles + cu.first + cu.at) * WT_TILE<D>;
 #pragma unroll 1
                 for (int j = 0; j < tiles && ok; ++j, ++x, src += WT_TILE<D>) {
-                    const int b = x % WT_STAGES;
-                    if (x >= WT_STAGES) ok = tc_wait(bar(sm.q_empty[b]), ((uint32_t)(x / WT_STAGES) & 1) ^ 1, limit, failed);
+                    const int b = x % WT_STAGES, cb = x % WT_CONSTS;
+                    if (x >= WT_CONSTS) ok = tc_wait(bar(sm.c_empty[cb]), ((uint32_t)(x / WT_CONSTS) & 1) ^ 1, limit, failed);
+                    if (ok && x >= WT_STAGES) ok = tc_wait(bar(sm.q_empty[b]), ((uint32_t)(x / WT_STAGES) & 1) ^ 1, limit, failed);
                     if (!ok) break;
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(sm.q_full[b])), "r"((uint32_t)WT_TILE<D>) : "memory");
-                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                                 ::"r"(q_s + ASX_AT(b, WT_STAGES, 372) * WT_TILE<D>), "l"(src), "r"((uint32_t)WT_TILE<D>), "r"(bar(sm.q_full[b])) : "memory");
+                    auto copy = [&](uint32_t to, const char* from, uint32_t bytes, uint32_t full) {
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full), "r"(bytes) : "memory");
+                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                     ::"r"(to), "l"(from), "r"(bytes), "r"(full) : "memory");
+                    };
+                    copy(q_s + ASX_AT(b, WT_STAGES, 372) * WT_MAT<D>, src, WT_MAT<D>, bar(sm.q_full[b]));
+                    copy(c_s + ASX_AT(cb, WT_CONSTS, 374) * (WT_ROWS * 8), src + WT_MAT<D>, WT_ROWS * 8, bar(sm.c_full[cb]));
                 }
                 if (ok && x < run) cu.next(t);
             }
             // copies in flight end before the CTA does
-            for (int i = max(0, x - WT_STAGES); i < x; ++i) {
+            auto landed = [&](uint32_t full, uint32_t parity) {
                 const long long start = clock64();
 #pragma unroll 1
-                while (!tc_try(bar(sm.q_full[i % WT_STAGES]), (uint32_t)(i / WT_STAGES) & 1) && clock64() - start < 2000000000LL) {}
-            }
+                while (!tc_try(full, parity) && clock64() - start < 2000000000LL) {}
+            };
+            for (int i = max(0, x - WT_STAGES); i < x; ++i) landed(bar(sm.q_full[i % WT_STAGES]), (uint32_t)(i / WT_STAGES) & 1);
+            for (int i = max(0, x - WT_CONSTS); i < x; ++i) landed(bar(sm.c_full[i % WT_CONSTS]), (uint32_t)(i / WT_CONSTS) & 1);
         }
     } else if (w == 0) {
         // ------------------------------------------------ issuing ------------------------------------------------
@@ -482,7 +467,7 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
                     if (ok && x >= WT_STAGES) ok = tc_wait(bar(sm.s_empty[b]), use ^ 1, limit, failed);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t q_d = tc_desc(q_s + b * WT_TILE<D>, 0);
+                    const uint64_t q_d = tc_desc(q_s + b * WT_MAT<D>, 0);
 #pragma unroll
                     for (int k = 0; k < KSTEPS; ++k) {
                         const uint32_t at = (k / 4) * (BLK >> 4) + (k % 4) * 2;
