@@ -29,6 +29,7 @@ struct VerifyArgs {
     double* codes_out;
     int* lane_status;
     RowCut* cuts;                           // [lanes][2 K + 1]: the target's rows, then the draft's
+    int *stop, *arrived;                    // [lanes] K + 1 - place of the first refusal known so far, [lanes][K] rows of a place that are done; 0 at first
 };
 
 __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int lane) {
@@ -41,7 +42,43 @@ __device__ __forceinline__ RowCut* cut_of(const VerifyArgs& a, int lane, int i, 
     return a.cuts + ASX_AT((long long)lane * (2 * a.K + 1) + (of_draft ? a.K + 1 + i : i), (long long)a.lanes * (2 * a.K + 1), 341);
 }
 
-// A CTA to a row: its kept tokens and their mass, by the general routine of the step.
+template <int DT>
+struct RowMass {
+    using Tr = Traits<DT>;
+    const char* row;
+    bool vec;
+    RowCut c;
+    __device__ RowMass(const char* r, const RowCut* cut) : row(r), vec((reinterpret_cast<uintptr_t>(r) & 15) == 0) {
+        // (another CTA may just have written it: past L1)
+        c.lmax = __ldcg(&cut->lmax); c.Z = __ldcg(&cut->Z);
+        c.T = __ldcg(&cut->T); c.tie = __ldcg(&cut->tie); c.status = __ldcg(&cut->status);
+    }
+    __device__ __forceinline__ double operator()(uint32_t key, int j, double inv_tau, const double* tbl) const {
+        return key > c.T || (key == c.T && j <= c.tie) ? exp_nonpos(((double)Tr::value_f(key) - c.lmax) * inv_tau, tbl) : 0.0;
+    }
+};
+
+// What becomes of the lane's drafted token i, both rows' cuts known: 0 accepted, 1 refused, else an error.
+template <int DT>
+__device__ __noinline__ int decide(const VerifyArgs& a, int lane, int i, const double* tbl) {
+    const int x = a.drafted[(size_t)lane * a.K + i];
+    const double u = a.u[(size_t)lane * a.K + i];
+    const RowMass<DT> p(target_row(a, lane, i), cut_of(a, lane, i, false));
+    if (x < 0 || x >= a.V) return AS_ERR_INVALID_ARG;
+    if (!(u >= 0.0 && u < 1.0) || p.c.status != ST_OK) return AS_ERR_NUMERIC;
+    const double px = p(Traits<DT>::load_key(p.row, x), x, a.inv_tau, tbl) / p.c.Z;
+    double qx = 1.0;
+    if (a.draft) {
+        const RowMass<DT> q(draft_row(a, lane, i), cut_of(a, lane, i, true));
+        if (q.c.status != ST_OK) return AS_ERR_NUMERIC;
+        qx = q(Traits<DT>::load_key(q.row, x), x, a.inv_tau, tbl) / q.c.Z;
+    }
+    return u * qx < px ? 0 : 1;
+}
+
+// A CTA to a row: its kept tokens and their mass, by the general routine of the step.  Rows come in the order of their places; whoever
+// finishes a place's last row looks what becomes of its token, and rows behind a refusal that is known by the time they start are left out.
+// (Which those are depends on timing, what comes out does not: nobody looks at them.)
 template <int DT>
 __global__ void __launch_bounds__(VF_NT) verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ GenericSmem<VF_NT> sm;
@@ -51,7 +88,8 @@ __global__ void __launch_bounds__(VF_NT) verify_rows_kernel(const __grid_constan
     const int per = a.draft ? 2 : 1, block = blockIdx.x / a.lanes, lane = blockIdx.x - block * a.lanes;
     const int i = block / per;
     const bool of_draft = block % per;
-    if (i > drafts_of(a, lane) - (of_draft ? 1 : 0)) return;
+    const int n = drafts_of(a, lane);
+    if (i > n - (of_draft ? 1 : 0) || a.K + 1 - i < __ldcg(a.stop + lane)) return;
     const char* row = of_draft ? draft_row(a, lane, i) : target_row(a, lane, i);
     GenericLane<DT, VF_NT> g(sm, row, a.V, (reinterpret_cast<uintptr_t>(row) & 15) == 0);
     g.inv_tau = a.inv_tau;
@@ -89,20 +127,17 @@ __global__ void __launch_bounds__(VF_NT) verify_rows_kernel(const __grid_constan
         c.Z = sm.chunk_sum[g.nchunks];
         c.T = p.T;
     }
-    if (threadIdx.x == 0) *cut_of(a, lane, i, of_draft) = c;
-}
-
-template <int DT>
-struct RowMass {
-    using Tr = Traits<DT>;
-    const char* row;
-    bool vec;
-    RowCut c;
-    __device__ RowMass(const char* r, const RowCut* cut) : row(r), vec((reinterpret_cast<uintptr_t>(r) & 15) == 0), c(*cut) {}
-    __device__ __forceinline__ double operator()(uint32_t key, int j, double inv_tau, const double* tbl) const {
-        return key > c.T || (key == c.T && j <= c.tie) ? exp_nonpos(((double)Tr::value_f(key) - c.lmax) * inv_tau, tbl) : 0.0;
+    if (threadIdx.x == 0) {
+        *cut_of(a, lane, i, of_draft) = c;
+        if (i < n) {
+            __threadfence();
+            if (!a.draft || atomicAdd(&a.arrived[(size_t)lane * a.K + i], 1) == 1) {
+                __threadfence();
+                if (decide<DT>(a, lane, i, sm.exp_tbl) != 0) atomicMax(&a.stop[lane], a.K + 1 - i);
+            }
+        }
     }
-};
+}
 
 // One CTA per lane: how many of its tokens are accepted, and the token behind them by its code, over masses
 // max(p - q Zp / Zq, 0) in units of 1 / Zp: sums of chunks in index order, the chunk that holds the code, the token in it.
@@ -128,25 +163,8 @@ __global__ void __launch_bounds__(VF_NT) verify_finish_kernel(const __grid_const
             for (int i0 = 0; i0 < n; i0 += 32) {
                 const int i = i0 + lane32;
                 int what = 0;
-                if (i < n) {
-                    const int x = a.drafted[(size_t)lane * a.K + i];
-                    const double u = a.u[(size_t)lane * a.K + i];
-                    const RowMass<DT> p(target_row(a, lane, i), cut_of(a, lane, i, false));
-                    if (x < 0 || x >= a.V) {
-                        what = AS_ERR_INVALID_ARG;
-                    } else if (!(u >= 0.0 && u < 1.0) || p.c.status != ST_OK) {
-                        what = AS_ERR_NUMERIC;
-                    } else {
-                        const double px = p(Tr::load_key(p.row, x), x, a.inv_tau, sm.exp_tbl) / p.c.Z;
-                        double qx = 1.0;
-                        if (a.draft) {
-                            const RowMass<DT> q(draft_row(a, lane, i), cut_of(a, lane, i, true));
-                            if (q.c.status != ST_OK) what = AS_ERR_NUMERIC;
-                            else qx = q(Tr::load_key(q.row, x), x, a.inv_tau, sm.exp_tbl) / q.c.Z;
-                        }
-                        if (what == 0) what = u * qx < px ? 0 : 1;
-                    }
-                }
+                // (rows behind a refusal may have been left out)
+                if (i < n && a.K + 1 - i >= a.stop[lane]) what = decide<DT>(a, lane, i, sm.exp_tbl);
                 const unsigned stop = __ballot_sync(FULL, what != 0);
                 if (stop) {
                     const int l = __ffs(stop) - 1;
@@ -992,7 +1010,8 @@ template <int DT>
 static cudaError_t launch_verify(const VerifyArgs& a, int sms, cudaStream_t st) {
     if ((a.top_k <= 0 || a.top_k >= a.V) && !(a.top_p > 0.0 && a.top_p < 1.0)) return launch_verify_lanes<DT>(a, sms, st);
     const unsigned rows = (unsigned)((long long)a.lanes * (a.draft ? 2 * a.K + 1 : a.K + 1));
-    cudaError_t e = launch_after(verify_rows_kernel<DT>, rows, VF_NT, 0, st, a);
+    cudaError_t e = cudaMemsetAsync(a.stop, 0, sizeof(int) * (size_t)a.lanes * (a.K + 1), st);
+    if (e == cudaSuccess) e = launch_after(verify_rows_kernel<DT>, rows, VF_NT, 0, st, a);
     if (e != cudaSuccess) return e;
     return launch_after(verify_finish_kernel<DT>, (unsigned)(a.lanes < 64 * sms ? a.lanes : 64 * sms), VF_NT, 0, st, a);
 }
@@ -1006,7 +1025,7 @@ extern "C" {
 size_t as_step_verify_work_bytes(int dtype, int lanes, int K, int V) {
     if (lanes < 1 || K < 0 || V < 1 || V > AS_MAX_V || (dtype != AS_F32 && dtype != AS_BF16)) return 0;
     if ((long long)lanes * (2LL * K + 1) > 0x7FFFFFFFLL) return 0;
-    return sizeof(RowCut) * (size_t)lanes * (2 * (size_t)K + 1);
+    return sizeof(RowCut) * (size_t)lanes * (2 * (size_t)K + 1) + sizeof(int) * (size_t)lanes * (K + 1);
 }
 
 int as_step_verify(const void* d_target, long long target_ld, const void* d_draft, long long draft_ld, int dtype, int lanes, int K, int V,
@@ -1040,6 +1059,8 @@ int as_step_verify(const void* d_target, long long target_ld, const void* d_draf
     a.top_p = top_p; a.top_k = top_k;
     a.tokens = d_tokens; a.accepted = d_accepted; a.codes_out = d_codes_out; a.lane_status = d_lane_status;
     a.cuts = static_cast<RowCut*>(d_work);
+    a.stop = reinterpret_cast<int*>(a.cuts + (size_t)lanes * (2 * (size_t)K + 1));
+    a.arrived = a.stop + lanes;
     const cudaError_t e = dtype == AS_F32 ? launch_verify<AS_F32>(a, di->sms, (cudaStream_t)stream) : launch_verify<AS_BF16>(a, di->sms, (cudaStream_t)stream);
     return e == cudaSuccess ? AS_OK : cuda_fail(e, "verify kernel launch");
 }
