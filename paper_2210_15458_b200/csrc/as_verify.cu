@@ -733,11 +733,12 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                         } else if (!(u >= 0.0 && u < 1.0) || p_bad || q_bad) {
                             what = AS_ERR_NUMERIC;
                         } else {
-                            const double px = token_mass<DT>(target_row(a, lane, i), x, MassRow(p.m, c256), c256, sm.exp_tbl) / p.s;
-                            const double qx = u * (a.draft ? token_mass<DT>(draft_row(a, lane, i), x, MassRow(q.m, c256), c256, sm.exp_tbl) / q.s : 1.0);
-                            // (a side that is 0 is so whatever the sums)
+                            const double ep = token_mass<DT>(target_row(a, lane, i), x, MassRow(p.m, c256), c256, sm.exp_tbl);
+                            const double eq = u * (a.draft ? token_mass<DT>(draft_row(a, lane, i), x, MassRow(q.m, c256), c256, sm.exp_tbl) : 1.0);
+                            // (a side that is 0 is so whatever the sums; a row too far out for sums in 32 bits has none)
                             const bool far = fabsf(p.m) * c > VN_FAR || (a.draft && fabsf(q.m) * c > VN_FAR);
-                            what = px > 0.0 && qx > 0.0 && (far || fabs(qx - px) <= VN_NEAR * fmax(qx, px)) ? 2 : qx < px ? 0 : 1;
+                            const double px = ep / p.s, qx = eq / q.s;
+                            what = ep == 0.0 ? 1 : eq == 0.0 ? 0 : far || fabs(qx - px) <= VN_NEAR * fmax(qx, px) ? 2 : qx < px ? 0 : 1;
                         }
                     }
                 }

@@ -1,0 +1,95 @@
+"""Offsets past 32 bits, no lanes, results that do not depend on scheduling: windowed attention, weights, eviction, trim, verification."""
+import pytest
+
+torch = pytest.importorskip("torch")
+from tests import test_gpu_cache4 as C  # noqa: E402
+from tests import test_gpu_evict as E  # noqa: E402
+from tests import test_gpu_verify as V  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2210_15458_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_pages_past_32_bits(B, T):
+    """The same lanes in pages at a pool's beginning and beyond its first 2^32 bytes."""
+    H, D, P, Hq = 8, 128, 128, 16
+    n = (5 << 30) // (H * (P // 16) * 18 * D)
+    pages = B.cache4_pages(n, H, D, P)
+    lens = [300, 260]
+    low, high = C.i32([[0, 1, 2], [3, 4, 5]]), C.i32([[n - 1, n - 3, n - 5], [n - 2, n - 6, n - 4]])
+    gen = torch.Generator().manual_seed(1)
+    k, v = torch.randn(2, 300, H, D, generator=gen).cuda(), torch.randn(2, 300, H, D, generator=gen).cuda()
+    q = torch.randn(2, T, Hq, D, generator=gen).bfloat16().cuda()
+    for t in (low, high):
+        B.as_cache4_append(pages, k, v, t, C.i32(lens))
+    got = []
+    for t in (low, high):
+        lse, w = torch.empty(2, T, Hq, device="cuda"), torch.zeros(2, H, 300, device="cuda")
+        out = B.as_cache4_attend(pages, q, t, C.i32(lens), 0.1, lse=lse, window=50, sinks=3)
+        B.as_cache4_attend(pages, q, t, C.i32(lens), 0.1, lse=lse)
+        B.as_cache4_weigh(pages, q, lse, t, C.i32(lens), 0.1, w)
+        weigh = w.clone()
+        B.as_cache4_evict(pages, w, t, C.i32(lens), C.i32([100, 90]), 20, first=C.i32([2, 2]))
+        got.append((out, weigh, w, torch.stack([E.tokens(pages, t, i, h, 90) for i in range(2) for h in range(H)])))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][1].sum() > 0
+
+
+@pytest.mark.parametrize("top_p", [1.0, 0.9])
+def test_rows_past_32_bits(B, top_p):
+    lanes, K, V_ = 12000, 1, 100003
+    t = torch.zeros(lanes, K + 1, V_, dtype=torch.bfloat16, device="cuda")
+    target, draft, drafted, u, codes = (x.cuda() for x in V.inputs(6, K, V_, "bf16", 3))
+    t[-6:] = target
+    d = torch.zeros(lanes, K, V_, dtype=torch.bfloat16, device="cuda")
+    d[-6:] = draft
+    all_drafted, all_u, all_codes = drafted[:1].expand(lanes, K).contiguous(), u[:1].expand(lanes, K).contiguous(), codes[:1].expand(lanes).contiguous()
+    all_drafted[-6:], all_u[-6:], all_codes[-6:] = drafted, u, codes
+    want = B.as_step_verify(target, draft, drafted, u, codes, 1.0, 0, top_p)
+    got = B.as_step_verify(t, d, all_drafted, all_u, all_codes, 1.0, 0, top_p)
+    assert torch.equal(got[0][-6:], want[0]) and torch.equal(got[1][-6:], want[1]) and (got[2][-6:] - want[2]).abs().max() < 1e-9
+    # rows of zeros: every token alike, so that the draft is accepted; the code takes token floor(code V) where nothing is cut
+    assert (got[1][:-6] == 1).all()
+    if top_p == 1.0:
+        assert (got[0][:-6, 1] == int(float(codes[0]) * V_)).all()
+
+
+def test_no_lanes(B):
+    pages = B.cache4_pages(4, 2, 64, 16)
+    table, n = torch.empty(0, 3, dtype=torch.int32, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    q, w = torch.empty(0, 1, 2, 64, device="cuda"), torch.empty(0, 2, 48, device="cuda")
+    assert B.as_cache4_attend(pages, q, table, n, 1.0, window=4).shape == q.shape
+    B.as_cache4_weigh(pages, q, torch.empty(0, 1, 2, device="cuda"), table, n, 1.0, w)
+    B.as_cache4_evict(pages, w, table, n, n)
+    x = torch.empty(0, 3, 8, device="cuda")
+    tokens, accepted, codes = B.as_step_verify(x, x[:, :2], torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, dtype=torch.float64, device="cuda"),
+                                               torch.empty(0, dtype=torch.float64, device="cuda"))
+    assert tokens.shape == (0, 3) and accepted.numel() == codes.numel() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top_p", [1.0, 0.9])
+def test_the_same_call_gives_the_same_bits(B, dtype, top_p):
+    """Tokens with p near q go through a list whose order depends on timing; rows behind a refusal may or may not be read."""
+    target, draft, drafted, u, codes = (x.cuda() for x in V.inputs(200, 3, 20011, dtype, 7, alike=1e-3))
+    u.fill_(0.9995)                                 # (many are refused, with little left of p - q)
+    first = B.as_step_verify(target, draft, drafted, u, codes, 1.0, 0, top_p)
+    assert (first[1] < 3).any()
+    for _ in range(20):
+        again = B.as_step_verify(target, draft, drafted, u, codes, 1.0, 0, top_p)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("offset", [1e4, -3e5, 1e12, 1e30])
+@pytest.mark.parametrize("temp", [1e-3, 1.0, 1e4])
+def test_logits_far_from_zero(B, offset, temp):
+    """p and q depend on differences of logits alone; far out those are multiples of a float's spacing."""
+    target, draft, drafted, u, codes = V.inputs(40, 2, 300, "f32", 11)
+    target, draft = target + offset, draft + offset
+    V.check(B, target, draft, drafted, u, codes, temp, 0, 1.0)
+    V.check(B, target, draft, drafted, u, codes, temp, 0, 0.9)
