@@ -364,6 +364,10 @@ __device__ __forceinline__ V peer(const V& mine, int rank, int ctas) {
     return got;
 }
 
+// The CTAs' values of a cluster, one to a thread of each warp (0 behind the last): what is done with them is the same everywhere.
+__device__ __forceinline__ double of_cluster(const double& mine, int ctas) { return (int)(threadIdx.x & 31) < ctas ? peer(mine, threadIdx.x & 31, ctas) : 0.0; }
+__device__ __forceinline__ double cluster_total(const double& mine, int ctas) { return ctas == 1 ? mine : warp_sum_d(of_cluster(mine, ctas)); }
+
 // A row as 16-byte granules from the boundary at or below its start: element e of granule g is token g E + e - off.
 template <int DT>
 struct Granules {
@@ -543,9 +547,8 @@ __device__ __forceinline__ double mass64(float x, const MassRow& r, double c256,
 }
 
 // of one token of a row: 0 where it counts as none
-template <int DT>
-__device__ __forceinline__ double token_mass(const char* row, int x, const MassRow& r, double c256, const double* tbl) {
-    const double e = mass64(Pass<DT>::load_f(row, x), r, c256, tbl);
+__device__ __forceinline__ double token_mass(float l, const MassRow& r, double c256, const double* tbl) {
+    const double e = mass64(l, r, c256, tbl);
     return e > VN_NONE ? e : 0.0;
 }
 
@@ -695,6 +698,18 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
 #pragma unroll 1
         while (!done) {
             const int count = min(batch, n + 1 - i0);
+            // (what the decisions need, on its way while the rows are summed)
+            int x = -1;
+            double u = 0.0;
+            float lp = 0.f, lq = 0.f;
+            if (tid < count && i0 + tid < n) {
+                x = a.drafted[(size_t)lane * a.K + i0 + tid];
+                u = a.u[(size_t)lane * a.K + i0 + tid];
+                if (x >= 0 && x < a.V) {
+                    lp = Pass<DT>::load_f(target_row(a, lane, i0 + tid), x);
+                    if (a.draft) lq = Pass<DT>::load_f(draft_row(a, lane, i0 + tid), x);
+                }
+            }
 #pragma unroll 1
             for (int b = 0; b < count; ++b) {
                 row_sum<DT>(target_row(a, lane, i0 + b), a.V, c, rank, ctas, ring, sm.warp[2 * b]);
@@ -707,34 +722,42 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                 sm.mine[tid] = r;
             }
             cluster_sync(ctas);
+            if (tid < 2 * VN_BATCH * VN_MAX_CTAS) {     // eight threads to a row, one to a CTA's part
+                const int row = tid / VN_MAX_CTAS, k = tid % VN_MAX_CTAS;
+                const bool there = row < 2 * count && (row % 2 == 0 || (a.draft && i0 + row / 2 < n));
+                RowSum r = {0.0, -INFINITY, 0};
+                if (there && k < ctas) r = peer(sm.mine[row], k, ctas);
+#pragma unroll
+                for (int o = 1; o < VN_MAX_CTAS; o <<= 1) {
+                    RowSum other;
+                    other.s = __shfl_xor_sync(FULL, r.s, o);
+                    other.m = __shfl_xor_sync(FULL, r.m, o);
+                    other.bad = __shfl_xor_sync(FULL, r.bad, o);
+                    r = join_sums(r, other, c);
+                }
+                if (k == 0) sm.row[row] = there ? r : RowSum{1.0, 0.f, 0};
+            }
+            __syncthreads();
             if (warp == 0) {
                 // a thread to a place
                 int what = 0;
                 RowSum p = {1.0, 0.f, 0}, q = {1.0, 0.f, 0};
                 const int i = i0 + lane32;
                 if (lane32 < count) {
-                    p = peer(sm.mine[2 * lane32], 0, ctas);
-                    for (int k = 1; k < ctas; ++k) p = join_sums(p, peer(sm.mine[2 * lane32], k, ctas), c);
-                    if (a.draft && i < n) {
-                        q = peer(sm.mine[2 * lane32 + 1], 0, ctas);
-                        for (int k = 1; k < ctas; ++k) q = join_sums(q, peer(sm.mine[2 * lane32 + 1], k, ctas), c);
-                    }
-                    sm.row[2 * lane32] = p;
-                    sm.row[2 * lane32 + 1] = q;
+                    p = sm.row[2 * lane32];
+                    q = sm.row[2 * lane32 + 1];
                     // 0 accepted, 1 refused, 2 too near, 3 the last place; else an error
                     const bool p_bad = p.bad || p.m == -INFINITY, q_bad = q.bad || q.m == -INFINITY;
                     if (i == n) {
                         what = p_bad ? AS_ERR_NUMERIC : 3;
                     } else {
-                        const int x = a.drafted[(size_t)lane * a.K + i];
-                        const double u = a.u[(size_t)lane * a.K + i];
                         if (x < 0 || x >= a.V) {
                             what = AS_ERR_INVALID_ARG;
                         } else if (!(u >= 0.0 && u < 1.0) || p_bad || q_bad) {
                             what = AS_ERR_NUMERIC;
                         } else {
-                            const double ep = token_mass<DT>(target_row(a, lane, i), x, MassRow(p.m, c256), c256, sm.exp_tbl);
-                            const double eq = u * (a.draft ? token_mass<DT>(draft_row(a, lane, i), x, MassRow(q.m, c256), c256, sm.exp_tbl) : 1.0);
+                            const double ep = token_mass(lp, MassRow(p.m, c256), c256, sm.exp_tbl);
+                            const double eq = u * (a.draft ? token_mass(lq, MassRow(q.m, c256), c256, sm.exp_tbl) : 1.0);
                             // (a side that is 0 is so whatever the sums; a row too far out for sums in 32 bits has none)
                             const bool far = fabsf(p.m) * c > VN_FAR || (a.draft && fabsf(q.m) * c > VN_FAR);
                             const double px = ep / p.s, qx = eq / q.s;
@@ -760,15 +783,10 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                 if (a.draft) pair_pass<DT, true>(sm, pair, 0.0, false);
                 else pair_pass<DT, false>(sm, pair, 0.0, false);
                 cluster_sync(ctas);
-                double zp = 0.0, zq = 0.0;
-                for (int k = 0; k < ctas; ++k) {
-                    const PairSum t = peer(sm.part, k, ctas);
-                    zp += t.zp;
-                    zq += t.zq;
-                }
+                const double zp = cluster_total(sm.part.zp, ctas), zq = cluster_total(sm.part.zq, ctas);
                 const int x = a.drafted[(size_t)lane * a.K + i];
-                const double px = token_mass<DT>(target_row(a, lane, i), x, pair.mp, c256, sm.exp_tbl) / zp;
-                const double qx = a.draft ? token_mass<DT>(draft_row(a, lane, i), x, pair.mq, c256, sm.exp_tbl) / zq : 1.0;
+                const double px = token_mass(Pass<DT>::load_f(target_row(a, lane, i), x), pair.mp, c256, sm.exp_tbl) / zp;
+                const double qx = a.draft ? token_mass(Pass<DT>::load_f(draft_row(a, lane, i), x), pair.mq, c256, sm.exp_tbl) / zq : 1.0;
                 if (a.u[(size_t)lane * a.K + i] * qx < px) {
                     i0 = i + 1;
                 } else {
@@ -803,14 +821,8 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                 if (l.q) pair_pass<DT, true>(sm, l, w, near);
                 else pair_pass<DT, false>(sm, l, w, near);
                 cluster_sync(ctas);
-                double zp = 0.0, zq = 0.0;
-                int most = 0;
-                for (int k = 0; k < ctas; ++k) {
-                    const PairSum t = peer(sm.part, k, ctas);
-                    zp += t.zp;
-                    zq += t.zq;
-                    most = max(most, t.listed);
-                }
+                const double zp = cluster_total(sm.part.zp, ctas), zq = cluster_total(sm.part.zq, ctas);
+                const int most = ctas == 1 ? sm.part.listed : __reduce_max_sync(FULL, lane32 < ctas ? peer(sm.part.listed, lane32, ctas) : 0);
                 ratio = l.q ? zp / zq : 0.0;
                 if (most > VN_LIST || vague) {
                     cluster_sync(ctas);
@@ -850,8 +862,7 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                     if (lane32 == 0) sm.rest = run;
                 }
                 cluster_sync(ctas);
-                total = 0.0;
-                for (int k = 0; k < ctas; ++k) total += peer(sm.rest, k, ctas);
+                total = cluster_total(sm.rest, ctas);
                 if (total > VN_NONE) break;
                 cluster_sync(ctas);
                 l.q = nullptr;              // p and q are alike in 64 bits
@@ -861,19 +872,18 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
             }
             const double t = (c_in == 1.0 ? ASX_ONE_BELOW : c_in) * total;
             // ---- the CTA, the chunk, the sub-row and the token whose interval holds t ----
-            int owner = -1, last = -1;
-            double base = 0.0, own_base = 0.0, last_base = 0.0;
-            for (int k = 0; k < ctas; ++k) {
-                const double r = peer(sm.rest, k, ctas);
-                if (r > 0.0) {
-                    if (owner < 0 && t < base + r) { owner = k; own_base = base; }
-                    last = k;
-                    last_base = base;
-                }
-                base += r;
+            int owner = 0;
+            double own_base = 0.0;
+            bool top = !(t < sm.rest);          // (one CTA) rounding at the top end: the last token
+            if (ctas > 1) {
+                const double r = of_cluster(sm.rest, ctas), upto = warp_incl_scan_d(r, lane32);
+                double before = __shfl_up_sync(FULL, upto, 1);
+                if (lane32 == 0) before = 0.0;
+                const unsigned has = __ballot_sync(FULL, r > 0.0), hit = __ballot_sync(FULL, r > 0.0 && t < upto);
+                top = hit == 0;
+                owner = hit ? __ffs(hit) - 1 : 31 - __clz(has);
+                own_base = __shfl_sync(FULL, before, owner);
             }
-            const bool top = owner < 0;     // rounding at the top end: the last token
-            if (top) { owner = last; own_base = last_base; }
             if (owner == rank) {
                 const int chunks = l.c1 - l.c0;
                 if (warp == 0) {
