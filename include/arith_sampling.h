@@ -194,7 +194,8 @@ int as_step_lattice(const void *d_logits, int dtype, int lanes, int V, long long
  *                range or a row that as_step could not use.  Rows, tokens and u behind the first refusal do not count.  Such a lane gets -1 throughout,
  *                accepts 0 tokens and keeps its code
  *   d_work       as_step_verify_work_bytes(...) bytes of device scratch, 256-byte aligned
- * Decisions are those of 64-bit arithmetic.  Errors: as as_step.
+ * Decisions are those of 64-bit arithmetic; a token that is less likely than 2^-950 times its row's likeliest may count as one of
+ * probability 0.  Errors: as as_step.
  */
 size_t as_step_verify_work_bytes(int dtype, int lanes, int K, int V);
 int as_step_verify(const void *d_target, long long target_ld, const void *d_draft, long long draft_ld, int dtype,

@@ -526,7 +526,7 @@ struct MassRow {
         sub = far ? m : 0.f;
         const double top = far ? 0.0 : m;
         mc = top * c256;
-        low = fmaxf((float)(top - 256000.0 / c256), -3.4e38f);      // (above -inf, whatever the temperature)
+        low = fmaxf((float)(top - 256000.0 / c256), -3.4e38f);      // (above -inf)
     }
 };
 __device__ __forceinline__ double mass64(float x, const MassRow& r, double c256, const double* tbl) {
@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
     sm.exp_tbl[tid] = ASX_T64[tid >> 2] * (tid & 2 ? 0x1.0163da9fb3335p+0 : 1.0) * (tid & 1 ? 0x1.00b1afa5abcbfp+0 : 1.0);
     __syncthreads();
     const double c256 = 256.0 * 1.4426950408889634 * a.inv_tau;
-    const float c = (float)fmin(1.4426950408889634 * a.inv_tau, 3e38);
+    const float c = (float)(1.4426950408889634 * a.inv_tau);
 #pragma unroll 1
     for (int lane = blockIdx.x / ctas; lane < a.lanes; lane += gridDim.x / ctas) {
         const int n = drafts_of(a, lane);
@@ -1019,7 +1019,9 @@ static cudaError_t launch_verify_lanes(const VerifyArgs& a, int sms, cudaStream_
 
 template <int DT>
 static cudaError_t launch_verify(const VerifyArgs& a, int sms, cudaStream_t st) {
-    if ((a.top_k <= 0 || a.top_k >= a.V) && !(a.top_p > 0.0 && a.top_p < 1.0)) return launch_verify_lanes<DT>(a, sms, st);
+    // (temperatures whose reciprocals come near a float's range, next to which -inf and the lowest float are no masks any more, take the general routine)
+    const bool tame = a.inv_tau >= 1e-30 && a.inv_tau <= 1e30;
+    if (tame && (a.top_k <= 0 || a.top_k >= a.V) && !(a.top_p > 0.0 && a.top_p < 1.0)) return launch_verify_lanes<DT>(a, sms, st);
     const unsigned rows = (unsigned)((long long)a.lanes * (a.draft ? 2 * a.K + 1 : a.K + 1));
     cudaError_t e = cudaMemsetAsync(a.stop, 0, sizeof(int) * (size_t)a.lanes * (a.K + 1), st);
     if (e == cudaSuccess) e = launch_after(verify_rows_kernel<DT>, rows, VF_NT, 0, st, a);

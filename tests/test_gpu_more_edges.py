@@ -1,4 +1,5 @@
 """Offsets past 32 bits, no lanes, results that do not depend on scheduling: windowed attention, weights, eviction, trim, verification."""
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -93,3 +94,16 @@ def test_logits_far_from_zero(B, offset, temp):
     target, draft = target + offset, draft + offset
     V.check(B, target, draft, drafted, u, codes, temp, 0, 1.0)
     V.check(B, target, draft, drafted, u, codes, temp, 0, 0.9)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temp", [1e-300, 1e-40, 1e-29, 1e29, 1e40, 1e300])
+@pytest.mark.parametrize("lanes", [3, 700])
+def test_temperatures_next_to_nothing_and_beyond_measure(B, dtype, temp, lanes):
+    """The largest logit alone, or all that are not masked alike."""
+    target, draft, drafted, u, codes = V.inputs(lanes, 2, 300, dtype, 13)
+    target[:, :, 7:200] = float("-inf")
+    draft[:, :, 5:150] = float("-inf")
+    with np.errstate(over="ignore"):
+        V.check(B, target, draft, drafted, u, codes, temp, 0, 1.0)
+        V.check(B, target, None, drafted, u, codes, temp, 0, 1.0)
