@@ -207,6 +207,7 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
         }
         const unsigned U = (unsigned)total * c.heads, G = min((unsigned)t.runs, U), k = blockIdx.x;
         if (k >= G) return;
+        if (tid == 0) t.info[ASX_AT(k, WT_MAX_RUNS, 365)] = make_int4(0, 0, 0, 0);  // (nothing to join, should a wait run out)
         const unsigned q = U / G, r = U - q * G;
         const unsigned from = q * k + r * k / G, n = q * (k + 1) + r * (k + 1) / G - from;
         unsigned at = (unsigned)before * c.heads;

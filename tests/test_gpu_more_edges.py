@@ -107,3 +107,30 @@ def test_temperatures_next_to_nothing_and_beyond_measure(B, dtype, temp, lanes):
     with np.errstate(over="ignore"):
         V.check(B, target, draft, drafted, u, codes, temp, 0, 1.0)
         V.check(B, target, None, drafted, u, codes, temp, 0, 1.0)
+
+
+@pytest.mark.parametrize("window", [None, 150])
+def test_a_wait_that_runs_out_reports_timeout_and_the_next_call_is_fine(B, window):
+    """The kernels for many rows with a bound of a thousand cycles on their waits, their scratch full of what is no answer."""
+    lens, T, H, sinks = [2700, 1900], 300, 2, 5
+    pages, table, k, v = C.filled(B, lens, H, 128, 64, 11, None, None)
+    q = torch.randn(2, T, 8, 128).cuda().bfloat16()
+    lse, weight = torch.empty(2, T, 8, device="cuda"), torch.zeros(2, H, 2700, device="cuda")
+    good = B.as_cache4_attend(pages, q, table, C.i32(lens), 0.09, lse=lse, window=window, sinks=sinks if window else 0)
+    kw = dict(window=window, sinks=sinks if window else 0, add=False)
+    B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.09, weight, **kw)
+    statuses = [C.i32([9, 9]), C.i32([9, 9])]
+    work = torch.full((B.as_cache4_weigh_work_bytes(pages, B.BF16, 2, T, 8),), 0x7F, dtype=torch.uint8, device="cuda")
+    try:
+        B.as_tune(B.TUNE_WAIT_KCYCLES, 1)
+        B.as_cache4_attend(pages, q, table, C.i32(lens), 0.09, window=window, sinks=sinks if window else 0, lane_status=statuses[0])
+        B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.09, torch.zeros_like(weight), lane_status=statuses[1], work=work, **kw)
+        torch.cuda.synchronize()
+    finally:
+        B.as_tune(B.TUNE_WAIT_KCYCLES, 0)
+    assert all(s.tolist() == [B.ERR_TIMEOUT, B.ERR_TIMEOUT] for s in statuses)
+    again = torch.zeros_like(weight)
+    B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.09, again, lane_status=statuses[1], work=work, **kw)
+    assert torch.equal(again, weight) and statuses[1].tolist() == [0, 0] and weight.sum() > 0
+    assert torch.equal(B.as_cache4_attend(pages, q, table, C.i32(lens), 0.09, window=window, sinks=sinks if window else 0, lane_status=statuses[0]), good)
+    assert statuses[0].tolist() == [0, 0]
