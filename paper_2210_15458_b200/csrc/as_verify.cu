@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(VF_NT) verify_finish_kernel(const __grid_const
 constexpr int VN_NT = 256, VN_NW = VN_NT / 32;
 constexpr int VN_CHUNKS = 128;              // of a CTA
 constexpr int VN_LIST = 256;
-constexpr int VN_BATCH = 8;                 // places whose rows are read before the decisions are taken
+constexpr int VN_BATCH = 4;                 // places, at most, whose rows are read before the decisions are taken
 constexpr int VN_MAX_CTAS = 8;
 constexpr int VN_U = 4, VN_STAGES = 3;      // granules of a thread at a time, steps that it has in flight or in use
 // Of a sum in 32 bits: terms are off by 2^-22 (the exponential) and 2^-23 of their exponent, at most 130 before they vanish; 32 of
@@ -997,11 +997,17 @@ static cudaError_t launch_verify_lanes(const VerifyArgs& a, int sms, cudaStream_
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    // CTAs to a lane: as many as find room side by side, two or three on an SM
-    int ctas = 1;
-    while (ctas < VN_MAX_CTAS && 2LL * ctas * a.lanes <= 2LL * sms) ctas *= 2;
-    // many lanes read no row that may not be needed; few read several places' rows between two meetings
-    const int batch = ctas == 1 ? 1 : VN_BATCH;
+    // CTAs to a lane: one on each SM, or as many as find room side by side, three on an SM, if a row has a step for each
+    // (bf16, 120 x 4 x 128256: 3 of them 127 us, 1 of them 184; 150 x 5 x 25391: 70 us with 2, 80 with 1; 150 x 4 x 4000: 32 us with 1, 37 with 2;
+    // 4 x 3 x 8000: 25 us with 8, 28 with 1)
+    const long long steps = ((long long)a.V * Traits<DT>::BYTES + VN_U * VN_NT * 16 - 1) / (VN_U * VN_NT * 16), room = 3LL * sms / a.lanes;
+    long long wanted = sms / a.lanes;
+    if (wanted < (steps < room ? steps : room)) wanted = steps < room ? steps : room;
+    const int ctas = (int)(wanted < 1 ? 1 : wanted > VN_MAX_CTAS ? VN_MAX_CTAS : wanted);
+    // Places whose rows are read before their decisions: a meeting costs about what a CTA's step does.  Rows of one step, four (30 x 5 x 32000: 36 us,
+    // 37 with two, 40 with eight; 759 x 8 x 2010: 87 us, 91 with one); longer ones, two if a cluster has to meet (1 x 7 x 127484: 34 us, 53
+    // with eight; 4 x 3 x 32000: 26 us, 30 with one), else one (500 x 8 x 50257 in 32 bits: 327 us, 333 with two).
+    const int batch = steps <= ctas ? VN_BATCH : ctas > 1 ? 2 : 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((a.lanes < 64 * sms ? a.lanes : 64 * sms) * ctas));
     cfg.blockDim = dim3(VN_NT);
