@@ -7,8 +7,6 @@ namespace asx {
 
 ASX_BOUNDS_READER(bounds_verify)
 
-constexpr int VF_NT = 512;
-
 // What a row's distribution needs besides the row: p_j = exp((l_j - lmax) / temp) / Z over the kept tokens, those whose key is
 // above T or equal to it and at an index up to `tie`.
 struct RowCut {
@@ -79,7 +77,7 @@ __device__ __noinline__ int decide(const VerifyArgs& a, int lane, int i, const d
 // A CTA to a row: its kept tokens and their mass, by the general routine of the step.  Rows come in the order of their places; whoever
 // finishes a place's last row looks what becomes of its token, and rows behind a refusal that is known by the time they start are left out.
 // (Which those are depends on timing, what comes out does not: nobody looks at them.)
-template <int DT>
+template <int DT, int VF_NT>
 __global__ void __launch_bounds__(VF_NT) verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ GenericSmem<VF_NT> sm;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -141,7 +139,7 @@ __global__ void __launch_bounds__(VF_NT) verify_rows_kernel(const __grid_constan
 
 // One CTA per lane: how many of its tokens are accepted, and the token behind them by its code, over masses
 // max(p - q Zp / Zq, 0) in units of 1 / Zp: sums of chunks in index order, the chunk that holds the code, the token in it.
-template <int DT>
+template <int DT, int VF_NT>
 __global__ void __launch_bounds__(VF_NT) verify_finish_kernel(const __grid_constant__ VerifyArgs a) {
     using Tr = Traits<DT>;
     constexpr int E = Tr::E, NW = VF_NT / 32;
@@ -1029,10 +1027,15 @@ static cudaError_t launch_verify(const VerifyArgs& a, int sms, cudaStream_t st) 
     const bool tame = a.inv_tau >= 1e-30 && a.inv_tau <= 1e30;
     if (tame && (a.top_k <= 0 || a.top_k >= a.V) && !(a.top_p > 0.0 && a.top_p < 1.0)) return launch_verify_lanes<DT>(a, sms, st);
     const unsigned rows = (unsigned)((long long)a.lanes * (a.draft ? 2 * a.K + 1 : a.K + 1));
+    // A CTA has 1024 threads where each finds an SM of its own and the row has 16 bytes for more than 512 of them: 5 x 2 x 38634, both cuts, 107 us in
+    // place of 133 with 512, 96 x 5 x 50257, nucleus, 367 in place of 385; else 512: 41 x 3 x 2836, nucleus, 51 us in place of 85 with 1024, 1 x 5 x 742 46 in
+    // place of 49.
+    const bool wide = (long long)a.V * Traits<DT>::BYTES > 512 * 16;
     cudaError_t e = cudaMemsetAsync(a.stop, 0, sizeof(int) * (size_t)a.lanes * (a.K + 1), st);
-    if (e == cudaSuccess) e = launch_after(verify_rows_kernel<DT>, rows, VF_NT, 0, st, a);
+    if (e == cudaSuccess) e = wide && rows <= (unsigned)sms ? launch_after(verify_rows_kernel<DT, 1024>, rows, 1024, 0, st, a) : launch_after(verify_rows_kernel<DT, 512>, rows, 512, 0, st, a);
     if (e != cudaSuccess) return e;
-    return launch_after(verify_finish_kernel<DT>, (unsigned)(a.lanes < 64 * sms ? a.lanes : 64 * sms), VF_NT, 0, st, a);
+    const unsigned grid = (unsigned)(a.lanes < 64 * sms ? a.lanes : 64 * sms);
+    return wide && a.lanes <= sms ? launch_after(verify_finish_kernel<DT, 1024>, grid, 1024, 0, st, a) : launch_after(verify_finish_kernel<DT, 512>, grid, 512, 0, st, a);
 }
 
 }  // namespace asx
