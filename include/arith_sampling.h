@@ -688,6 +688,10 @@ int as_pages_trim(const int32_t *d_keep, const int32_t *d_gone, int lanes, int m
  *                         top-k is first looked for through bins of the logit value (two passes
  *                         over the row for a nucleus of any width), and the radix select takes
  *                         the rows that the bins cannot settle; the results are the same
+ *   AS_TUNE_WINDOW_GROUPS 1 = as_cache4_attend_window reads shared beginnings once for a group
+ *                         whatever the window.  By default each lane reads its own window where
+ *                         the windows of all lanes are small together; results differ by
+ *                         rounding alone
  * Returns AS_ERR_INVALID_ARG for an unknown key or value.  The keys are process-wide; a launch
  * reads each once (concurrent calls see the old or the new value).
  */
@@ -700,6 +704,7 @@ int as_pages_trim(const int32_t *d_keep, const int32_t *d_gone, int lanes, int m
 #define AS_TUNE_WAIT_KCYCLES 7
 #define AS_TUNE_DEBUG_NO_COPY 8
 #define AS_TUNE_RADIX_NUCLEUS 9
+#define AS_TUNE_WINDOW_GROUPS 10
 int as_tune(int key, int value);
 
 /* Text of the calling thread's most recent error ("" if none). Never NULL. */

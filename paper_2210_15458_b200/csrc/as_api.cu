@@ -25,8 +25,9 @@ struct Tune {
     void operator=(int x) { v.store(x, std::memory_order_relaxed); }
 };
 static Tune g_tune_path, g_tune_cluster, g_tune_ctas, g_tune_stages, g_tune_minb, g_tune_serial,
-    g_tune_wait_kcycles, g_tune_no_copy, g_tune_radix_nucleus;
+    g_tune_wait_kcycles, g_tune_no_copy, g_tune_radix_nucleus, g_tune_window_groups;
 
+bool window_groups_now() { return g_tune_window_groups != 0; }
 long long wait_cycles_now() {
     const int k = g_tune_wait_kcycles;
     return k > 0 ? (long long)k * 1000 : ST_WAIT_CYCLES;
@@ -594,6 +595,10 @@ int as_tune(int key, int value) {
         case AS_TUNE_RADIX_NUCLEUS:
             if (value != 0 && value != 1) return set_err(AS_ERR_INVALID_ARG, "AS_TUNE_RADIX_NUCLEUS takes 0 or 1");
             g_tune_radix_nucleus = value;
+            return AS_OK;
+        case AS_TUNE_WINDOW_GROUPS:
+            if (value != 0 && value != 1) return set_err(AS_ERR_INVALID_ARG, "AS_TUNE_WINDOW_GROUPS takes 0 or 1");
+            g_tune_window_groups = value;
             return AS_OK;
         default:
             return set_err(AS_ERR_INVALID_ARG, "unknown tuning key %d", key);

@@ -121,13 +121,21 @@ static cudaError_t launch_pass(const AttendArgs& a, PassArgs& p, Kernel kernel, 
     return launch_mma<DT, D, 1, WIN>(a, p, sms, st);
 }
 
+// Whether a pass over shared beginnings is worth its three kernels: windows that are small together each lane reads by itself, most of
+// them from L2.  Lanes x 8 heads of 128, four query heads to each, contexts of 6000, own / shared, us: 128 lanes, windows of 512 (75 MB)
+// 37 / 48..55, 1024 (151 MB) 54 / 53..56, 2048 84 / 62; 32 lanes, 2048 (75 MB) 34 / 48, 4096 49 / 53.
+inline bool by_groups(const AttendArgs& a, int D, int window, int sinks) {
+    const long long most = (long long)a.c.max_pages << a.c.page_shift, tokens = (long long)window + sinks;
+    return window_groups_now() || (long long)a.c.lanes * a.c.heads * (tokens < most ? tokens : most) * (D * 18 / 16) > 1LL << 27;
+}
+
 template <int DT, int D, bool WIN>
 static int launch_attend(const AttendArgs& a, int N, const int* shared, int window, int sinks, void* work, int sms, cudaStream_t st) {
     AttendPlan pl = plan_attend(DT, a.c.lanes, a.c.T, a.c.heads, a.q_heads, D, N, work);
     pl.own.window = pl.pre.window = window;
     pl.own.sinks = pl.pre.sinks = sinks;
     cudaError_t e = cudaSuccess;
-    if (shared && N > 1) {
+    if (shared && N > 1 && (!WIN || by_groups(a, D, window, sinks))) {
         attend_shared_kernel<<<a.c.lanes / N, 128, 0, st>>>(a.c, N, shared, pl.begin, WIN ? pl.shortest : nullptr);
         pl.own.begin = pl.pre.begin = pl.begin;
         pl.pre.shortest = pl.shortest;

@@ -19,6 +19,7 @@ int check_scalars(int dtype, int V, long long ld, double temp, double top_p);   
 int check_data(const void* data, int dtype);
 
 long long wait_cycles_now();                        // bound on every on-device wait, in clock cycles (AS_TUNE_WAIT_KCYCLES)
+bool window_groups_now();                           // shared beginnings by groups whatever the window (AS_TUNE_WINDOW_GROUPS)
 
 constexpr size_t SMEM_OPTIN_MAX = 232448;           // 227 KB per CTA on sm_100
 

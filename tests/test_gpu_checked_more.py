@@ -31,6 +31,12 @@ def test_window(B, dtype, D, lens, T, Hq, H, P, window, sinks):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,T,Hq,H,D,P,shared,tails,window,sinks", W.SHARED)
+def test_window_by_groups(B, dtype, N, T, Hq, H, D, P, shared, tails, window, sinks):  # noqa: F811
+    W.test_shared_beginnings_by_groups(B, dtype, N, T, Hq, H, D, P, shared, tails, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("lens,T,Hq,H,P,window,sinks", G.SHAPES)
 def test_weigh(B, dtype, D, lens, T, Hq, H, P, window, sinks):  # noqa: F811

@@ -74,12 +74,15 @@ def test_attention(B, dtype, D, lens, T, Hq, H, P, window, sinks):
     check(B, dtype, out, lse, q, k, v, lens, scale, window, sinks)
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("N,T,Hq,H,D,P,shared,tails,window,sinks", [
+SHARED = [
     (2, 1, 2, 1, 64, 16, [32], [1, 9], 20, 2), (3, 1, 4, 2, 128, 16, [0, 48], [5, 1, 17, 1, 2, 40], 30, 4), (16, 1, 8, 2, 128, 64, [640], list(range(1, 17)), 300, 70),
     (32, 1, 4, 1, 64, 32, [320], [1] * 31 + [70], 50, 0), (33, 1, 8, 1, 128, 64, [1024, 64], [1 + i % 7 for i in range(66)], 128, 17),
     (5, 1, 40, 4, 64, 128, [256], [3, 1, 4, 1, 200], 100, 1), (4, 3, 4, 2, 64, 16, [160], [6, 9, 40, 200], 60, 5), (4, 40, 4, 1, 128, 32, [96], [40, 41, 60, 45], 64, 3),
-    (2, 1, 4, 2, 64, 16, [160], [100, 90], 64, 0), (64, 1, 4, 1, 64, 128, [1280], [1 + i for i in range(64)], 700, 128)])
+    (2, 1, 4, 2, 64, 16, [160], [100, 90], 64, 0), (64, 1, 4, 1, 64, 128, [1280], [1 + i for i in range(64)], 700, 128)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,T,Hq,H,D,P,shared,tails,window,sinks", SHARED)
 def test_shared_beginnings(B, dtype, N, T, Hq, H, D, P, shared, tails, window, sinks):
     lens = [shared[i // N] + t for i, t in enumerate(tails)]
     gen = torch.Generator().manual_seed(N)
@@ -90,6 +93,23 @@ def test_shared_beginnings(B, dtype, N, T, Hq, H, D, P, shared, tails, window, s
         lse = torch.empty(len(lens), T, Hq, device="cuda")
         out = B.as_cache4_attend(pages, q, table, C.i32(lens), scale, N=N, shared=hint, lse=lse, window=window, sinks=sinks)
         check(B, dtype, out, lse, q, k, v, lens, scale, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,T,Hq,H,D,P,shared,tails,window,sinks", SHARED)
+def test_shared_beginnings_by_groups(B, dtype, N, T, Hq, H, D, P, shared, tails, window, sinks):
+    """The same where small windows are read by groups as well."""
+    try:
+        B.as_tune(B.TUNE_WINDOW_GROUPS, 1)
+        test_shared_beginnings(B, dtype, N, T, Hq, H, D, P, shared, tails, window, sinks)
+    finally:
+        B.as_tune(B.TUNE_WINDOW_GROUPS, 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_windows_that_are_read_by_groups_unasked(B, dtype):
+    """64 lanes x 8 heads x 1900 tokens of 144 bytes are more than 2^27 bytes."""
+    test_shared_beginnings(B, dtype, 32, 1, 8, 8, 128, 64, [2048, 1984], [1 + i % 9 for i in range(64)], 1900, 4)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
