@@ -407,7 +407,9 @@ template <int D> __host__ __device__ __forceinline__ constexpr int state_floats(
 // products is token 4 (l / 2 mod 4) + (l mod 2) + 2 (l / 8) of the tile.
 // Bound by issue slots: 364 instructions for a tile of 16 tokens at head dimension 128, conversions and products mostly
 // (60 % of the slots, ALU pipe 54 %, DRAM 52 %: no unit is full, 3.5 warps a scheduler do not hide every wait).  128 lanes of up to 8192 tokens, 32 heads on 8: 178 to 194 us (4.2 to 4.6 TB/s); in 32
-// bits, 12 lanes of up to 30001: 95 us (3.1 TB/s).
+// bits, 12 lanes of up to 30001: 95 us (3.1 TB/s).  With a window (WIN) the tokens between the sinks and the first row's window are no
+// places at all, and only units that a row's window or length cuts are masked: 64 lanes of up to 30000 with the last 4096: 74 us, the join 7
+// (3.7 TB/s), the same units busy.
 template <int DT, int D, int NT, bool SOLO, bool WIN>
 __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ PassArgs p) {
     using Ti = Tile4<D>;

@@ -133,6 +133,10 @@ __device__ __forceinline__ void move_tokens(const EvictArgs& e, int lane, int he
 // that come free below the new end and by the tokens that stay from behind it, a list of each at a time; then the recent tokens move down in
 // their order, a batch being read before it is written.
 // Few lanes and heads: a cluster of CTAs to one, each of which selects for itself and moves its share of the tokens.
+// Only what changes its place is read and written, and the recent tokens alone keep their order: a token that stays in front of the new
+// end does not move.  Bound by latency: 64 x 8 heads, 2112 tokens to 2048 with 512 recent ones 50 us (1.8 TB/s of what has to move; issue slots 38 %, DRAM
+// 23 %), selection a third of it; 8 x 8 heads, up to 30000 to 4096, 111 us: selection 40, then 3700 tokens from all over the cache to
+// each head, whose tiles are brought into L2 whole (without that 204 us).
 template <int D, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 1) evict_kernel(const __grid_constant__ EvictArgs e, int room, int ctas) {
     extern __shared__ __align__(16) char ev_smem[];
@@ -395,10 +399,13 @@ static cudaError_t launch_evict_nt(const EvictArgs& e, size_t most, int ctas, in
 }
 template <int D>
 static cudaError_t launch_evict(const EvictArgs& e, int sms, cudaStream_t st) {
-    // Many lanes and heads: small CTAs, four on an SM; few: the largest there are, each with an SM's shared memory, several to one as
-    // long as they all run side by side.
-    const long long items = (long long)e.c.lanes * e.c.heads;
-    if (items > 2LL * sms) return launch_evict_nt<D, 256, false>(e, 56 * 1024, 1, sms, st);
+    // Many lanes and heads: small CTAs, four on an SM, if the keys find room there; few, or long ones: the largest there are, each with an SM's
+    // shared memory, several to one as long as they all run side by side.  Small / large, us: 2112 tokens, 8 heads, 32 lanes 29 / 51, 64 lanes 46 / 101, 16
+    // lanes 27 / 27; up to 30000 tokens, 40 lanes 555 / 374, 8 lanes 288 / 113 (one to each 153).
+    const long long items = (long long)e.c.lanes * e.c.heads, tokens = (long long)e.c.max_pages << e.c.page_shift;
+    constexpr size_t SMALL = 56 * 1024;
+    const bool fits = (e.weight_ld < tokens ? e.weight_ld : tokens) <= (long long)(SMALL - sizeof(EvictSmem<256>)) / 4;
+    if (fits && items > sms) return launch_evict_nt<D, 256, false>(e, SMALL, 1, sms, st);
     int ctas = 1;
     while (ctas < EV_MAX_CTAS && 2 * ctas * items <= sms) ctas *= 2;
     return ctas == 1 ? launch_evict_nt<D, 1024, false>(e, SMEM_OPTIN_MAX, 1, sms, st) : launch_evict_nt<D, 1024, true>(e, SMEM_OPTIN_MAX, ctas, sms, st);

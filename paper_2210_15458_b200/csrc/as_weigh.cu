@@ -7,9 +7,10 @@ namespace asx {
 
 ASX_BOUNDS_READER(bounds_weigh)
 
-// bf16 rows beyond 16 go to the tensor cores' 128-row tiles; up to 16 fit the instructions on registers.  32-bit ones stay there
-// whatever their number: an f16 operand holds half of one.
-static bool many_rows(int dtype, int rows) { return dtype == AS_BF16 && rows > 16; }
+// bf16 rows beyond 48 go to the tensor cores' 128-row tiles; up to 48 are taken 16 at a time by the instructions on registers.  32 lanes of up to
+// 8192 tokens, 8 heads, registers / tensor cores, us: 16 rows 53 / 283, 20 to 32 rows 151 / 271..292, 64 rows 297 / 275, 128 rows 653 / 301.  32-bit
+// ones stay on registers whatever their number: an f16 operand holds half of one.
+static bool many_rows(int dtype, int rows) { return dtype == AS_BF16 && rows > 48; }
 
 struct WeighPlan {
     int *eff, *from, *begin, *steps;
@@ -41,7 +42,7 @@ static WeighPlan plan_weigh(int dtype, int lanes, int T, int heads, int q_heads,
 
 // One CTA per lane: the length and beginning that the other kernels use, the lane's status, 0 for the places that no row looks at (in
 // between the sinks and the first row's window) where sums are not added to older ones, and the lane's steps if the tensor cores are to
-// take them (t.steps not null).
+// take them (t.steps not null).  Latency, 3 to 5 us.
 static __global__ void __launch_bounds__(128) weigh_start_kernel(const __grid_constant__ WeighTcArgs t, const CacheArgs c, const int* first, int* eff, int* from, int* begin, int* steps) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -124,6 +125,7 @@ template <int DT, int D>
 static int launch_weigh(WeighArgs& wa, const WeighPlan& pl, int sms, cudaStream_t st) {
     cudaError_t e;
     if (many_rows(DT, wa.p.rows)) e = launch_weigh_tc<D>(wa, pl, sms, st);
+    else if (DT == AS_BF16 && wa.p.rows > 16) e = launch_weigh_mma<DT, D, DT == AS_BF16 ? 2 : 1, true>(wa, sms, st);
     else if (DT == AS_BF16 && wa.p.rows > 8) e = launch_weigh_mma<DT, D, DT == AS_BF16 ? 2 : 1, false>(wa, sms, st);
     else if (DT == AS_F32 && wa.p.rows > 8) e = launch_weigh_mma<DT, D, 1, DT == AS_F32>(wa, sms, st);
     else e = launch_weigh_mma<DT, D, 1, false>(wa, sms, st);

@@ -32,8 +32,12 @@ template <int D> struct WeighSmem {
     RunSmem run;
 };
 
-// A warp has a run of its own.  Scores are formed as in attention, S^T = K q^T (tokens x rows); rows beyond 8 NT (MANY) are taken 8 NT
-// at a time on the same keys.
+// Up to 48 rows, or 32-bit ones.  A warp has a run of its own: tokens of all lanes and heads are dealt out to the warps in equal contiguous
+// runs of pairs of tiles, and as sums stay with their tokens nothing is joined.  Scores are formed as in attention, S^T = K q^T (tokens x
+// rows), so that a token's sum is over neighbouring threads' columns: two shuffles; rows beyond 8 NT (MANY) are taken 8 NT at a time on the same keys.
+// Bound by issue slots: about 240 instructions for a tile of 16 tokens at head dimension 128, widening the keys mostly (59 % of the slots, ALU
+// pipe 40 %, DRAM 37 %, 3.8 warps a scheduler).  64 lanes of up to 8192 tokens, 32 heads on 8: 70 us (3.2 TB/s, 49 % of a copy's rate); a page's id is
+// fetched a unit ahead, the old weight while the scores are formed (84 us without both).
 template <int DT, int D, int NT, bool MANY>
 __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant__ WeighArgs wa) {
     using Ti = Tile4<D>;
