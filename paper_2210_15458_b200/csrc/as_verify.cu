@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(VF_NT) verify_finish_kernel(const __grid_const
 // those within VN_NEAR of e_p = w e_q is known to have p > q or not, and
 //   sum of max(p - q, 0) over a chunk = A / Zp - B / Zq,   A, B the masses of its tokens with p > q;
 // the few others are listed and added once Zp and Zq are known.
-// Bound by instructions: 1024 x 4 x 128256 in bf16 takes 617 us where its bytes take 199 (issue slots 60 %, special-function unit 39 %, 64-bit pipe
+// Bound by instructions: 1024 x 4 x 128256 in bf16 takes 618 to 632 us where its bytes take 199 (issue slots 60 %, special-function unit 39 %, 64-bit pipe
 // 25 %), about half of it the rows in 32 bits, half the last pair in 64; all of it in 64 bits took 1013 us, exponentials by the step's routine
 // 3254.  4 x 3 x 32000: 25 us, of which the host's call 22; row sums a fifth of the kernel, decisions, chunk sums and the pick by single warps most of it.
 // ---------------------------------------------------------------------------
