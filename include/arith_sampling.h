@@ -536,7 +536,8 @@ int as_cache4_attend(const as_cache4 *cache, const void *d_q, long long q_ld, in
  * as_cache4_attend with a sliding window: a query token at position p looks at positions p - window + 1 .. p and at the first
  * `sinks` of its lane.  Everything else as as_cache4_attend, its scratch included (as_cache4_attend_work_bytes): chunks, shared
  * beginnings, rows that see nothing.  Pages that lie wholly between the sinks and the first query token's window are not
- * looked up: a lane may have given them up (as_pages_trim).
+ * looked up: a lane may have given them up (as_pages_trim), each lane of a group on its own; a shared beginning is looked up in the
+ * row of the group's shortest lane, which has to hold what its window and sinks reach.
  *   window  >= 1;  sinks  >= 0
  * Errors: as as_cache4_attend, plus AS_ERR_INVALID_ARG for window < 1 or sinks < 0.
  */

@@ -58,7 +58,7 @@ struct PassArgs {
     int runs;
     long long wait_cycles;
     int window, sinks;                      // (of kernels built with WIN alone)
-    const int* shortest;                    // [lanes / N] length of a group's shortest lane
+    const int2* shortest;                   // [lanes / N] length of a group's shortest lane, and which lane that is
 };
 
 __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad = nullptr) {
@@ -71,12 +71,16 @@ __device__ __forceinline__ int lane_len(const CacheArgs& c, int lane, bool* bad 
 // entry sees lies between those two parts and is stepped over, whole tiles of 16 tokens at a time: tokens are counted without
 // the `skip` positions from `at` on (both multiples of 16), and a place in a page is looked up at real().  Pages that lie wholly in between
 // are not even looked up.  [sinks, low): counted places that no row sees.
+// The lane whose row of the table names the pages of a shared beginning is the group's shortest: its window reaches furthest back,
+// and what the others' windows have left behind they may have given up.
 template <bool WIN> struct Hole {
     __device__ __forceinline__ int real(int pos) const { return pos; }
+    __device__ __forceinline__ int holder(int lane0) const { return lane0; }
 };
 template <> struct Hole<true> {
-    int at, skip, low;
+    int at, skip, low, lane;
     __device__ __forceinline__ int real(int pos) const { return pos >= at ? pos + skip : pos; }
+    __device__ __forceinline__ int holder(int) const { return lane; }
 };
 
 // the tokens [lo, hi) that the rows of an entry read; behind a tile's last row nothing is seen
@@ -90,9 +94,10 @@ __device__ __forceinline__ void token_range(const AttendArgs& a, const PassArgs&
         hi = max(lo, hi - a.c.T + 1 + a.by_g.div(last));
     }
     if constexpr (WIN) {
-        // (the lanes of a group differ in length: the shortest one's window reaches furthest back)
-        const int first = p.prefix ? p.shortest[ASX_AT(b, a.c.lanes / p.N, 171)] - a.c.T + 1
-                                   : lane_len(a.c, b) - a.c.T + 1 + a.by_g.div((entry - b * p.row_tiles) * p.tile_rows);
+        // (the lanes of a group differ in length)
+        const int2 by = p.prefix ? p.shortest[ASX_AT(b, a.c.lanes / p.N, 171)] : make_int2(0, b);
+        const int first = p.prefix ? by.x - a.c.T + 1 : lane_len(a.c, b) - a.c.T + 1 + a.by_g.div((entry - b * p.row_tiles) * p.tile_rows);
+        hole.lane = by.y;
         const int low = max(0, first - p.window);
         hole.at = max(lo, (p.sinks + 15) & ~15);
         hole.skip = max(0, min(low & ~15, hi) - hole.at);       // (hi is cut by `low` only where it ends a page)
@@ -435,7 +440,7 @@ __global__ void __launch_bounds__(AT_NT) attend_mma_kernel(const __grid_constant
     int page = 0;
     auto look = [&]() {                             // page id of the half-warp's tile under `ahead`
         const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
-        if (pos < ahead.hi) page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 127) * c.max_pages + ASX_AT(ahead.hole.real(pos) >> c.page_shift, c.max_pages, 128)];
+        if (pos < ahead.hi) page = c.table[(size_t)ASX_AT(ahead.hole.holder(ahead.lane0), c.lanes, 127) * c.max_pages + ASX_AT(ahead.hole.real(pos) >> c.page_shift, c.max_pages, 128)];
     };
     auto issue = [&](int stage) {
         const int pos = ahead.lo + ((SOLO ? ahead.u : ahead.u * AT_W + w) * 2 + half) * 16;
@@ -834,20 +839,24 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
 }
 
 // One CTA per group: the shared beginning that can be used (0 where the caller's does not fit), and, if `shortest` is not null, the
-// length of the group's shortest lane.
-static __global__ void __launch_bounds__(128) attend_shared_kernel(const CacheArgs c, int N, const int* shared, int* begin, int* shortest) {
+// group's shortest lane, the first of equal ones.
+static __global__ void __launch_bounds__(128) attend_shared_kernel(const CacheArgs c, int N, const int* shared, int* begin, int2* shortest) {
     const int gr = blockIdx.x, s = shared[gr];
-    __shared__ int least;
-    if (threadIdx.x == 0) least = 0x7FFFFFFF;
+    __shared__ unsigned long long least;            // (length, lane)
+    if (threadIdx.x == 0) least = ~0ull;
     __syncthreads();
     bool ok = s > 0 && (s & ((1 << c.page_shift) - 1)) == 0;
-    int len = 0x7FFFFFFF;
-    for (int j = threadIdx.x; j < N; j += 128) len = min(len, lane_len(c, gr * N + j));
-    atomicMin(&least, len);
-    ok = __syncthreads_and(ok && s <= len);
+    unsigned long long mine = ~0ull;
+    for (int j = threadIdx.x; j < N; j += 128) {
+        const unsigned long long one = (unsigned long long)lane_len(c, gr * N + j) << 32 | (unsigned)(gr * N + j);
+        mine = one < mine ? one : mine;
+    }
+    atomicMin(&least, mine);
+    __syncthreads();
+    ok = ok && s <= (int)(least >> 32);
     if (threadIdx.x == 0) {
         begin[gr] = ok ? s : 0;
-        if (shortest) shortest[gr] = least;
+        if (shortest) shortest[gr] = make_int2((int)(least >> 32), (int)(least & 0xFFFFFFFFu));
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }

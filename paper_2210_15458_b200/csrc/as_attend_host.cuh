@@ -17,7 +17,8 @@ enum Kernel { MMA_8, MMA_16, TC_128, TC_256 };      // rows of a tile and the ke
 struct AttendPlan {
     Kernel own_kernel, pre_kernel;  // of the lanes' own pass and of that over shared beginnings
     PassArgs own, pre;
-    int *begin, *shortest;
+    int* begin;
+    int2* shortest;
     size_t bytes;
 };
 
@@ -43,7 +44,7 @@ static AttendPlan plan_attend(int dtype, int lanes, int T, int heads, int q_head
         return q;
     };
     pl.begin = reinterpret_cast<int*>(take(sizeof(int) * (size_t)(lanes / N)));
-    pl.shortest = reinterpret_cast<int*>(take(sizeof(int) * (size_t)(lanes / N)));      // (with a window)
+    pl.shortest = reinterpret_cast<int2*>(take(sizeof(int2) * (size_t)(lanes / N)));    // (with a window)
     auto pass = [&](PassArgs& p, Kernel& kernel, int n, int group, bool prefix) {
         p.n = n; p.group = group; p.prefix = prefix; p.N = N;
         p.rows = group * T * g;

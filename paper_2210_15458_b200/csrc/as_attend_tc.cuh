@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(TC_NT, 1) attend_tc_kernel(const __grid_consta
                         pos = ahead.hole.real(pos);
                     }
                     if (seen) {
-                        page = c.table[(size_t)ASX_AT(ahead.lane0, c.lanes, 159) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 160)];
+                        page = c.table[(size_t)ASX_AT(ahead.hole.holder(ahead.lane0), c.lanes, 159) * c.max_pages + ASX_AT(pos >> c.page_shift, c.max_pages, 160)];
                         next_base = c.pages + ((size_t)ASX_AT(ahead.head, c.heads, 161) * tiles_per_page + ((pos & page_mask) >> 4)) * Ti::BYTES;
                         next_lane = ahead.lane0;
                         next_real = true;

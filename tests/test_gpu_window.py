@@ -156,3 +156,33 @@ def test_bad_lengths_and_pages(B):
     out = B.as_cache4_attend(pages, q, bad, C.i32([40, 40, 1 << 29]), 0.1, lane_status=status, window=10, sinks=2)
     assert status.tolist() == [0, B.ERR_INVALID_ARG, B.ERR_INVALID_ARG]
     assert torch.equal(out[0], good[0]) and torch.isfinite(out).all() and not out[2].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,T,Hq,H,D,P,shared,tails,window,sinks", [
+    (2, 1, 2, 1, 64, 16, [320, 160], [300, 1, 90, 200], 64, 5), (3, 1, 4, 2, 128, 16, [480], [200, 400, 30], 150, 0), (4, 3, 4, 1, 64, 32, [640], [90, 3, 500, 250], 200, 40),
+    (33, 1, 8, 1, 128, 64, [1024], [1 + 37 * (32 - i) % 700 for i in range(33)], 400, 17), (40, 1, 8, 2, 64, 16, [512, 0], [600 - 7 * i for i in range(80)], 333, 1)])
+def test_shared_beginnings_that_longer_lanes_have_given_up(B, dtype, N, T, Hq, H, D, P, shared, tails, window, sinks):
+    """Each lane gives up what its own window has left behind; a shorter one of its group still sees, and holds, some of it."""
+    lens = [shared[i // N] + t for i, t in enumerate(tails)]
+    gen = torch.Generator().manual_seed(N)
+    pages, table, k, v = C.filled(B, lens, H, D, P, 6, None, None, shared, N)
+    q = (torch.randn(len(lens), T, Hq, D, generator=gen) * 1.5).to(C.DT[dtype]).cuda()
+    held = table[table >= 0].long()
+    ref = torch.bincount(held, minlength=pages.shape[0]).int()
+    low = [max(n - T + 1 - window, 0) for n in lens]
+    gone = C.i32([[-(-sinks // P) * P, x] for x in low])
+    cut, left = table.clone(), ref.clone()
+    B.as_pages_trim(None, cut, C.i32(lens), left, P, gone=gone)
+    assert any(((cut[i // N * N] < 0) & (cut[i] >= 0))[:shared[i // N] // P].any() for i in range(len(lens)))
+    pages[(left == 0).nonzero().flatten()] = 0xFF           # (and pages that nobody holds may hold anything)
+    scale, status = 1 / math.sqrt(D), C.i32([9] * len(lens))
+    for groups in (0, 1):
+        try:
+            B.as_tune(B.TUNE_WINDOW_GROUPS, groups)
+            lse = torch.empty(len(lens), T, Hq, device="cuda")
+            out = B.as_cache4_attend(pages, q, cut, C.i32(lens), scale, N=N, shared=C.i32(shared), lse=lse, window=window, sinks=sinks, lane_status=status)
+        finally:
+            B.as_tune(B.TUNE_WINDOW_GROUPS, 0)
+        assert (status == 0).all()
+        check(B, dtype, out, lse, q, k, v, lens, scale, window, sinks)
