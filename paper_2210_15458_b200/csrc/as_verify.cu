@@ -516,11 +516,12 @@ __device__ __forceinline__ void row_sum(const char* row, int V, float c, int ran
 }
 
 // Masses in 64 bits: 2^(t / 256), t = (x - m) 256 log2(e) / temp, = 2^n 2^(j / 256) exp(f ln2 / 256), |f| <= 1/2, the last factor by a polynomial of
-// degree 4 (truncation 4e-17).  Logits far below m are raised to where their mass is 2^-1000: what is below VN_NONE counts as none, masked
-// tokens among it, and 2^20 of them do not come up to it.  t is one fused multiply-add: the rounding of m's product is the same for all of
+// degree 4 (truncation 4e-17).  Logits far below m are raised to where their mass is 2^-1000: a token of VN_NONE or less counts as none,
+// masked tokens among it.  Sums are over all tokens, those too; a chunk whose sum is above VN_SOME has a token that counts, as 2^20
+// of those that do not come up to 2^-960.  t is one fused multiply-add: the rounding of m's product is the same for all of
 // a row.  Maxima beyond VN_FAR are taken off the logits first (which is exact: differences that matter are multiples of a
 // float's spacing there).
-constexpr double VN_NONE = 0x1p-950;
+constexpr double VN_NONE = 0x1p-980, VN_SOME = 0x1p-955;
 struct MassRow {
     float sub, low;
     double mc;
@@ -835,7 +836,9 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                 }
                 // ---- chunks' masses of max(p - q, 0) in units of 1 / Zp; listed tokens in the order of their indices ----
                 const int chunks = l.c1 - l.c0, listed = near ? sm.listed : 0;
-                for (int i = tid; i < chunks; i += VN_NT) sm.a[i] = sm.a[i] > VN_NONE ? fmax(fma(-ratio, sm.b[i], sm.a[i]), 0.0) : 0.0;
+                // (a chunk that comes out above 0 has a token that does: of those in its sum one is above VN_NONE, and all of them have
+                // p > q by w, which is Zp / Zq or so near to it that those listed apart are the only ones for which it matters)
+                for (int i = tid; i < chunks; i += VN_NT) sm.a[i] = sm.a[i] > VN_SOME ? fmax(fma(-ratio, sm.b[i], sm.a[i]), 0.0) : 0.0;
                 for (int i = tid; i < listed; i += VN_NT) {
                     int before = 0;
                     for (int k = 0; k < listed; ++k) before += sm.list_j[k] < sm.list_j[i];
@@ -897,7 +900,7 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                         if (bal) end = i + 31 - __clz(bal);
                         if (hit) pick = i + __ffs(hit) - 1;
                     }
-                    if (lane32 == 0) { sm.chunk = pick < 0 ? end : pick; sm.force_last = top || pick < 0; }
+                    if (lane32 == 0) { sm.chunk = max(pick < 0 ? end : pick, 0); sm.force_last = top || pick < 0; }
                 }
                 __syncthreads();
                 const int ci = sm.chunk + l.c0;
@@ -907,7 +910,7 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                     const int g = (ci * l.R + r) * 32 + lane32;
                     auto take = [&](int e, double ep, double eq) {
                         const double d = fma(-ratio, eq, ep);
-                        ev[e] = d > VN_NONE ? d : 0.0;
+                        ev[e] = ep > VN_NONE && d > 0.0 ? d : 0.0;
                     };
                     if (l.q) l.template each<true>(g, l.load(g), take);
                     else l.template each<false>(g, l.load(g), take);
@@ -939,7 +942,7 @@ __global__ void __launch_bounds__(VN_NT, 3) verify_lane_kernel(const __grid_cons
                     __syncthreads();
                 }
                 const bool force_sub = sub < 0;
-                if (force_sub) { sub = sub_end; sub_start = end_start; }
+                if (force_sub) { sub = max(sub_end, 0); sub_start = end_start; }    // (whatever the sums say, nothing in front of the chunk is read)
                 if (warp == 0) {
                     double ev[E], local = 0.0;
                     rest(sub, ev);

@@ -268,3 +268,48 @@ def test_tokens_are_distributed_as_the_targets(B):
     assert float(((got - want) ** 2 / want).sum()) < 24.3       # 0.001 of such draws lie above
     share = float(torch.minimum(torch.softmax(p, 0), torch.softmax(q, 0)).sum())
     assert abs(float((accepted > 0).double().mean()) - share) < 4 * math.sqrt(share * (1 - share) / lanes)
+
+
+def deep_rows(V, dtype, temp, bits, place, margin=4096):
+    """(a row of V logits inside a larger buffer of large ones, first and last token that are likely): the tokens of a stretch of several hundred
+    have 2^-bits of the likeliest one's probability."""
+    buffer = torch.full((V + 2 * margin,), 50.0)
+    row = buffer[margin:margin + V]
+    row.copy_(torch.linspace(-2.0, 0.0, V) * temp)
+    n = V // 3
+    row[:n] = row[V - n:] = float(-bits * math.log(2) * temp)
+    if place == "front":
+        row[V - n:] = -temp
+    if place == "end":
+        row[:n] = -temp
+    likely = (row > -100 * temp).nonzero().flatten()
+    return buffer.to(DT[dtype]).cuda()[margin:margin + V], int(likely[0]), int(likely[-1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temp", [1.0, 0.02])
+@pytest.mark.parametrize("V", [900, 4099, 50257])
+@pytest.mark.parametrize("place", ["front", "end", "both"])
+def test_chunks_of_tokens_next_to_nothing(B, dtype, temp, V, place):
+    """Chunks whose tokens are so unlikely that some of them count as impossible, with codes that lie at the intervals' very ends."""
+    for bits in (930, 945, 949, 951, 953, 955, 957, 960, 965, 970, 975, 979, 981, 985, 990, 999, 1005, 1030):
+        row, low, high = deep_rows(V, dtype, temp, bits, place)
+        for code in (0.0, 1.0, ONE_BELOW):
+            codes = torch.tensor([code], dtype=torch.float64, device="cuda")
+            status = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+            none = torch.empty(1, 0, dtype=torch.int32, device="cuda")
+            u = torch.tensor([[ONE_BELOW]], dtype=torch.float64, device="cuda")
+            got = [B.as_step_verify(row.view(1, 1, V), None, none, u[:, :0], codes, temp, lane_status=status)]
+            # a likely token is looked up and refused; one is drawn and refused: q has no token but it, or the stretch as well, less likely still
+            x = torch.tensor([[(low + high) // 2]], dtype=torch.int32, device="cuda")
+            two = row.view(1, 1, V).expand(1, 2, V).contiguous()
+            got.append(B.as_step_verify(two, None, x, u, codes, temp))
+            for other in (float("-inf"), float(-(bits + 20) * math.log(2) * temp)):
+                q = torch.full((1, 1, V), other, device="cuda")
+                q[0, 0, int(x)] = 0.0
+                got.append(B.as_step_verify(two, q.to(DT[dtype]), x, u, codes, temp))
+            assert int(status[0]) == 0
+            for tokens, accepted, out in got:
+                token = int(tokens[0, 0])
+                # (a token less likely than 2^-950 may count as impossible or not)
+                assert int(accepted[0]) == 0 and (0 <= token <= low if code == 0.0 else high <= token < V) and 0.0 <= float(out[0]) < 1.0
