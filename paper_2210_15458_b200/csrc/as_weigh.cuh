@@ -124,13 +124,21 @@ __global__ void __launch_bounds__(WG_NT) weigh_mma_kernel(const __grid_constant_
                 low_max = 0;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const int row = (rt * NT + n) * 8 + r;
-                    const float up = row_queries<DT, D>(row < p.rows ? query_row<DT, D>(a, cu.lane0, cu.head, row) + cc * (D / 4) : nullptr,
+                    float of[2];                    // the log-sums of the thread's two columns
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int rw = (rt * NT + n) * 8 + 2 * cc + h;
+                        of[h] = rw < p.rows ? wa.lse[out_row(a, cu.lane0, cu.head, rw)] : -INFINITY;
+                    }
+                    // (a row that sees nothing is not read: whatever it holds, its scores are 0)
+                    const int row = (rt * NT + n) * 8 + r, from_lane = (lane & ~3) | (r >> 1);
+                    const float even = __shfl_sync(0xFFFFFFFFu, of[0], from_lane), odd = __shfl_sync(0xFFFFFFFFu, of[1], from_lane);
+                    const float up = row_queries<DT, D>((r & 1 ? odd : even) == -INFINITY ? nullptr : query_row<DT, D>(a, cu.lane0, cu.head, row) + cc * (D / 4),
                                                         [&](int part, int j, int h) -> uint32_t& { return qf[part][n][j][h]; });
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int rw = (rt * NT + n) * 8 + 2 * cc + h;
-                        const float lse = rw < p.rows ? wa.lse[out_row(a, cu.lane0, cu.head, rw)] : -INFINITY;
+                        const float lse = of[h];
                         const int rl = lse == -INFINITY ? 0 : row_limit(a, cu.lane0, rw);
                         k2[n][h] = __shfl_sync(0xFFFFFFFFu, up, 4 * (2 * cc + h)) * to_log2;
                         z[n][h] = lse * 1.44269504088896f;

@@ -132,3 +132,27 @@ def test_bad_lanes(B):
     w.fill_(2.0)
     B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.1, w, first=C.i32([41, 40, 0, 0, 0]), lane_status=status)
     assert status.tolist() == [E, 0, 0, 0, 0] and (w[:2] == 2.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,Hq", [(2, 2), (5, 4), (10, 4), (24, 4), (40, 4), (130, 4)])
+def test_rows_that_see_nothing_may_hold_anything(B, dtype, T, Hq):
+    """Padding in front of a short lane, and rows that the caller has taken out by an lse of -inf."""
+    H, D, P = 2, 64, 16
+    lens = [T // 2, 150, T + 20, 1, 0]
+    pages, table, k, v = C.filled(B, lens, H, D, P, 5, None, None)
+    q = torch.randn(5, T, Hq, D, generator=torch.Generator().manual_seed(3)).to(C.DT[dtype]).cuda()
+    lse = torch.empty(5, T, Hq, device="cuda")
+    B.as_cache4_attend(pages, q, table, C.i32(lens), 0.1, lse=lse)
+    lse[1, T // 2:, ::2] = -math.inf
+    lse[2] = -math.inf
+    W = max(lens)
+    old = torch.rand(5, H, W, device="cuda")
+    clean, got = old.clone(), old.clone()
+    B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.1, clean)
+    for i, bad in enumerate((math.nan, math.inf, -math.inf)):
+        q[:, :, :, i::3] = torch.where((lse == -math.inf).unsqueeze(3), torch.full_like(q[:, :, :, i::3], bad), q[:, :, :, i::3])
+    B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.1, got)
+    assert torch.equal(got, clean) and torch.isfinite(got).all()
+    own = max(lens[2] - T, 0)
+    assert torch.equal(got[2, :, :own], old[2, :, :own]) and not got[2, :, own:lens[2]].any()
