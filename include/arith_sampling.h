@@ -561,8 +561,8 @@ int as_cache4_attend_window(const as_cache4 *cache, const void *d_q, long long q
  *   d_first    NULL (0) or [lanes] i32 device: positions in front of it are left alone (a beginning that is kept anyway)
  *   d_lane_status  NULL or [lanes]: AS_OK, or AS_ERR_INVALID_ARG for a d_len outside [0, max_pages * page_size] or above weight_ld,
  *              a d_first outside [0, d_len] (the lane's weights are then left as they were) or a page id outside [0, n_pages) (page 0
- *              is read in its place), or AS_ERR_TIMEOUT: a wait of the kernel for many rows, bounded by AS_TUNE_WAIT_KCYCLES, ran out, and
- *              weights of the call may be missing
+ *              is read in its place), or AS_ERR_TIMEOUT: a wait of the kernel for many rows, bounded by AS_TUNE_WAIT_KCYCLES, ran out: each
+ *              weight is then what it was or what the call should have made it
  *   d_work     as_cache4_weigh_work_bytes(...) bytes of device scratch, 256-byte aligned
  * Scores, weights and sums are in 32 bits; results do not depend on scheduling.
  * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED, AS_ERR_CUDA as for as_cache4_attend.

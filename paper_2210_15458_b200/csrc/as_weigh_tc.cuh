@@ -24,7 +24,8 @@ struct WeighTcArgs {
     int row_tiles;
     const int* steps;                       // [lanes] pairs of a token tile and a row tile that it needs, of one head
     float* part;                            // [2 * runs][128] sums of token tiles that a run saw in part
-    int4* info;                             // [runs] (lane, head, token tile, bits: 1 its first token tile was begun by another run, 2 that one ends here)
+    int4* info;                             // [runs] (lane, head, token tile, bits: 1 its first token tile was begun by another run, 2 that one ends here, 4 the
+                                            // run has come to its end)
     int runs;
 };
 
@@ -118,6 +119,7 @@ struct WeighTcSmem {
     uint32_t tmem;
     int failed;
     int start[5];                           // lane, head, token tile, step within it; steps of the run
+    int4 info;                              // of the run, for the join
     int warp_sum[WT_NT / 32];
     float sum[2][WT_GROUPS - 1][TC_KV];
 };
@@ -214,7 +216,7 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
         }
         const unsigned U = (unsigned)total * c.heads, G = min((unsigned)t.runs, U), k = blockIdx.x;
         if (k >= G) return;
-        if (tid == 0) t.info[ASX_AT(k, WT_MAX_RUNS, 365)] = make_int4(0, 0, 0, 0);  // (nothing to join, should a wait run out)
+        if (tid == 0) sm.info = make_int4(0, 0, 0, 0);
         const unsigned q = U / G, r = U - q * G;
         const unsigned from = q * k + r * k / G, n = q * (k + 1) + r * (k + 1) / G - from;
         unsigned at = (unsigned)before * c.heads;
@@ -344,7 +346,7 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
                 const bool begun = cu.at > 0, ends = cu.at + tiles == cu.n;
                 if (begun || !ends) t.part[(size_t)ASX_AT(2 * blockIdx.x + (begun ? 0 : 1), 2 * WT_MAX_RUNS, 364) * TC_KV + r] = sum;
                 else if (place < cu.l.hi) put_weight(wa, cu.lane, cu.head, pos, wa.first[cu.lane], cu.l.len, sum);
-                if (unit == 0 && r == 0) t.info[ASX_AT(blockIdx.x, WT_MAX_RUNS, 365)] = make_int4(cu.lane, cu.head, cu.tile, (begun ? 1 : 0) | (ends ? 2 : 0));
+                if (unit == 0 && r == 0) sm.info = make_int4(cu.lane, cu.head, cu.tile, (begun ? 1 : 0) | (ends ? 2 : 0) | 4);
             }
             x += tiles;
             if (x < run) cu.next(t);
@@ -497,6 +499,8 @@ __global__ void __launch_bounds__(WT_NT, 1) weigh_tc_kernel(const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // (of a run in which a wait has run out, none of the sums in scratch are joined: some may never have been written)
+    if (tid == 0) t.info[ASX_AT(blockIdx.x, WT_MAX_RUNS, 365)] = sm.failed ? make_int4(0, 0, 0, 0) : sm.info;
     if (sm.failed && tid == 0) {
 #pragma unroll 1
         for (int j = 0; j < c.lanes; ++j) flag_lane(c.lane_status, j, AS_ERR_TIMEOUT);
@@ -517,9 +521,10 @@ static __global__ void __launch_bounds__(TC_KV) weigh_join_kernel(const __grid_c
     __syncthreads();
     if (k >= (int)min((unsigned)t.runs, all * t.w.a.c.heads)) return;
     const int4 i = t.info[k];
-    if ((i.w & 3) != 3) return;                 // (a tile that runs on is joined where it ends)
+    if (i.w != 7) return;                       // (a tile that runs on is joined where it ends)
     int c0 = k - 1;
-    while (c0 > 0 && (t.info[c0].w & 3) == 1) --c0;     // (a run inside one token tile)
+    while (c0 > 0 && t.info[c0].w == 5) --c0;   // (a run inside one token tile)
+    if (!(t.info[c0].w & 4)) return;            // (a wait has run out there: the tile's weights stay as they are)
     float sum = t.part[(size_t)(2 * c0 + 1) * TC_KV + r];
     for (int j = c0 + 1; j <= k; ++j) sum += t.part[(size_t)(2 * j) * TC_KV + r];
     const WeighLane l(t.w, i.x);

@@ -134,3 +134,30 @@ def test_a_wait_that_runs_out_reports_timeout_and_the_next_call_is_fine(B, windo
     assert torch.equal(again, weight) and statuses[1].tolist() == [0, 0] and weight.sum() > 0
     assert torch.equal(B.as_cache4_attend(pages, q, table, C.i32(lens), 0.09, window=window, sinks=sinks if window else 0, lane_status=statuses[0]), good)
     assert statuses[0].tolist() == [0, 0]
+
+
+def test_weights_of_a_call_whose_waits_run_out_are_old_or_right(B):
+    """Bounds that some of the kernel's runs keep and others do not, the scratch full of what is no answer."""
+    lens, T, H, Hq = [6000, 4100, 777], 300, 2, 8
+    pages, table, k, v = C.filled(B, lens, H, 128, 64, 11, None, None)
+    q = torch.randn(3, T, Hq, 128, generator=torch.Generator().manual_seed(2)).cuda().bfloat16()
+    lse, old = torch.empty(3, T, Hq, device="cuda"), 1 + torch.rand(3, H, 6000, device="cuda")
+    B.as_cache4_attend(pages, q, table, C.i32(lens), 0.09, lse=lse)
+    for add in (True, False):
+        right = old.clone()
+        B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.09, right, add=add)
+        found = []
+        for kcycles in (1, 2, 3, 4, 5, 6, 8, 10, 13, 16, 20, 25, 32, 40, 50, 64, 80, 100) * 3:
+            w, status = old.clone(), C.i32([9] * 3)
+            work = torch.full((B.as_cache4_weigh_work_bytes(pages, B.BF16, 3, T, Hq),), 0x7F, dtype=torch.uint8, device="cuda")
+            try:
+                B.as_tune(B.TUNE_WAIT_KCYCLES, kcycles)
+                B.as_cache4_weigh(pages, q, lse, table, C.i32(lens), 0.09, w, add=add, lane_status=status, work=work)
+                torch.cuda.synchronize()
+            finally:
+                B.as_tune(B.TUNE_WAIT_KCYCLES, 0)
+            out = status.tolist()
+            found.append((kcycles, out, int(((w != old) & (w != right)).sum())))
+            assert out in ([0] * 3, [B.ERR_TIMEOUT] * 3)
+            assert out != [0] * 3 or torch.equal(w, right)
+        assert any(out != [0] * 3 for _, out, _ in found) and all(n == 0 for _, _, n in found), found
