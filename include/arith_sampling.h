@@ -619,7 +619,8 @@ int as_cache4_evict(const as_cache4 *cache, const float *d_weight, long long wei
  * as_pages_grow: lane i gets the pages for d_add[i] >= 0 more tokens and its length grows by them, in
  * place.  Lanes that the free pages do not reach keep what they have: once a lane's pages do not
  * suffice, neither do those of the lanes behind it that need any (AS_ERR_NO_PAGES); a lane that would
- * pass max_pages or has a bad length or a negative d_add: AS_ERR_INVALID_ARG, unchanged.
+ * pass max_pages or has a bad length or a negative d_add, or whose partly filled last page has been given up (as_pages_trim; its
+ * table entry is negative) while it wants more tokens: AS_ERR_INVALID_ARG, unchanged.
  *
  * as_pages_compact: with U pages in use, every page in use at U or above moves into a free page
  * below U (the lowest into the lowest), so that the pool's end is free.  Table entries that name a page in use follow it;
@@ -629,7 +630,8 @@ int as_cache4_evict(const as_cache4 *cache, const float *d_weight, long long wei
  * as_pages_trim: lane i is cut to d_keep[i] tokens (a lane that is not longer keeps its length) and gives up the pages behind
  * them; of what is left it gives up the pages that lie wholly within positions d_gone[i][0] .. d_gone[i][1] - 1, say those that a
  * sliding window has left behind.  Table entries of pages given up become -1.  A lane that has given up pages in its middle can
- * grow and be trimmed, to 0 tokens as well, but as_pages_fork reads it as out of range.
+ * grow and be trimmed, to 0 tokens as well, but as_pages_fork reads it as out of range, and so does as_cache4_evict where the pages
+ * lie behind d_first.  Cut to within a page that it has given up, it has to be cut to a page's end or beginning before it can grow.
  *   d_keep     NULL (no lane is cut) or [lanes] i32;  d_gone  NULL or [lanes, 2] i32
  *   d_table_out, d_len_out, d_ref_out  may be d_table, d_len and d_ref
  *   d_lane_status  NULL or [lanes]: AS_OK, or AS_ERR_INVALID_ARG: a length or a page within it out of range (-1, given up before,

@@ -233,25 +233,28 @@ __global__ void __launch_bounds__(PL_NT) grow_kernel(const GrowArgs a, const Pag
     for (int base = 0; base < a.lanes; base += PL_NT) {
         const int i = base + tid;
         int need = 0;
+        bool bad = false;
         if (i < a.lanes) {
             const int len = a.len[i], add = a.add[i];
-            if (len >= 0 && add >= 0 && (long long)len + add <= most)
-                need = pages_of(len + add, a.page_size) - pages_of(len, a.page_size);
+            bad = len < 0 || add < 0 || (long long)len + add > most;
+            // (a part page that the lane has given up: its next token would have no place)
+            if (!bad && add > 0 && len % a.page_size != 0) bad = a.table[(size_t)i * a.max_pages + ASX_AT(len / a.page_size, a.max_pages, 219)] < 0;
+            if (!bad) need = pages_of(len + add, a.page_size) - pages_of(len, a.page_size);
         }
         int total;
         // (more than every page cannot be had: with at most 2^20 pages the sums stay within 32 bits)
         const int r = min(wanted, a.n_pages + 1) + block_scan(min(need, a.n_pages + 1), warp_sum, total) - min(need, a.n_pages + 1);
-        if (i < a.lanes) w.off[i] = r;
+        if (i < a.lanes) w.off[i] = bad ? -1 : r;
         wanted = min(wanted + total, a.n_pages + 1);
     }
     const int got = collect(a.ref, 0, a.n_pages, false, min(wanted, a.n_pages), w.free_page, a.n_pages, warp_sum);
     for (int i = tid; i < a.lanes; i += PL_NT) {
-        const int len = a.len[i], add = a.add[i];
+        const int len = a.len[i], add = a.add[i], r = w.off[i];
         int status = AS_OK;
-        if (len < 0 || add < 0 || (long long)len + add > most) {
+        if (r < 0) {
             status = AS_ERR_INVALID_ARG;
         } else {
-            const int have = pages_of(len, a.page_size), need = pages_of(len + add, a.page_size) - have, r = w.off[i];
+            const int have = pages_of(len, a.page_size), need = pages_of(len + add, a.page_size) - have;
             if (need > 0 && r + need > got) {
                 status = AS_ERR_NO_PAGES;
             } else {

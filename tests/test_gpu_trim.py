@@ -116,3 +116,27 @@ def test_trimmed_lanes_grow_again(B):
     assert torch.equal(held.int(), r)
     B.as_pages_trim(i32([0] * 3), t, n, r, P)
     assert not r.any() and (t == -1).all()
+
+
+def test_a_lane_cut_into_what_it_has_given_up(B):
+    """Its last page is partly filled and not there: it cannot grow before it is cut to a page's end."""
+    P = 16
+    t, n, r = i32([[-1] * 8] * 4), i32([0] * 4), i32([0] * 40)
+    B.as_pages_grow(i32([100, 100, 100, 40]), t, n, r, P)
+    B.as_pages_trim(None, t, n, r, P, gone=i32([[16, 64], [16, 64], [16, 64], [0, 0]]))
+    status = i32([9] * 4)
+    B.as_pages_trim(i32([40, 48, 70, 40]), t, n, r, P, lane_status=status)
+    assert status.tolist() == [0] * 4 and n.tolist() == [40, 48, 70, 40]
+    held = (t.clone(), n.clone(), r.clone())
+    B.as_pages_grow(i32([5, 0, 0, 0]), t, n, r, P, lane_status=status)
+    assert status.tolist() == [B.ERR_INVALID_ARG, 0, 0, 0]
+    assert all(torch.equal(a, b) for a, b in zip(held, (t, n, r)))
+    B.as_pages_grow(i32([0, 5, 5, 10]), t, n, r, P, lane_status=status)
+    assert status.tolist() == [0] * 4 and n.tolist() == [40, 53, 75, 50]
+    B.as_pages_trim(i32([32, 53, 75, 50]), t, n, r, P)
+    B.as_pages_grow(i32([20, 1, 1, 1]), t, n, r, P, lane_status=status)
+    assert status.tolist() == [0] * 4 and n.tolist() == [52, 54, 76, 51]
+    # every token that came in by growing has a page, and the counts are right
+    for i, (a, b) in enumerate(((32, 52), (48, 54), (70, 76), (40, 51))):
+        assert all(int(t[i, p // P]) >= 0 for p in range(a, b))
+    assert torch.equal(torch.bincount(t[t >= 0].long(), minlength=40).int(), r)
