@@ -318,11 +318,14 @@ constexpr int VN_LIST = 256;
 constexpr int VN_BATCH = 4;                 // places, at most, whose rows are read before the decisions are taken
 constexpr int VN_MAX_CTAS = 8;
 constexpr int VN_U = 4, VN_STAGES = 3;      // granules of a thread at a time, steps that it has in flight or in use
-// Of a sum in 32 bits: terms are off by 2^-22 (the exponential) and 2^-23 of their exponent, at most 130 before they vanish; 32 of
-// them are added up before 64 bits take over (2^-19): 2^-15.5 in all, and two sums to a ratio.  Maxima beyond VN_FAR in units of
-// log 2 (nothing that a model says) are left to 64 bits altogether.
-constexpr double VN_NEAR = 1.0 / 8192;
-constexpr int VN_NEAR_BITS = 13;
+// Of a sum in 32 bits: terms are off by 2^-22 (the exponential) and 2^-23 of their exponent, at most 130 before they vanish (2^-16 in all); 32 of
+// them are added up before 64 bits take over (2^-19).  Where a thread's running maximum goes up its sum is scaled by a factor that is off by
+// 2^-22, at most 256 times, once for each step of a row of 2^20 tokens in 32 bits (2^-14).  Sums are then joined up to 16 times (5 in a
+// warp, 8 warps, 3 in a cluster), by such factors too (2^-18).  The factors' exponents are off by 1.5 x 2^-23 of themselves, and a sum that
+// counts has not more than 60 of those in all (2^-17).  That makes 2^-13.3, and 2^-12.3 for the ratio of two sums; a row that falls, or hardly rises, has
+// 2^-15.  Maxima beyond VN_FAR in units of log 2 (nothing that a model says) are left to 64 bits altogether.
+constexpr double VN_NEAR = 1.0 / 4096;
+constexpr int VN_NEAR_BITS = 12;
 constexpr float VN_FAR = 1e6f;
 
 struct RowSum { double s; float m; int bad; };

@@ -161,3 +161,25 @@ def test_weights_of_a_call_whose_waits_run_out_are_old_or_right(B):
             assert out in ([0] * 3, [B.ERR_TIMEOUT] * 3)
             assert out != [0] * 3 or torch.equal(w, right)
         assert any(out != [0] * 3 for _, out, _ in found) and all(n == 0 for _, _, n in found), found
+
+
+@pytest.mark.parametrize("rise,other", [(0.5, 3.0), (3.0, 0.5), (20.0, 18.0), (200.0, 190.0)])
+def test_long_rows_that_rise_all_the_way(B, rise, other):
+    """Rows of nearly 2^20 tokens, summed by one CTA to a lane, whose running maxima go up at every step; u at and around the border."""
+    lanes, V_ = 240, (1 << 20) - 5
+    t, d = torch.linspace(-rise, 0, V_, device="cuda"), torch.linspace(-other, 0, V_, device="cuda")
+    x = V_ - 9 if rise < other else V_ // 2 if rise < 10 else V_ - 40000
+    # (64-bit sums on the GPU; both probabilities are within 1e-12 of themselves)
+    px, qx = (float(torch.softmax(r.double(), 0)[x]) for r in (t, d))
+    if px > qx:
+        t, d, px, qx = d, t, qx, px
+    delta = torch.tensor([s * 2.0 ** -(8 + k / 4) for k in range(lanes // 2) for s in (1, -1)], dtype=torch.float64)
+    u = (px / qx * (1 + delta)).view(lanes, 1)
+    assert u.max() < 1
+    target = t.expand(lanes, 2, V_).contiguous()
+    draft = d.expand(lanes, 1, V_).contiguous()
+    drafted = torch.full((lanes, 1), x, dtype=torch.int32, device="cuda")
+    codes = torch.full((lanes,), 0.37, dtype=torch.float64, device="cuda")
+    tokens, accepted, _ = B.as_step_verify(target, draft, drafted, u.cuda(), codes)
+    sure = delta.abs() > 1e-11
+    assert torch.equal((accepted.cpu() == 1)[sure], (delta < 0)[sure]) and int(sure.sum()) > 200
