@@ -98,3 +98,19 @@ def test_verify(B, dtype, temp, top_k, top_p, lanes, K, V_):  # noqa: F811
     tokens, accepted, out = Guarded((lanes, K + 1), torch.int32), Guarded((lanes,), torch.int32), Guarded((lanes,), torch.float64)
     V.check(B, target, draft, drafted, u, codes, temp, top_k, top_p, work=work.view, tokens=tokens.view, accepted=accepted.view, codes_out=out.view)
     assert all(x.intact() for x in (work, tokens, accepted, out))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("lanes,H,D,P,top,recent", [(38, 4, 64, 16, 1500, 40), (310, 1, 64, 32, 130, 17), (30, 3, 128, 32, 1500, 33)])
+def test_evict_many(B, lanes, H, D, P, top, recent, in_place):  # noqa: F811
+    E.test_many_lanes_and_heads(B, lanes, H, D, P, top, recent, "ties", in_place)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_evict_long(B, in_place):  # noqa: F811
+    E.test_middles_beyond_shared_memory(B, [40000, 300], [20000, 100], [7, 3], 90, 1, 64, 64, "ties", in_place)
+
+
+@pytest.mark.parametrize("place", ["front", "end"])
+def test_verify_next_to_nothing(B, place):  # noqa: F811
+    V.test_chunks_of_tokens_next_to_nothing(B, "bf16", 1.0, 4099, place)

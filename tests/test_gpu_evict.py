@@ -136,3 +136,73 @@ def test_refused_lanes_keep_what_they_have(B):
     rest[mine] = False
     assert torch.equal(pages[rest], before[rest]) and torch.equal(pages[table[6, 0].long()], before[table[6, 0].long()])
     assert torch.equal(pages[table[7, 6].long()], before[table[7, 6].long()])
+
+
+def spoilt(w, kind, gen):
+    """Weights with many equal ones, or with zeros, infinities, NaN and negative ones among them."""
+    if kind == "ties":
+        return (w * 2).floor().clamp(max=5)
+    if kind == "odd":
+        r = torch.rand(w.shape, generator=gen)
+        w = torch.where(r < 0.1, torch.zeros_like(w), w)
+        for lo, x in ((0.1, float("inf")), (0.2, float("nan")), (0.5, -0.0), (0.55, float("-inf"))):
+            w[(r > lo) & (r < lo + 0.05)] = x
+    return w
+
+
+def compare(B, lens, keeps, firsts, recent, H, D, P, W, kind, in_place, lanes=None):
+    """The call against the model, in these lanes (None: all); what no lane holds stays."""
+    gen = torch.Generator().manual_seed(len(lens) + recent)
+    w = spoilt(torch.exp(2 * torch.randn(len(lens), H, W, generator=gen)), kind, gen)
+    before, pages, table, out, status = run(B, lens, keeps, firsts, recent, H, D, P, w, in_place)
+    assert status == [0] * len(lens)
+    for i in range(len(lens)) if lanes is None else lanes:
+        n, kept = lens[i], min(lens[i], keeps[i])
+        for h in range(H):
+            src, wo = model(w[i, h].tolist(), n, keeps[i], firsts[i], recent)
+            assert torch.equal(torch.nan_to_num(out[i, h], 123.0), torch.nan_to_num(torch.tensor(wo), 123.0))
+            if n > 0:
+                old, new = tokens(before, table, i, h, n), tokens(pages, table, i, h, n)
+                assert torch.equal(new[:kept], old[src[:kept]]) and torch.equal(new[kept:], old[kept:])
+    free = torch.ones(pages.shape[0], dtype=torch.bool)
+    free[table[table >= 0].long()] = False
+    assert torch.equal(pages[free], before[free])
+
+
+def ragged(n, top, recent, seed):
+    """(lengths, ends, beginnings) of n lanes: some shorter than they may be, some cut by one, some to next to nothing."""
+    rng = random.Random(seed)
+    lens = [rng.choice((0, 1, top, rng.randint(1, top))) for _ in range(n)]
+    firsts = [rng.choice((0, rng.randint(0, 40))) for _ in lens]
+    keeps = [f + recent + rng.choice((0, 1, max(0, m - f - recent - 1), rng.randint(0, top))) for f, m in zip(firsts, lens)]
+    return lens, keeps, firsts
+
+
+# More lanes and heads than SMs take small thread blocks if a lane's weights fit those, else large ones; half as many large ones; fewer clusters of them.
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd"])
+@pytest.mark.parametrize("lanes,H,D,P,top,recent", [(38, 4, 64, 16, 1500, 40), (80, 2, 128, 64, 700, 0), (310, 1, 64, 32, 130, 17), (200, 3, 128, 16, 90, 20), (75, 2, 64, 128, 8100, 500),
+                                                    (30, 3, 128, 32, 1500, 33), (100, 1, 64, 16, 3000, 1000), (37, 4, 64, 64, 400, 0), (160, 1, 64, 64, 8500, 64)])
+def test_many_lanes_and_heads(B, lanes, H, D, P, top, recent, kind, in_place):
+    lens, keeps, firsts = ragged(lanes, top, recent, lanes)
+    W = max(lens) + 2
+    compare(B, lens, keeps, firsts, recent, H, D, P, W, kind, in_place, None if top <= 1500 else range(0, lanes, 9))
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd"])
+@pytest.mark.parametrize("lens,keeps,firsts,recent,H,D,P", [
+    ([40000, 300], [20000, 100], [7, 3], 90, 1, 64, 64), ([50001], [1000], [0], 0, 2, 64, 128), ([37000, 36000, 40], [36999, 35000, 30], [100, 0, 2], 20, 1, 128, 16),
+    ([60000], [30000], [16], 25000, 1, 64, 64),
+    # (middles of 35549, 35550 and 35551 tokens)
+    ([36000, 36001, 36002], [20000, 20000, 35000], [51, 51, 51], 400, 1, 64, 64)])
+def test_middles_beyond_shared_memory(B, lens, keeps, firsts, recent, H, D, P, kind, in_place):
+    """Weights that do not fit a thread block's shared memory are read again, while places among them are being filled."""
+    compare(B, lens, keeps, firsts, recent, H, D, P, max(lens) + 5, kind, in_place)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_a_long_middle_among_many_lanes(B, in_place):
+    lens = [39000 if i == 41 else 37111 if i == 3 else 10 + 13 * i for i in range(80)]
+    keeps = [20000 if i == 41 else 3000 if i == 3 else 5 + 12 * i for i in range(80)]
+    compare(B, lens, keeps, [2] * 80, 3, 1, 64, 64, 39000, "ties", in_place)
