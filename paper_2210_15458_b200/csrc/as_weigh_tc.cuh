@@ -138,7 +138,6 @@ struct WeighCursor {
         first = s.x;
         n = s.y;
     }
-    __device__ __forceinline__ bool have(const WeighTcArgs& t) const { return lane < t.w.a.c.lanes; }
     // the next token tile that any row looks at
     __device__ __noinline__ void next(const WeighTcArgs& t) {
         at = 0;
