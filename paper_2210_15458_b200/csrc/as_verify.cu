@@ -1038,9 +1038,11 @@ static cudaError_t launch_verify(const VerifyArgs& a, int sms, cudaStream_t st) 
     const bool tame = a.inv_tau >= 1e-30 && a.inv_tau <= 1e30;
     if (tame && (a.top_k <= 0 || a.top_k >= a.V) && !(a.top_p > 0.0 && a.top_p < 1.0)) return launch_verify_lanes<DT>(a, sms, st);
     const unsigned rows = (unsigned)((long long)a.lanes * (a.draft ? 2 * a.K + 1 : a.K + 1));
-    // A CTA has 1024 threads where each finds an SM of its own and the row has 16 bytes for more than 512 of them: 5 x 2 x 38634, both cuts, 107 us in
-    // place of 133 with 512, 96 x 5 x 50257, nucleus, 367 in place of 385; else 512: 41 x 3 x 2836, nucleus, 51 us in place of 85 with 1024, 1 x 5 x 742 46 in
-    // place of 49.
+    // A CTA of either kernel has 1024 threads where each finds an SM of its own and the row has 16 bytes for more than 512 of them, else 512.
+    // us with 1024 / 512 threads in the one kernel, the other as it is, logits of spread 2.  Rows: 5 x 2 x 38634, both cuts, 127 / 162 in 32 bits and 114 / 136
+    // in bf16, 20 x 3 x 50257 in bf16, nucleus, 179 / 194; more rows than SMs, nucleus: 41 x 3 x 2836 in 32 bits 89 / 55, 200 x 2 x 32000 in bf16 435 / 355,
+    // 96 x 5 x 50257 in 32 bits 632 / 627; a short row, 1 x 5 x 742: 47 / 38.  Tokens: 96 x 5 x 50257 627 / 667, 20 x 3 x 50257 179 / 219, 140 x 2 x 32000
+    // 271 / 295, 41 x 3 x 2836 55 / 57; more lanes than SMs, 200 x 2 x 32000: 351 / 355.
     const bool wide = (long long)a.V * Traits<DT>::BYTES > 512 * 16;
     cudaError_t e = cudaMemsetAsync(a.stop, 0, sizeof(int) * (size_t)a.lanes * (a.K + 1), st);
     if (e == cudaSuccess) e = wide && rows <= (unsigned)sms ? launch_after(verify_rows_kernel<DT, 1024>, rows, 1024, 0, st, a) : launch_after(verify_rows_kernel<DT, 512>, rows, 512, 0, st, a);

@@ -1,7 +1,8 @@
 // Attention weights of cached tokens, summed over the rows that look at them.
 //
 // For a token t of a lane and key head: w_t = sum over query rows r of 2^(s_rt - z_r), scores s and the rows' log-sums z in units of
-// log 2.  The log-sums are known, so there is no running maximum, and a token's sum belongs to one warp or thread: nothing is joined.
+// log 2.  The log-sums are known, so there is no running maximum.  Here, for few rows, a token's sum belongs to one warp and nothing is
+// joined; the kernel for many rows adds up what groups of threads and CTAs have of it.
 #pragma once
 #include "as_attend.cuh"
 
