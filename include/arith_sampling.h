@@ -584,10 +584,11 @@ int as_cache4_weigh(const as_cache4 *cache, const void *d_q, long long q_ld, int
  *   d_keep     [lanes] i32 device, >= d_first + recent for a lane that is cut;  recent >= 0
  *   d_first    NULL (0) or [lanes] i32 device
  *   d_weight_out  [lanes, heads, weight_ld]; may be d_weight, otherwise the two must not overlap
- *   d_ref      NULL, or [n_pages] i32 device (see below): a lane that would write into a page that other lanes hold too is refused
+ *   d_ref      NULL, or [n_pages] i32 device (see below): a lane that is cut is refused if other lanes hold a page too that it has, in
+ *              part at least, from d_first up to d_keep: its tokens may have to go there
  *   d_lane_status  NULL or [lanes]: AS_OK, or AS_ERR_INVALID_ARG (a d_len outside [0, max_pages * page_size] or above weight_ld, a negative
- *              d_keep or d_first, d_first + recent > d_keep, a page id outside [0, n_pages), a page held by others): the lane then keeps
- *              tokens and weights as they are
+ *              d_keep or d_first, d_first + recent > d_keep, from d_first on a page id outside [0, n_pages), that of a page given up
+ *              among them, a page held by others): the lane then keeps tokens and weights as they are
  * Errors: AS_ERR_INVALID_ARG, AS_ERR_UNSUPPORTED, AS_ERR_CUDA.
  */
 int as_cache4_evict(const as_cache4 *cache, const float *d_weight, long long weight_ld, int lanes,

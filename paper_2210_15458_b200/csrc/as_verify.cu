@@ -78,7 +78,7 @@ __device__ __noinline__ int decide(const VerifyArgs& a, int lane, int i, const d
 // finishes a place's last row looks what becomes of its token, and rows behind a refusal that is known by the time they start are left out.
 // (Which those are depends on timing, what comes out does not: nobody looks at them.)
 // Bound by the general routine's instructions, some 92 us for a row of 50257 alone, hardly by bytes (issue slots 61 %, DRAM 7 %): 96 x 5 x 50257 in 32
-// bits with a nucleus of 0.95: 276 us, 296 with all rows read, and the next kernel 37.
+// bits with a nucleus of 0.95: 276 us, 296 with all rows read, and the next kernel 37 (wide nuclei, of logits of spread 2: 627 us in all).
 template <int DT, int VF_NT>
 __global__ void __launch_bounds__(VF_NT) verify_rows_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ GenericSmem<VF_NT> sm;
@@ -308,9 +308,9 @@ __global__ void __launch_bounds__(VF_NT) verify_finish_kernel(const __grid_const
 // those within VN_NEAR of e_p = w e_q is known to have p > q or not, and
 //   sum of max(p - q, 0) over a chunk = A / Zp - B / Zq,   A, B the masses of its tokens with p > q;
 // the few others are listed and added once Zp and Zq are known.
-// Bound by instructions: 1024 x 4 x 128256 in bf16 takes 618 to 632 us where its bytes take 199 (issue slots 60 %, special-function unit 39 %, 64-bit pipe
+// Bound by instructions: 1024 x 4 x 128256 in bf16 takes 600 to 643 us where its bytes take 199 (issue slots 60 %, special-function unit 39 %, 64-bit pipe
 // 25 %), about half of it the rows in 32 bits, half the last pair in 64; all of it in 64 bits took 1013 us, exponentials by the step's routine
-// 3254.  4 x 3 x 32000: 25 us, of which the host's call 22; row sums a fifth of the kernel, decisions, chunk sums and the pick by single warps most of it.
+// 3254.  4 x 3 x 32000: 24 us, the kernel 20 of them; row sums a fifth of it, decisions, chunk sums and the pick by single warps most of the rest.
 // ---------------------------------------------------------------------------
 constexpr int VN_NT = 256, VN_NW = VN_NT / 32;
 constexpr int VN_CHUNKS = 128;              // of a CTA
