@@ -453,7 +453,7 @@ __device__ __forceinline__ void row_sum(const char* row, int V, float c, int ran
 #pragma unroll
     for (int i = 0; i < VN_STAGES - 1; ++i) issue(first + i * step, i);
     typename P::Acc acc = P::init();
-    float m = -INFINITY, ref = 0.f;         // terms are 2^(x c - ref), ref = m c rounded
+    float m = -INFINITY, ref = 0.f;         // terms are 2^(x c - ref), ref = m c rounded; 0 where a finite number has masked all that the thread has seen
     double s = 0.0;
     const uint64_t cc = two(c, c);
     int stage = 0;
@@ -479,7 +479,7 @@ __device__ __forceinline__ void row_sum(const char* row, int V, float c, int ran
         P::merge(acc, now);
         const float top = P::part_max(now);
         if (top > m) {
-            const float to = top * c;
+            const float to = fmaxf(top * c, -2.f * VN_FAR);
             s *= (double)ex2_approx(m == -INFINITY ? -INFINITY : ref - to);
             m = top;
             ref = to;
@@ -505,8 +505,9 @@ __device__ __forceinline__ void row_sum(const char* row, int V, float c, int ran
     RowSum r;
     r.bad = max(k0, k1) >= Traits<DT>::KEY_PINF || min(k0, k1) < Traits<DT>::KEY_NINF;      // +inf or a NaN
     r.m = m;
-    // (what the rounding of ref has put on every term comes off; the product of two floats is exact in a double)
-    r.s = m == -INFINITY ? 0.0 : s * (double)ex2_approx((float)((double)ref - (double)m * (double)c));
+    // (What the rounding of ref has put on every term comes off; the product of two floats is exact in a double.  Not beyond VN_FAR, where that
+    // may be any power of two: the sum vanishes beside the others', or the row's maximum lies out there too and no sum of it is used.)
+    r.s = m == -INFINITY ? 0.0 : fabsf(ref) > VN_FAR ? s : s * (double)ex2_approx((float)((double)ref - (double)m * (double)c));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         RowSum other;

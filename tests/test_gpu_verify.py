@@ -313,3 +313,29 @@ def test_chunks_of_tokens_next_to_nothing(B, dtype, temp, V, place):
                 token = int(tokens[0, 0])
                 # (a token less likely than 2^-950 may count as impossible or not)
                 assert int(accepted[0]) == 0 and (0 <= token <= low if code == 0.0 else high <= token < V) and 0.0 <= float(out[0]) < 1.0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temp", [0.3, 1.0, 40.0])
+@pytest.mark.parametrize("mask", ["lowest", -1e30, -1e10, -1e9, -1e5])
+@pytest.mark.parametrize("lanes,V", [(40, 17), (20, 1000), (5, 50257), (500, 3000)])
+def test_tokens_masked_by_finite_numbers(B, dtype, temp, mask, lanes, V):
+    """Single tokens and whole stretches, so that threads see nothing else; the target's masks, the draft's, both."""
+    K = 2
+    target, draft, drafted, u, codes = inputs(lanes, K, V, dtype, 31)
+    low = torch.finfo(DT[dtype]).min if mask == "lowest" else mask
+    gen = torch.Generator().manual_seed(4)
+    for rows in (target, draft):
+        masked = torch.rand(rows.shape, generator=gen) < 0.3
+        masked |= torch.rand(rows.shape[0], rows.shape[1], -(-V // 16), generator=gen).lt(0.4).repeat_interleave(16, 2)[:, :, :V]
+        masked[torch.rand(rows.shape[:2], generator=gen) < 0.3] = False
+        masked[:, :, V // 2] = False
+        rows[masked] = low
+    some = slice(0, 40)
+    check(B, target[some], draft[some], drafted[some], u[some], codes[some], temp, 0, 1.0)
+    check(B, target[some], None, drafted[some], u[some], codes[some], temp, 0, 1.0)
+    check(B, target[some], draft[some], drafted[some], u[some], codes[some], temp, 0, 0.9)
+    # many lanes at a time, a thread block to each, decide as few do
+    few = B.as_step_verify(target[some].cuda(), draft[some].cuda(), drafted[some].cuda(), u[some].cuda(), codes[some].cuda(), temp)
+    many = B.as_step_verify(target.cuda(), draft.cuda(), drafted.cuda(), u.cuda(), codes.cuda(), temp)
+    assert torch.equal(few[0], many[0][some]) and torch.equal(few[1], many[1][some])
